@@ -10,6 +10,8 @@ namespace psgd {
 // Records a printf-style message for psgd_last_error() on this thread and returns `code`.
 int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
 void clear_error();
+// The flags that the kernels of psgd_tokens.hip raised on the current device (bit 1 of psgd_device_status()), cleared if asked for.
+int token_status(int clear, int* word);
 
 // Launch arithmetic of the persistent grids: plain host functions, kept apart from the kernels so that a CPU
 // build can check them (every column group covered once, grids within the partials buffer).

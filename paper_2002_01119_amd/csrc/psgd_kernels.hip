@@ -999,7 +999,9 @@ int psgd_device_status(int clear) {
         e = hipMemcpyToSymbol(HIP_SYMBOL(g_status_word), &zero, sizeof(int));
         if (e != hipSuccess) return hip_fail(e, "hipMemcpyToSymbol");
     }
-    return word;
+    int tokens = 0;
+    if (int rc = token_status(clear, &tokens)) return rc;
+    return word | tokens;
 }
 
 }  // extern "C"

@@ -1,0 +1,635 @@
+// Linear layers of all learners, forward and backward (gfx950).
+//
+//     y = act(x W' + b) + residual                                   dz = dy act'(z),  dx = dz W,  dW = dz' x,  db = sum_t dz
+//
+// All three products are C[m, n] = sum_k P[m, k] Q[n, k] with C's columns next to each other:
+//     forward  m token, n output, k input    P = x  [m][k]   Q = W [n][k]
+//     dx       m token, n input,  k output   P = dz [m][k]   Q = W [k][n]
+//     dW       m output, n input, k token    P = dz [k][m]   Q = x [k][n]
+// so an operand comes with k along its rows or down its columns, and one kernel serves them all: it brings either into the same LDS tile,
+// rows of 128 bytes of k, and multiplies from there with the matrix instructions of the type (bf16 32x32x16, float 32x32x2, both summing
+// in fp32).  2 m n k operations against (m + n) k elements: bound by the matrix cores on batches, by reading W at a few tokens.
+#include "psgd_rows.h"
+
+#include <initializer_list>
+
+namespace psgd {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+struct Operand {          // element (row, col) of learner i at p + i * learner + row * pitch + col
+    const char* p;
+    int64_t learner, pitch;
+};
+
+constexpr float kLog2E = 1.44269504088896341f;
+
+template <int ACT> __device__ __forceinline__ float act_of(float z) {
+    if (ACT == PSGD_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (ACT == PSGD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+    if (ACT == PSGD_ACT_SILU) return z / (1.0f + __builtin_amdgcn_exp2f(-z * kLog2E));
+    return z;
+}
+template <int ACT> __device__ __forceinline__ float slope_of(float z) {
+    if (ACT == PSGD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+    if (ACT == PSGD_ACT_GELU)
+        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __builtin_amdgcn_exp2f(-0.5f * kLog2E * z * z) * 0.39894228040143268f;
+    if (ACT == PSGD_ACT_SILU) {
+        const float p = 1.0f / (1.0f + __builtin_amdgcn_exp2f(-z * kLog2E));
+        return p * (1.0f + z * (1.0f - p));
+    }
+    return 1.0f;
+}
+
+// ------------------------------------------------------------------------------------------------ the product
+// What follows the sum over k: y = act(z) + residual, z = sum + bias.
+struct Epilogue {
+    Operand y, z, residual, bias;
+    int act;
+};
+struct GemmArgs {
+    Operand p, q;
+    Epilogue out;
+    float* partial;         // split > 1: [split][learners][m][n] sums of parts of k, without an epilogue
+    int64_t m, n, k;
+    int learners, split;
+    int tiles_m, tiles_n;
+};
+
+constexpr int kRowBytes = 128;                     // a row of the LDS tile: 64 bf16 or 32 floats of k, as eight chunks of 16 bytes
+template <typename T> constexpr int kDepth = kRowBytes / (int)sizeof(T);
+
+// Chunk c of row r lies at place c ^ (r & 7) of its row: eight lanes that read one chunk of eight rows, or write eight chunks of one row, then
+// touch all banks once.
+__device__ __forceinline__ int tile_place(int r, int c) { return r * kRowBytes + ((c ^ (r & 7)) << 4); }
+
+// Four consecutive elements, any alignment.
+__device__ __forceinline__ void load_4(const float* p, int64_t left, float (&v)[4]) { widen<float>(load_cols(p, left), v); }
+__device__ __forceinline__ void load_4(const uint16_t* p, int64_t left, float (&v)[4]) {
+    if (left >= 4) {
+        const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+        v[0] = low_bf16(r.x), v[1] = high_bf16(r.x), v[2] = low_bf16(r.y), v[3] = high_bf16(r.y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = i < left ? load_1(p + i) : 0.0f;
+    }
+}
+__device__ __forceinline__ void store_4(float* p, const float (&v)[4], int64_t left) { store_cols<float>(p, v, left); }
+__device__ __forceinline__ void store_4(uint16_t* p, const float (&v)[4], int64_t left) {
+    if (left >= 4) {
+        *reinterpret_cast<u32x2_any*>(p) = (u32x2){two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < left) store_1(p + i, v[i]);
+    }
+}
+
+// What is left of an output's four columns after the sum over k.
+template <typename T>
+__device__ __forceinline__ void finish(const Epilogue& a, int64_t learner, int64_t m, int64_t n, int64_t left, const float (&bias)[4], float (&v)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += bias[e];
+    if (a.z.p) store_4(reinterpret_cast<T*>(const_cast<char*>(a.z.p)) + learner * a.z.learner + m * a.z.pitch + n, v, left);
+    if (a.act == PSGD_ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_RELU>(v[e]);
+    } else if (a.act == PSGD_ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_GELU>(v[e]);
+    } else if (a.act == PSGD_ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_SILU>(v[e]);
+    }
+    if (a.residual.p) {
+        float r[4];
+        load_4(reinterpret_cast<const T*>(a.residual.p) + learner * a.residual.learner + m * a.residual.pitch + n, left, r);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += r[e];
+    }
+    store_4(reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + learner * a.y.learner + m * a.y.pitch + n, v, left);
+}
+
+// Up to four words of elements, any alignment.
+typedef uint32_t u32_any __attribute__((aligned(2)));
+template <int WORDS, typename T> __device__ __forceinline__ u32x4 load_words(const T* p) {
+    if constexpr (WORDS == 4) {
+        return load_raw(p);
+    } else if constexpr (WORDS == 2) {
+        const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+        return (u32x4){r.x, r.y, 0u, 0u};
+    } else {
+        return (u32x4){*reinterpret_cast<const u32_any*>(p), 0u, 0u, 0u};
+    }
+}
+// The same element by element, the ones from `last` on alike: a row's end inside the words.
+template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const float* p, int64_t last) {
+    u32x4 v = {};
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v[i] = __float_as_uint(p[i < last ? i : last]);
+    return v;
+}
+template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const uint16_t* p, int64_t last) {
+    u32x4 v = {};
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) v[i] = (uint32_t)p[2 * i < last ? 2 * i : last] | (uint32_t)p[2 * i + 1 < last ? 2 * i + 1 : last] << 16;
+    return v;
+}
+
+// One operand's way into LDS: ROWS rows by a tile's depth of k, through the registers of NT lanes.  ALONG: memory has k along its rows; then a
+// lane brings chunks.  Otherwise memory's rows are k: a lane brings blocks of E values of k (E elements to 16 bytes) by WIDE rows of the tile, and
+// turns them.
+template <typename T, int ROWS, int NT, bool ALONG> struct Bring {
+    static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / NT;      // chunks a lane brings
+    static constexpr int WIDE = COUNT < E ? COUNT : E, BLOCKS = COUNT / WIDE, WORDS = WIDE * (int)sizeof(T) / 4;
+    static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0, "whole chunks and blocks a lane");
+    static constexpr int SIDE = ALONG ? 4 : WORDS, LINES = COUNT * 4 / SIDE;     // as loaded: whole chunks, or E lines a block
+    u32x4 raw[LINES];          // of which the first SIDE words
+
+    // rows from `row0` (of `rows`), k from k0 up to `end`
+    __device__ __forceinline__ void fetch(const T* base, int64_t pitch, int64_t row0, int64_t rows, int64_t k0, int64_t end) {
+        const int tid = threadIdx.x, c = tid % 8;
+        const int64_t k = k0 + c * E, left = end - k;
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) {
+                int64_t r = row0 + tid / 8 + j * (NT / 8);
+                r = r < rows ? r : rows - 1;              // rows beyond the last are multiplied but not stored
+                raw[j] = load_cols(base + r * pitch + k, left);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < BLOCKS; ++s) {
+                const int64_t r = row0 + (tid / 8 + s * (NT / 8)) * WIDE;
+                const T* from = base + k * pitch + r;
+                if (r + WIDE <= rows && left >= E) {
+#pragma unroll
+                    for (int j = 0; j < E; ++j) raw[s * E + j] = load_words<WORDS>(from + j * pitch);
+                } else {          // columns and values of k that there are; k beyond the end counts as zero, the tile's rows beyond the last are not stored
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const int64_t kj = k + j < end ? k + j : end - 1, rj = r < rows ? r : rows - 1;
+                        const u32x4 v = load_words_to<WORDS>(base + kj * pitch + rj, rows - 1 - rj);
+                        raw[s * E + j] = k + j < end ? v : (u32x4){};
+                    }
+                }
+            }
+        }
+    }
+
+    __device__ __forceinline__ void put(char* tile) const {
+        const int tid = threadIdx.x, c = tid % 8;
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) 
+                *reinterpret_cast<u32x4*>(tile + tile_place(tid / 8 + j * (NT / 8), c)) = raw[j];
+        } else {
+#pragma unroll
+            for (int s = 0; s < BLOCKS; ++s)
+#pragma unroll
+                for (int e = 0; e < WIDE; ++e) {
+                    u32x4 v;
+                    if constexpr (sizeof(T) == 4) {
+                        v = (u32x4){raw[s * 4][e], raw[s * 4 + 1][e], raw[s * 4 + 2][e], raw[s * 4 + 3][e]};
+                    } else {
+                        const uint32_t pick = e % 2 ? 0x07060302u : 0x05040100u;      // the upper or lower halves of two words
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(raw[s * 8 + 2 * j + 1][e / 2], raw[s * 8 + 2 * j][e / 2], pick);
+                    }
+                    *reinterpret_cast<u32x4*>(tile + tile_place((tid / 8 + s * (NT / 8)) * WIDE + e, c)) = v;
+                }
+        }
+    }
+};
+
+__device__ __forceinline__ void multiply(u32x4 a, u32x4 b, f32x16& c, uint16_t) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// Sixteen bytes of a lane are four values of k; the halves of the wavefront hold different ones, so instruction j sums two values of k.
+__device__ __forceinline__ void multiply(u32x4 a, u32x4 b, f32x16& c, float) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0, 0);
+}
+
+// The tile that workgroup `id` of `total` takes.  Consecutive workgroups go to the eight dies in turn; this gives each die a contiguous stretch
+// of tiles, and walks eight tiles of m for each of n, so that the tiles a die works on at a time share operands in its L2.
+struct Tile {
+    int learner, part, tm, tn;
+};
+__device__ __forceinline__ Tile tile_of(const GemmArgs& a) {
+    const uint32_t id = blockIdx.x, total = gridDim.x, q = total / 8, r = total % 8, die = id % 8;
+    uint32_t t = die * q + (die < r ? die : r) + id / 8;
+    const uint32_t each = (uint32_t)a.tiles_m * a.tiles_n;
+    Tile o;
+    o.part = (int)(t / each) % a.split;
+    o.learner = (int)(t / each) / a.split;
+    t %= each;
+    const uint32_t band = 8u * a.tiles_n, first = t / band * 8, high = min(8u, (uint32_t)a.tiles_m - first);
+    t %= band;
+    o.tm = (int)(first + t % high);
+    o.tn = (int)(t / high);
+    return o;
+}
+
+template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG>
+__global__ __launch_bounds__(256) void gemm_kernel(GemmArgs a) {
+    constexpr int NT = 256, TM = BM / 64, TN = BN / 64, BK = kDepth<T>;      // four wavefronts, two by two; 32 x 32 tiles of each
+    extern __shared__ __attribute__((aligned(128))) char lds[];
+    constexpr int kP = BM * kRowBytes, kBoth = (BM + BN) * kRowBytes;
+    const Tile t = tile_of(a);
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const T* p = reinterpret_cast<const T*>(a.p.p) + t.learner * a.p.learner;
+    const T* q = reinterpret_cast<const T*>(a.q.p) + t.learner * a.q.learner;
+    const int64_t m0 = (int64_t)t.tm * BM, n0 = (int64_t)t.tn * BN;
+    // this part's stretch of k, in whole tiles
+    const int64_t tiles = (a.k + BK - 1) / BK, from = tiles * t.part / a.split, to = tiles * (t.part + 1) / a.split;
+    f32x16 acc[TN][TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) acc[i][j] = (f32x16){};
+    Bring<T, BM, NT, P_ALONG> bp;
+    Bring<T, BN, NT, Q_ALONG> bq;
+    if (from < to) {
+        bp.fetch(p, a.p.pitch, m0, a.m, from * BK, a.k);
+        bq.fetch(q, a.q.pitch, n0, a.n, from * BK, a.k);
+        bp.put(lds);
+        bq.put(lds + kP);
+    }
+    __syncthreads();
+    const int mw = wave % 2 * (BM / 2) + lane % 32, nw = wave / 2 * (BN / 2) + lane % 32;
+    for (int64_t tile = from; tile < to; ++tile) {
+        const char* now = lds + (tile - from) % 2 * kBoth;
+        char* next = lds + (tile - from + 1) % 2 * kBoth;
+        const bool more = tile + 1 < to;
+        if (more) {
+            bp.fetch(p, a.p.pitch, m0, a.m, (tile + 1) * BK, a.k);
+            bq.fetch(q, a.q.pitch, n0, a.n, (tile + 1) * BK, a.k);
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            u32x4 fp[TM], fq[TN];
+#pragma unroll
+            for (int j = 0; j < TM; ++j) fp[j] = *reinterpret_cast<const u32x4*>(now + tile_place(mw + 32 * j, 2 * s + lane / 32));
+#pragma unroll
+            for (int i = 0; i < TN; ++i) fq[i] = *reinterpret_cast<const u32x4*>(now + kP + tile_place(nw + 32 * i, 2 * s + lane / 32));
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+#pragma unroll
+                for (int j = 0; j < TM; ++j) multiply(fq[i], fp[j], acc[i][j], T{});
+        }
+        if (more) {
+            bp.put(next);
+            bq.put(next + kP);
+        }
+        __syncthreads();
+    }
+    // Lane l holds column l % 32 of m and, of each 32 of n, four stretches of four: 8 g + 4 (l / 32) .. + 3.  Through LDS, 32 rows of m at a time, so that
+    // C's rows are read and written side by side.
+    constexpr int WN = BN / 2, PITCH = WN + 4, ACROSS = WN / 4;          // a lane takes four columns: 64 / ACROSS rows at a time
+    float* mine = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
+    const int64_t n = n0 + wave / 2 * WN + lane % ACROSS * 4, left = a.n - n;
+    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.out.bias.p && left > 0 && !a.partial) load_4(reinterpret_cast<const T*>(a.out.bias.p) + t.learner * a.out.bias.learner + n, left, bias);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4*>(mine + lane % 32 * PITCH + 32 * i + 8 * g + lane / 32 * 4) =
+                    (f32x4){acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        __syncthreads();
+        if (left > 0) {
+#pragma unroll 1
+            for (int r = lane / ACROSS; r < 32; r += kWave / ACROSS) {
+                const int64_t m = m0 + wave % 2 * (BM / 2) + 32 * j + r;
+                if (m >= a.m) break;
+                const f32x4 sum = *reinterpret_cast<const f32x4*>(mine + r * PITCH + lane % ACROSS * 4);
+                float v[4] = {sum.x, sum.y, sum.z, sum.w};
+                if (a.partial) store_4(a.partial + (((int64_t)t.part * a.learners + t.learner) * a.m + m) * a.n + n, v, left);
+                else finish<T>(a.out, t.learner, m, n, left, bias, v);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ dz and db
+struct SlopeArgs {
+    Operand dy, z;
+    char* dz;              // [n][t][pitch] elements of T, or NULL
+    int64_t dz_pitch;
+    float* partial;        // [n][slabs][o] column sums, or NULL
+    int64_t t, o;
+};
+// dz = dy act'(z) and its sums down the columns: 64 lanes side by side, four rows at a time, a slab of one learner's rows a workgroup.
+template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
+    constexpr int E = kPer<T>;
+    __shared__ float rest[4][kWave * E];
+    const int lane = threadIdx.x % kWave, line = threadIdx.x / kWave;
+    const int64_t i = blockIdx.z, col = ((int64_t)blockIdx.x * kWave + lane) * E, left = a.o - col;
+    const int64_t r0 = a.t * blockIdx.y / gridDim.y, r1 = a.t * (blockIdx.y + 1) / gridDim.y;
+    float sum[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    if (left > 0) {
+        for (int64_t r = r0 + line; r < r1; r += 4) {
+            float v[E];
+            widen<T>(load_cols(reinterpret_cast<const T*>(a.dy.p) + i * a.dy.learner + r * a.dy.pitch + col, left), v);
+            if (ACT != PSGD_ACT_NONE) {
+                float z[E];
+                widen<T>(load_cols(reinterpret_cast<const T*>(a.z.p) + i * a.z.learner + r * a.z.pitch + col, left), z);
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] *= slope_of<ACT>(z[e]);
+                store_cols<T>(reinterpret_cast<T*>(a.dz) + (i * a.t + r) * a.dz_pitch + col, v, left);
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += v[e];
+        }
+    }
+    if (!a.partial) return;
+#pragma unroll
+    for (int e = 0; e < E; ++e) rest[line][e * kWave + lane] = sum[e];
+    __syncthreads();
+    for (int c = threadIdx.x; c < kWave * E; c += 256) {
+        const int at = c % E * kWave + c / E;
+        const int64_t column = (int64_t)blockIdx.x * kWave * E + c;
+        if (column < a.o) a.partial[(i * gridDim.y + blockIdx.y) * a.o + column] = (rest[0][at] + rest[1][at]) + (rest[2][at] + rest[3][at]);
+    }
+}
+
+// Adds up `parts` arrays of [learners][rows][cols] floats in order: the slabs of db (rows = 1, parts within a learner), or parts of k with the
+// product's epilogue.
+struct JoinArgs {
+    const float* partial;
+    int64_t parts, part_stride, learner_stride;
+    Epilogue out;
+    int64_t rows, cols;
+};
+template <typename T> __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    const int64_t i = blockIdx.z, quads = (a.cols + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.rows * quads) return;
+    const int64_t r = at / quads, c = at % quads * 4, left = a.cols - c;
+    const float* p = a.partial + i * a.learner_stride + r * a.cols + c;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t s = 0; s < a.parts; ++s) {
+        float w[4];
+        load_4(p + s * a.part_stride, left, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += w[e];
+    }
+    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (a.out.bias.p) load_4(reinterpret_cast<const T*>(a.out.bias.p) + i * a.out.bias.learner + c, left, bias);
+    finish<T>(a.out, i, r, c, left, bias, v);
+}
+
+// ------------------------------------------------------------------------------------------------ launches
+inline Operand operand(const psgd_view* v) {
+    return v ? Operand{static_cast<const char*>(v->data), v->learner, v->row} : Operand{nullptr, 0, 0};
+}
+
+struct Plan {
+    int tile, split;             // rows and columns of a workgroup's tile; parts of k
+    size_t bytes(int learners, int64_t m, int64_t n) const {
+        return split > 1 ? up256((size_t)split * learners * m * n * sizeof(float)) : 0;
+    }
+};
+inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// The largest tile of which there are enough to fill the chip; then parts of k, as long as each keeps eight tiles of depth.
+inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
+    const int64_t depth = parts_of(k, kRowBytes / bytes);
+    Plan plan{64, 1};
+    if (m < 1 || n < 1) return plan;          // nothing to multiply
+    for (int tile : {256, 128}) {
+        if (parts_of(m, tile) * parts_of(n, tile) * learners >= cus) {
+            plan.tile = tile;
+            return plan;
+        }
+    }
+    const int64_t count = parts_of(m, 64) * parts_of(n, 64) * learners;
+    int64_t split = cus / count;
+    if (split > depth / 8) split = depth / 8;
+    plan.split = split < 1 ? 1 : split > 64 ? 64 : (int)split;
+    return plan;
+}
+
+template <typename T, int TILE, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
+    a.tiles_m = (int)parts_of(a.m, TILE);
+    a.tiles_n = (int)parts_of(a.n, TILE);
+    constexpr size_t lds = (size_t)4 * TILE * kRowBytes;
+    auto fn = gemm_kernel<T, TILE, TILE, P_ALONG, Q_ALONG>;
+    if (lds >= 64 * 1024) {          // opted in once a kernel and device
+        static bool done[64] = {false};
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
+        if (e != hipSuccess) return hip_error(e, "hipGetDevice");
+        if (dev < 0 || dev >= 64 || !__atomic_load_n(&done[dev], __ATOMIC_RELAXED)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            if (e != hipSuccess) return hip_error(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
+            if (dev >= 0 && dev < 64) __atomic_store_n(&done[dev], true, __ATOMIC_RELAXED);
+        }
+    }
+    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
+    if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), lds, s, a);
+    return PSGD_OK;
+}
+
+template <typename T, bool P_ALONG, bool Q_ALONG>
+int launch_gemm(GemmArgs a, const Plan& plan, float* room, hipStream_t s) {
+    a.split = plan.split;
+    a.partial = plan.split > 1 ? room : nullptr;
+    int rc;
+    if (plan.tile == 256) rc = launch_tiles<T, 256, P_ALONG, Q_ALONG>(a, s);
+    else if (plan.tile == 128) rc = launch_tiles<T, 128, P_ALONG, Q_ALONG>(a, s);
+    else rc = launch_tiles<T, 64, P_ALONG, Q_ALONG>(a, s);
+    if (rc || plan.split == 1) return rc;
+    const JoinArgs j{room, plan.split, a.learners * a.m * a.n, a.m * a.n, a.out, a.m, a.n};
+    hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(a.m * parts_of(a.n, 4), 256), 1, a.learners), dim3(256), 0, s, j);
+    return PSGD_OK;
+}
+
+inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cus) {
+    const int64_t across = parts_of(o, kWave * 16 / bytes) * learners;
+    if (across < 1) return 1;
+    int64_t slabs = parts_of((int64_t)cus * 4, across);
+    if (slabs > parts_of(t, 16)) slabs = parts_of(t, 16);
+    return slabs < 1 ? 1 : slabs > 65535 ? 65535 : slabs;
+}
+
+struct GradRoom {
+    size_t dz, sums, product, total;
+    int64_t dz_pitch;
+};
+inline GradRoom grad_room(int act, int learners, int64_t t, int64_t in, int64_t out, int bytes, int cus, bool dx, bool dw, bool db) {
+    GradRoom r{};
+    r.dz_pitch = parts_of(out, 16 / bytes) * (16 / bytes);
+    r.dz = act != PSGD_ACT_NONE ? up256((size_t)learners * t * r.dz_pitch * bytes) : 0;
+    r.sums = db ? up256((size_t)learners * slope_slabs(learners, t, out, bytes, cus) * out * sizeof(float)) : 0;
+    const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus).bytes(learners, t, in) : 0;
+    const size_t b = dw ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
+    r.product = a > b ? a : b;
+    r.total = r.dz + r.sums + r.product;
+    return r;
+}
+
+inline int check_linear_sizes(const char* name, int n, int64_t t, int64_t in, int64_t out, int act) {
+    if (int rc = check_counts(name, n, t, in)) return rc;
+    if (int rc = check_counts(name, n, t, out)) return rc;
+    if (act < PSGD_ACT_NONE || act > PSGD_ACT_SILU) return fail(PSGD_EINVAL, "%s: act=%d", name, act);
+    return PSGD_OK;
+}
+inline int check_room(const char* name, void* workspace, size_t have, size_t need) {
+    if (need && (!workspace || have < need || reinterpret_cast<uintptr_t>(workspace) % 256))
+        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
+    return PSGD_OK;
+}
+
+template <typename T> int linear_of(const GemmArgs& a, const Plan& plan, void* workspace, hipStream_t s) {
+    return launch_gemm<T, true, true>(a, plan, static_cast<float*>(workspace), s);
+}
+
+template <typename T>
+int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, const psgd_view* w, const psgd_view* dx, const psgd_view* dw,
+                   const psgd_view* db, int act, int n, int64_t t, int64_t in, int64_t out, char* room, int cus, hipStream_t s) {
+    const GradRoom r = grad_room(act, n, t, in, out, sizeof(T), cus, dx, dw, db);
+    float* sums = reinterpret_cast<float*>(room + r.dz);
+    float* product = reinterpret_cast<float*>(room + r.dz + r.sums);
+    Operand dz = operand(dy);
+    if (act != PSGD_ACT_NONE || db) {
+        const SlopeArgs a{operand(dy), operand(z), act != PSGD_ACT_NONE ? room : nullptr, r.dz_pitch, db ? sums : nullptr, t, out};
+        const int64_t slabs = slope_slabs(n, t, out, sizeof(T), cus);
+        const dim3 grid((unsigned)parts_of(out, kWave * kPer<T>), (unsigned)slabs, n);
+        if (act == PSGD_ACT_NONE) hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_NONE>), grid, dim3(256), 0, s, a);
+        else if (act == PSGD_ACT_RELU) hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_RELU>), grid, dim3(256), 0, s, a);
+        else if (act == PSGD_ACT_GELU) hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_GELU>), grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_SILU>), grid, dim3(256), 0, s, a);
+        if (act != PSGD_ACT_NONE) dz = Operand{room, t * r.dz_pitch, r.dz_pitch};
+        if (db) {
+            const JoinArgs j{sums, slabs, out, slabs * out, Epilogue{Operand{static_cast<char*>(db->data), db->learner, out}, {}, {}, {}, PSGD_ACT_NONE}, 1, out};
+            hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(parts_of(out, 4), 256), 1, n), dim3(256), 0, s, j);
+        }
+    }
+    if (dx) {
+        const GemmArgs a{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
+        if (int rc = launch_gemm<T, true, false>(a, gemm_plan(n, t, in, out, sizeof(T), cus), product, s)) return rc;
+    }
+    if (dw) {
+        const GemmArgs a{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
+        if (int rc = launch_gemm<T, false, false>(a, gemm_plan(n, out, in, t, sizeof(T), cus), product, s)) return rc;
+    }
+    return PSGD_OK;
+}
+
+}  // namespace
+}  // namespace psgd
+
+extern "C" {
+
+size_t psgd_linear_workspace(const psgd_view* x, const psgd_view* w, int n, int64_t t, int64_t in, int64_t out) {
+    using namespace psgd;
+    int cus = 0;
+    if (!x || !w || check_linear_sizes("psgd_linear_workspace", n, t, in, out, 0) || t == 0 || out == 0 || compute_units(&cus)) return 0;
+    return gemm_plan(n, t, out, in, elem_bytes(x->type), cus).bytes(n, t, out);
+}
+
+int psgd_linear(const psgd_view* x, const psgd_view* w, const psgd_view* bias, const psgd_view* residual, const psgd_view* y,
+                const psgd_view* z, int act, int n, int64_t t, int64_t in, int64_t out, void* workspace, size_t workspace_bytes,
+                void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_linear";
+    clear_error();
+    if (!x || !w || !y) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (int rc = check_linear_sizes(name, n, t, in, out, act)) return rc;
+    for (const psgd_view* v : {x, w, y, bias, residual, z})
+        if (v && (!float_type(v->type) || v->type != x->type)) return fail(PSGD_EINVAL, "%s: all operands must be float or bf16 alike", name);
+    if (t == 0 || out == 0) return PSGD_OK;
+    const Extent ex{"x", x, n, t, in}, ew{"w", w, n, out, in}, ey{"y", y, n, t, out};
+    const Extent eb{"bias", bias ? bias : w, n, 1, bias ? out : 0}, er{"residual", residual ? residual : x, n, t, residual ? out : 0};
+    const Extent ez{"z", z ? z : y, n, t, z ? out : 0};
+    for (const Extent* e : {&ex, &ew, &eb, &er})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    for (const Extent* e : {&ey, &ez})
+        if (int rc = check_operand(name, *e, true)) return rc;
+    for (const Extent* e : {&ex, &ew, &eb}) {
+        if (int rc = refuse_overlap(name, ey, *e)) return rc;
+        if (int rc = refuse_overlap(name, ez, *e)) return rc;
+    }
+    if (int rc = refuse_overlap(name, ey, er, true)) return rc;
+    if (int rc = refuse_overlap(name, ez, er)) return rc;
+    if (int rc = refuse_overlap(name, ez, ey)) return rc;
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    const Plan plan = gemm_plan(n, t, out, in, elem_bytes(x->type), cus);
+    const size_t need = plan.bytes(n, t, out);
+    if (int rc = check_room(name, workspace, workspace_bytes, need)) return rc;
+    psgd_view vw;
+    const Extent room = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&ex, &ew, &eb, &er, &ey, &ez})
+        if (int rc = refuse_overlap(name, room, *e)) return rc;
+    const GemmArgs a{operand(x), operand(w), Epilogue{operand(y), operand(z), operand(residual), operand(bias), act}, nullptr, t, out, in, n, 1, 0, 0};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (int rc = x->type == PSGD_F32 ? linear_of<float>(a, plan, workspace, s) : linear_of<uint16_t>(a, plan, workspace, s)) return rc;
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+
+size_t psgd_linear_grad_workspace(const psgd_view* dy, const psgd_view* x, const psgd_view* w, const psgd_view* dx, const psgd_view* dw,
+                                  const psgd_view* db, int act, int n, int64_t t, int64_t in, int64_t out) {
+    using namespace psgd;
+    int cus = 0;
+    if (!dy || !x || !w || check_linear_sizes("psgd_linear_grad_workspace", n, t, in, out, act) || compute_units(&cus)) return 0;
+    return grad_room(act, n, t, in, out, elem_bytes(x->type), cus, dx, dw, db).total;
+}
+
+int psgd_linear_grad(const psgd_view* dy, const psgd_view* z, const psgd_view* x, const psgd_view* w, const psgd_view* dx,
+                     const psgd_view* dw, const psgd_view* db, int act, int n, int64_t t, int64_t in, int64_t out, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_linear_grad";
+    clear_error();
+    if (!dy || !x || !w) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (int rc = check_linear_sizes(name, n, t, in, out, act)) return rc;
+    if (act != PSGD_ACT_NONE && !z) return fail(PSGD_EINVAL, "%s: z is needed for the activation's slope", name);
+    if (act == PSGD_ACT_NONE) z = nullptr;
+    for (const psgd_view* v : {dy, x, w, z, dx, dw, db})
+        if (v && (!float_type(v->type) || v->type != x->type)) return fail(PSGD_EINVAL, "%s: all operands must be float or bf16 alike", name);
+    if (!dx && !dw && !db) return PSGD_OK;
+    const Extent edy{"dy", dy, n, t, out}, ex{"x", x, n, t, in}, ew{"w", w, n, out, in}, ez{"z", z ? z : dy, n, t, z ? out : 0};
+    const Extent edx{"dx", dx ? dx : x, n, t, dx ? in : 0}, edw{"dw", dw ? dw : w, n, out, dw ? in : 0}, edb{"db", db ? db : w, n, 1, db ? out : 0};
+    for (const Extent* e : {&edy, &ex, &ew, &ez})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    for (const Extent* e : {&edx, &edw, &edb}) {
+        if (int rc = check_operand(name, *e, true)) return rc;
+        for (const Extent* o : {&edy, &ex, &ew, &ez})
+            if (int rc = refuse_overlap(name, *e, *o)) return rc;
+    }
+    if (int rc = refuse_overlap(name, edx, edw)) return rc;
+    if (int rc = refuse_overlap(name, edx, edb)) return rc;
+    if (int rc = refuse_overlap(name, edw, edb)) return rc;
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    const size_t need = grad_room(act, n, t, in, out, elem_bytes(x->type), cus, dx, dw, db).total;
+    if (int rc = check_room(name, workspace, workspace_bytes, need)) return rc;
+    psgd_view vw;
+    const Extent room = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&edy, &ex, &ew, &ez, &edx, &edw, &edb})
+        if (int rc = refuse_overlap(name, room, *e)) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* p = static_cast<char*>(workspace);
+    if (t == 0) dx = nullptr;
+    if (in == 0) dx = dw = nullptr;
+    if (out == 0) dw = db = nullptr;
+    if (int rc = x->type == PSGD_F32 ? linear_grad_of<float>(dy, z, x, w, dx, dw, db, act, n, t, in, out, p, cus, s)
+                                     : linear_grad_of<uint16_t>(dy, z, x, w, dx, dw, db, act, n, t, in, out, p, cus, s))
+        return rc;
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+
+}  // extern "C"

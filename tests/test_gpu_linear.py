@@ -1,0 +1,261 @@
+"""Linear layers of all learners, forward and backward, against their formulas in 64 bits."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from oracle import layers_oracle as orc  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2002_01119_amd import layers as m
+    m.load()
+    torch.cuda.set_device(0)
+    return m
+
+
+def normal(shape, dtype, seed, sigma=1.0):
+    return torch.empty(shape).normal_(0.0, sigma, generator=torch.Generator().manual_seed(seed)).to(dtype).to("cuda:0")
+
+
+def rows(n, t, c, dtype, seed=None, pitch=0, lead=0, sigma=1.0):
+    whole = torch.full((lead + n * t * (c + pitch),), float("nan"), dtype=dtype, device="cuda:0")
+    v = whole[lead:].view(n, t, c + pitch)[:, :, :c]
+    if seed is not None:
+        v.copy_(normal((n, t, c), dtype, seed, sigma))
+    return v
+
+
+def layer(n, i, o, dtype, seed=None, off=0):
+    """(rows of flat vectors, w, b) with w and b views of the rows."""
+    d = off + o * i + o + 3
+    flat = torch.full((n, d), float("nan"), dtype=dtype, device="cuda:0")
+    w, b = flat.as_strided((n, o, i), (d, max(i, 1), 1), off), flat[:, off + o * i:off + o * i + o]
+    if seed is not None:
+        w.copy_(normal((n, o, i), dtype, seed, max(i, 1) ** -0.5))
+        b.copy_(normal((n, o), dtype, seed + 1, 0.3))
+    return flat, w, b
+
+
+def untouched(flat, w, b, off):
+    n, o, i = w.shape
+    mask = torch.ones_like(flat, dtype=torch.bool)
+    mask[:, off:off + o * i + o] = False
+    assert torch.isnan(flat[mask]).all()
+
+
+# tiles of 64, 128 and 256, parts of k, single tokens, sizes that nothing divides
+SHAPES = [(1, 1, 1, 1), (2, 1, 8, 3), (1, 3, 5, 7), (3, 1, 1000, 771), (2, 7, 64, 64), (1, 17, 333, 65), (2, 40, 129, 130), (1, 65, 1024, 48),
+          (2, 257, 100, 71), (1, 300, 70, 1029), (5, 130, 520, 264), (1, 2, 9000, 40), (1, 33, 4097, 100), (4, 512, 512, 512), (16, 32, 256, 512),
+          (1, 1, 4096, 4096), (2, 16, 1500, 2000), (1, 9, 640, 640)]
+
+
+@pytest.mark.parametrize("n,t,i,o", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_forward(layers, n, t, i, o, dtype, act):
+    pitch, lead, off = (3, 1, 5) if (i + o) % 2 else (0, 0, 0)
+    flat, w, b = layer(n, i, o, dtype, 1, off)
+    x, y, z, r = rows(n, t, i, dtype, 3, pitch, lead), rows(n, t, o, dtype, None, pitch, lead), rows(n, t, o, dtype), rows(n, t, o, dtype, 4, pitch)
+    layers.linear(x, w, y, bias=b, act=act, residual=r, z=z)
+    torch.cuda.synchronize()
+    want, bound = orc.linear(x, w, b, act, r, dtype)
+    orc.assert_within(y, want[0], bound[0], "y")
+    orc.assert_within(z, want[1], bound[1], "z")
+    plain = rows(n, t, o, dtype)
+    layers.linear(x, w, plain, act=act)
+    torch.cuda.synchronize()
+    want, bound = orc.linear(x, w, None, act, None, dtype)
+    orc.assert_within(plain, want[0], bound[0], "y without bias")
+
+
+@pytest.mark.parametrize("n,t,i,o", SHAPES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["none", "silu"])
+def test_backward(layers, n, t, i, o, dtype, act):
+    pitch, lead, off = (3, 1, 5) if (i + o) % 2 else (0, 0, 0)
+    _, w, _ = layer(n, i, o, dtype, 1, off)
+    x, dy = rows(n, t, i, dtype, 3, pitch, lead), rows(n, t, o, dtype, 4, pitch, lead)
+    z = rows(n, t, o, dtype, 5, pitch) if act != "none" else None
+    dx = rows(n, t, i, dtype, None, pitch, lead)
+    grads, dw, db = layer(n, i, o, dtype, None, off)
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db, act=act, z=z)
+    torch.cuda.synchronize()
+    want, bound = orc.linear_grad(dy, x, w, act, z, dtype)
+    for got, v, e, what in zip((dx, dw, db), want, bound, ("dx", "dw", "db")):
+        orc.assert_within(got, v, e, what)
+    untouched(grads, dw, db, off)
+
+
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_activations_at_their_ends(layers, act, dtype):
+    n, t, o = 1, 2, 16
+    z = torch.tensor([-1e30, -200.0, -88.0, -30.0, -5.0, -1.0, -1e-3, -1e-30, 0.0, 1e-30, 1e-3, 1.0, 5.0, 30.0, 200.0, 1e30], device="cuda:0")
+    z = z.to(dtype).expand(n, t, o).contiguous()
+    x, w = torch.zeros((n, t, 1), dtype=dtype, device="cuda:0"), torch.zeros((n, o, 1), dtype=dtype, device="cuda:0")
+    y = torch.empty((n, t, o), dtype=dtype, device="cuda:0")
+    layers.linear(x, w, y, bias=z[:, 0].contiguous(), act=act)
+    want, bound = orc.linear(x, w, z[:, 0], act, None, dtype)
+    orc.assert_within(y, want[0], bound[0], "y")
+    dy, db = normal((n, t, o), dtype, 1), torch.empty((n, o), dtype=dtype, device="cuda:0")
+    layers.linear_grad(dy, x, w, db=db, act=act, z=z)
+    want, bound = orc.linear_grad(dy, x, w, act, z, dtype)
+    orc.assert_within(db, want[2], bound[2], "db")
+
+
+def test_outputs_asked_for_one_at_a_time(layers):
+    n, t, i, o = 2, 70, 140, 90
+    _, w, _ = layer(n, i, o, BF16, 1)
+    x, dy, z = rows(n, t, i, BF16, 3), rows(n, t, o, BF16, 4), rows(n, t, o, BF16, 5)
+    dx = rows(n, t, i, BF16)
+    _, dw, db = layer(n, i, o, BF16)
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db, act="relu", z=z)
+    for name, all_of in (("dx", dx), ("dw", dw), ("db", db)):
+        alone = torch.empty_like(all_of).fill_(float("nan")) if name != "dx" else rows(n, t, i, BF16)
+        layers.linear_grad(dy, x, w, act="relu", z=z, **{name: alone})
+        assert torch.equal(alone, all_of), name
+    layers.linear_grad(dy, x, w, act="relu", z=z)
+
+
+def test_shared_inputs_other_orders_and_residual_in_place(layers):
+    n, t, i, o = 3, 20, 200, 136
+    _, w, b = layer(1, i, o, F32, 1)
+    w, b = w.expand(n, o, i), b.expand(n, o)                                  # one layer for all learners
+    x = rows(1, t, i, F32, 3).expand(n, t, i)                                 # one batch for all learners
+    y = torch.empty((t, n, o), device="cuda:0").transpose(0, 1)               # tokens outermost in memory
+    r = rows(n, t, o, F32, 4)
+    layers.linear(x, w, y, bias=b, act="silu", residual=r)
+    want, bound = orc.linear(x, w, b, "silu", r, F32)
+    orc.assert_within(y, want[0], bound[0], "y")
+    over = r.contiguous().clone()
+    layers.linear(x, w, over, bias=b, act="silu", residual=over)
+    assert torch.equal(over, y.contiguous())
+    dy = rows(n, t, o, F32, 5)
+    dx, dw, db = torch.empty((t, n, i), device="cuda:0").transpose(0, 1), torch.empty((n, o, i), device="cuda:0"), torch.empty((n, o), device="cuda:0")
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db)
+    want, bound = orc.linear_grad(dy, x, w, "none", None, F32)
+    for got, v, e, what in zip((dx, dw, db), want, bound, ("dx", "dw", "db")):
+        orc.assert_within(got, v, e, what)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_learner_is_the_learner_alone_and_the_same_bits_again(layers, dtype):
+    n, t, i, o = 3, 100, 300, 200
+    _, w, b = layer(n, i, o, dtype, 1)
+    x, y = rows(n, t, i, dtype, 3), rows(n, t, o, dtype)
+    layers.linear(x, w, y, bias=b)
+    again = rows(n, t, o, dtype)
+    layers.linear(x, w, again, bias=b)
+    assert torch.equal(y, again)
+    for k in range(n):                  # rows of other learners do not enter
+        other = x.clone()
+        other[[j for j in range(n) if j != k]] = float("nan")
+        layers.linear(other, w, again, bias=b)
+        assert torch.equal(again[k], y[k]) and (n == 1 or torch.isnan(again[(k + 1) % n]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_that_are_not_finite_stay_apart(layers, dtype):
+    """A row of x that is not finite reaches its own outputs only, also where a tile is cut off."""
+    n, t, i, o = 1, 70, 100, 75
+    _, w, b = layer(n, i, o, dtype, 1)
+    x = rows(n, t, i, dtype, 3)
+    clean, dirty = rows(n, t, o, dtype), rows(n, t, o, dtype)
+    layers.linear(x, w, clean, bias=b)
+    x[0, 69] = float("nan")
+    x[0, 3, 5] = float("inf")
+    layers.linear(x, w, dirty, bias=b)
+    keep = [r for r in range(t) if r not in (3, 69)]
+    assert torch.equal(dirty[0, keep], clean[0, keep]) and not torch.isfinite(dirty[0, 3]).any() and torch.isnan(dirty[0, 69]).all()
+
+
+def test_sizes_of_zero(layers):
+    x, w = torch.empty((2, 3, 0), device="cuda:0"), torch.empty((2, 5, 0), device="cuda:0")
+    b, y, z = normal((2, 5), F32, 1), torch.empty((2, 3, 5), device="cuda:0"), torch.empty((2, 3, 5), device="cuda:0")
+    layers.linear(x, w, y, bias=b, act="relu", z=z)
+    assert torch.equal(z, b[:, None].expand(2, 3, 5)) and torch.equal(y, z.clamp(min=0.0))
+    x, w = torch.empty((2, 0, 4), device="cuda:0"), normal((2, 5, 4), F32, 1)
+    y, dw, db = torch.empty((2, 0, 5), device="cuda:0"), torch.full((2, 5, 4), 7.0, device="cuda:0"), torch.full((2, 5), 7.0, device="cuda:0")
+    layers.linear(x, w, y)
+    layers.linear_grad(y, x, w, dx=torch.empty_like(x), dw=dw, db=db)
+    torch.cuda.synchronize()
+    assert not dw.any() and not db.any()
+
+
+def test_offsets_beyond_32_bits(layers):
+    n, t, i, o = 2, 33, 72, 40
+    far = (1 << 31) + 8
+    _, w, b = layer(n, i, o, BF16, 1)
+    x = torch.empty(2 * far, dtype=BF16, device="cuda:0").as_strided((n, t, i), (far, 1 << 24, 1))
+    x.copy_(normal((n, t, i), BF16, 3))
+    y = rows(n, t, o, BF16)
+    layers.linear(x, w, y, bias=b)
+    want, bound = orc.linear(x, w, b, "none", None, BF16)
+    orc.assert_within(y, want[0], bound[0], "y")
+    near, dw, dy = x.contiguous(), torch.empty((n, o, i), dtype=BF16, device="cuda:0"), rows(n, t, o, BF16, 4)
+    layers.linear_grad(dy, x, w, dw=dw)
+    want, bound = orc.linear_grad(dy, near, w, "none", None, BF16)
+    orc.assert_within(dw, want[1], bound[1], "dw")
+    layers.linear_grad(dy, near, w, dx=x)
+    orc.assert_within(x.contiguous(), want[0], bound[0], "dx")
+
+
+def test_gradient_against_differences(layers):
+    n, t, i, o, e = 2, 9, 33, 21, 1e-5
+    _, w, b = layer(n, i, o, F32, 1)
+    x, dy = rows(n, t, i, F32, 3), rows(n, t, o, F32, 4)
+    z, y = rows(n, t, o, F32), rows(n, t, o, F32)
+    layers.linear(x, w, y, bias=b, act="gelu", z=z)
+    dx, dw, db = torch.empty_like(x), torch.empty((n, o, i), device="cuda:0"), torch.empty((n, o), device="cuda:0")
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db, act="gelu", z=z)
+    _, bounds = orc.linear_grad(dy, x, w, "gelu", z, F32)
+    _, (_, b_z) = orc.linear(x, w, b, "gelu", None, F32)
+    x, w, b, dy = (orc.f64(v) for v in (x, w, b, dy))
+    value = lambda x, w, b: float((dy * orc.act("gelu", torch.matmul(x, w.transpose(1, 2)) + b[:, None])).sum())  # noqa: E731
+    for k, (at, got, bound) in enumerate(zip((x, w, b), (dx, dw, db), bounds)):
+        way = torch.empty(at.shape, dtype=torch.float64).normal_(generator=torch.Generator().manual_seed(50 + k))
+        args = [[v + s * e * way if j == k else v for j, v in enumerate((x, w, b))] for s in (1, -1)]
+        slope = (value(*args[0]) - value(*args[1])) / (2 * e)
+        # z entered the kernel rounded: the slope's own slope is at most 1 there
+        moved = (torch.matmul(way.abs(), w.abs().transpose(1, 2)) if k == 0 else torch.matmul(x.abs(), way.abs().transpose(1, 2)) if k == 1
+                 else way.abs()[:, None].expand(n, t, o))
+        assert abs(slope - float((orc.f64(got) * way).sum())) <= float((bound * way.abs()).sum()) + float((dy.abs() * b_z * moved).sum()) + 1e-7
+
+
+def test_other_streams_workspaces_and_graphs(layers):
+    n, t, i, o = 2, 65, 2000, 130
+    _, w, b = layer(n, i, o, BF16, 1)
+    x, dy, z, y = rows(n, t, i, BF16, 3), rows(n, t, o, BF16, 4), rows(n, t, o, BF16), rows(n, t, o, BF16)
+    layers.linear(x, w, y, bias=b, act="gelu", z=z)
+    dx, dw, db = torch.empty_like(x), torch.empty((n, o, i), dtype=BF16, device="cuda:0"), torch.empty((n, o), dtype=BF16, device="cuda:0")
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db, act="gelu", z=z)
+    torch.cuda.synchronize()
+    want = [v.clone() for v in (y, dx, dw, db)]
+    outs = [torch.empty_like(v) for v in want]
+
+    def both(**kw):
+        layers.linear(x, w, outs[0], bias=b, act="gelu", **kw)
+        layers.linear_grad(dy, x, w, dx=outs[1], dw=outs[2], db=outs[3], act="gelu", z=z, **kw)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    both(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(outs, want))
+    both(workspace=torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda:0"))
+    assert all(torch.equal(a, c) for a, c in zip(outs, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for k in range(3):
+        for v in outs:
+            v.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(outs, want)), k
