@@ -125,67 +125,119 @@ template <int WORDS, typename T> __device__ __forceinline__ u32x4 load_words(con
         return (u32x4){*reinterpret_cast<const u32_any*>(p), 0u, 0u, 0u};
     }
 }
-// The same element by element, the ones from `last` on alike: a row's end inside the words.
-template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const float* p, int64_t last) {
+// The same element by element, none beyond p[last]: the ones behind it repeat it.  No branches: loads that wait for one another would cost more.
+template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const float* p, int last) {
     u32x4 v = {};
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) v[i] = __float_as_uint(p[i < last ? i : last]);
     return v;
 }
-template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const uint16_t* p, int64_t last) {
+template <int WORDS> __device__ __forceinline__ u32x4 load_words_to(const uint16_t* p, int last) {
     u32x4 v = {};
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) v[i] = (uint32_t)p[2 * i < last ? 2 * i : last] | (uint32_t)p[2 * i + 1 < last ? 2 * i + 1 : last] << 16;
     return v;
 }
+// A chunk from its element `by` on, zeros behind.
+template <typename T> __device__ __forceinline__ u32x4 chunk_from(u32x4 v, int by) {
+    const int words = by * (int)sizeof(T) / 4;
+    if (words & 1) v = (u32x4){v.y, v.z, v.w, 0u};
+    if (words & 2) v = (u32x4){v.z, v.w, 0u, 0u};
+    if (words & 4) v = (u32x4){};
+    if (sizeof(T) == 2 && by % 2) v = (u32x4){v.x >> 16 | v.y << 16, v.y >> 16 | v.z << 16, v.z >> 16 | v.w << 16, v.w >> 16};
+    return v;
+}
+// `left` < kPer<T> elements of a row that has no more, one after the other, zeros behind.
+template <typename T> __device__ __forceinline__ u32x4 chunk_of_few(const T* p, int left) {
+    u32x4 v = {};
+#pragma unroll 1
+    for (int e = 0; e < left; ++e) {
+        const uint32_t x = sizeof(T) == 4 ? __float_as_uint(load_1(p + e)) : __float_as_uint(load_1(p + e)) >> 16 << e % 2 * 16;
+        const int word = e * (int)sizeof(T) / 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] |= i == word ? x : 0u;
+    }
+    return v;
+}
 
 // One operand's way into LDS: ROWS rows by a tile's depth of k, through the registers of NT lanes.  ALONG: memory has k along its rows; then a
 // lane brings chunks.  Otherwise memory's rows are k: a lane brings blocks of E values of k (E elements to 16 bytes) by WIDE rows of the tile, and
-// turns them.
+// turns them.  Rows of the tile beyond the operand's last are not stored by anyone, so they may hold anything: chunks of the last row again, or
+// what LDS held before.  A block that would reach beyond the last row is one that ends there.
 template <typename T, int ROWS, int NT, bool ALONG> struct Bring {
     static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / NT;      // chunks a lane brings
     static constexpr int WIDE = COUNT < E ? COUNT : E, BLOCKS = COUNT / WIDE, WORDS = WIDE * (int)sizeof(T) / 4;
     static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0, "whole chunks and blocks a lane");
     static constexpr int SIDE = ALONG ? 4 : WORDS, LINES = COUNT * 4 / SIDE;     // as loaded: whole chunks, or E lines a block
+    static constexpr int STARTS = ALONG ? COUNT : BLOCKS;
     u32x4 raw[LINES];          // of which the first SIDE words
+    const T* from[STARTS];     // where the lane's chunks and blocks start, at k = 0
+    int place[STARTS];         // and the row of the tile
+    int64_t pitch;
+    int few;                   // rows of an operand that has fewer than a block, else 0
 
-    // rows from `row0` (of `rows`), k from k0 up to `end`
-    __device__ __forceinline__ void fetch(const T* base, int64_t pitch, int64_t row0, int64_t rows, int64_t k0, int64_t end) {
-        const int tid = threadIdx.x, c = tid % 8;
-        const int64_t k = k0 + c * E, left = end - k;
+    // rows from `row0` of `rows`
+    __device__ __forceinline__ void start(const T* base, int64_t pitch_, int64_t row0, int64_t rows) {
+        const int line = threadIdx.x / 8, c = threadIdx.x % 8;
+        pitch = pitch_;
+        few = !ALONG && rows < WIDE ? (int)rows : 0;
+#pragma unroll
+        for (int j = 0; j < STARTS; ++j) {
+            if constexpr (ALONG) {
+                place[j] = line + j * (NT / 8);
+                const int64_t r = row0 + place[j];
+                from[j] = base + (r < rows ? r : rows - 1) * pitch + c * E;
+            } else {
+                int64_t r = row0 + (line + j * (NT / 8)) * WIDE;
+                if (r + WIDE > rows) r = few ? 0 : rows - WIDE;
+                place[j] = (int)(r - row0);
+                from[j] = base + c * E * pitch + r;
+            }
+        }
+    }
+    // The whole depth from k0 is there.
+    __device__ __forceinline__ void fetch(int64_t k0) {
+        if constexpr (ALONG) {
+#pragma unroll
+            for (int j = 0; j < COUNT; ++j) raw[j] = load_raw(from[j] + k0);
+        } else {
+#pragma unroll
+            for (int s = 0; s < BLOCKS; ++s)
+#pragma unroll
+                for (int j = 0; j < E; ++j) raw[s * E + j] = load_words<WORDS>(from[s] + (k0 + j) * pitch);
+        }
+    }
+    // Only k < end is there, the rest counts as zero; or the operand has fewer rows than a block.
+    __device__ __forceinline__ void fetch_upto(int64_t k0, int64_t end) {
+        const int c = threadIdx.x % 8, left = (int)(end - k0) - c * E;       // of the lane's E values of k
         if constexpr (ALONG) {
 #pragma unroll
             for (int j = 0; j < COUNT; ++j) {
-                int64_t r = row0 + tid / 8 + j * (NT / 8);
-                r = r < rows ? r : rows - 1;              // rows beyond the last are multiplied but not stored
-                raw[j] = load_cols(base + r * pitch + k, left);
+                const T* p = from[j] + k0;
+                if (end < E) {
+                    raw[j] = chunk_of_few(p, left);
+                } else {                                                      // the row's last whole chunk, moved up
+                    const int by = left >= E ? 0 : left <= 0 ? E : E - left;
+                    raw[j] = chunk_from<T>(load_raw(p - (left >= E ? 0 : E - left)), by);
+                }
             }
         } else {
 #pragma unroll
-            for (int s = 0; s < BLOCKS; ++s) {
-                const int64_t r = row0 + (tid / 8 + s * (NT / 8)) * WIDE;
-                const T* from = base + k * pitch + r;
-                if (r + WIDE <= rows && left >= E) {
+            for (int s = 0; s < BLOCKS; ++s)
 #pragma unroll
-                    for (int j = 0; j < E; ++j) raw[s * E + j] = load_words<WORDS>(from + j * pitch);
-                } else {          // columns and values of k that there are; k beyond the end counts as zero, the tile's rows beyond the last are not stored
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const int64_t kj = k + j < end ? k + j : end - 1, rj = r < rows ? r : rows - 1;
-                        const u32x4 v = load_words_to<WORDS>(base + kj * pitch + rj, rows - 1 - rj);
-                        raw[s * E + j] = k + j < end ? v : (u32x4){};
-                    }
+                for (int j = 0; j < E; ++j) {
+                    const T* p = from[s] + (k0 + (j < left ? j : left - 1)) * pitch;      // the last line again, possibly of another chunk
+                    const u32x4 v = few ? load_words_to<WORDS>(p, few - 1) : load_words<WORDS>(p);
+                    raw[s * E + j] = j < left ? v : (u32x4){};
                 }
-            }
         }
     }
 
     __device__ __forceinline__ void put(char* tile) const {
-        const int tid = threadIdx.x, c = tid % 8;
+        const int c = threadIdx.x % 8;
         if constexpr (ALONG) {
 #pragma unroll
-            for (int j = 0; j < COUNT; ++j) 
-                *reinterpret_cast<u32x4*>(tile + tile_place(tid / 8 + j * (NT / 8), c)) = raw[j];
+            for (int j = 0; j < COUNT; ++j) *reinterpret_cast<u32x4*>(tile + tile_place(place[j], c)) = raw[j];
         } else {
 #pragma unroll
             for (int s = 0; s < BLOCKS; ++s)
@@ -199,7 +251,8 @@ template <typename T, int ROWS, int NT, bool ALONG> struct Bring {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(raw[s * 8 + 2 * j + 1][e / 2], raw[s * 8 + 2 * j][e / 2], pick);
                     }
-                    *reinterpret_cast<u32x4*>(tile + tile_place((tid / 8 + s * (NT / 8)) * WIDE + e, c)) = v;
+                    // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
+                    *reinterpret_cast<u32x4*>(tile + tile_place((place[s] + e) & (ROWS - 1), c)) = v;
                 }
         }
     }
@@ -253,38 +306,71 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs a) {
         for (int j = 0; j < TM; ++j) acc[i][j] = (f32x16){};
     Bring<T, BM, NT, P_ALONG> bp;
     Bring<T, BN, NT, Q_ALONG> bq;
-    if (from < to) {
-        bp.fetch(p, a.p.pitch, m0, a.m, from * BK, a.k);
-        bq.fetch(q, a.q.pitch, n0, a.n, from * BK, a.k);
-        bp.put(lds);
-        bq.put(lds + kP);
-    }
-    __syncthreads();
+    bp.start(p, a.p.pitch, m0, a.m);
+    bq.start(q, a.q.pitch, n0, a.n);
     const int mw = wave % 2 * (BM / 2) + lane % 32, nw = wave / 2 * (BN / 2) + lane % 32;
-    for (int64_t tile = from; tile < to; ++tile) {
-        const char* now = lds + (tile - from) % 2 * kBoth;
-        char* next = lds + (tile - from + 1) % 2 * kBoth;
-        const bool more = tile + 1 < to;
-        if (more) {
-            bp.fetch(p, a.p.pitch, m0, a.m, (tile + 1) * BK, a.k);
-            bq.fetch(q, a.q.pitch, n0, a.n, (tile + 1) * BK, a.k);
-        }
+    // The chunks of one step of 16 bytes of k, and its products.
+    struct Step {
+        u32x4 p[TM], q[TN];
+    };
+    auto read = [&](const char* now, int s, Step& f) {
+#pragma unroll
+        for (int j = 0; j < TM; ++j) f.p[j] = *reinterpret_cast<const u32x4*>(now + tile_place(mw + 32 * j, 2 * s + lane / 32));
+#pragma unroll
+        for (int i = 0; i < TN; ++i) f.q[i] = *reinterpret_cast<const u32x4*>(now + kP + tile_place(nw + 32 * i, 2 * s + lane / 32));
+    };
+    auto products = [&](const Step& f) {
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j) multiply(f.q[i], f.p[j], acc[i][j], T{});
+    };
+    // A tile of k: each step's chunks are read while the one before is multiplied, and `between` (what brings the next tile) goes before the last
+    // step's products.  The fences keep the compiler from sinking loads to where they are used.
+    auto multiply_tile = [&](const char* now, auto between) {
+        Step f[2];
+        read(now, 0, f[0]);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            u32x4 fp[TM], fq[TN];
-#pragma unroll
-            for (int j = 0; j < TM; ++j) fp[j] = *reinterpret_cast<const u32x4*>(now + tile_place(mw + 32 * j, 2 * s + lane / 32));
-#pragma unroll
-            for (int i = 0; i < TN; ++i) fq[i] = *reinterpret_cast<const u32x4*>(now + kP + tile_place(nw + 32 * i, 2 * s + lane / 32));
-#pragma unroll
-            for (int i = 0; i < TN; ++i)
-#pragma unroll
-                for (int j = 0; j < TM; ++j) multiply(fq[i], fp[j], acc[i][j], T{});
+            if (s < 3) read(now, s + 1, f[(s + 1) % 2]);
+            else between();
+            __builtin_amdgcn_sched_barrier(0);
+            products(f[s % 2]);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (more) {
-            bp.put(next);
-            bq.put(next + kP);
+    };
+    // Tiles of k that are there to their end: the next one travels while this one is multiplied.
+    const int64_t last = a.k / BK, whole = bp.few || bq.few ? from : to < last ? to : last;
+    int64_t tile = from;
+    if (tile < whole) {
+        bp.fetch(tile * BK);
+        bq.fetch(tile * BK);
+        bp.put(lds);
+        bq.put(lds + kP);
+        __syncthreads();
+        int side = 0;
+        for (; tile + 1 < whole; ++tile) {
+            bp.fetch((tile + 1) * BK);
+            bq.fetch((tile + 1) * BK);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply_tile(lds + side, [&] {
+                bp.put(lds + kBoth - side);
+                bq.put(lds + kBoth - side + kP);
+            });
+            side = kBoth - side;
+            __syncthreads();
         }
+        multiply_tile(lds + side, [] {});
+        ++tile;
+        __syncthreads();
+    }
+    for (; tile < to; ++tile) {
+        bp.fetch_upto(tile * BK, a.k);
+        bq.fetch_upto(tile * BK, a.k);
+        bp.put(lds);
+        bq.put(lds + kP);
+        __syncthreads();
+        multiply_tile(lds, [] {});
         __syncthreads();
     }
     // Lane l holds column l % 32 of m and, of each 32 of n, four stretches of four: 8 g + 4 (l / 32) .. + 3.  Through LDS, 32 rows of m at a time, so that
