@@ -12,6 +12,7 @@
 #include "psgd_rows.h"
 
 #include <initializer_list>
+#include <type_traits>
 
 namespace psgd {
 namespace {
@@ -27,18 +28,28 @@ struct Operand {          // element (row, col) of learner i at p + i * learner 
 
 constexpr float kLog2E = 1.44269504088896341f;
 
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+// erf by Hastings' rational approximation (Abramowitz and Stegun 7.1.26), off by at most 1.5e-7 anywhere: a seventh of the instructions of one that is
+// exact to the last place, which the epilogue of a large tile waits for.  What it leaves in z Phi(z) is 8e-8 |z|.
+__device__ __forceinline__ float erf_of(float x) {
+    const float a = __builtin_fabsf(x), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, a, 1.0f));
+    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+    p = __builtin_fmaf(p, t, 1.421413741f);
+    p = __builtin_fmaf(p, t, -0.284496736f);
+    p = __builtin_fmaf(p, t, 0.254829592f);
+    return __builtin_copysignf(1.0f - p * t * exp_of(-a * a), x);
+}
 template <int ACT> __device__ __forceinline__ float act_of(float z) {
     if (ACT == PSGD_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == PSGD_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    if (ACT == PSGD_ACT_SILU) return z / (1.0f + __builtin_amdgcn_exp2f(-z * kLog2E));
+    if (ACT == PSGD_ACT_GELU) return 0.5f * z * (1.0f + erf_of(z * 0.70710678118654752f));
+    if (ACT == PSGD_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
     return z;
 }
 template <int ACT> __device__ __forceinline__ float slope_of(float z) {
     if (ACT == PSGD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (ACT == PSGD_ACT_GELU)
-        return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * __builtin_amdgcn_exp2f(-0.5f * kLog2E * z * z) * 0.39894228040143268f;
+    if (ACT == PSGD_ACT_GELU) return 0.5f * (1.0f + erf_of(z * 0.70710678118654752f)) + z * exp_of(-0.5f * z * z) * 0.39894228040143268f;
     if (ACT == PSGD_ACT_SILU) {
-        const float p = 1.0f / (1.0f + __builtin_amdgcn_exp2f(-z * kLog2E));
+        const float p = __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
         return p * (1.0f + z * (1.0f - p));
     }
     return 1.0f;
@@ -62,55 +73,40 @@ struct GemmArgs {
 constexpr int kRowBytes = 128;                     // a row of the LDS tile: 64 bf16 or 32 floats of k, as eight chunks of 16 bytes
 template <typename T> constexpr int kDepth = kRowBytes / (int)sizeof(T);
 
-// Chunk c of row r lies at place c ^ (r & 7) of its row: eight lanes that read one chunk of eight rows, or write eight chunks of one row, then
-// touch all banks once.
-__device__ __forceinline__ int tile_place(int r, int c) { return r * kRowBytes + ((c ^ (r & 7)) << 4); }
-
-// Four consecutive elements, any alignment.
-__device__ __forceinline__ void load_4(const float* p, int64_t left, float (&v)[4]) { widen<float>(load_cols(p, left), v); }
-__device__ __forceinline__ void load_4(const uint16_t* p, int64_t left, float (&v)[4]) {
-    if (left >= 4) {
-        const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
-        v[0] = low_bf16(r.x), v[1] = high_bf16(r.x), v[2] = low_bf16(r.y), v[3] = high_bf16(r.y);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = i < left ? load_1(p + i) : 0.0f;
-    }
-}
-__device__ __forceinline__ void store_4(float* p, const float (&v)[4], int64_t left) { store_cols<float>(p, v, left); }
-__device__ __forceinline__ void store_4(uint16_t* p, const float (&v)[4], int64_t left) {
-    if (left >= 4) {
-        *reinterpret_cast<u32x2_any*>(p) = (u32x2){two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < left) store_1(p + i, v[i]);
-    }
+// Where chunk c of row r lies.  LDS serves 16 lanes of a 16-byte access at a time, from 64 banks: two rows.  Lanes that read one chunk of 16 rows
+// next to each other, that write the eight chunks of two rows, or four chunks of four rows eight or four apart (turned blocks) find them in
+// 16 different places.  (Chunk c at place c ^ (r & 7), which serves eight lanes at a time: twice the time for each read.)  Rows 32 apart differ
+// by a constant.
+__device__ __forceinline__ int tile_place(int r, int c) {
+    const int pair = r >> 1, half = (r ^ (pair >> 1) ^ (pair >> 2)) & 1;
+    return pair * (2 * kRowBytes) + half * kRowBytes + (((c ^ pair ^ (r >> 2 & 4)) & 7) << 4);
 }
 
-// What is left of an output's four columns after the sum over k.
+// What is left of an output's 16 bytes of columns after the sum over k.
 template <typename T>
-__device__ __forceinline__ void finish(const Epilogue& a, int64_t learner, int64_t m, int64_t n, int64_t left, const float (&bias)[4], float (&v)[4]) {
+__device__ __forceinline__ void finish(const Epilogue& a, int64_t learner, int64_t m, int64_t n, int64_t left, const float (&bias)[kPer<T>],
+                                       float (&v)[kPer<T>]) {
+    constexpr int E = kPer<T>;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += bias[e];
-    if (a.z.p) store_4(reinterpret_cast<T*>(const_cast<char*>(a.z.p)) + learner * a.z.learner + m * a.z.pitch + n, v, left);
+    for (int e = 0; e < E; ++e) v[e] += bias[e];
+    if (a.z.p) store_cols<T>(reinterpret_cast<T*>(const_cast<char*>(a.z.p)) + learner * a.z.learner + m * a.z.pitch + n, v, left);
     if (a.act == PSGD_ACT_RELU) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_RELU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_RELU>(v[e]);
     } else if (a.act == PSGD_ACT_GELU) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_GELU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_GELU>(v[e]);
     } else if (a.act == PSGD_ACT_SILU) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = act_of<PSGD_ACT_SILU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_SILU>(v[e]);
     }
     if (a.residual.p) {
-        float r[4];
-        load_4(reinterpret_cast<const T*>(a.residual.p) + learner * a.residual.learner + m * a.residual.pitch + n, left, r);
+        float r[E];
+        widen<T>(load_cols(reinterpret_cast<const T*>(a.residual.p) + learner * a.residual.learner + m * a.residual.pitch + n, left), r);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += r[e];
+        for (int e = 0; e < E; ++e) v[e] += r[e];
     }
-    store_4(reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + learner * a.y.learner + m * a.y.pitch + n, v, left);
+    store_cols<T>(reinterpret_cast<T*>(const_cast<char*>(a.y.p)) + learner * a.y.learner + m * a.y.pitch + n, v, left);
 }
 
 // Up to four words of elements, any alignment.
@@ -160,100 +156,121 @@ template <typename T> __device__ __forceinline__ u32x4 chunk_of_few(const T* p, 
     return v;
 }
 
-// One operand's way into LDS: ROWS rows by a tile's depth of k, through the registers of NT lanes.  ALONG: memory has k along its rows; then a
-// lane brings chunks.  Otherwise memory's rows are k: a lane brings blocks of E values of k (E elements to 16 bytes) by WIDE rows of the tile, and
-// turns them.  Rows of the tile beyond the operand's last are not stored by anyone, so they may hold anything: chunks of the last row again, or
-// what LDS held before.  A block that would reach beyond the last row is one that ends there.
-template <typename T, int ROWS, int NT, bool ALONG> struct Bring {
-    static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / NT;      // chunks a lane brings
+// One operand's way into LDS: ROWS rows by a tile's depth of k, through the registers of LANES lanes (half of the workgroup; the other half brings
+// the other operand).  ALONG: memory has k along its rows; then a lane brings chunks.  Otherwise memory's rows are k: a lane brings blocks of E
+// values of k (E elements to 16 bytes) by WIDE rows of the tile, and turns them.  Rows of the tile beyond the operand's last are not stored by
+// anyone, so they may hold anything: chunks of the last row again, or what LDS held before.  A block that would reach beyond the last row
+// is one that ends there.
+template <typename T, int ROWS, int LANES> struct Bring {
+    static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / LANES;      // chunks a lane brings
     static constexpr int WIDE = COUNT < E ? COUNT : E, BLOCKS = COUNT / WIDE, WORDS = WIDE * (int)sizeof(T) / 4;
     static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0, "whole chunks and blocks a lane");
-    static constexpr int SIDE = ALONG ? 4 : WORDS, LINES = COUNT * 4 / SIDE;     // as loaded: whole chunks, or E lines a block
-    static constexpr int STARTS = ALONG ? COUNT : BLOCKS;
-    u32x4 raw[LINES];          // of which the first SIDE words
-    const T* from[STARTS];     // where the lane's chunks and blocks start, at k = 0
-    int place[STARTS];         // and the row of the tile
+
+    const T* base;             // of the tile's first row, or column, at the lane's first k
     int64_t pitch;
+    int line, c;               // the lane's first chunk or block, and its chunk of k
+    int rows;                  // of the operand from the tile's first on, at most INT_MAX / 2
     int few;                   // rows of an operand that has fewer than a block, else 0
 
-    // rows from `row0` of `rows`
-    __device__ __forceinline__ void start(const T* base, int64_t pitch_, int64_t row0, int64_t rows) {
-        const int line = threadIdx.x / 8, c = threadIdx.x % 8;
-        pitch = pitch_;
-        few = !ALONG && rows < WIDE ? (int)rows : 0;
-#pragma unroll
-        for (int j = 0; j < STARTS; ++j) {
-            if constexpr (ALONG) {
-                place[j] = line + j * (NT / 8);
-                const int64_t r = row0 + place[j];
-                from[j] = base + (r < rows ? r : rows - 1) * pitch + c * E;
-            } else {
-                int64_t r = row0 + (line + j * (NT / 8)) * WIDE;
-                if (r + WIDE > rows) r = few ? 0 : rows - WIDE;
-                place[j] = (int)(r - row0);
-                from[j] = base + c * E * pitch + r;
-            }
+    template <bool ALONG> __device__ __forceinline__ void start(const T* p, int64_t pitch_, int64_t row0, int64_t all) {
+        const int tid = threadIdx.x % LANES;
+        if (ALONG) {
+            line = tid / 8;
+            c = tid % 8;
+        } else {      // four lanes side by side along memory's rows: lanes that jump from row to row are served one a cycle
+            const int w = tid / kWave;
+            line = tid % 4 + tid / 16 % 4 * 4 + w % (LANES / 128) * 16;
+            c = tid / 4 % 4 + w / (LANES / 128) * 4;
         }
+        pitch = pitch_;
+        rows = (int)(all - row0 < (1 << 30) ? all - row0 : (1 << 30));
+        few = !ALONG && all < WIDE ? (int)all : 0;
+        base = ALONG ? p + row0 * pitch + c * E : p + c * E * pitch + row0;
     }
-    // The whole depth from k0 is there.
-    __device__ __forceinline__ void fetch(int64_t k0) {
-        if constexpr (ALONG) {
+    // Where chunk or block j starts in memory, from `base`, and in the tile.  Computed where it is used: kept, they would cost registers that the
+    // products need.
+    template <bool ALONG> __device__ __forceinline__ int row_of(int j) const {
+        const int r = ALONG ? line + j * (LANES / 8) : (line + j * (LANES / 8)) * WIDE;
+        return ALONG || few || r + WIDE <= rows ? r : rows - WIDE;
+    }
+    template <bool ALONG> __device__ __forceinline__ const T* from(int j) const {
+        if (ALONG) {
+            const int r = row_of<ALONG>(j);
+            return base + (r < rows ? r : rows - 1) * pitch;
+        }
+        return base + (few ? 0 : row_of<ALONG>(j));
+    }
+    // The whole depth from k0 is there.  Chunks, or lines, first to end - 1.
+    static constexpr int loads(bool along) { return along ? COUNT : BLOCKS * E; }
+    template <bool ALONG> __device__ __forceinline__ void fetch(u32x4 (&raw)[COUNT], int64_t k0, int first = 0, int end = loads(ALONG)) {
+        asm volatile("" : "+v"(line));                  // not outside of the loop
 #pragma unroll
-            for (int j = 0; j < COUNT; ++j) raw[j] = load_raw(from[j] + k0);
-        } else {
-#pragma unroll
-            for (int s = 0; s < BLOCKS; ++s)
-#pragma unroll
-                for (int j = 0; j < E; ++j) raw[s * E + j] = load_words<WORDS>(from[s] + (k0 + j) * pitch);
+        for (int l = first; l < end; ++l) {
+            if constexpr (ALONG) raw[l] = load_raw(from<true>(l) + k0);
+            else keep(raw, l, load_words<WORDS>(from<false>(l / E) + (k0 + l % E) * pitch));
+            __builtin_amdgcn_sched_barrier(0);      // one address at a time
         }
     }
     // Only k < end is there, the rest counts as zero; or the operand has fewer rows than a block.
-    __device__ __forceinline__ void fetch_upto(int64_t k0, int64_t end) {
-        const int c = threadIdx.x % 8, left = (int)(end - k0) - c * E;       // of the lane's E values of k
-        if constexpr (ALONG) {
+    template <bool ALONG> __device__ __forceinline__ void fetch_upto(u32x4 (&raw)[COUNT], int64_t k0, int64_t end) {
+        const int left = (int)(end - k0) - c * E;       // of the lane's E values of k
 #pragma unroll
-            for (int j = 0; j < COUNT; ++j) {
-                const T* p = from[j] + k0;
+        for (int s = 0; s < (ALONG ? COUNT : BLOCKS); ++s) {
+            const T* p = from<ALONG>(s);
+            if constexpr (ALONG) {
                 if (end < E) {
-                    raw[j] = chunk_of_few(p, left);
+                    raw[s] = chunk_of_few(p + k0, left);
                 } else {                                                      // the row's last whole chunk, moved up
                     const int by = left >= E ? 0 : left <= 0 ? E : E - left;
-                    raw[j] = chunk_from<T>(load_raw(p - (left >= E ? 0 : E - left)), by);
+                    raw[s] = chunk_from<T>(load_raw(p + k0 - (left >= E ? 0 : E - left)), by);
                 }
-            }
-        } else {
-#pragma unroll
-            for (int s = 0; s < BLOCKS; ++s)
+            } else {
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    const T* p = from[s] + (k0 + (j < left ? j : left - 1)) * pitch;      // the last line again, possibly of another chunk
-                    const u32x4 v = few ? load_words_to<WORDS>(p, few - 1) : load_words<WORDS>(p);
-                    raw[s * E + j] = j < left ? v : (u32x4){};
+                    const T* q = p + (k0 + (j < left ? j : left - 1)) * pitch;      // the last line again, possibly of another chunk
+                    const u32x4 v = few ? load_words_to<WORDS>(q, few - 1) : load_words<WORDS>(q);
+                    keep(raw, s * E + j, j < left ? v : (u32x4){});
                 }
+            }
         }
     }
+    // Lines of WORDS words, one after the other in the registers.
+    static __device__ __forceinline__ void keep(u32x4 (&raw)[COUNT], int n, u32x4 v) {
+#pragma unroll
+        for (int w = 0; w < WORDS; ++w) raw[(n * WORDS + w) / 4][(n * WORDS + w) % 4] = v[w];
+    }
+    static __device__ __forceinline__ uint32_t word(const u32x4 (&raw)[COUNT], int n, int w) { return raw[(n * WORDS + w) / 4][(n * WORDS + w) % 4]; }
 
-    __device__ __forceinline__ void put(char* tile) const {
-        const int c = threadIdx.x % 8;
+    template <bool ALONG> __device__ __forceinline__ void put(const u32x4 (&raw)[COUNT], char* tile, int first = 0, int end = COUNT) const {
+#pragma unroll
+        for (int n = first; n < end; ++n) {
+            if constexpr (ALONG) {
+                *reinterpret_cast<u32x4*>(tile + tile_place(row_of<true>(n), c)) = raw[n];
+            } else {
+                const int s = n / WIDE, e = n % WIDE;
+                u32x4 v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if constexpr (sizeof(T) == 4)
+                        v[j] = word(raw, s * 4 + j, e);
+                    else      // the upper or lower halves of two words
+                        v[j] = __builtin_amdgcn_perm(word(raw, s * 8 + 2 * j + 1, e / 2), word(raw, s * 8 + 2 * j, e / 2), e % 2 ? 0x07060302u : 0x05040100u);
+                // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
+                *reinterpret_cast<u32x4*>(tile + tile_place(((few ? 0 : row_of<false>(s)) + e) & (ROWS - 1), c)) = v;
+            }
+        }
+    }
+    // Slot `slot` of `slots` in a tile's products: this lane's part of putting the next tile, which is in `raw`, into LDS, and of sending for the
+    // one behind it, so that what is sent for travels for the time of a tile.  Chunks go one after the other, spread over the tile (2 % faster than
+    // all at once); blocks are turned, which takes all of their lines, so they go together (in quarters: 4 % slower).
+    template <bool ALONG> __device__ __forceinline__ void turn_over(u32x4 (&raw)[COUNT], char* tile, bool more, int64_t k0, int slot, int slots) {
         if constexpr (ALONG) {
-#pragma unroll
-            for (int j = 0; j < COUNT; ++j) *reinterpret_cast<u32x4*>(tile + tile_place(place[j], c)) = raw[j];
-        } else {
-#pragma unroll
-            for (int s = 0; s < BLOCKS; ++s)
-#pragma unroll
-                for (int e = 0; e < WIDE; ++e) {
-                    u32x4 v;
-                    if constexpr (sizeof(T) == 4) {
-                        v = (u32x4){raw[s * 4][e], raw[s * 4 + 1][e], raw[s * 4 + 2][e], raw[s * 4 + 3][e]};
-                    } else {
-                        const uint32_t pick = e % 2 ? 0x07060302u : 0x05040100u;      // the upper or lower halves of two words
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) v[j] = __builtin_amdgcn_perm(raw[s * 8 + 2 * j + 1][e / 2], raw[s * 8 + 2 * j][e / 2], pick);
-                    }
-                    // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
-                    *reinterpret_cast<u32x4*>(tile + tile_place((place[s] + e) & (ROWS - 1), c)) = v;
-                }
+            const int first = slot * COUNT / slots, end = (slot + 1) * COUNT / slots;
+            put<true>(raw, tile, first, end);
+            if (more) fetch<true>(raw, k0, first, end);
+        } else if (slot == slots / 4) {
+            put<false>(raw, tile);
+            if (more) fetch<false>(raw, k0);
         }
     }
 };
@@ -287,9 +304,10 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& a) {
     return o;
 }
 
-template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG>
-__global__ __launch_bounds__(256) void gemm_kernel(GemmArgs a) {
-    constexpr int NT = 256, TM = BM / 64, TN = BN / 64, BK = kDepth<T>;      // four wavefronts, two by two; 32 x 32 tiles of each
+template <typename T, int BM, int BN, int ACROSS_N, bool P_ALONG, bool Q_ALONG>
+__global__ __launch_bounds__(128 * ACROSS_N) void gemm_kernel(GemmArgs a) {
+    // wavefronts, two along m by ACROSS_N along n; 32 x 32 tiles of each
+    constexpr int NT = 128 * ACROSS_N, TM = BM / 64, TN = BN / 32 / ACROSS_N, BK = kDepth<T>, WN = BN / ACROSS_N;
     extern __shared__ __attribute__((aligned(128))) char lds[];
     constexpr int kP = BM * kRowBytes, kBoth = (BM + BN) * kRowBytes;
     const Tile t = tile_of(a);
@@ -304,82 +322,92 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs a) {
     for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int j = 0; j < TM; ++j) acc[i][j] = (f32x16){};
-    Bring<T, BM, NT, P_ALONG> bp;
-    Bring<T, BN, NT, Q_ALONG> bq;
-    bp.start(p, a.p.pitch, m0, a.m);
-    bq.start(q, a.q.pitch, n0, a.n);
-    const int mw = wave % 2 * (BM / 2) + lane % 32, nw = wave / 2 * (BN / 2) + lane % 32;
+    static_assert(BM == BN, "the halves of the workgroup bring as many chunks a lane");
+    static_assert(BM == BN, "the halves of the workgroup bring as many chunks a lane");
+    const bool first = __builtin_amdgcn_readfirstlane(threadIdx.x) < NT / 2;      // which operand the wavefront brings
+    Bring<T, BM, NT / 2> bring;
+    u32x4 raw[bring.COUNT];
+    char* const mine_at = first ? lds : lds + kP;
+    if (first) bring.template start<P_ALONG>(p, a.p.pitch, m0, a.m);
+    else bring.template start<Q_ALONG>(q, a.q.pitch, n0, a.n);
+    const bool few = (!P_ALONG && a.m < bring.WIDE) || (!Q_ALONG && a.n < bring.WIDE);      // the same for the whole workgroup
+    const int mw = wave % 2 * (BM / 2) + lane % 32, nw = wave / 2 * WN + lane % 32;
     // The chunks of one step of 16 bytes of k, and its products.
     struct Step {
         u32x4 p[TM], q[TN];
     };
+    int at_p = tile_place(mw, lane / 32), at_q = kP + tile_place(nw, lane / 32);      // step s: place ^ (s << 5)
     auto read = [&](const char* now, int s, Step& f) {
+        asm volatile("" : "+v"(at_p), "+v"(at_q));      // one register each, not one a step
 #pragma unroll
-        for (int j = 0; j < TM; ++j) f.p[j] = *reinterpret_cast<const u32x4*>(now + tile_place(mw + 32 * j, 2 * s + lane / 32));
+        for (int j = 0; j < TM; ++j) f.p[j] = *reinterpret_cast<const u32x4*>(now + (at_p ^ (s << 5)) + 32 * j * kRowBytes);
 #pragma unroll
-        for (int i = 0; i < TN; ++i) f.q[i] = *reinterpret_cast<const u32x4*>(now + kP + tile_place(nw + 32 * i, 2 * s + lane / 32));
+        for (int i = 0; i < TN; ++i) f.q[i] = *reinterpret_cast<const u32x4*>(now + (at_q ^ (s << 5)) + 32 * i * kRowBytes);
     };
-    auto products = [&](const Step& f) {
-#pragma unroll
-        for (int i = 0; i < TN; ++i)
-#pragma unroll
-            for (int j = 0; j < TM; ++j) multiply(f.q[i], f.p[j], acc[i][j], T{});
-    };
-    // A tile of k: each step's chunks are read while the one before is multiplied, and `between` (what brings the next tile) goes before the last
-    // step's products.  The fences keep the compiler from sinking loads to where they are used.
-    auto multiply_tile = [&](const char* now, auto between) {
+    // A tile of k: each step's chunks are read while the one before is multiplied, and the next tile is brought in between (turn_over).  The fences
+    // keep the compiler from sinking loads to their uses.
+    auto multiply_tile = [&](const char* now, auto meanwhile) {
         Step f[2];
         read(now, 0, f[0]);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             if (s < 3) read(now, s + 1, f[(s + 1) % 2]);
-            else between();
-            __builtin_amdgcn_sched_barrier(0);
-            products(f[s % 2]);
-            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                meanwhile(s * TN + i);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int j = 0; j < TM; ++j) multiply(f[s % 2].q[i], f[s % 2].p[j], acc[i][j], T{});
+            }
         }
     };
-    // Tiles of k that are there to their end: the next one travels while this one is multiplied.
-    const int64_t last = a.k / BK, whole = bp.few || bq.few ? from : to < last ? to : last;
-    int64_t tile = from;
-    if (tile < whole) {
-        bp.fetch(tile * BK);
-        bq.fetch(tile * BK);
-        bp.put(lds);
-        bq.put(lds + kP);
-        __syncthreads();
-        int side = 0;
-        for (; tile + 1 < whole; ++tile) {
-            bp.fetch((tile + 1) * BK);
-            bq.fetch((tile + 1) * BK);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply_tile(lds + side, [&] {
-                bp.put(lds + kBoth - side);
-                bq.put(lds + kBoth - side + kP);
-            });
-            side = kBoth - side;
+    // The same loop for both halves of the workgroup, each with its operand's way.  Tiles of k that are there to their end, then what is cut off.
+    auto walk = [&](auto along) {
+        constexpr bool ALONG = decltype(along)::value;
+        const int64_t last = a.k / BK, whole = few ? from : to < last ? to : last;
+        int64_t tile = from;
+        if (tile < whole) {
+            bring.template fetch<ALONG>(raw, tile * BK);
+            bring.template put<ALONG>(raw, mine_at);
+            if (tile + 1 < whole) bring.template fetch<ALONG>(raw, (tile + 1) * BK);
+            __syncthreads();
+            int side = 0;
+            for (; tile + 2 < whole; ++tile) {
+                multiply_tile(lds + side, [&](int slot) {
+                    bring.template turn_over<ALONG>(raw, mine_at + (kBoth - side), true, (tile + 2) * BK, slot, 4 * TN);
+                });
+                side = kBoth - side;
+                __syncthreads();
+            }
+            if (tile + 1 < whole) {
+                multiply_tile(lds + side, [&](int slot) { bring.template turn_over<ALONG>(raw, mine_at + (kBoth - side), false, 0, slot, 4 * TN); });
+                side = kBoth - side;
+                ++tile;
+                __syncthreads();
+            }
+            multiply_tile(lds + side, [](int) {});
+            ++tile;
             __syncthreads();
         }
-        multiply_tile(lds + side, [] {});
-        ++tile;
-        __syncthreads();
-    }
-    for (; tile < to; ++tile) {
-        bp.fetch_upto(tile * BK, a.k);
-        bq.fetch_upto(tile * BK, a.k);
-        bp.put(lds);
-        bq.put(lds + kP);
-        __syncthreads();
-        multiply_tile(lds, [] {});
-        __syncthreads();
-    }
+        for (; tile < to; ++tile) {
+            bring.template fetch_upto<ALONG>(raw, tile * BK, a.k);
+            bring.template put<ALONG>(raw, mine_at);
+            __syncthreads();
+            multiply_tile(lds, [](int) {});
+            __syncthreads();
+        }
+    };
+    if (P_ALONG == Q_ALONG || first) walk(std::integral_constant<bool, P_ALONG>{});
+    else walk(std::integral_constant<bool, Q_ALONG>{});
     // Lane l holds column l % 32 of m and, of each 32 of n, four stretches of four: 8 g + 4 (l / 32) .. + 3.  Through LDS, 32 rows of m at a time, so that
     // C's rows are read and written side by side.
-    constexpr int WN = BN / 2, PITCH = WN + 4, ACROSS = WN / 4;          // a lane takes four columns: 64 / ACROSS rows at a time
+    constexpr int E = kPer<T>, PITCH = WN + 4, ACROSS = WN / E;          // a lane takes 16 bytes of C's columns: 64 / ACROSS rows at a time
     float* mine = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
-    const int64_t n = n0 + wave / 2 * WN + lane % ACROSS * 4, left = a.n - n;
-    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.out.bias.p && left > 0 && !a.partial) load_4(reinterpret_cast<const T*>(a.out.bias.p) + t.learner * a.out.bias.learner + n, left, bias);
+    const int64_t n = n0 + wave / 2 * WN + lane % ACROSS * E, left = a.n - n;
+    float bias[E] = {};
+    if (a.out.bias.p && left > 0 && !a.partial)
+        widen<T>(load_cols(reinterpret_cast<const T*>(a.out.bias.p) + t.learner * a.out.bias.learner + n, left), bias);
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
 #pragma unroll
@@ -390,14 +418,26 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs a) {
                     (f32x4){acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
         __syncthreads();
         if (left > 0) {
-#pragma unroll 1
+#pragma unroll 2
             for (int r = lane / ACROSS; r < 32; r += kWave / ACROSS) {
                 const int64_t m = m0 + wave % 2 * (BM / 2) + 32 * j + r;
+                float v[E];
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const f32x4 sum = *reinterpret_cast<const f32x4*>(mine + r * PITCH + lane % ACROSS * E + e);
+                    v[e] = sum.x, v[e + 1] = sum.y, v[e + 2] = sum.z, v[e + 3] = sum.w;
+                }
                 if (m >= a.m) break;
-                const f32x4 sum = *reinterpret_cast<const f32x4*>(mine + r * PITCH + lane % ACROSS * 4);
-                float v[4] = {sum.x, sum.y, sum.z, sum.w};
-                if (a.partial) store_4(a.partial + (((int64_t)t.part * a.learners + t.learner) * a.m + m) * a.n + n, v, left);
-                else finish<T>(a.out, t.learner, m, n, left, bias, v);
+                if (a.partial) {
+                    float* to = a.partial + (((int64_t)t.part * a.learners + t.learner) * a.m + m) * a.n + n;
+#pragma unroll
+                    for (int e = 0; e < E; e += 4) {
+                        const float w[4] = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+                        store_cols<float>(to + e, w, left - e);
+                    }
+                } else {
+                    finish<T>(a.out, t.learner, m, n, left, bias, v);
+                }
             }
         }
         __syncthreads();
@@ -457,19 +497,24 @@ struct JoinArgs {
     int64_t rows, cols;
 };
 template <typename T> __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
-    const int64_t i = blockIdx.z, quads = (a.cols + 3) / 4, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= a.rows * quads) return;
-    const int64_t r = at / quads, c = at % quads * 4, left = a.cols - c;
+    constexpr int E = kPer<T>;
+    const int64_t i = blockIdx.z, across = (a.cols + E - 1) / E, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= a.rows * across) return;
+    const int64_t r = at / across, c = at % across * E, left = a.cols - c;
     const float* p = a.partial + i * a.learner_stride + r * a.cols + c;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float v[E] = {};
+#pragma unroll 4
     for (int64_t s = 0; s < a.parts; ++s) {
         float w[4];
-        load_4(p + s * a.part_stride, left, w);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += w[e];
+        for (int e = 0; e < E; e += 4) {
+            widen<float>(load_cols(p + s * a.part_stride + e, left - e), w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[e + k] += w[k];
+        }
     }
-    float bias[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (a.out.bias.p) load_4(reinterpret_cast<const T*>(a.out.bias.p) + i * a.out.bias.learner + c, left, bias);
+    float bias[E] = {};
+    if (a.out.bias.p) widen<T>(load_cols(reinterpret_cast<const T*>(a.out.bias.p) + i * a.out.bias.learner + c, left), bias);
     finish<T>(a.out, i, r, c, left, bias, v);
 }
 
@@ -486,29 +531,45 @@ struct Plan {
 };
 inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// The largest tile of which there are enough to fill the chip; then parts of k, as long as each keeps eight tiles of depth.
+// What a tile costs, in us: a step of 128 bytes of k with nothing else on the compute unit, the same when the unit is full (a share of it), and what
+// comes before and after the steps.  Measured (products of 512 to 4096 a side, each tile with 1 to 16 parts of k): large tiles do the most with what
+// they read, small ones fill the chip and wait less.
+struct TileCost {
+    int tile, resident;
+    float alone, shared, ends;
+};
+constexpr TileCost kCosts[2][3] = {{{256, 1, 1.9f, 1.9f, 10.0f}, {128, 2, 0.8f, 0.5f, 6.0f}, {64, 4, 0.5f, 0.3f, 2.5f}},        // bf16
+                                   {{256, 1, 8.0f, 8.0f, 10.0f}, {128, 2, 2.4f, 2.4f, 6.0f}, {64, 4, 0.7f, 0.55f, 2.5f}}};       // float
+
+// The tile and the parts of k of the least cost.  Parts cost a second kernel and their sums' way through memory.
 inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
-    const int64_t depth = parts_of(k, kRowBytes / bytes);
-    Plan plan{64, 1};
-    if (m < 1 || n < 1) return plan;          // nothing to multiply
-    for (int tile : {256, 128}) {
-        if (parts_of(m, tile) * parts_of(n, tile) * learners >= cus) {
-            plan.tile = tile;
-            return plan;
+    Plan best{64, 1};
+    if (m < 1 || n < 1) return best;          // nothing to multiply
+    const int64_t steps = parts_of(k, kRowBytes / bytes);
+    float least = INFINITY;
+    for (const TileCost& c : kCosts[bytes == 4]) {
+        const int64_t tiles = parts_of(m, c.tile) * parts_of(n, c.tile) * learners;
+        for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (split > 1 && (steps < 2 * split || tiles * split > 8 * (int64_t)cus)) break;
+            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * c.resident;
+            const float deep = (float)parts_of(groups, cus), rounds = (float)parts_of(groups, room);
+            const float step = groups <= room ? (deep * c.shared > c.alone ? deep * c.shared : c.alone) : deep * c.shared;
+            float us = (float)each * step + rounds * c.ends;
+            if (split > 1) us += 4.0f + (float)(split + 1) * (float)(m * n * learners) * 4.0f / 3.5e6f;
+            if (us < least) {
+                least = us;
+                best = Plan{c.tile, split};
+            }
         }
     }
-    const int64_t count = parts_of(m, 64) * parts_of(n, 64) * learners;
-    int64_t split = cus / count;
-    if (split > depth / 8) split = depth / 8;
-    plan.split = split < 1 ? 1 : split > 64 ? 64 : (int)split;
-    return plan;
+    return best;
 }
 
-template <typename T, int TILE, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
+template <typename T, int TILE, int ACROSS_N, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
     a.tiles_m = (int)parts_of(a.m, TILE);
     a.tiles_n = (int)parts_of(a.n, TILE);
     constexpr size_t lds = (size_t)4 * TILE * kRowBytes;
-    auto fn = gemm_kernel<T, TILE, TILE, P_ALONG, Q_ALONG>;
+    auto fn = gemm_kernel<T, TILE, TILE, ACROSS_N, P_ALONG, Q_ALONG>;
     if (lds >= 64 * 1024) {          // opted in once a kernel and device
         static bool done[64] = {false};
         int dev = 0;
@@ -522,7 +583,7 @@ template <typename T, int TILE, bool P_ALONG, bool Q_ALONG> int launch_tiles(Gem
     }
     const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
     if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
-    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(256), lds, s, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(128 * ACROSS_N), lds, s, a);
     return PSGD_OK;
 }
 
@@ -531,12 +592,12 @@ int launch_gemm(GemmArgs a, const Plan& plan, float* room, hipStream_t s) {
     a.split = plan.split;
     a.partial = plan.split > 1 ? room : nullptr;
     int rc;
-    if (plan.tile == 256) rc = launch_tiles<T, 256, P_ALONG, Q_ALONG>(a, s);
-    else if (plan.tile == 128) rc = launch_tiles<T, 128, P_ALONG, Q_ALONG>(a, s);
-    else rc = launch_tiles<T, 64, P_ALONG, Q_ALONG>(a, s);
+    if (plan.tile == 256) rc = launch_tiles<T, 256, 4, P_ALONG, Q_ALONG>(a, s);
+    else if (plan.tile == 128) rc = launch_tiles<T, 128, 2, P_ALONG, Q_ALONG>(a, s);
+    else rc = launch_tiles<T, 64, 2, P_ALONG, Q_ALONG>(a, s);
     if (rc || plan.split == 1) return rc;
     const JoinArgs j{room, plan.split, a.learners * a.m * a.n, a.m * a.n, a.out, a.m, a.n};
-    hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(a.m * parts_of(a.n, 4), 256), 1, a.learners), dim3(256), 0, s, j);
+    hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(a.m * parts_of(a.n, kPer<T>), 256), 1, a.learners), dim3(256), 0, s, j);
     return PSGD_OK;
 }
 
@@ -598,7 +659,7 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
         if (act != PSGD_ACT_NONE) dz = Operand{room, t * r.dz_pitch, r.dz_pitch};
         if (db) {
             const JoinArgs j{sums, slabs, out, slabs * out, Epilogue{Operand{static_cast<char*>(db->data), db->learner, out}, {}, {}, {}, PSGD_ACT_NONE}, 1, out};
-            hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(parts_of(out, 4), 256), 1, n), dim3(256), 0, s, j);
+            hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(parts_of(out, kPer<T>), 256), 1, n), dim3(256), 0, s, j);
         }
     }
     if (dx) {
