@@ -6,11 +6,14 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/core/Allocator.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "psgd.h"
+#include "psgd_layers.h"
 
 namespace {
 
@@ -270,6 +273,214 @@ PyObject* synth_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
     });
 }
 
+// ------------------------------------------------------------------------------------------------ layers and losses (psgd_layers.h)
+struct Layers {
+    decltype(&psgd_layer_norm) layer_norm = nullptr;
+    decltype(&psgd_layer_norm_grad) layer_norm_grad = nullptr;
+    decltype(&psgd_layer_norm_grad_workspace) layer_norm_grad_workspace = nullptr;
+    decltype(&psgd_linear) linear = nullptr;
+    decltype(&psgd_linear_workspace) linear_workspace = nullptr;
+    decltype(&psgd_linear_grad) linear_grad = nullptr;
+    decltype(&psgd_linear_grad_workspace) linear_grad_workspace = nullptr;
+    decltype(&psgd_token_logprobs) token_logprobs = nullptr;
+    decltype(&psgd_token_logprobs_workspace) token_logprobs_workspace = nullptr;
+    decltype(&psgd_distill) distill = nullptr;
+} layers;
+int layers_device() { return layers.distill ? static_cast<int>(c10::hip::current_device()) : -1; }
+
+// An operand as the library takes it; None is no operand.
+struct Operand {
+    psgd_view v{};
+    bool there = false;
+    const psgd_view* get() const { return there ? &v : nullptr; }
+};
+// The sizes in `shape` that are negative are taken from the tensor, the others have to be its.
+bool operand(PyObject* o, int dev, std::initializer_list<int64_t*> shape, Operand& x, bool optional = false) {
+    if (o == Py_None) return optional;
+    const at::Tensor* t = plain(o, dev);
+    if (!t || t->dim() != static_cast<int64_t>(shape.size())) return false;
+    int64_t dims = 0;
+    for (int64_t* size : shape) {
+        const int64_t have = t->size(dims++);
+        if (*size < 0) *size = have;
+        if (*size != have) return false;
+    }
+    const c10::ScalarType type = t->scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16 && type != at::kInt) return false;
+    if (t->size(dims - 1) > 1 && t->stride(dims - 1) != 1) return false;
+    x.v.data = t->data_ptr();
+    x.v.learner = t->size(0) > 1 ? t->stride(0) : 0;
+    x.v.row = dims == 3 && t->size(1) > 1 ? t->stride(1) : 0;
+    x.v.type = type == at::kFloat ? PSGD_F32 : type == at::kBFloat16 ? PSGD_BF16 : PSGD_I32;
+    x.there = true;
+    return true;
+}
+template <typename T> bool vector(PyObject* o, int dev, int64_t numel, c10::ScalarType type, T*& p) {
+    p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o, dev);
+    if (!t || t->scalar_type() != type || t->numel() != numel || !t->is_contiguous()) return false;
+    p = static_cast<T*>(t->data_ptr());
+    return true;
+}
+// `bytes` of torch's allocator for work on stream `s`: kept until the call has returned, after which the stream's order keeps it.  Only for the current
+// stream, on which the allocator hands them out.
+bool workspace(int dev, size_t bytes, void* s, c10::DataPtr& room) {
+    if (!bytes) return true;
+    if (s != c10::hip::getCurrentHIPStream(static_cast<c10::DeviceIndex>(dev)).stream()) return false;
+    room = c10::GetAllocator(c10::kCUDA)->allocate(bytes);
+    return room.get() != nullptr;
+}
+
+// layer_norm(x, gain, bias, y, eps, mean, rstd, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, c = -1;
+        Operand x, g, b, y;
+        float eps, *mean, *rstd;
+        void* s;
+        if (count != 8 || dev < 0 || !operand(a[0], dev, {&n, &t, &c}, x) || !operand(a[1], dev, {&n, &c}, g) ||
+            !operand(a[2], dev, {&n, &c}, b, true) || !operand(a[3], dev, {&n, &t, &c}, y) || !number(a[4], eps) || n > PSGD_MAX_N ||
+            !vector(a[5], dev, n * t, at::kFloat, mean) || !vector(a[6], dev, n * t, at::kFloat, rstd) || !stream_of(a[7], dev, s))
+            return NOT_MINE;
+        Unlocked run;
+        return layers.layer_norm(x.get(), g.get(), b.get(), y.get(), mean, rstd, static_cast<int>(n), t, c, eps, s);
+    });
+}
+
+// layer_norm_grad(dy, x, gain, mean, rstd, dx, dgain, dbias, add, stream)
+PyObject* layer_norm_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, c = -1;
+        Operand dy, x, g, dx, dg, db, add;
+        float *mean, *rstd;
+        void* s;
+        c10::DataPtr room;
+        if (count != 10 || dev < 0 || !operand(a[0], dev, {&n, &t, &c}, dy) || !operand(a[1], dev, {&n, &t, &c}, x) ||
+            !operand(a[2], dev, {&n, &c}, g) || n > PSGD_MAX_N || !vector(a[3], dev, n * t, at::kFloat, mean) ||
+            !vector(a[4], dev, n * t, at::kFloat, rstd) || !operand(a[5], dev, {&n, &t, &c}, dx) || !operand(a[6], dev, {&n, &c}, dg, true) ||
+            !operand(a[7], dev, {&n, &c}, db, true) || !operand(a[8], dev, {&n, &t, &c}, add, true) || !stream_of(a[9], dev, s))
+            return NOT_MINE;
+        const size_t need = dg.there || db.there ? layers.layer_norm_grad_workspace(static_cast<int>(n), t, c) : 0;
+        if (!workspace(dev, need, s, room)) return NOT_MINE;
+        Unlocked run;
+        return layers.layer_norm_grad(dy.get(), x.get(), g.get(), mean, rstd, add.get(), dx.get(), dg.get(), db.get(), static_cast<int>(n), t, c,
+                                      room.get(), need, s);
+    });
+}
+
+// linear(x, w, y, bias, act, residual, z, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, i = -1, o = -1, act;
+        Operand x, w, y, b, r, z;
+        void* s;
+        c10::DataPtr room;
+        if (count != 8 || dev < 0 || !operand(a[0], dev, {&n, &t, &i}, x) || !operand(a[1], dev, {&n, &o, &i}, w) || n > PSGD_MAX_N ||
+            !operand(a[2], dev, {&n, &t, &o}, y) || !operand(a[3], dev, {&n, &o}, b, true) || !integer(a[4], act) ||
+            !operand(a[5], dev, {&n, &t, &o}, r, true) || !operand(a[6], dev, {&n, &t, &o}, z, true) || !stream_of(a[7], dev, s))
+            return NOT_MINE;
+        const size_t need = layers.linear_workspace(x.get(), w.get(), static_cast<int>(n), t, i, o);
+        if (!workspace(dev, need, s, room)) return NOT_MINE;
+        Unlocked run;
+        return layers.linear(x.get(), w.get(), b.get(), r.get(), y.get(), z.get(), static_cast<int>(act), static_cast<int>(n), t, i, o,
+                             room.get(), need, s);
+    });
+}
+
+// linear_grad(dy, x, w, dx, dw, db, act, z, stream)
+PyObject* linear_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, i = -1, o = -1, act;
+        Operand dy, x, w, dx, dw, db, z;
+        void* s;
+        c10::DataPtr room;
+        if (count != 9 || dev < 0 || !operand(a[0], dev, {&n, &t, &o}, dy) || !operand(a[1], dev, {&n, &t, &i}, x) ||
+            !operand(a[2], dev, {&n, &o, &i}, w) || n > PSGD_MAX_N || !operand(a[3], dev, {&n, &t, &i}, dx, true) ||
+            !operand(a[4], dev, {&n, &o, &i}, dw, true) || !operand(a[5], dev, {&n, &o}, db, true) || !integer(a[6], act) ||
+            !operand(a[7], dev, {&n, &t, &o}, z, true) || !stream_of(a[8], dev, s))
+            return NOT_MINE;
+        const size_t need = layers.linear_grad_workspace(dy.get(), x.get(), w.get(), dx.get(), dw.get(), db.get(), static_cast<int>(act),
+                                                         static_cast<int>(n), t, i, o);
+        if (!workspace(dev, need, s, room)) return NOT_MINE;
+        Unlocked run;
+        return layers.linear_grad(dy.get(), z.get(), x.get(), w.get(), dx.get(), dw.get(), db.get(), static_cast<int>(act), static_cast<int>(n),
+                                  t, i, o, room.get(), need, s);
+    });
+}
+
+// token_logprobs(logits, tokens, logp, entropy, top_logp, top_idx, stream)
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, v = -1, k = 0;
+        Operand x, tok;
+        float *logp, *entropy, *top;
+        int32_t* idx;
+        void* s;
+        c10::DataPtr room;
+        if (count != 7 || dev < 0 || !operand(a[0], dev, {&n, &t, &v}, x) || n > PSGD_MAX_N) return NOT_MINE;
+        const at::Tensor* given = plain(a[1], dev);
+        if (!given || given->scalar_type() != at::kInt || given->dim() != 2 || given->size(0) != n || given->size(1) != t) return NOT_MINE;
+        tok.v = psgd_view{given->data_ptr(), n > 1 ? given->stride(0) : 0, t > 1 ? given->stride(1) : 0, PSGD_I32};
+        if (a[5] != Py_None) {
+            const at::Tensor* at = plain(a[5], dev);
+            if (!at || at->dim() != 3) return NOT_MINE;
+            k = at->size(2);
+        }
+        if ((a[4] == Py_None) != (a[5] == Py_None) || k > PSGD_MAX_TOP || !vector(a[2], dev, n * t, at::kFloat, logp) ||
+            !vector(a[3], dev, n * t, at::kFloat, entropy) || !vector(a[4], dev, n * t * k, at::kFloat, top) ||
+            !vector(a[5], dev, n * t * k, at::kInt, idx) || !stream_of(a[6], dev, s))
+            return NOT_MINE;
+        const size_t need = layers.token_logprobs_workspace(static_cast<int>(n), t, v, static_cast<int>(k));
+        if (!workspace(dev, need, s, room)) return NOT_MINE;
+        Unlocked run;
+        return layers.token_logprobs(x.get(), &tok.v, logp, entropy, top, idx, static_cast<int>(k), static_cast<int>(n), t, v, room.get(), need, s);
+    });
+}
+
+// distill(logits, top_idx, top_logit, loss, tau, weight, dlogits, stream)
+PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = layers_device();
+        int64_t n = -1, t = -1, v = -1, k = -1;
+        Operand x, idx, top, g;
+        float tau, *loss, *weight;
+        void* s;
+        if (count != 8 || dev < 0 || !operand(a[0], dev, {&n, &t, &v}, x) || n > PSGD_MAX_N || !operand(a[1], dev, {&n, &t, &k}, idx) ||
+            !operand(a[2], dev, {&n, &t, &k}, top) || k > PSGD_MAX_SLOTS || !vector(a[3], dev, n * t, at::kFloat, loss) || !number(a[4], tau) ||
+            !vector(a[5], dev, n * t, at::kFloat, weight) || !operand(a[6], dev, {&n, &t, &v}, g, true) || !stream_of(a[7], dev, s))
+            return NOT_MINE;
+        Unlocked run;
+        return layers.distill(x.get(), idx.get(), top.get(), weight, loss, g.get(), tau, static_cast<int>(k), static_cast<int>(n), t, v, s);
+    });
+}
+
+// bind_layers(addresses of the functions, in the order of struct Layers)
+PyObject* bind_layers(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    void* p[10];
+    if (count != 10) return answer(NOT_MINE);
+    for (int i = 0; i < 10; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    layers.layer_norm = reinterpret_cast<decltype(layers.layer_norm)>(p[0]);
+    layers.layer_norm_grad = reinterpret_cast<decltype(layers.layer_norm_grad)>(p[1]);
+    layers.layer_norm_grad_workspace = reinterpret_cast<decltype(layers.layer_norm_grad_workspace)>(p[2]);
+    layers.linear = reinterpret_cast<decltype(layers.linear)>(p[3]);
+    layers.linear_workspace = reinterpret_cast<decltype(layers.linear_workspace)>(p[4]);
+    layers.linear_grad = reinterpret_cast<decltype(layers.linear_grad)>(p[5]);
+    layers.linear_grad_workspace = reinterpret_cast<decltype(layers.linear_grad_workspace)>(p[6]);
+    layers.token_logprobs = reinterpret_cast<decltype(layers.token_logprobs)>(p[7]);
+    layers.token_logprobs_workspace = reinterpret_cast<decltype(layers.token_logprobs_workspace)>(p[8]);
+    layers.distill = reinterpret_cast<decltype(layers.distill)>(p[9]);
+    return answer(0);
+}
+
 // bind(addresses of the functions, in the order of struct Library)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
     void* p[7];
@@ -290,7 +501,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 #define PSGD_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PSGD_METHOD(mix_step),  PSGD_METHOD(mix_full), PSGD_METHOD(mix_step_d1d), PSGD_METHOD(build_mixing_device),
-                         PSGD_METHOD(consensus_dist_async), PSGD_METHOD(consensus_dist), PSGD_METHOD(synth_grad), PSGD_METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         PSGD_METHOD(consensus_dist_async), PSGD_METHOD(consensus_dist), PSGD_METHOD(synth_grad), PSGD_METHOD(bind),
+                         PSGD_METHOD(layer_norm), PSGD_METHOD(layer_norm_grad), PSGD_METHOD(linear), PSGD_METHOD(linear_grad),
+                         PSGD_METHOD(token_logprobs), PSGD_METHOD(distill), PSGD_METHOD(bind_layers), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -12,6 +12,8 @@ learners); outputs are the caller's tensors.  Work is enqueued on `stream` (None
 taken from torch's allocator on that stream, or is the caller's `workspace` (a contiguous uint8 tensor of at least the bytes that the
 function's *_workspace says).  There is no fallback: what the library refuses raises `psgd.PsgdError`, a tensor that is not what a call
 takes raises ValueError.
+
+Calls that are plainly in order take the short way of the _call extension, as psgd.py's do.
 """
 import ctypes
 
@@ -31,6 +33,7 @@ class View(ctypes.Structure):
 
 _lib = None
 _types = None
+_ext = None              # the extension, once bound to the library's functions
 
 
 def load():
@@ -57,7 +60,26 @@ def load():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
     _lib = lib
+    _bind()
     return lib
+
+
+def _bind():
+    """Hand the extension, if psgd.py has it, the addresses of the loaded library's functions."""
+    global _ext
+    _ext = None
+    if psgd._call is not None and hasattr(psgd._call, "bind_layers"):
+        psgd._call.bind_layers(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in EXPORTS))
+        _ext = psgd._call
+
+
+def _short(name, *args):
+    """Whether the short way has made the call."""
+    if _ext is None:
+        if _lib is None or psgd._call is None or not hasattr(psgd._call, "bind_layers"):
+            return False
+        _bind()
+    return psgd._answered(getattr(_ext, name)(*args))
 
 
 def _view(what, t, shape):
@@ -119,6 +141,8 @@ def _workspace(given, need, stream):
 def layer_norm(x, gain, bias, y, eps=1e-5, mean=None, rstd=None, stream=None):
     """Enqueue y = (x - m) r gain + bias over the last dimension; m and r to mean and rstd ([n, t] float32, both or neither).
     x, y [n, t, c] of one type (y may be x), gain and bias [n, c] of one type (bias may be None)."""
+    if _short("layer_norm", x, gain, bias, y, eps, mean, rstd, stream):
+        return
     import torch
     n, t, c = _shape("x", x, 3)
     vx, vg, vb, vy = _view("x", x, (n, t, c)), _view("gain", gain, (n, c)), _view("bias", bias, (n, c)), _view("y", y, (n, t, c))
@@ -134,6 +158,8 @@ def layer_norm_grad_workspace(n, t, c):
 def layer_norm_grad(dy, x, gain, mean, rstd, dx, dgain=None, dbias=None, add=None, workspace=None, stream=None):
     """Enqueue the backward pass of layer_norm: dx (plus `add`, the gradient that reaches x by another way), dgain and dbias from dy.
     dx may be dy or add; dgain and dbias [n, c] are float32 or bfloat16 alike, whatever x and gain are."""
+    if workspace is None and _short("layer_norm_grad", dy, x, gain, mean, rstd, dx, dgain, dbias, add, stream):
+        return
     import torch
     n, t, c = _shape("x", x, 3)
     vdy, vx, vg = _view("dy", dy, (n, t, c)), _view("x", x, (n, t, c)), _view("gain", gain, (n, c))
@@ -156,11 +182,13 @@ def _act(act):
 def linear(x, w, y, bias=None, act="none", residual=None, z=None, workspace=None, stream=None):
     """Enqueue z = x w' + bias, y = act(z) + residual for every learner: x [n, t, in], w [n, out, in], bias [n, out], y, residual and z
     [n, t, out], all of one type.  z is written where it is given (linear_grad wants it unless act is "none"); residual may be y."""
+    a = _act(act)
+    if workspace is None and _short("linear", x, w, y, bias, a, residual, z, stream):
+        return
     n, t, i = _shape("x", x, 3)
     o = _shape("w", w, 3)[1]
     vx, vw, vb = _view("x", x, (n, t, i)), _view("w", w, (n, o, i)), _view("bias", bias, (n, o))
     vr, vy, vz = _view("residual", residual, (n, t, o)), _view("y", y, (n, t, o)), _view("z", z, (n, t, o))
-    a = _act(act)
     psgd._on_current_device(x, w, bias, residual, y, z)
     lib = load()
     room, pw, bw = _workspace(workspace, lib.psgd_linear_workspace(vx, vw, n, t, i, o), stream)
@@ -169,11 +197,13 @@ def linear(x, w, y, bias=None, act="none", residual=None, z=None, workspace=None
 
 def linear_grad(dy, x, w, dx=None, dw=None, db=None, act="none", z=None, workspace=None, stream=None):
     """Enqueue the backward pass of linear: with dz = dy act'(z), dx = dz w, dw = dz' x, db = sum_t dz, each where it is given."""
+    a = _act(act)
+    if workspace is None and _short("linear_grad", dy, x, w, dx, dw, db, a, z, stream):
+        return
     n, t, i = _shape("x", x, 3)
     o = _shape("w", w, 3)[1]
     vdy, vz, vx, vw = _view("dy", dy, (n, t, o)), _view("z", z, (n, t, o)), _view("x", x, (n, t, i)), _view("w", w, (n, o, i))
     vdx, vdw, vdb = _view("dx", dx, (n, t, i)), _view("dw", dw, (n, o, i)), _view("db", db, (n, o))
-    a = _act(act)
     psgd._on_current_device(dy, z, x, w, dx, dw, db)
     lib = load()
     room, pw, bw = _workspace(workspace, lib.psgd_linear_grad_workspace(vdy, vx, vw, vdx, vdw, vdb, a, n, t, i, o), stream)
@@ -183,6 +213,8 @@ def linear_grad(dy, x, w, dx=None, dw=None, db=None, act="none", z=None, workspa
 def token_logprobs(logits, tokens, logp, entropy=None, top_logp=None, top_idx=None, workspace=None, stream=None):
     """Enqueue log softmax(logits) at `tokens` ([n, t] int32; negative: none given, 0) into logp, each row's entropy, and the k largest log
     probabilities with their columns ([n, t, k] float32 and int32, largest first, equal ones by column)."""
+    if workspace is None and _short("token_logprobs", logits, tokens, logp, entropy, top_logp, top_idx, stream):
+        return
     import torch
     n, t, v = _shape("logits", logits, 3)
     vl = _view("logits", logits, (n, t, v))
@@ -204,6 +236,8 @@ def distill(logits, top_idx, top_logit, loss, tau=1.0, weight=None, dlogits=None
     """Enqueue the distillation loss of every row against a teacher's k top logits, weight tau^2 KL(p || q), into loss ([n, t] float32), and
     where `dlogits` is given the gradient of the logits (it may be `logits`).  top_idx [n, t, k] int32 (negative: no slot), top_logit
     [n, t, k] float32 (logits or log probabilities), weight [n, t] float32 or None."""
+    if _short("distill", logits, top_idx, top_logit, loss, tau, weight, dlogits, stream):
+        return
     import torch
     n, t, v = _shape("logits", logits, 3)
     k = _shape("top_idx", top_idx, 3)[2]
