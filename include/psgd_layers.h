@@ -109,9 +109,8 @@ int psgd_linear_grad(const psgd_view* dy, const psgd_view* z, const psgd_view* x
  * +inf gives NaN for logp, entropy and top_logp.  A token >= v gives NaN and raises bit 1 of psgd_device_status().
  * v in 1..2^31-1, k in 0..min(v, PSGD_MAX_TOP).
  */
-size_t psgd_token_logprobs_workspace(int n, int64_t t, int64_t v, int k);
 int psgd_token_logprobs(const psgd_view* logits, const psgd_view* tokens, float* logp, float* entropy, float* top_logp, int32_t* top_idx,
-                        int k, int n, int64_t t, int64_t v, void* workspace, size_t workspace_bytes, void* stream);
+                        int k, int n, int64_t t, int64_t v, void* stream);
 
 /*
  * psgd_distill - distillation from a teacher's top logits, loss and gradient.  With p the softmax of a row's given teacher logits / tau

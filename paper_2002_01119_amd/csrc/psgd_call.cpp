@@ -283,7 +283,6 @@ struct Layers {
     decltype(&psgd_linear_grad) linear_grad = nullptr;
     decltype(&psgd_linear_grad_workspace) linear_grad_workspace = nullptr;
     decltype(&psgd_token_logprobs) token_logprobs = nullptr;
-    decltype(&psgd_token_logprobs_workspace) token_logprobs_workspace = nullptr;
     decltype(&psgd_distill) distill = nullptr;
 } layers;
 int layers_device() { return layers.distill ? static_cast<int>(c10::hip::current_device()) : -1; }
@@ -422,7 +421,6 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
         float *logp, *entropy, *top;
         int32_t* idx;
         void* s;
-        c10::DataPtr room;
         if (count != 7 || dev < 0 || !operand(a[0], dev, {&n, &t, &v}, x) || n > PSGD_MAX_N) return NOT_MINE;
         const at::Tensor* given = plain(a[1], dev);
         if (!given || given->scalar_type() != at::kInt || given->dim() != 2 || given->size(0) != n || given->size(1) != t) return NOT_MINE;
@@ -436,10 +434,8 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t count) {
             !vector(a[3], dev, n * t, at::kFloat, entropy) || !vector(a[4], dev, n * t * k, at::kFloat, top) ||
             !vector(a[5], dev, n * t * k, at::kInt, idx) || !stream_of(a[6], dev, s))
             return NOT_MINE;
-        const size_t need = layers.token_logprobs_workspace(static_cast<int>(n), t, v, static_cast<int>(k));
-        if (!workspace(dev, need, s, room)) return NOT_MINE;
         Unlocked run;
-        return layers.token_logprobs(x.get(), &tok.v, logp, entropy, top, idx, static_cast<int>(k), static_cast<int>(n), t, v, room.get(), need, s);
+        return layers.token_logprobs(x.get(), &tok.v, logp, entropy, top, idx, static_cast<int>(k), static_cast<int>(n), t, v, s);
     });
 }
 
@@ -462,9 +458,9 @@ PyObject* distill(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 // bind_layers(addresses of the functions, in the order of struct Layers)
 PyObject* bind_layers(PyObject*, PyObject* const* a, Py_ssize_t count) {
-    void* p[10];
-    if (count != 10) return answer(NOT_MINE);
-    for (int i = 0; i < 10; ++i) {
+    void* p[9];
+    if (count != 9) return answer(NOT_MINE);
+    for (int i = 0; i < 9; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -476,8 +472,7 @@ PyObject* bind_layers(PyObject*, PyObject* const* a, Py_ssize_t count) {
     layers.linear_grad = reinterpret_cast<decltype(layers.linear_grad)>(p[5]);
     layers.linear_grad_workspace = reinterpret_cast<decltype(layers.linear_grad_workspace)>(p[6]);
     layers.token_logprobs = reinterpret_cast<decltype(layers.token_logprobs)>(p[7]);
-    layers.token_logprobs_workspace = reinterpret_cast<decltype(layers.token_logprobs_workspace)>(p[8]);
-    layers.distill = reinterpret_cast<decltype(layers.distill)>(p[9]);
+    layers.distill = reinterpret_cast<decltype(layers.distill)>(p[8]);
     return answer(0);
 }
 

@@ -654,16 +654,9 @@ template <typename T, int TILE, int ACROSS_N, bool P_ALONG, bool Q_ALONG> int la
     a.tiles_n = (int)parts_of(a.n, TILE);
     constexpr size_t lds = (size_t)4 * TILE * kRowBytes;
     auto fn = gemm_kernel<T, TILE, TILE, ACROSS_N, P_ALONG, Q_ALONG>;
-    if (lds >= 64 * 1024) {          // opted in once a kernel and device
-        static bool done[64] = {false};
-        int dev = 0;
-        hipError_t e = hipGetDevice(&dev);
-        if (e != hipSuccess) return hip_error(e, "hipGetDevice");
-        if (dev < 0 || dev >= 64 || !__atomic_load_n(&done[dev], __ATOMIC_RELAXED)) {
-            e = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            if (e != hipSuccess) return hip_error(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
-            if (dev >= 0 && dev < 64) __atomic_store_n(&done[dev], true, __ATOMIC_RELAXED);
-        }
+    if (lds >= 64 * 1024) {
+        static LdsRecord record;
+        if (int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, record)) return rc;
     }
     const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
     if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");

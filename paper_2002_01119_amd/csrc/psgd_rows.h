@@ -161,6 +161,21 @@ template <typename OP, int W> __device__ __forceinline__ void group_all_2(float&
 // ------------------------------------------------------------------------------------------------ host: operands and checks
 inline int hip_error(hipError_t e, const char* what) { return fail(PSGD_EHIP, "%s: %s", what, hipGetErrorString(e)); }
 
+// A kernel that is launched with more than 64 KB of LDS is opted in, once a device (`done`: its own record).
+struct LdsRecord {
+    bool done[64];
+};
+inline int allow_lds(const void* fn, size_t bytes, LdsRecord& record) {
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return hip_error(e, "hipGetDevice");
+    if (dev >= 0 && dev < 64 && __atomic_load_n(&record.done[dev], __ATOMIC_RELAXED)) return PSGD_OK;
+    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return hip_error(e, "hipFuncSetAttribute(MaxDynamicSharedMemorySize)");
+    if (dev >= 0 && dev < 64) __atomic_store_n(&record.done[dev], true, __ATOMIC_RELAXED);
+    return PSGD_OK;
+}
+
 inline int elem_bytes(int type) { return type == PSGD_BF16 ? 2 : 4; }
 
 // Compute units of the current device, asked for once a device.

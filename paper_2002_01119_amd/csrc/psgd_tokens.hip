@@ -65,77 +65,151 @@ struct LogArgs {
     Rows logits, tokens;
     float *logp, *entropy, *top_logp;
     int32_t* top_idx;
-    int k;
-    int64_t t;
+    int k, keep;            // keep: floats of LDS for a row's batches' maxima, 0 if they do not fit
+    int64_t t, rows;
     int32_t v;
 };
 
-constexpr int kGroupsRanked = 256;       // groups of lanes whose largest logits give the threshold
-constexpr int kCandidates = 2048;
+constexpr int kUnroll = 4;               // 16-byte groups a lane has on their way: a batch
+
+// Rows of a workgroup: one, or one for each of four wavefronts.
+template <int B> constexpr int kRowsOf = B == kWave ? 4 : 1;
+// Between the lanes of a row.  A wavefront's own accesses to LDS are in order, so there only the compiler has to keep them.
+template <int B> __device__ __forceinline__ void row_sync() {
+    if constexpr (B == kWave) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
+
+// What finding the k largest takes of LDS, for rows of B lanes.  Lanes are joined to at most 256 groups.
+template <int B> struct TopRoom {
+    static constexpr int GROUPS = B < 256 ? B : 256, LIST = B < 256 ? 512 : B < 1024 ? 1024 : 2048;
+    static constexpr int BATCHES = B < 256 ? 128 : 256;
+    uint64_t group[GROUPS], list[LIST], best[B / kWave];
+    uint32_t batch[BATCHES];         // first 16-byte groups of the batches to read again
+    uint64_t limit;
+    int count, batches;
+};
+// Bytes of batches' maxima that a workgroup keeps; rows with more (beyond 393 216 floats) have all batches looked at.
+template <int B> constexpr int kBatchRoom = B == 1024 ? 96 * 1024 : 40 * 1024;
 
 // The k largest of a row, ties by ascending column.  Every lane knows the largest of its logits and the first 16-byte group that
-// holds it.  Of kGroupsRanked groups of lanes the k-th best such pair is a threshold that at least k logits reach, and no logit
-// outside of the lanes that reach it can be among the k: only those lanes look at their logits again and put what reaches the threshold
-// into a list in LDS, whose members are ranked by counting.  Typically that is k lanes of 1024 and little more than k logits.  A row
-// that overflows the list (long runs in order within one lane's groups) or holds NaN is searched k times instead.
-template <typename T, int B>
-__device__ void top_of_row(const LogArgs& a, const T* x, int64_t row, float best, uint32_t best_at, float m, float log_s, bool bad) {
-    constexpr int E = kPer<T>;
-    __shared__ uint64_t group[kGroupsRanked], list[kCandidates];
-    __shared__ uint64_t limit, wave_best[B / kWave];
-    __shared__ int count;
-    const int tid = threadIdx.x;
-    const uint32_t v = (uint32_t)a.v, groups = (v + E - 1) / E;      // 16-byte groups of the row: lane `tid` has tid, tid + B, ...
-    const uint64_t own = (uint32_t)tid < groups ? rank_of(order_of(best), best_at) : rank_of(0, (uint32_t)tid);
-    auto emit = [&](int place, uint64_t r) {
-        const float z = logit_of((uint32_t)(r >> 32));
-        a.top_idx[row * a.k + place] = (int32_t) ~(uint32_t)r;
-        a.top_logp[row * a.k + place] = bad ? NAN : (m == -INFINITY ? -INFINITY : (z - m) - log_s);
-    };
+// holds it, and in LDS the largest of each of its batches.  Of up to 256 groups of lanes the k-th best is a threshold that at least k logits
+// reach, and no logit outside of the batches that reach it can be among the k: only those are read again, all lanes' at once, and what
+// reaches the threshold goes into a list in LDS, whose members are ranked by counting.  Typically that is k batches and little more than k
+// logits.  A row that overflows the list (long runs in order within one lane's groups) or holds NaN is searched k times instead.
+// (Before the batches' maxima were kept, and with the threshold by counting in every lane, this took as long as reading the row: 4096 rows of 32 000
+// floats 158 us, 84 without it.)
+template <typename T, int B, typename EMIT>
+__device__ void top_of_row(const LogArgs& a, TopRoom<B>& room, const float* batch_max, const T* x, uint32_t v, float m, float best, uint32_t best_at, bool bad,
+                           const EMIT& emit) {
+    constexpr int E = kPer<T>, U = kUnroll, GROUPS = TopRoom<B>::GROUPS, PART = B / GROUPS;
+    const int tid = threadIdx.x % B;
+    const uint32_t groups = (v + E - 1) / E;      // 16-byte groups of the row: lane `tid` has tid, tid + B, ...
     bool listed = !bad;
     if (listed) {
-        uint64_t g = own;
-        constexpr int PART = B / kGroupsRanked;
+        uint64_t g = (uint32_t)tid < groups ? rank_of(order_of(best), best_at) : rank_of(0, (uint32_t)tid);
 #pragma unroll
         for (int d = 1; d < PART; d *= 2) {
             const uint64_t o = __shfl_xor((unsigned long long)g, d);
             g = o > g ? o : g;
         }
-        if (tid % PART == 0) group[tid / PART] = g;
-        if (tid == 0) count = 0;
-        __syncthreads();
-        int above = 0;
-        const int from = tid % PART * (kGroupsRanked / PART);
-#pragma unroll 8
-        for (int j = 0; j < kGroupsRanked / PART; ++j) above += group[from + j] > g;
+        if (tid % PART == 0) room.group[tid / PART] = g;
+        if (tid == 0) room.count = room.batches = 0;
+        row_sync<B>();
+        if (tid < kWave) {
+            // one wavefront: the largest order that k groups reach, bit by bit, and no further than to a few more than k
+            constexpr int HELD = GROUPS / kWave;
+            uint32_t o[HELD];
 #pragma unroll
-        for (int d = 1; d < PART; d *= 2) above += __shfl_xor(above, d);
-        if (above == a.k - 1 && tid % PART == 0) limit = g;
-        __syncthreads();
-        const uint64_t lim = limit;
-        const uint32_t lim_order = (uint32_t)(lim >> 32), lim_at = ~(uint32_t)lim;
-        if (own >= lim && (uint32_t)tid < groups) {
-            for (uint32_t q = tid; q < groups; q += B) {
+            for (int h = 0; h < HELD; ++h) o[h] = (uint32_t)(room.group[h * kWave + tid] >> 32);
+            uint32_t t = 0;
+            int reach = GROUPS;
+            const uint32_t top = order_of(m);
+            for (uint32_t bit = 0x80000000u; bit && reach > a.k + 8; bit >>= 1) {
+                if ((t | bit) > top) continue;                 // nobody
+                int c = 0;
+#pragma unroll
+                for (int h = 0; h < HELD; ++h) c += __popcll(__ballot(o[h] >= (t | bit)));
+                if (c >= a.k) {
+                    t |= bit;
+                    reach = c;
+                }
+            }
+            uint64_t lim = (uint64_t)t << 32;                  // every place
+            if (reach > 2 * a.k + 16) {                        // equal ones: the k-th with its place
+                for (int h = 0; h < HELD; ++h) {
+                    const uint64_t mine = room.group[h * kWave + tid];
+                    int above = 0;
+                    for (int j = 0; j < GROUPS; ++j) above += room.group[j] > mine;
+                    if (above == a.k - 1) room.limit = mine;
+                }
+            } else if (tid == 0) {
+                room.limit = lim;
+            }
+        }
+        row_sync<B>();
+        const uint64_t lim = room.limit;
+        const uint32_t lim_order = (uint32_t)(lim >> 32), lim_at = ~(uint32_t)lim, whole = v / E;
+        // the threshold as a logit: there is no NaN here, and below -inf's order there is nothing
+        const float lim_logit = lim_order <= order_of(-INFINITY) ? -INFINITY : logit_of(lim_order);
+        auto look = [&](uint32_t q) {
+            u32x4 raw[U];
+            if (q + (U - 1) * B < whole) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = load_raw(x + (int64_t)(q + u * B) * E);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t col = (int64_t)(q + u * B) * E;
+                    raw[u] = load_cols(x + col, v - col, kMasked<T>);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t at = q + u * B;
                 float z[E];
-                widen<T>(load_cols(x + (int64_t)q * E, (int64_t)v - (int64_t)q * E, kMasked<T>), z);
+                widen<T>(raw[u], z);
+                if (at >= groups || !(largest<T>(z) >= lim_logit)) continue;
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const uint32_t o = order_of(z[e]), col = q * E + e;
-                    if (col < v && (o > lim_order || (o == lim_order && q <= lim_at))) {
-                        const int p = atomicAdd(&count, 1);       // the order in the list does not matter
-                        if (p < kCandidates) list[p] = rank_of(o, col);
+                    const uint32_t o = order_of(z[e]), col = at * E + e;
+                    if (z[e] >= lim_logit && (o > lim_order || at <= lim_at) && col < v) {
+                        const int p = atomicAdd(&room.count, 1);       // the order in the list does not matter
+                        if (p < TopRoom<B>::LIST) room.list[p] = rank_of(o, col);
                     }
                 }
             }
+        };
+        // The batches are listed first, so that all of them are read at once: a wavefront that reads as it finds them waits for each.
+        bool all = batch_max == nullptr;
+        if (!all) {
+            int b = 0;
+            for (uint32_t q = tid; q < groups; q += U * B, ++b) {
+                if (!(batch_max[b * B + tid] >= lim_logit)) continue;
+                const int p = atomicAdd(&room.batches, 1);
+                if (p < TopRoom<B>::BATCHES) room.batch[p] = q;
+            }
+            row_sync<B>();
+            const int listed_batches = room.batches;
+            all = listed_batches > TopRoom<B>::BATCHES;
+            if (!all)
+                for (int p = tid; p < listed_batches; p += B) look(room.batch[p]);
         }
-        __syncthreads();
-        const int found = count;
-        listed = found <= kCandidates;
+        if (all)
+            for (uint32_t q = tid; q < groups; q += U * B) look(q);
+        row_sync<B>();
+        const int found = room.count;
+        listed = found <= TopRoom<B>::LIST;
         if (listed) {
             for (int c = tid; c < found; c += B) {
-                const uint64_t r = list[c];
+                const uint64_t r = room.list[c];
                 int place = 0;
-                for (int j = 0; j < found; ++j) place += list[j] > r;
+#pragma unroll 8
+                for (int j = 0; j < found; ++j) place += room.list[j] > r;
                 if (place < a.k) emit(place, r);
             }
         }
@@ -159,28 +233,43 @@ __device__ void top_of_row(const LogArgs& a, const T* x, int64_t row, float best
             const uint64_t o = __shfl_xor((unsigned long long)most, d);
             most = o > most ? o : most;
         }
-        __syncthreads();
-        if (tid % kWave == 0) wave_best[tid / kWave] = most;
-        __syncthreads();
-        most = wave_best[0];
-        for (int w = 1; w < B / kWave; ++w) most = wave_best[w] > most ? wave_best[w] : most;
+        row_sync<B>();
+        if (tid % kWave == 0) room.best[tid / kWave] = most;
+        row_sync<B>();
+        most = room.best[0];
+        for (int w = 1; w < B / kWave; ++w) most = room.best[w] > most ? room.best[w] : most;
         if (tid == 0) emit(place, most);
         last = most;
     }
 }
 
-template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds__(B) void logprobs_kernel(LogArgs a) {
-    constexpr int E = kPer<T>, U = 4, W = B / kWave;
+// What a row's statistics say, once they are whole.
+struct Said {
+    float m, s, a, log_s;
+    bool bad, empty;
+    __device__ __forceinline__ Said(float m_, float s_, float a_)
+        : m(m_), s(s_), a(a_), log_s(logf(s_)), bad(m_ != m_ || m_ == INFINITY), empty(m_ == -INFINITY) {}
+    __device__ __forceinline__ float of(float z) const { return bad ? NAN : empty ? -INFINITY : (z - m) - log_s; }
+    __device__ __forceinline__ float entropy() const { return bad ? NAN : empty ? 0.0f : log_s - a / s; }
+};
+template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds__(B * kRowsOf<B>) void logprobs_kernel(LogArgs a) {
+    constexpr int E = kPer<T>, U = kUnroll, W = B / kWave, ROWS = kRowsOf<B>;
     __shared__ float room[W], room2[2 * W];
-    const int64_t row = blockIdx.x, i = row / a.t, r = row % a.t;
+    extern __shared__ float batches[];               // TOP: [row][batch][B], if a.keep says that they fit
+    const int slot = ROWS > 1 ? threadIdx.x / B : 0;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + slot;
+    if (ROWS > 1 && row >= a.rows) return;
+    const int64_t i = row / a.t, r = row % a.t;
     const T* x = at<T>(a.logits, i, r);
     const int32_t v = a.v;
-    const uint32_t tid = threadIdx.x, groups = ((uint32_t)v + E - 1) / E, whole = (uint32_t)v / E;
+    float* batch_max = batches + slot * a.keep;
+    const uint32_t tid = threadIdx.x % B, groups = ((uint32_t)v + E - 1) / E, whole = (uint32_t)v / E;
     Online o;
     float best = -INFINITY;
     uint32_t best_at = tid;
+    float* mine = TOP && a.keep ? batch_max + tid : nullptr;
     auto batch = [&](const u32x4 (&raw)[U], uint32_t q) {
-        float z[U][E], m = o.m;
+        float z[U][E], m = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             widen<T>(raw[u], z[u]);
@@ -192,7 +281,11 @@ template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds_
             }
             m = Max::of(m, l);
         }
-        o.move<ENTROPY>(m);
+        if (TOP && mine) {
+            *mine = m;
+            mine += B;
+        }
+        o.move<ENTROPY>(Max::of(o.m, m));
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -217,8 +310,7 @@ template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds_
     const float m = group_all<Max, W>(o.m, room);
     o.move<ENTROPY>(m);
     group_all_2<Sum, W>(o.s, o.a, room2);
-    const bool bad = m != m || m == INFINITY, empty = m == -INFINITY;
-    const float log_s = logf(o.s);
+    const Said said(m, o.s, o.a);
     if (tid == 0) {
         const int32_t token = *at<int32_t>(a.tokens, i, r);
         float lp = 0.0f;
@@ -226,12 +318,18 @@ template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds_
             lp = NAN;
             atomicOr(&g_token_status, kTokenFlag);
         } else if (token >= 0) {
-            lp = bad ? NAN : empty ? -INFINITY : (load_1(x + token) - m) - log_s;
+            lp = said.of(load_1(x + token));
         }
         a.logp[row] = lp;
-        if (ENTROPY) a.entropy[row] = bad ? NAN : empty ? 0.0f : log_s - o.a / o.s;
+        if (ENTROPY) a.entropy[row] = said.entropy();
     }
-    if (TOP) top_of_row<T, B>(a, x, row, best, best_at, m, log_s, bad);
+    if constexpr (TOP) {
+        __shared__ TopRoom<B> top[ROWS];
+        top_of_row<T, B>(a, top[slot], a.keep ? batch_max : nullptr, x, (uint32_t)v, m, best, best_at, said.bad, [&](int place, uint64_t rank) {
+            a.top_idx[row * a.k + place] = (int32_t) ~(uint32_t)rank;
+            a.top_logp[row * a.k + place] = said.of(logit_of((uint32_t)(rank >> 32)));
+        });
+    }
 }
 
 struct DistillArgs {
@@ -410,19 +508,42 @@ inline Rows rows_of(const psgd_view* v) {
     return v ? Rows{static_cast<char*>(v->data), v->learner, v->row} : Rows{nullptr, 0, 0};
 }
 
-template <typename T> void launch_logprobs(const LogArgs& a, int64_t rows, hipStream_t s) {
-#define PSGD_LOG(B, EN, TOP) hipLaunchKernelGGL((logprobs_kernel<T, B, EN, TOP>), dim3((unsigned)rows), dim3(B), 0, s, a)
+// Lanes for a row.  us, k = 20, rows x columns, 64 / 256 / 1024 lanes: 64 000 x 500 bf16 88 / 266 / 3549; 3200 x 1000 float 11 / 15 / 41; 4096 x 32 000
+// bf16 63 / 65 / 111, float 126 / 111 / 127; 4096 x 131 072 bf16 368 / 201 / 209; 256 x 200 000 float 288 / 105 / 66.  64 lanes have as many groups
+// of lanes, of which the 33rd best and beyond are no good threshold.  (Cutting a few long rows into parts that a second kernel joins was no faster: the
+// search's latency counts twice then.  1 x 131 072 bf16 20.5, uncut 16.9.)
+inline int lanes_of_row(int64_t rows, int64_t groups, int k, int cus) {
+    if (k <= 32 && (groups <= 256 || (groups <= 2048 && rows >= 4 * (int64_t)cus))) return 64;
+    return groups <= 1024 || rows >= 4 * (int64_t)cus ? 256 : 1024;
+}
+
+template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
+    const int64_t groups = ((int64_t)a.v + kPer<T> - 1) / kPer<T>;
+    const int lanes = lanes_of_row(a.rows, groups, a.k, cus);
+#define PSGD_LOG(B, EN, TOP)                                                                                                \
+    do {                                                                                                                    \
+        if (B == 1024 && TOP && lds > 40 * 1024) {                                                                          \
+            static LdsRecord record;                                                                                        \
+            if (int rc = allow_lds(reinterpret_cast<const void*>(logprobs_kernel<T, B, EN, TOP>), kBatchRoom<B>, record)) return rc; \
+        }                                                                                                                   \
+        hipLaunchKernelGGL((logprobs_kernel<T, B, EN, TOP>), dim3((unsigned)((a.rows + kRowsOf<B> - 1) / kRowsOf<B>)), dim3(B * kRowsOf<B>), lds, s, a); \
+    } while (0)
 #define PSGD_LOG_B(B)                                                                                                       \
     do {                                                                                                                    \
+        const int64_t floats = (groups + B * kUnroll - 1) / (B * kUnroll) * B;                                              \
+        a.keep = a.k > 0 && floats * kRowsOf<B> * 4 <= kBatchRoom<B> ? (int)floats : 0;                                        \
+        const size_t lds = (size_t)a.keep * kRowsOf<B> * sizeof(float);                                                     \
         if (a.entropy && a.k) PSGD_LOG(B, true, true);                                                                      \
         else if (a.entropy) PSGD_LOG(B, true, false);                                                                       \
         else if (a.k) PSGD_LOG(B, false, true);                                                                             \
         else PSGD_LOG(B, false, false);                                                                                     \
     } while (0)
-    if (a.v > 256 * 16 * kPer<T>) PSGD_LOG_B(1024);
-    else PSGD_LOG_B(256);
+    if (lanes == 1024) PSGD_LOG_B(1024);
+    else if (lanes == 256) PSGD_LOG_B(256);
+    else PSGD_LOG_B(64);
 #undef PSGD_LOG_B
 #undef PSGD_LOG
+    return PSGD_OK;
 }
 
 template <typename T> void launch_distill(const DistillArgs& a, int64_t rows, hipStream_t s) {
@@ -467,21 +588,11 @@ int token_status(int clear, int* word) {
 
 extern "C" {
 
-size_t psgd_token_logprobs_workspace(int n, int64_t t, int64_t v, int k) {
-    (void)n;
-    (void)t;
-    (void)v;
-    (void)k;
-    return 0;
-}
-
 int psgd_token_logprobs(const psgd_view* logits, const psgd_view* tokens, float* logp, float* entropy, float* top_logp, int32_t* top_idx,
-                        int k, int n, int64_t t, int64_t v, void* workspace, size_t workspace_bytes, void* stream) {
+                        int k, int n, int64_t t, int64_t v, void* stream) {
     using namespace psgd;
     const char* name = "psgd_token_logprobs";
     clear_error();
-    (void)workspace;
-    (void)workspace_bytes;
     if (!logits || !tokens) return fail(PSGD_EINVAL, "%s: null operand", name);
     if (int rc = check_rows(name, n, t, v)) return rc;
     if (!float_type(logits->type) || tokens->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: logits must be float or bf16, tokens int32", name);
@@ -503,10 +614,11 @@ int psgd_token_logprobs(const psgd_view* logits, const psgd_view* tokens, float*
         for (int q = 0; q < p; ++q)
             if (int rc = refuse_overlap(name, outs[p], outs[q])) return rc;
     }
-    const LogArgs a{rows_of(logits), rows_of(tokens), logp, entropy, top_logp, top_idx, k, t, (int32_t)v};
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    const LogArgs a{rows_of(logits), rows_of(tokens), logp, entropy, top_logp, top_idx, k, 0, t, rows, (int32_t)v};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (logits->type == PSGD_F32) launch_logprobs<float>(a, rows, s);
-    else launch_logprobs<uint16_t>(a, rows, s);
+    if (int rc = logits->type == PSGD_F32 ? launch_logprobs<float>(a, cus, s) : launch_logprobs<uint16_t>(a, cus, s)) return rc;
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);
 }

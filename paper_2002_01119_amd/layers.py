@@ -24,7 +24,7 @@ ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 MAX_TOP, MAX_SLOTS = 64, 1024
 
 EXPORTS = ("psgd_layer_norm", "psgd_layer_norm_grad", "psgd_layer_norm_grad_workspace", "psgd_linear", "psgd_linear_workspace",
-           "psgd_linear_grad", "psgd_linear_grad_workspace", "psgd_token_logprobs", "psgd_token_logprobs_workspace", "psgd_distill")
+           "psgd_linear_grad", "psgd_linear_grad_workspace", "psgd_token_logprobs", "psgd_distill")
 
 
 class View(ctypes.Structure):
@@ -52,8 +52,7 @@ def load():
         "psgd_linear_workspace": (size, [view] * 2 + shape4),
         "psgd_linear_grad": (i32, [view] * 7 + [i32] + shape4 + work + [vp]),
         "psgd_linear_grad_workspace": (size, [view] * 6 + [i32] + shape4),
-        "psgd_token_logprobs": (i32, [view] * 2 + [vp] * 4 + [i32] + shape3 + work + [vp]),
-        "psgd_token_logprobs_workspace": (size, shape3 + [i32]),
+        "psgd_token_logprobs": (i32, [view] * 2 + [vp] * 4 + [i32] + shape3 + [vp]),
         "psgd_distill": (i32, [view] * 3 + [vp, vp, view, f32, i32] + shape3 + [vp]),
     }
     for name, (res, args) in signatures.items():
@@ -210,10 +209,10 @@ def linear_grad(dy, x, w, dx=None, dw=None, db=None, act="none", z=None, workspa
     psgd._check(lib.psgd_linear_grad(vdy, vz, vx, vw, vdx, vdw, vdb, a, n, t, i, o, pw, bw, psgd._stream_handle(stream)))
 
 
-def token_logprobs(logits, tokens, logp, entropy=None, top_logp=None, top_idx=None, workspace=None, stream=None):
+def token_logprobs(logits, tokens, logp, entropy=None, top_logp=None, top_idx=None, stream=None):
     """Enqueue log softmax(logits) at `tokens` ([n, t] int32; negative: none given, 0) into logp, each row's entropy, and the k largest log
     probabilities with their columns ([n, t, k] float32 and int32, largest first, equal ones by column)."""
-    if workspace is None and _short("token_logprobs", logits, tokens, logp, entropy, top_logp, top_idx, stream):
+    if _short("token_logprobs", logits, tokens, logp, entropy, top_logp, top_idx, stream):
         return
     import torch
     n, t, v = _shape("logits", logits, 3)
@@ -227,9 +226,7 @@ def token_logprobs(logits, tokens, logp, entropy=None, top_logp=None, top_idx=No
     pl, pe = _vector("logp", logp, n * t, torch.float32), _vector("entropy", entropy, n * t, torch.float32)
     ptl, pti = _vector("top_logp", top_logp, n * t * k, torch.float32), _vector("top_idx", top_idx, n * t * k, torch.int32)
     psgd._on_current_device(logits, tokens, logp, entropy, top_logp, top_idx)
-    lib = load()
-    room, pw, bw = _workspace(workspace, lib.psgd_token_logprobs_workspace(n, t, v, k), stream)
-    psgd._check(lib.psgd_token_logprobs(vl, vt, pl, pe, ptl, pti, k, n, t, v, pw, bw, psgd._stream_handle(stream)))
+    psgd._check(load().psgd_token_logprobs(vl, vt, pl, pe, ptl, pti, k, n, t, v, psgd._stream_handle(stream)))
 
 
 def distill(logits, top_idx, top_logit, loss, tau=1.0, weight=None, dlogits=None, stream=None):

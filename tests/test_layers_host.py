@@ -134,7 +134,7 @@ def logprobs(lib, n=N, t=T, v=V, k=K, logp=OUT, entropy=OUT + 1024, top=OUT + 20
     at = At()
     o = dict(logits=at(T * V, V), tokens=at(T, 1, I32))
     o.update(over)
-    return lib.psgd_token_logprobs(o["logits"], o["tokens"], logp, entropy, top, idx, k, n, t, v, None, 0, None)
+    return lib.psgd_token_logprobs(o["logits"], o["tokens"], logp, entropy, top, idx, k, n, t, v, None)
 
 
 @pytest.mark.parametrize("change,code,text", [
