@@ -5,7 +5,7 @@
 //     dg = sum_t dy h,   db = sum_t dy
 //
 // About ten vector operations an element against 4 bytes (forward, bf16) to 16 (backward, float, add): bound by HBM.  So every array is
-// touched once: a row stays in the registers of W wavefronts (W = 1, 4 or 16; a lane holds NV groups of 16 bytes) between the load and the
+// touched once: a row stays in the registers of 16 to 1024 lanes (a lane holds NV groups of 16 bytes) between the load and the
 // store, the variance is taken from there in a second pass, and a lane keeps the gain's and bias's columns for all rows
 // it walks.  The gradients of gain and bias are sums down the columns, which those same lanes own: each workgroup walks a slab of one
 // learner's rows with running sums in registers and leaves one partial row, and a second kernel adds the slabs up in a fixed order.
@@ -37,15 +37,29 @@ struct NormArgs {
     float eps, count;       // count: c, divided by (a row of one value has that value for its mean)
 };
 
-// Workgroups of one wavefront a row have this many rows at a time, the others one.
-constexpr int kRowsApart = 4;
-template <int W> constexpr int kGroupRows = W == 1 ? kRowsApart : 1;
-template <int W> constexpr int kGroupThreads = kWave * W * kGroupRows<W>;
+// A row takes 16, 32, 64, 256 or 1024 lanes; a workgroup has 256 lanes or 1024, and a row or as many as that makes.
+template <int LANES> constexpr int kGroupThreads = LANES < 256 ? 256 : LANES;
+template <int LANES> constexpr int kGroupRows = kGroupThreads<LANES> / LANES;
+template <int LANES> constexpr int kRowWaves = LANES < kWave ? 1 : LANES / kWave;
 
-template <typename T, typename P, int W, int NV>
-__global__ __launch_bounds__(kGroupThreads<W>) void norm_kernel(NormArgs a) {
-    constexpr int E = kPer<T>, LANES = kWave * W;
-    __shared__ float room[2][W > 1 ? W : 1];
+// Sums over a row's lanes, in every one of them.  `room`: LDS for the wavefronts of a row, which nothing else reads until the next barrier after this call's own.
+template <int LANES> __device__ __forceinline__ float row_sum(float v, float* room) {
+    if constexpr (LANES <= kWave) return wave_all<Sum, LANES>(v);
+    else return group_all<Sum, LANES / kWave>(v, room);
+}
+template <int LANES> __device__ __forceinline__ void row_sums(float& a, float& b, float* room) {
+    if constexpr (LANES <= kWave) {
+        a = wave_all<Sum, LANES>(a);
+        b = wave_all<Sum, LANES>(b);
+    } else {
+        group_all_2<Sum, LANES / kWave>(a, b, room);
+    }
+}
+
+template <typename T, typename P, int LANES, int NV>
+__global__ __launch_bounds__(kGroupThreads<LANES>) void norm_kernel(NormArgs a) {
+    constexpr int E = kPer<T>;
+    __shared__ float room[2][kRowWaves<LANES>];
     const int lane = threadIdx.x % LANES;
     const int64_t i = blockIdx.y;
     float g[NV][E], b[NV][E];
@@ -62,8 +76,8 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_kernel(NormArgs a) {
             for (int k = 0; k < E; ++k) b[j][k] = 0.0f;
         }
     }
-    const int64_t step = (int64_t)gridDim.x * kGroupRows<W>;
-    for (int64_t r = (int64_t)blockIdx.x * kGroupRows<W> + threadIdx.x / LANES; r < a.t; r += step) {
+    const int64_t step = (int64_t)gridDim.x * kGroupRows<LANES>;
+    for (int64_t r = (int64_t)blockIdx.x * kGroupRows<LANES> + threadIdx.x / LANES; r < a.t; r += step) {
         const T* x = at<T>(a.x, i, r) + lane * E;
         float v[NV][E];
         float sum = 0.0f;
@@ -73,7 +87,7 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_kernel(NormArgs a) {
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int k = 0; k < E; ++k) sum += v[j][k];
-        const float m = group_all<Sum, W>(sum, room[0]) / a.count;
+        const float m = row_sum<LANES>(sum, room[0]) / a.count;
         float sq = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
@@ -82,7 +96,7 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_kernel(NormArgs a) {
                 v[j][k] = k < left[j] ? v[j][k] - m : 0.0f;
                 sq += v[j][k] * v[j][k];
             }
-        const float var = group_all<Sum, W>(sq, room[1]) / a.count;
+        const float var = row_sum<LANES>(sq, room[1]) / a.count;
         const float rs = 1.0f / sqrtf(var + a.eps);
         if (a.mean && lane == 0) {
             a.mean[i * a.t + r] = m;
@@ -143,15 +157,15 @@ struct NormGradArgs {
     float inv_c;
 };
 
-template <typename T, typename P, int W, int NV, bool ADD>
-__global__ __launch_bounds__(kGroupThreads<W>) void norm_grad_kernel(NormGradArgs a) {
-    constexpr int E = kPer<T>, LANES = kWave * W;
-    __shared__ float room[2][2 * W];
-    extern __shared__ float sums[];      // W == 1: [2][LANES * NV * E], to join the wavefronts' sums
+template <typename T, typename P, int LANES, int NV, bool ADD>
+__global__ __launch_bounds__(kGroupThreads<LANES>) void norm_grad_kernel(NormGradArgs a) {
+    constexpr int E = kPer<T>, ROWS = kGroupRows<LANES>;
+    __shared__ float room[2][2 * kRowWaves<LANES>];
+    extern __shared__ float sums[];      // several rows at a time: [2][NV * E * LANES], to join their lanes' sums
     const int lane = threadIdx.x % LANES;
     const int64_t i = blockIdx.y;
     // 1024 lanes have 128 registers each: they fetch the gain again for each use, and `add` when it is wanted
-    constexpr bool HELD = W < 16;
+    constexpr bool HELD = LANES < 1024;
     float g[HELD ? NV : 1][E], dg[NV][E], db[NV][E];
     int left[NV];
 #pragma unroll
@@ -162,9 +176,9 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_grad_kernel(NormGradArg
 #pragma unroll
         for (int k = 0; k < E; ++k) dg[j][k] = db[j][k] = 0.0f;
     }
-    const int64_t step = (int64_t)gridDim.x * kGroupRows<W>;
+    const int64_t step = (int64_t)gridDim.x * kGroupRows<LANES>;
     int turn = 0;
-    for (int64_t r = (int64_t)blockIdx.x * kGroupRows<W> + threadIdx.x / LANES; r < a.t; r += step, turn ^= 1) {
+    for (int64_t r = (int64_t)blockIdx.x * kGroupRows<LANES> + threadIdx.x / LANES; r < a.t; r += step, turn ^= 1) {
         const T *px = at<T>(a.x, i, r) + lane * E, *pdy = at<T>(a.dy, i, r) + lane * E;
         const T* padd = ADD ? at<T>(a.add, i, r) + lane * E : nullptr;
         u32x4 rx[NV], rdy[NV], radd[NV];
@@ -192,7 +206,7 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_grad_kernel(NormGradArg
             }
         }
         // two rooms in turn: a wavefront may be a row ahead of one that still reads
-        group_all_2<Sum, W>(s1, s2, room[turn]);
+        row_sums<LANES>(s1, s2, room[turn]);
         const float mu = s1 * a.inv_c, muh = s2 * a.inv_c;
         T* pdx = at<T>(a.dx, i, r) + lane * E;
 #pragma unroll
@@ -217,25 +231,25 @@ __global__ __launch_bounds__(kGroupThreads<W>) void norm_grad_kernel(NormGradArg
     }
     if (!a.partial) return;
     float* part = a.partial + (i * gridDim.x + blockIdx.x) * 2 * a.c;
-    if constexpr (W == 1) {
-        for (int w = 0; w < kRowsApart; ++w) {          // one wavefront after the other: a fixed order
-            if ((int)threadIdx.x / kWave == w) {
+    if constexpr (ROWS > 1) {
+        for (int w = 0; w < ROWS; ++w) {                // one row's lanes after the other: a fixed order
+            if ((int)threadIdx.x / LANES == w) {
 #pragma unroll
                 for (int j = 0; j < NV; ++j)
 #pragma unroll
                     for (int k = 0; k < E; ++k) {
-                        float *q0 = &sums[(j * E + k) * kWave + lane], *q1 = q0 + NV * E * kWave;
+                        float *q0 = &sums[(j * E + k) * LANES + lane], *q1 = q0 + NV * E * LANES;
                         *q0 = w ? *q0 + dg[j][k] : dg[j][k];
                         *q1 = w ? *q1 + db[j][k] : db[j][k];
                     }
             }
             __syncthreads();
         }
-        for (int e = threadIdx.x; e < NV * E * kWave; e += kGroupThreads<W>) {
-            const int k = e % E, l = e / E % kWave, j = e / (E * kWave);      // column (j * 64 + l) * E + k
+        for (int e = threadIdx.x; e < NV * E * LANES; e += kGroupThreads<LANES>) {
+            const int k = e % E, l = e / E % LANES, j = e / (E * LANES);      // column (j * LANES + l) * E + k
             if (e < a.c) {
-                part[e] = sums[(j * E + k) * kWave + l];
-                part[a.c + e] = sums[(NV * E + j * E + k) * kWave + l];
+                part[e] = sums[(j * E + k) * LANES + l];
+                part[a.c + e] = sums[(NV * E + j * E + k) * LANES + l];
             }
         }
     } else {
@@ -325,25 +339,25 @@ template <typename T> __global__ __launch_bounds__(256) void norm_slab_kernel(No
         }
 }
 
-// Adds the slabs up: 64 columns a workgroup, its four wavefronts a quarter of the slabs each.
-template <typename G> __global__ __launch_bounds__(256) void norm_params_kernel(const float* partial, int64_t slabs, Vecs dgain, Vecs dbias, int64_t c) {
-    __shared__ float rest[4][kWave];
+// Adds the slabs up: 64 columns a workgroup, its sixteen wavefronts every sixteenth slab each.
+constexpr int kSumWaves = 16;
+template <typename G>
+__global__ __launch_bounds__(kSumWaves* kWave) void norm_params_kernel(const float* partial, int64_t slabs, Vecs dgain, Vecs dbias, int64_t c) {
+    __shared__ float rest[kSumWaves][kWave];
     const int64_t i = blockIdx.y, col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;     // of 2 c: gain's, then bias's
     const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
-    float s0 = 0.0f, s1 = 0.0f;
+    float sum = 0.0f;
     if (col < 2 * c) {
         const float* p = partial + i * slabs * 2 * c + col;
-        int64_t s = w;
-        for (; s + 4 < slabs; s += 8) {
-            s0 += p[s * 2 * c];
-            s1 += p[(s + 4) * 2 * c];
-        }
-        if (s < slabs) s0 += p[s * 2 * c];
+#pragma unroll 4
+        for (int64_t s = w; s < slabs; s += kSumWaves) sum += p[s * 2 * c];
     }
-    rest[w][l] = s0 + s1;
+    rest[w][l] = sum;
     __syncthreads();
     if (w == 0 && col < 2 * c) {
-        const float v = (rest[0][l] + rest[1][l]) + (rest[2][l] + rest[3][l]);
+        float v = rest[0][l];
+#pragma unroll
+        for (int k = 1; k < kSumWaves; ++k) v += rest[k][l];
         if (col < c) {
             if (dgain.p) store_1(at<G>(dgain, i) + col, v);
         } else if (dbias.p) {
@@ -352,23 +366,27 @@ template <typename G> __global__ __launch_bounds__(256) void norm_params_kernel(
     }
 }
 
-// How a row of c columns is held: W wavefronts, NV 16-byte groups a lane; W = 0: not at all.
+// How a row of c columns is held: so many lanes, NV 16-byte groups each; none: not at all.
 struct Hold {
-    int w, nv;
+    int lanes, nv;
 };
-// Forward: up to 32 elements of a row a lane (16 with 16 wavefronts).
 inline Hold forward_hold(int64_t c, int bytes) {
-    const int64_t groups = (c + 1023 / bytes) / (1024 / bytes);       // 1 KB of the row: 16 bytes of each of 64 lanes
-    if (groups <= 1) return {1, 1};
-    if (groups <= 2) return {1, 2};
-    if (groups <= 4) return {4, 1};
-    if (groups <= 8) return {4, 2};
-    if (groups <= 16) return {4, 4};
-    if (groups <= 32) return {16, 2};
-    if (groups <= 64 && bytes == 4) return {16, 4};
+    const int64_t groups = (c * bytes + 15) / 16;
+    if (groups <= 16) return {16, 1};
+    if (groups <= 32) return {32, 1};
+    if (groups <= 64) return {64, 1};
+    if (groups <= 128) return {64, 2};
+    if (groups <= 256) return {64, 4};            // bf16 32 768 x 2048: 44.6 us, by 256 lanes 51.6; backward 120 / 114
+    if (groups <= 512) return {256, 2};
+    if (groups <= 1024) return {256, 4};
+    if (groups <= 2048) return {1024, 2};
+    if (groups <= 4096 && bytes == 4) return {1024, 4};
     return {0, 0};
 }
-inline Hold backward_hold(int64_t c, int bytes) { return forward_hold(c, bytes); }
+inline Hold backward_hold(int64_t c, int bytes) {
+    const Hold h = forward_hold(c, bytes);
+    return h.lanes == 64 && h.nv == 4 ? Hold{256, 1} : h;
+}
 
 // Workgroups for each learner: enough rows at a time to fill the chip, no more than there are.
 inline int64_t groups_per_learner(int64_t t, int rows, int n, int64_t chip) {
@@ -376,10 +394,14 @@ inline int64_t groups_per_learner(int64_t t, int rows, int n, int64_t chip) {
     const int64_t g = most < fair ? most : fair;
     return g < 1 ? 1 : g;
 }
-constexpr int kSlabChip = 512;      // slabs of the backward pass, all learners together
-inline int64_t backward_slabs(int n, int64_t t, int64_t c) {
-    (void)c;
-    return groups_per_learner(t, 1, n, kSlabChip);
+// Slabs of the backward pass: two workgroups a compute unit, which leave as many partial rows behind; narrow rows, whose partial sums are little, as many as
+// are resident; the widest one.  us, slabs of all learners 256 / 512 / 1024: bf16 32 768 x 2048 164 / 114 / 130, float 1024 x 16 384 54 / 64 / 83.
+inline int64_t backward_slabs(int n, int64_t t, int64_t c, int bytes) {
+    const Hold h = backward_hold(c, bytes);
+    const int rows = h.lanes && h.lanes < 256 ? 256 / h.lanes : 1;
+    const int64_t chip = h.lanes && h.lanes <= 64 && h.nv == 1 ? 2048 : h.lanes == 1024 ? 256 : 512;
+    const int64_t g = groups_per_learner(t, rows, n, chip), turns = (t + rows - 1) / rows;
+    return g > 64 && 4 * g > turns ? (turns > 256 ? turns / 4 : 64) : g;      // four turns each, or the sums cost more than the rows
 }
 
 inline Rows rows_of(const psgd_view* v) {
@@ -389,14 +411,14 @@ inline Vecs vecs_of(const psgd_view* v) { return v ? Vecs{static_cast<char*>(v->
 
 template <typename T, typename P> void launch_norm(const NormArgs& a, int n, int cus, hipStream_t s) {
     const Hold h = forward_hold(a.c, sizeof(T));
-#define PSGD_NORM(W_, NV_)                                                                                                  \
-    if (h.w == W_ && h.nv == NV_) {                                                                                         \
-        const int64_t g = groups_per_learner(a.t, kGroupRows<W_>, n, (int64_t)cus * 2048 / kGroupThreads<W_>);              \
-        hipLaunchKernelGGL((norm_kernel<T, P, W_, NV_>), dim3((unsigned)g, n), dim3(kGroupThreads<W_>), 0, s, a);           \
+#define PSGD_NORM(L_, NV_)                                                                                                  \
+    if (h.lanes == L_ && h.nv == NV_) {                                                                                     \
+        const int64_t g = groups_per_learner(a.t, kGroupRows<L_>, n, (int64_t)cus * 2048 / kGroupThreads<L_>);              \
+        hipLaunchKernelGGL((norm_kernel<T, P, L_, NV_>), dim3((unsigned)g, n), dim3(kGroupThreads<L_>), 0, s, a);           \
         return;                                                                                                             \
     }
-    PSGD_NORM(1, 1) PSGD_NORM(1, 2) PSGD_NORM(4, 1) PSGD_NORM(4, 2) PSGD_NORM(4, 4) PSGD_NORM(16, 2)
-    if constexpr (sizeof(T) == 4) PSGD_NORM(16, 4)
+    PSGD_NORM(16, 1) PSGD_NORM(32, 1) PSGD_NORM(64, 1) PSGD_NORM(64, 2) PSGD_NORM(64, 4) PSGD_NORM(256, 2) PSGD_NORM(256, 4) PSGD_NORM(1024, 2)
+    if constexpr (sizeof(T) == 4) PSGD_NORM(1024, 4)
 #undef PSGD_NORM
     const int64_t g = groups_per_learner(a.t, 1, n, (int64_t)cus * 2);
     hipLaunchKernelGGL((norm_long_kernel<T, P>), dim3((unsigned)g, n), dim3(1024), 0, s, a);
@@ -404,14 +426,15 @@ template <typename T, typename P> void launch_norm(const NormArgs& a, int n, int
 
 template <typename T, typename P, bool ADD> void launch_norm_grad(const NormGradArgs& a, int n, int slabs, hipStream_t s) {
     const Hold h = backward_hold(a.c, sizeof(T));
-#define PSGD_NORM_GRAD(W_, NV_)                                                                                             \
-    if (h.w == W_ && h.nv == NV_) {                                                                                         \
-        const size_t lds = W_ == 1 && a.partial ? (size_t)2 * NV_ * kPer<T> * kWave * sizeof(float) : 0;                    \
-        hipLaunchKernelGGL((norm_grad_kernel<T, P, W_, NV_, ADD>), dim3(slabs, n), dim3(kGroupThreads<W_>), lds, s, a);      \
+#define PSGD_NORM_GRAD(L_, NV_)                                                                                             \
+    if (h.lanes == L_ && h.nv == NV_) {                                                                                     \
+        const size_t lds = kGroupRows<L_> > 1 && a.partial ? (size_t)2 * NV_ * kPer<T> * L_ * sizeof(float) : 0;            \
+        hipLaunchKernelGGL((norm_grad_kernel<T, P, L_, NV_, ADD>), dim3(slabs, n), dim3(kGroupThreads<L_>), lds, s, a);      \
         return;                                                                                                             \
     }
-    PSGD_NORM_GRAD(1, 1) PSGD_NORM_GRAD(1, 2) PSGD_NORM_GRAD(4, 1) PSGD_NORM_GRAD(4, 2) PSGD_NORM_GRAD(4, 4) PSGD_NORM_GRAD(16, 2)
-    if constexpr (sizeof(T) == 4) PSGD_NORM_GRAD(16, 4)
+    PSGD_NORM_GRAD(16, 1) PSGD_NORM_GRAD(32, 1) PSGD_NORM_GRAD(64, 1) PSGD_NORM_GRAD(64, 2) PSGD_NORM_GRAD(256, 1) PSGD_NORM_GRAD(256, 2)
+    PSGD_NORM_GRAD(256, 4) PSGD_NORM_GRAD(1024, 2)
+    if constexpr (sizeof(T) == 4) PSGD_NORM_GRAD(1024, 4)
 #undef PSGD_NORM_GRAD
     if (a.partial) {
         const int64_t across = (a.c + 256 * kPer<T> - 1) / (256 * kPer<T>);
@@ -473,7 +496,9 @@ int psgd_layer_norm(const psgd_view* x, const psgd_view* gain, const psgd_view* 
 
 size_t psgd_layer_norm_grad_workspace(int n, int64_t t, int64_t c) {
     if (n < 1 || n > PSGD_MAX_N || t < 0 || c < 1 || t > INT32_MAX || c > INT32_MAX) return 0;
-    return psgd::up256((size_t)n * psgd::backward_slabs(n, t, c) * 2 * c * sizeof(float));
+    // rows of the two types have different numbers of slabs; the larger serves either
+    const int64_t a = psgd::backward_slabs(n, t, c, 2), b = psgd::backward_slabs(n, t, c, 4);
+    return psgd::up256((size_t)n * (a > b ? a : b) * 2 * c * sizeof(float));
 }
 
 int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_view* gain, const float* mean, const float* rstd,
@@ -521,7 +546,7 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
             if (int rc = refuse_overlap(name, ew, *o)) return rc;
     }
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const int64_t slabs = backward_slabs(n, t, c);
+    const int64_t slabs = backward_slabs(n, t, c, elem_bytes(x->type));
     const NormGradArgs a{rows_of(dy),   rows_of(x), rows_of(add), rows_of(dx), vecs_of(gain), mean, rstd,
                          params ? static_cast<float*>(workspace) : nullptr, t, c, 1.0f / (float)c};
     if (t > 0) {
@@ -541,9 +566,9 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
         const dim3 grid((unsigned)((2 * c + kWave - 1) / kWave), n);
         const int64_t count = t > 0 ? slabs : 0;
         if (params->type == PSGD_F32)
-            hipLaunchKernelGGL((norm_params_kernel<float>), grid, dim3(256), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
+            hipLaunchKernelGGL((norm_params_kernel<float>), grid, dim3(kSumWaves * kWave), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
         else
-            hipLaunchKernelGGL((norm_params_kernel<uint16_t>), grid, dim3(256), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
+            hipLaunchKernelGGL((norm_params_kernel<uint16_t>), grid, dim3(kSumWaves * kWave), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);

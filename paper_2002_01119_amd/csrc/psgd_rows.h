@@ -117,13 +117,17 @@ template <int CTRL> __device__ __forceinline__ float dpp(float v) {
 }
 // Over the 64 lanes, in every lane: neighbours, pairs, halves of a row of 16 mirrored, then rows and halves exchanged.  All of it in the
 // vector unit; the order is the same in every lane, so all hold the same bits.
-template <typename OP> __device__ __forceinline__ float wave_all(float v) {
+// LANES: over 16 or 32 lanes that belong together instead.
+template <typename OP, int LANES = kWave> __device__ __forceinline__ float wave_all(float v) {
+    static_assert(LANES == 16 || LANES == 32 || LANES == kWave, "rows of 16 lanes");
     v = OP::of(v, dpp<0xB1>(v));    // quad_perm 1 0 3 2
     v = OP::of(v, dpp<0x4E>(v));    // quad_perm 2 3 0 1
     v = OP::of(v, dpp<0x141>(v));   // row_half_mirror
     v = OP::of(v, dpp<0x140>(v));   // row_mirror
+    if constexpr (LANES == 16) return v;
     auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     v = OP::of(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    if constexpr (LANES == 32) return v;
     auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return OP::of(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
