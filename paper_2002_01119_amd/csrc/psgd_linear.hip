@@ -289,8 +289,8 @@ __device__ __forceinline__ void multiply(u32x4 a, u32x4 b, f32x16& c, float) {
 struct Tile {
     int learner, part, tm, tn;
 };
-__device__ __forceinline__ Tile tile_of(const GemmArgs& a) {
-    const uint32_t id = blockIdx.x, total = gridDim.x, q = total / 8, r = total % 8, die = id % 8;
+__device__ __forceinline__ Tile tile_of(const GemmArgs& a, uint32_t id, uint32_t total) {
+    const uint32_t q = total / 8, r = total % 8, die = id % 8;
     uint32_t t = die * q + (die < r ? die : r) + id / 8;
     const uint32_t each = (uint32_t)a.tiles_m * a.tiles_n;
     Tile o;
@@ -304,13 +304,15 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& a) {
     return o;
 }
 
+extern __shared__ __attribute__((aligned(128))) char lds[];
+
+// Workgroup `id` of `total` that this product has.
 template <typename T, int BM, int BN, int ACROSS_N, bool P_ALONG, bool Q_ALONG>
-__global__ __launch_bounds__(128 * ACROSS_N) void gemm_kernel(GemmArgs a) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32_t total) {
     // wavefronts, two along m by ACROSS_N along n; 32 x 32 tiles of each
     constexpr int NT = 128 * ACROSS_N, TM = BM / 64, TN = BN / 32 / ACROSS_N, BK = kDepth<T>, WN = BN / ACROSS_N;
-    extern __shared__ __attribute__((aligned(128))) char lds[];
     constexpr int kP = BM * kRowBytes, kBoth = (BM + BN) * kRowBytes;
-    const Tile t = tile_of(a);
+    const Tile t = tile_of(a, id, total);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const T* p = reinterpret_cast<const T*>(a.p.p) + t.learner * a.p.learner;
     const T* q = reinterpret_cast<const T*>(a.q.p) + t.learner * a.q.learner;
@@ -444,6 +446,17 @@ __global__ __launch_bounds__(128 * ACROSS_N) void gemm_kernel(GemmArgs a) {
     }
 }
 
+template <typename T, int BM, int BN, int ACROSS_N, bool P_ALONG, bool Q_ALONG>
+__global__ __launch_bounds__(128 * ACROSS_N) void gemm_kernel(GemmArgs a) {
+    gemm_tile<T, BM, BN, ACROSS_N, P_ALONG, Q_ALONG>(a, blockIdx.x, gridDim.x);
+}
+// The backward pass' two products side by side, dx's workgroups first: neither fills the chip then, and a workgroup alone on its compute unit waits for
+// most of its time.
+template <typename T, int TILE> __global__ __launch_bounds__(256) void gemm_pair_kernel(GemmArgs dx, GemmArgs dw, uint32_t first) {
+    if (blockIdx.x < first) gemm_tile<T, TILE, TILE, 2, true, false>(dx, blockIdx.x, first);
+    else gemm_tile<T, TILE, TILE, 2, false, false>(dw, blockIdx.x - first, gridDim.x - first);
+}
+
 // ------------------------------------------------------------------------------------------------ a few tokens
 // The forward product of up to TOK tokens: W is read once, 1 KB of one row at a time, which is all it costs; the tokens come from the first-level
 // cache.  A wavefront takes R rows of W (outputs) and keeps R x TOK sums a lane, joined at the end.  bf16 tokens beyond four would cost the vector unit
@@ -572,8 +585,27 @@ template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kern
     }
 }
 
-// Adds up `parts` arrays of [learners][rows][cols] floats in order: the slabs of db (rows = 1, parts within a learner), or parts of k with the
-// product's epilogue.
+// Adds the slabs of db up: 64 columns a workgroup, its sixteen wavefronts every sixteenth slab each.
+constexpr int kSumWaves = 16;
+template <typename T> __global__ __launch_bounds__(kSumWaves* kWave) void sum_slabs_kernel(const float* partial, int64_t slabs, int64_t o, Operand db) {
+    __shared__ float rest[kSumWaves][kWave];
+    const int64_t i = blockIdx.y, col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;
+    const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+    float sum = 0.0f;
+    if (col < o) {
+#pragma unroll 4
+        for (int64_t s = w; s < slabs; s += kSumWaves) sum += partial[(i * slabs + s) * o + col];
+    }
+    rest[w][l] = sum;
+    __syncthreads();
+    if (w || col >= o) return;
+    float v = rest[0][l];
+#pragma unroll
+    for (int k = 1; k < kSumWaves; ++k) v += rest[k][l];
+    store_1(reinterpret_cast<T*>(const_cast<char*>(db.p)) + i * db.learner + col, v);
+}
+
+// Adds up `parts` arrays of [learners][rows][cols] floats in order, parts of k, with the product's epilogue.
 struct JoinArgs {
     const float* partial;
     int64_t parts, part_stride, learner_stride;
@@ -678,6 +710,25 @@ int launch_gemm(GemmArgs a, const Plan& plan, float* room, hipStream_t s) {
     return PSGD_OK;
 }
 
+template <typename T, int TILE> int launch_pair(GemmArgs dx, GemmArgs dw, hipStream_t s) {
+    int64_t count[2];
+    int k = 0;
+    for (GemmArgs* a : {&dx, &dw}) {
+        a->tiles_m = (int)parts_of(a->m, TILE);
+        a->tiles_n = (int)parts_of(a->n, TILE);
+        count[k++] = (int64_t)a->tiles_m * a->tiles_n * a->learners;
+    }
+    if (count[0] + count[1] > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear_grad: too many tiles");
+    constexpr size_t bytes = (size_t)4 * TILE * kRowBytes;
+    auto fn = gemm_pair_kernel<T, TILE>;
+    if (bytes >= 64 * 1024) {
+        static LdsRecord record;
+        if (int rc = allow_lds(reinterpret_cast<const void*>(fn), bytes, record)) return rc;
+    }
+    hipLaunchKernelGGL(fn, dim3((unsigned)(count[0] + count[1])), dim3(256), bytes, s, dx, dw, (uint32_t)count[0]);
+    return PSGD_OK;
+}
+
 inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cus) {
     const int64_t across = parts_of(o, kWave * 16 / bytes) * learners;
     if (across < 1) return 1;
@@ -760,18 +811,18 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
         else hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_SILU>), grid, dim3(256), 0, s, a);
         if (act != PSGD_ACT_NONE) dz = Operand{room, t * r.dz_pitch, r.dz_pitch};
         if (db) {
-            const JoinArgs j{sums, slabs, out, slabs * out, Epilogue{Operand{static_cast<char*>(db->data), db->learner, out}, {}, {}, {}, PSGD_ACT_NONE}, 1, out};
-            hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(parts_of(out, kPer<T>), 256), 1, n), dim3(256), 0, s, j);
+            hipLaunchKernelGGL((sum_slabs_kernel<T>), dim3((unsigned)parts_of(out, kWave), n), dim3(kSumWaves * kWave), 0, s, sums, slabs, out, operand(db));
         }
     }
-    if (dx) {
-        const GemmArgs a{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
-        if (int rc = launch_gemm<T, true, false>(a, gemm_plan(n, t, in, out, sizeof(T), cus), product, s)) return rc;
-    }
-    if (dw) {
-        const GemmArgs a{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
-        if (int rc = launch_gemm<T, false, false>(a, gemm_plan(n, out, in, t, sizeof(T), cus), product, s)) return rc;
-    }
+    GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
+    GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
+    const Plan px = gemm_plan(n, t, in, out, sizeof(T), cus), pw = gemm_plan(n, out, in, t, sizeof(T), cus);
+    if (dx && dw && px.split == 1 && pw.split == 1 && px.tile == pw.tile && px.tile < 256)
+        return px.tile == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
+    if (dx)
+        if (int rc = launch_gemm<T, true, false>(ax, px, product, s)) return rc;
+    if (dw)
+        if (int rc = launch_gemm<T, false, false>(aw, pw, product, s)) return rc;
     return PSGD_OK;
 }
 
