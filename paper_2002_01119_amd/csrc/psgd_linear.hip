@@ -12,6 +12,7 @@
 #include "psgd_rows.h"
 
 #include <initializer_list>
+#include <iterator>
 #include <type_traits>
 
 namespace psgd {
@@ -161,16 +162,25 @@ template <typename T> __device__ __forceinline__ u32x4 chunk_of_few(const T* p, 
 // values of k (E elements to 16 bytes) by WIDE rows of the tile, and turns them.  Rows of the tile beyond the operand's last are not stored by
 // anyone, so they may hold anything: chunks of the last row again, or what LDS held before.  A block that would reach beyond the last row
 // is one that ends there.
+//
+// Where a chunk or block starts is one 32-bit offset a lane behind an address that is the same for all lanes, and its place in LDS one exclusive or:
+// the products leave little time for anything else on the vector unit, and the float ones run on its own multipliers.  (64-bit addresses a lane,
+// computed where they were used, 24 instructions a load: bf16 8192^3 929 TFLOP/s forward and 1030 for dx and dW, now 1071 and 1100; float 4096^3
+// 125 to 131, now 136 to 139; float tiles of 64, 100.)
 template <typename T, int ROWS, int LANES> struct Bring {
-    static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / LANES;      // chunks a lane brings
+    static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / LANES, LINES = LANES / 8;      // chunks a lane brings; rows or blocks side by side
     static constexpr int WIDE = COUNT < E ? COUNT : E, BLOCKS = COUNT / WIDE, WORDS = WIDE * (int)sizeof(T) / 4;
     static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0, "whole chunks and blocks a lane");
 
-    const T* base;             // of the tile's first row, or column, at the lane's first k
+    const T* base;             // of the tile's first row, or column
     int64_t pitch;
     int line, c;               // the lane's first chunk or block, and its chunk of k
     int rows;                  // of the operand from the tile's first on, at most INT_MAX / 2
     int few;                   // rows of an operand that has fewer than a block, else 0
+    int last;                  // ALONG: the last LINES rows of which there is one, and
+    uint32_t off[2 > BLOCKS ? 2 : BLOCKS];      // where the lane's chunk is in LINES rows, and in the last ones; else where its blocks are, and WIDE behind
+    int place;                 // of the first chunk in the tile
+    bool cut;                  // a block ends with the operand's last row instead of beginning at a multiple of WIDE
 
     template <bool ALONG> __device__ __forceinline__ void start(const T* p, int64_t pitch_, int64_t row0, int64_t all) {
         const int tid = threadIdx.x % LANES;
@@ -185,29 +195,48 @@ template <typename T, int ROWS, int LANES> struct Bring {
         pitch = pitch_;
         rows = (int)(all - row0 < (1 << 30) ? all - row0 : (1 << 30));
         few = !ALONG && all < WIDE ? (int)all : 0;
-        base = ALONG ? p + row0 * pitch + c * E : p + c * E * pitch + row0;
+        base = ALONG ? p + row0 * pitch : p + row0;
+        const int size = (int)sizeof(T);
+        if (ALONG) {
+            last = (rows < ROWS ? rows - 1 : ROWS - 1) / LINES;
+            const int end = rows - 1 - last * LINES;
+            off[0] = (uint32_t)line * (uint32_t)pitch * size + c * 16;
+            off[1] = (uint32_t)(line < end ? line : end) * (uint32_t)pitch * size + c * 16;
+            place = tile_place(line, c);
+        } else {
+            cut = rows < ROWS && rows % WIDE;
+#pragma unroll
+            for (int j = 0; j < BLOCKS; ++j) off[j] = (uint32_t)(c * E) * (uint32_t)pitch * size + (uint32_t)(row_of<false>(j) + WIDE) * size;
+            place = tile_place(line * WIDE, c);
+        }
     }
-    // Where chunk or block j starts in memory, from `base`, and in the tile.  Computed where it is used: kept, they would cost registers that the
-    // products need.
+    // Rows so long that 32-bit offsets of a tile could end are brought by fetch_upto alone.
+    static __device__ __forceinline__ bool too_long(int64_t pitch) { return pitch > 1 << 24; }
+    // The row of chunk or block j.
     template <bool ALONG> __device__ __forceinline__ int row_of(int j) const {
-        const int r = ALONG ? line + j * (LANES / 8) : (line + j * (LANES / 8)) * WIDE;
+        const int r = ALONG ? line + j * LINES : (line + j * LINES) * WIDE;
         return ALONG || few || r + WIDE <= rows ? r : rows - WIDE;
     }
     template <bool ALONG> __device__ __forceinline__ const T* from(int j) const {
         if (ALONG) {
             const int r = row_of<ALONG>(j);
-            return base + (r < rows ? r : rows - 1) * pitch;
+            return base + (r < rows ? r : rows - 1) * pitch + c * E;
         }
-        return base + (few ? 0 : row_of<ALONG>(j));
+        return base + c * E * pitch + (few ? 0 : row_of<ALONG>(j));
     }
     // The whole depth from k0 is there.  Chunks, or lines, first to end - 1.
     static constexpr int loads(bool along) { return along ? COUNT : BLOCKS * E; }
     template <bool ALONG> __device__ __forceinline__ void fetch(u32x4 (&raw)[COUNT], int64_t k0, int first = 0, int end = loads(ALONG)) {
-        asm volatile("" : "+v"(line));                  // not outside of the loop
+        if (ALONG) asm volatile("" : "+v"(off[0]), "+v"(off[1]));      // the choice between them is not made outside of the loop
 #pragma unroll
         for (int l = first; l < end; ++l) {
-            if constexpr (ALONG) raw[l] = load_raw(from<true>(l) + k0);
-            else keep(raw, l, load_words<WORDS>(from<false>(l / E) + (k0 + l % E) * pitch));
+            if constexpr (ALONG) {
+                const char* at = reinterpret_cast<const char*>(base + (int64_t)((l < last ? l : last) * LINES) * pitch + k0);
+                raw[l] = load_raw(reinterpret_cast<const T*>(at + (l < last ? off[0] : off[1])));
+            } else {
+                const char* at = reinterpret_cast<const char*>(base + (k0 + l % E) * pitch - WIDE);
+                keep(raw, l, load_words<WORDS>(reinterpret_cast<const T*>(at + off[l / E])));
+            }
             __builtin_amdgcn_sched_barrier(0);      // one address at a time
         }
     }
@@ -241,12 +270,15 @@ template <typename T, int ROWS, int LANES> struct Bring {
     }
     static __device__ __forceinline__ uint32_t word(const u32x4 (&raw)[COUNT], int n, int w) { return raw[(n * WORDS + w) / 4][(n * WORDS + w) % 4]; }
 
-    template <bool ALONG> __device__ __forceinline__ void put(const u32x4 (&raw)[COUNT], char* tile, int first = 0, int end = COUNT) const {
+    // tile_place is made of exclusive ors of the bits of r and c: the place of r ^ e is that of r, exclusive or that of e.
+    template <bool ALONG> __device__ __forceinline__ void put(const u32x4 (&raw)[COUNT], char* tile, int first = 0, int end = COUNT) {
+        asm volatile("" : "+v"(place), "+v"(line));      // places are made where they are used: kept, they would cost registers that the products need
+        if constexpr (ALONG) {
 #pragma unroll
-        for (int n = first; n < end; ++n) {
-            if constexpr (ALONG) {
-                *reinterpret_cast<u32x4*>(tile + tile_place(row_of<true>(n), c)) = raw[n];
-            } else {
+            for (int n = first; n < end; ++n) *reinterpret_cast<u32x4*>(tile + (place ^ tile_place(n * LINES, 0))) = raw[n];
+        } else {
+#pragma unroll
+            for (int n = first; n < end; ++n) {
                 const int s = n / WIDE, e = n % WIDE;
                 u32x4 v;
 #pragma unroll
@@ -255,8 +287,9 @@ template <typename T, int ROWS, int LANES> struct Bring {
                         v[j] = word(raw, s * 4 + j, e);
                     else      // the upper or lower halves of two words
                         v[j] = __builtin_amdgcn_perm(word(raw, s * 8 + 2 * j + 1, e / 2), word(raw, s * 8 + 2 * j, e / 2), e % 2 ? 0x07060302u : 0x05040100u);
+                if (!cut && !few) *reinterpret_cast<u32x4*>(tile + (place ^ tile_place(s * LINES * WIDE + e, 0))) = v;
                 // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
-                *reinterpret_cast<u32x4*>(tile + tile_place(((few ? 0 : row_of<false>(s)) + e) & (ROWS - 1), c)) = v;
+                else *reinterpret_cast<u32x4*>(tile + tile_place(((few ? 0 : row_of<false>(s)) + e) & (ROWS - 1), c)) = v;
             }
         }
     }
@@ -272,6 +305,30 @@ template <typename T, int ROWS, int LANES> struct Bring {
             put<false>(raw, tile);
             if (more) fetch<false>(raw, k0);
         }
+    }
+};
+
+// A wavefront's part of bringing a tile of k: one operand of a square tile (half of the wavefronts bring the other), or its share of both.
+template <bool ALONG, typename Bring> struct BringOne {
+    Bring& b;
+    u32x4 (&raw)[Bring::COUNT];
+    char* at;
+    __device__ __forceinline__ void fetch(int64_t k0) { b.template fetch<ALONG>(raw, k0); }
+    __device__ __forceinline__ void fetch_upto(int64_t k0, int64_t end) { b.template fetch_upto<ALONG>(raw, k0, end); }
+    __device__ __forceinline__ void put(int side) { b.template put<ALONG>(raw, at + side); }
+    __device__ __forceinline__ void turn_over(int side, bool more, int64_t k0, int slot, int slots) {
+        b.template turn_over<ALONG>(raw, at + side, more, k0, slot, slots);
+    }
+};
+template <typename One, typename Other> struct BringBoth {
+    One& p;
+    Other& q;
+    __device__ __forceinline__ void fetch(int64_t k0) { p.fetch(k0), q.fetch(k0); }
+    __device__ __forceinline__ void fetch_upto(int64_t k0, int64_t end) { p.fetch_upto(k0, end), q.fetch_upto(k0, end); }
+    __device__ __forceinline__ void put(int side) { p.put(side), q.put(side); }
+    __device__ __forceinline__ void turn_over(int side, bool more, int64_t k0, int slot, int slots) {
+        p.turn_over(side, more, k0, slot, slots);
+        q.turn_over(side, more, k0, slot, slots);
     }
 };
 
@@ -306,11 +363,17 @@ __device__ __forceinline__ Tile tile_of(const GemmArgs& a, uint32_t id, uint32_t
 
 extern __shared__ __attribute__((aligned(128))) char lds[];
 
+// The wavefronts of a workgroup, along m and along n.
+template <int BM, int BN> struct TileShape {
+    static constexpr int ACROSS_M = BM > BN ? 4 : BM < BN ? 1 : 2, ACROSS_N = BM > BN ? 1 : BM < BN || BM == 256 ? 4 : 2;
+    static constexpr int LANES = kWave * ACROSS_M * ACROSS_N;
+};
+
 // Workgroup `id` of `total` that this product has.
-template <typename T, int BM, int BN, int ACROSS_N, bool P_ALONG, bool Q_ALONG>
+template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG>
 __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32_t total) {
-    // wavefronts, two along m by ACROSS_N along n; 32 x 32 tiles of each
-    constexpr int NT = 128 * ACROSS_N, TM = BM / 64, TN = BN / 32 / ACROSS_N, BK = kDepth<T>, WN = BN / ACROSS_N;
+    using Shape = TileShape<BM, BN>;
+    constexpr int NT = Shape::LANES, ACROSS_M = Shape::ACROSS_M, WM = BM / ACROSS_M, WN = BN / Shape::ACROSS_N, TM = WM / 32, TN = WN / 32, BK = kDepth<T>;
     constexpr int kP = BM * kRowBytes, kBoth = (BM + BN) * kRowBytes;
     const Tile t = tile_of(a, id, total);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
@@ -324,16 +387,14 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
     for (int i = 0; i < TN; ++i)
 #pragma unroll
         for (int j = 0; j < TM; ++j) acc[i][j] = (f32x16){};
-    static_assert(BM == BN, "the halves of the workgroup bring as many chunks a lane");
-    static_assert(BM == BN, "the halves of the workgroup bring as many chunks a lane");
-    const bool first = __builtin_amdgcn_readfirstlane(threadIdx.x) < NT / 2;      // which operand the wavefront brings
-    Bring<T, BM, NT / 2> bring;
-    u32x4 raw[bring.COUNT];
-    char* const mine_at = first ? lds : lds + kP;
-    if (first) bring.template start<P_ALONG>(p, a.p.pitch, m0, a.m);
-    else bring.template start<Q_ALONG>(q, a.q.pitch, n0, a.n);
-    const bool few = (!P_ALONG && a.m < bring.WIDE) || (!Q_ALONG && a.n < bring.WIDE);      // the same for the whole workgroup
-    const int mw = wave % 2 * (BM / 2) + lane % 32, nw = wave / 2 * WN + lane % 32;
+    // which operand the wavefront brings, if one
+    constexpr bool SQUARE = BM == BN;
+    const bool first = __builtin_amdgcn_readfirstlane(threadIdx.x) < NT / 2;
+    using BringP = Bring<T, BM, SQUARE ? NT / 2 : NT>;
+    using BringQ = Bring<T, BN, SQUARE ? NT / 2 : NT>;
+    const bool slow = (!P_ALONG && a.m < BringP::WIDE) || (!Q_ALONG && a.n < BringQ::WIDE) ||      // the same for the whole workgroup
+                      BringP::too_long(a.p.pitch) || BringQ::too_long(a.q.pitch);
+    const int mw = wave % ACROSS_M * WM + lane % 32, nw = wave / ACROSS_M * WN + lane % 32;
     // The chunks of one step of 16 bytes of k, and its products.
     struct Step {
         u32x4 p[TM], q[TN];
@@ -364,26 +425,23 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
             }
         }
     };
-    // The same loop for both halves of the workgroup, each with its operand's way.  Tiles of k that are there to their end, then what is cut off.
-    auto walk = [&](auto along) {
-        constexpr bool ALONG = decltype(along)::value;
-        const int64_t last = a.k / BK, whole = few ? from : to < last ? to : last;
+    // Tiles of k that are there to their end, then what is cut off.
+    auto walk = [&](auto& bring) {
+        const int64_t last = a.k / BK, whole = slow ? from : to < last ? to : last;
         int64_t tile = from;
         if (tile < whole) {
-            bring.template fetch<ALONG>(raw, tile * BK);
-            bring.template put<ALONG>(raw, mine_at);
-            if (tile + 1 < whole) bring.template fetch<ALONG>(raw, (tile + 1) * BK);
+            bring.fetch(tile * BK);
+            bring.put(0);
+            if (tile + 1 < whole) bring.fetch((tile + 1) * BK);
             __syncthreads();
             int side = 0;
             for (; tile + 2 < whole; ++tile) {
-                multiply_tile(lds + side, [&](int slot) {
-                    bring.template turn_over<ALONG>(raw, mine_at + (kBoth - side), true, (tile + 2) * BK, slot, 4 * TN);
-                });
+                multiply_tile(lds + side, [&](int slot) { bring.turn_over(kBoth - side, true, (tile + 2) * BK, slot, 4 * TN); });
                 side = kBoth - side;
                 __syncthreads();
             }
             if (tile + 1 < whole) {
-                multiply_tile(lds + side, [&](int slot) { bring.template turn_over<ALONG>(raw, mine_at + (kBoth - side), false, 0, slot, 4 * TN); });
+                multiply_tile(lds + side, [&](int slot) { bring.turn_over(kBoth - side, false, 0, slot, 4 * TN); });
                 side = kBoth - side;
                 ++tile;
                 __syncthreads();
@@ -393,20 +451,39 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
             __syncthreads();
         }
         for (; tile < to; ++tile) {
-            bring.template fetch_upto<ALONG>(raw, tile * BK, a.k);
-            bring.template put<ALONG>(raw, mine_at);
+            bring.fetch_upto(tile * BK, a.k);
+            bring.put(0);
             __syncthreads();
             multiply_tile(lds, [](int) {});
             __syncthreads();
         }
     };
-    if (P_ALONG == Q_ALONG || first) walk(std::integral_constant<bool, P_ALONG>{});
-    else walk(std::integral_constant<bool, Q_ALONG>{});
+    if constexpr (SQUARE) {      // the same loop for both halves of the workgroup, each with its operand's way
+        BringP bring;
+        u32x4 raw[BringP::COUNT];
+        char* const at = first ? lds : lds + kP;
+        if (first) bring.template start<P_ALONG>(p, a.p.pitch, m0, a.m);
+        else bring.template start<Q_ALONG>(q, a.q.pitch, n0, a.n);
+        BringOne<P_ALONG, BringP> one{bring, raw, at};
+        BringOne<Q_ALONG, BringP> other{bring, raw, at};
+        if (P_ALONG == Q_ALONG || first) walk(one);
+        else walk(other);
+    } else {
+        BringP bring_p;
+        BringQ bring_q;
+        u32x4 raw_p[BringP::COUNT], raw_q[BringQ::COUNT];
+        bring_p.template start<P_ALONG>(p, a.p.pitch, m0, a.m);
+        bring_q.template start<Q_ALONG>(q, a.q.pitch, n0, a.n);
+        BringOne<P_ALONG, BringP> one{bring_p, raw_p, lds};
+        BringOne<Q_ALONG, BringQ> other{bring_q, raw_q, lds + kP};
+        BringBoth<decltype(one), decltype(other)> both{one, other};
+        walk(both);
+    }
     // Lane l holds column l % 32 of m and, of each 32 of n, four stretches of four: 8 g + 4 (l / 32) .. + 3.  Through LDS, 32 rows of m at a time, so that
     // C's rows are read and written side by side.
     constexpr int E = kPer<T>, PITCH = WN + 4, ACROSS = WN / E;          // a lane takes 16 bytes of C's columns: 64 / ACROSS rows at a time
     float* mine = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
-    const int64_t n = n0 + wave / 2 * WN + lane % ACROSS * E, left = a.n - n;
+    const int64_t n = n0 + wave / ACROSS_M * WN + lane % ACROSS * E, left = a.n - n;
     float bias[E] = {};
     if (a.out.bias.p && left > 0 && !a.partial)
         widen<T>(load_cols(reinterpret_cast<const T*>(a.out.bias.p) + t.learner * a.out.bias.learner + n, left), bias);
@@ -422,7 +499,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
         if (left > 0) {
 #pragma unroll 2
             for (int r = lane / ACROSS; r < 32; r += kWave / ACROSS) {
-                const int64_t m = m0 + wave % 2 * (BM / 2) + 32 * j + r;
+                const int64_t m = m0 + wave % ACROSS_M * WM + 32 * j + r;
                 float v[E];
 #pragma unroll
                 for (int e = 0; e < E; e += 4) {
@@ -446,15 +523,15 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
     }
 }
 
-template <typename T, int BM, int BN, int ACROSS_N, bool P_ALONG, bool Q_ALONG>
-__global__ __launch_bounds__(128 * ACROSS_N) void gemm_kernel(GemmArgs a) {
-    gemm_tile<T, BM, BN, ACROSS_N, P_ALONG, Q_ALONG>(a, blockIdx.x, gridDim.x);
+template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG>
+__global__ __launch_bounds__((TileShape<BM, BN>::LANES)) void gemm_kernel(GemmArgs a) {
+    gemm_tile<T, BM, BN, P_ALONG, Q_ALONG>(a, blockIdx.x, gridDim.x);
 }
 // The backward pass' two products side by side, dx's workgroups first: neither fills the chip then, and a workgroup alone on its compute unit waits for
 // most of its time.
 template <typename T, int TILE> __global__ __launch_bounds__(256) void gemm_pair_kernel(GemmArgs dx, GemmArgs dw, uint32_t first) {
-    if (blockIdx.x < first) gemm_tile<T, TILE, TILE, 2, true, false>(dx, blockIdx.x, first);
-    else gemm_tile<T, TILE, TILE, 2, false, false>(dw, blockIdx.x - first, gridDim.x - first);
+    if (blockIdx.x < first) gemm_tile<T, TILE, TILE, true, false>(dx, blockIdx.x, first);
+    else gemm_tile<T, TILE, TILE, false, false>(dw, blockIdx.x - first, gridDim.x - first);
 }
 
 // ------------------------------------------------------------------------------------------------ a few tokens
@@ -640,7 +717,7 @@ inline Operand operand(const psgd_view* v) {
 }
 
 struct Plan {
-    int tile, split;             // rows and columns of a workgroup's tile; parts of k
+    int rows, cols, split;       // of a workgroup's tile; parts of k
     size_t bytes(int learners, int64_t m, int64_t n) const {
         return split > 1 ? up256((size_t)split * learners * m * n * sizeof(float)) : 0;
     }
@@ -651,20 +728,23 @@ inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // comes before and after the steps.  Measured (products of 512 to 4096 a side, each tile with 1 to 16 parts of k): large tiles do the most with what
 // they read, small ones fill the chip and wait less.
 struct TileCost {
-    int tile, resident;
+    int rows, cols, resident;
     float alone, shared, ends;
 };
-constexpr TileCost kCosts[2][3] = {{{256, 1, 1.9f, 1.9f, 10.0f}, {128, 2, 0.8f, 0.5f, 6.0f}, {64, 4, 0.5f, 0.3f, 2.5f}},        // bf16
-                                   {{256, 1, 8.0f, 8.0f, 10.0f}, {128, 2, 2.4f, 2.4f, 6.0f}, {64, 4, 0.7f, 0.55f, 2.5f}}};       // float
+constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.9f, 1.9f, 10.0f}, {128, 128, 2, 0.8f, 0.5f, 6.0f}, {64, 64, 4, 0.5f, 0.3f, 2.5f}};
+constexpr TileCost kCostsFloat[] = {{256, 256, 1, 8.0f, 8.0f, 10.0f}, {128, 128, 2, 2.4f, 2.4f, 6.0f}, {64, 64, 4, 0.7f, 0.55f, 2.5f},
+                                    {128, 32, 4, 0.7f, 0.55f, 2.5f}, {32, 128, 4, 0.7f, 0.55f, 2.5f}};
 
 // The tile and the parts of k of the least cost.  Parts cost a second kernel and their sums' way through memory.
 inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
-    Plan best{64, 1};
+    Plan best{64, 64, 1};
     if (m < 1 || n < 1) return best;          // nothing to multiply
     const int64_t steps = parts_of(k, kRowBytes / bytes);
     float least = INFINITY;
-    for (const TileCost& c : kCosts[bytes == 4]) {
-        const int64_t tiles = parts_of(m, c.tile) * parts_of(n, c.tile) * learners;
+    const TileCost* const costs = bytes == 4 ? kCostsFloat : kCostsBf16;
+    for (const TileCost* at = costs; at < costs + (bytes == 4 ? std::size(kCostsFloat) : std::size(kCostsBf16)); ++at) {
+        const TileCost& c = *at;
+        const int64_t tiles = parts_of(m, c.rows) * parts_of(n, c.cols) * learners;
         for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (split > 1 && (steps < 2 * split || tiles * split > 8 * (int64_t)cus)) break;
             const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * c.resident;
@@ -674,25 +754,25 @@ inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, 
             if (split > 1) us += 4.0f + (float)(split + 1) * (float)(m * n * learners) * 4.0f / 3.5e6f;
             if (us < least) {
                 least = us;
-                best = Plan{c.tile, split};
+                best = Plan{c.rows, c.cols, split};
             }
         }
     }
     return best;
 }
 
-template <typename T, int TILE, int ACROSS_N, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
-    a.tiles_m = (int)parts_of(a.m, TILE);
-    a.tiles_n = (int)parts_of(a.n, TILE);
-    constexpr size_t lds = (size_t)4 * TILE * kRowBytes;
-    auto fn = gemm_kernel<T, TILE, TILE, ACROSS_N, P_ALONG, Q_ALONG>;
+template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
+    a.tiles_m = (int)parts_of(a.m, BM);
+    a.tiles_n = (int)parts_of(a.n, BN);
+    constexpr size_t lds = (size_t)2 * (BM + BN) * kRowBytes;
+    auto fn = gemm_kernel<T, BM, BN, P_ALONG, Q_ALONG>;
     if (lds >= 64 * 1024) {
         static LdsRecord record;
         if (int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, record)) return rc;
     }
     const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
     if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
-    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(128 * ACROSS_N), lds, s, a);
+    hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(TileShape<BM, BN>::LANES), lds, s, a);
     return PSGD_OK;
 }
 
@@ -701,9 +781,18 @@ int launch_gemm(GemmArgs a, const Plan& plan, float* room, hipStream_t s) {
     a.split = plan.split;
     a.partial = plan.split > 1 ? room : nullptr;
     int rc;
-    if (plan.tile == 256) rc = launch_tiles<T, 256, 4, P_ALONG, Q_ALONG>(a, s);
-    else if (plan.tile == 128) rc = launch_tiles<T, 128, 2, P_ALONG, Q_ALONG>(a, s);
-    else rc = launch_tiles<T, 64, 2, P_ALONG, Q_ALONG>(a, s);
+    if (plan.rows == 256) {
+        rc = launch_tiles<T, 256, 256, P_ALONG, Q_ALONG>(a, s);
+    } else if (plan.rows == 128 && plan.cols == 128) {
+        rc = launch_tiles<T, 128, 128, P_ALONG, Q_ALONG>(a, s);
+    } else if (plan.rows == plan.cols) {
+        rc = launch_tiles<T, 64, 64, P_ALONG, Q_ALONG>(a, s);
+    } else if constexpr (sizeof(T) == 4) {
+        if (plan.rows == 128) rc = launch_tiles<T, 128, 32, P_ALONG, Q_ALONG>(a, s);
+        else rc = launch_tiles<T, 32, 128, P_ALONG, Q_ALONG>(a, s);
+    } else {
+        return fail(PSGD_EINVAL, "psgd_linear: no such tile");
+    }
     if (rc || plan.split == 1) return rc;
     const JoinArgs j{room, plan.split, a.learners * a.m * a.n, a.m * a.n, a.out, a.m, a.n};
     hipLaunchKernelGGL((join_kernel<T>), dim3((unsigned)parts_of(a.m * parts_of(a.n, kPer<T>), 256), 1, a.learners), dim3(256), 0, s, j);
@@ -771,7 +860,7 @@ inline bool four_outputs(int learners, int64_t out, int cus) { return out * lear
 // wavefront) 39 / 29, eight of them (four) 155 / 182; eight tokens 26 / 29.
 inline int most_few(int learners, int64_t out, int bytes, int cus) { return bytes == 2 ? 4 : four_outputs(learners, out, cus) ? 16 : 8; }
 inline Plan forward_plan(int learners, int64_t t, int64_t out, int64_t in, int bytes, int cus) {
-    return t <= most_few(learners, out, bytes, cus) ? Plan{64, 1} : gemm_plan(learners, t, out, in, bytes, cus);
+    return t <= most_few(learners, out, bytes, cus) ? Plan{64, 64, 1} : gemm_plan(learners, t, out, in, bytes, cus);
 }
 
 template <typename T> int linear_of(const GemmArgs& a, const Plan& plan, void* workspace, int cus, hipStream_t s) {
@@ -817,8 +906,8 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
     GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
     const Plan px = gemm_plan(n, t, in, out, sizeof(T), cus), pw = gemm_plan(n, out, in, t, sizeof(T), cus);
-    if (dx && dw && px.split == 1 && pw.split == 1 && px.tile == pw.tile && px.tile < 256)
-        return px.tile == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
+    if (dx && dw && px.split == 1 && pw.split == 1 && px.rows == px.cols && px.rows == pw.rows && pw.rows == pw.cols && px.rows < 256)
+        return px.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
     if (dx)
         if (int rc = launch_gemm<T, true, false>(ax, px, product, s)) return rc;
     if (dw)

@@ -205,6 +205,41 @@ def test_offsets_beyond_32_bits(layers):
     orc.assert_within(x.contiguous(), want[0], bound[0], "dx")
 
 
+def test_rows_too_long_for_offsets_of_32_bits(layers):
+    n, t, i, o = 1, 70, 136, 40
+    _, w, b = layer(n, i, o, BF16, 1)
+    far = (1 << 24) + 24
+    x = torch.empty(t * far, dtype=BF16, device="cuda:0").as_strided((n, t, i), (t * far, far, 1))
+    x.copy_(normal((n, t, i), BF16, 3))
+    y, dw, dy = rows(n, t, o, BF16), torch.empty((n, o, i), dtype=BF16, device="cuda:0"), rows(n, t, o, BF16, 4)
+    layers.linear(x, w, y, bias=b)
+    want, bound = orc.linear(x, w, b, "none", None, BF16)
+    orc.assert_within(y, want[0], bound[0], "y")
+    layers.linear_grad(dy, x, w, dw=dw)
+    want, bound = orc.linear_grad(dy, x.contiguous(), w, "none", None, BF16)
+    orc.assert_within(dw, want[1], bound[1], "dw")
+
+
+# products with few rows or few columns, cut at every place of a block of four, with parts of k and without
+@pytest.mark.parametrize("n,t,i,o", [(2, 700, 520, 16), (1, 300, 1111, 25), (3, 129, 64, 34), (1, 1030, 300, 31), (2, 600, 16, 700), (1, 515, 27, 1000),
+                                     (4, 260, 33, 140), (2, 24, 1200, 900), (1, 31, 2050, 515), (3, 18, 70, 300), (1, 130, 96, 130), (8, 200, 400, 3)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_narrow_products(layers, n, t, i, o, dtype):
+    pitch, lead, off = (3, 1, 5) if (i + o) % 2 else (0, 0, 0)
+    _, w, b = layer(n, i, o, dtype, 1, off)
+    x, y, dy = rows(n, t, i, dtype, 3, pitch, lead), rows(n, t, o, dtype, None, pitch, lead), rows(n, t, o, dtype, 4, pitch, lead)
+    layers.linear(x, w, y, bias=b, act="relu")
+    want, bound = orc.linear(x, w, b, "relu", None, dtype)
+    orc.assert_within(y, want[0], bound[0], "y")
+    dx = rows(n, t, i, dtype, None, pitch, lead)
+    grads, dw, db = layer(n, i, o, dtype, None, off)
+    layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db)
+    want, bound = orc.linear_grad(dy, x, w, "none", None, dtype)
+    for got, v, e, what in zip((dx, dw, db), want, bound, ("dx", "dw", "db")):
+        orc.assert_within(got, v, e, what)
+    untouched(grads, dw, db, off)
+
+
 def test_gradient_against_differences(layers):
     n, t, i, o, e = 2, 9, 33, 21, 1e-5
     _, w, b = layer(n, i, o, F32, 1)
