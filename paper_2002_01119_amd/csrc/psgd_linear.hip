@@ -731,7 +731,7 @@ struct TileCost {
     int rows, cols, resident;
     float alone, shared, ends;
 };
-constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.9f, 1.9f, 10.0f}, {128, 128, 2, 0.8f, 0.5f, 6.0f}, {64, 64, 4, 0.5f, 0.3f, 2.5f}};
+constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.75f, 1.75f, 9.0f}, {128, 128, 2, 0.7f, 0.45f, 5.0f}, {64, 64, 4, 0.53f, 0.25f, 2.2f}};
 constexpr TileCost kCostsFloat[] = {{256, 256, 1, 8.0f, 8.0f, 10.0f}, {128, 128, 2, 2.4f, 2.4f, 6.0f}, {64, 64, 4, 0.7f, 0.55f, 2.5f},
                                     {128, 32, 4, 0.7f, 0.55f, 2.5f}, {32, 128, 4, 0.7f, 0.55f, 2.5f}};
 
