@@ -536,8 +536,7 @@ template <typename T, int TILE> __global__ __launch_bounds__(256) void gemm_pair
 
 // ------------------------------------------------------------------------------------------------ a few tokens
 // The forward product of up to TOK tokens: W is read once, 1 KB of one row at a time, which is all it costs; the tokens come from the first-level
-// cache.  A wavefront takes R rows of W (outputs) and keeps R x TOK sums a lane, joined at the end.  bf16 tokens beyond four would cost the vector unit
-// more than the reading takes; from there on the tiles are as fast.  One token of eight learners, 4096 x 4096: bf16 62 us by tiles, float 181.
+// cache.  A wavefront takes R rows of W (outputs) and keeps R x TOK sums a lane, joined at the end.
 struct FewArgs {
     Operand x, w;
     Epilogue out;
@@ -616,6 +615,46 @@ template <typename T, int TOK, int R> __global__ __launch_bounds__(256) void few
                                  : v;
     if (o.residual.p) v += load_1(reinterpret_cast<const T*>(o.residual.p) + i * o.residual.learner + t * o.residual.pitch + n);
     store_1(reinterpret_cast<T*>(const_cast<char*>(o.y.p)) + i * o.y.learner + t * o.y.pitch + n, v);
+}
+
+// dW = dz' x of up to TOK tokens: little more than writing dW, which is done in rows.  A lane keeps 16 bytes of columns of x; a wavefront takes up to 64
+// rows (outputs), whose dz it reads at once, a row a lane.  (dx of so few tokens is left to the tiles: W read like this, with its sums beside it, was
+// slower at every size but one, 8 to 200 % at four tokens.)
+struct FewGradArgs {
+    Operand dz, x, dw;
+    int64_t t, in, out;
+    int rows;                      // of dW to a wavefront, at most 64
+};
+template <typename T, int TOK> __global__ __launch_bounds__(256) void few_tokens_grad_kernel(FewGradArgs a) {
+    constexpr int E = kPer<T>;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t i = blockIdx.z, col0 = (int64_t)blockIdx.x * kWave * E, col = col0 + lane * E, left = a.in - col;
+    const int64_t first = ((int64_t)blockIdx.y * 4 + wave) * a.rows;
+    if (first >= a.out) return;
+    const int count = (int)(a.out - first < a.rows ? a.out - first : a.rows);
+    const T* dz = reinterpret_cast<const T*>(a.dz.p) + i * a.dz.learner + first;
+    T* dw = reinterpret_cast<T*>(const_cast<char*>(a.dw.p)) + i * a.dw.learner + first * a.dw.pitch + col;
+    float x[TOK][E] = {}, d[TOK];
+#pragma unroll
+    for (int t = 0; t < TOK; ++t) {
+        d[t] = t < a.t && lane < count ? load_1(dz + t * a.dz.pitch + lane) : 0.0f;
+        if (t < a.t && left > 0) widen<T>(load_cols(reinterpret_cast<const T*>(a.x.p) + i * a.x.learner + t * a.x.pitch + col, left), x[t]);
+    }
+    auto walk = [&](auto inside) {
+        for (int r = 0; r < count; ++r) {
+            float v[E] = {};
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+                const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(d[t]), r));
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = __builtin_fmaf(f, x[t][e], v[e]);
+            }
+            if (inside) store_cols<T>(dw + r * a.dw.pitch, v, E);
+            else if (left > 0) store_cols<T>(dw + r * a.dw.pitch, v, left);
+        }
+    };
+    if (col0 + kWave * E <= a.in) walk(std::true_type{});
+    else walk(std::false_type{});
 }
 
 // ------------------------------------------------------------------------------------------------ dz and db
@@ -826,6 +865,10 @@ inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cu
     return slabs < 1 ? 1 : slabs > 65535 ? 65535 : slabs;
 }
 
+// Whether few_tokens_grad_kernel makes dW.  us, it / tiles: 4 tokens of eight learners 6400 x 4096 float 155 / 282, bf16 86 / 144, of one 4096 x 4096
+// 13 / 25 and 10 / 15; 16 float tokens 167 / 282 and 19 / 25.
+inline bool few_tokens_grad(int64_t t, int bytes) { return t >= 1 && t <= (bytes == 2 ? 4 : 16); }
+
 struct GradRoom {
     size_t dz, sums, product, total;
     int64_t dz_pitch;
@@ -836,7 +879,7 @@ inline GradRoom grad_room(int act, int learners, int64_t t, int64_t in, int64_t 
     r.dz = act != PSGD_ACT_NONE ? up256((size_t)learners * t * r.dz_pitch * bytes) : 0;
     r.sums = db ? up256((size_t)learners * slope_slabs(learners, t, out, bytes, cus) * out * sizeof(float)) : 0;
     const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus).bytes(learners, t, in) : 0;
-    const size_t b = dw ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
+    const size_t b = dw && !few_tokens_grad(t, bytes) ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
     r.product = a > b ? a : b;
     r.total = r.dz + r.sums + r.product;
     return r;
@@ -856,9 +899,10 @@ inline int check_room(const char* name, void* workspace, size_t have, size_t nee
 
 // Four outputs a wavefront where that leaves eight wavefronts for each compute unit.
 inline bool four_outputs(int learners, int64_t out, int cus) { return out * learners >= (int64_t)cus * 32; }
-// Tokens that few_tokens_kernel takes: no tiles then, and no parts of k.  us, float, 16 tokens, this kernel / tiles: one 4096 x 4096 (an output a
-// wavefront) 39 / 29, eight of them (four) 155 / 182; eight tokens 26 / 29.
-inline int most_few(int learners, int64_t out, int bytes, int cus) { return bytes == 2 ? 4 : four_outputs(learners, out, cus) ? 16 : 8; }
+// Tokens that few_tokens_kernel takes: no tiles then, and no parts of k.  us, this kernel / tiles: float 1 token 4096 x 4096 12 / 19, of eight learners
+// 97 / 125, 4 tokens of eight learners 106 / 131; 8 tokens with an output a wavefront 4 x 1024 x 1024 7 / 12, with four 16 x 4489 x 4696 324 / 291 and
+// 16 x 4096 x 2048 125 / 126; bf16 1 token 4096 x 4096 5 / 12, 4 tokens 8 / 13 and of sixteen learners, 4489 x 4696, 165 / 235.
+inline int most_few(int learners, int64_t out, int bytes, int cus) { return bytes == 2 || four_outputs(learners, out, cus) ? 4 : 8; }
 inline Plan forward_plan(int learners, int64_t t, int64_t out, int64_t in, int bytes, int cus) {
     return t <= most_few(learners, out, bytes, cus) ? Plan{64, 64, 1} : gemm_plan(learners, t, out, in, bytes, cus);
 }
@@ -875,10 +919,7 @@ template <typename T> int linear_of(const GemmArgs& a, const Plan& plan, void* w
     if (a.m <= 1) PSGD_FEW(1);
     else if (a.m <= 2) PSGD_FEW(2);
     else if (a.m <= 4) PSGD_FEW(4);
-    else if constexpr (sizeof(T) == 4) {
-        if (a.m <= 8) PSGD_FEW(8);
-        else hipLaunchKernelGGL((few_tokens_kernel<T, 16, 4>), dim3((unsigned)parts_of(a.n, 16), a.learners), dim3(256), 0, s, f);
-    }
+    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_tokens_kernel<T, 8, 1>), dim3((unsigned)parts_of(a.n, 4), a.learners), dim3(256), 0, s, f);
 #undef PSGD_FEW
     return PSGD_OK;
 }
@@ -906,12 +947,28 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
     GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
     const Plan px = gemm_plan(n, t, in, out, sizeof(T), cus), pw = gemm_plan(n, out, in, t, sizeof(T), cus);
-    if (dx && dw && px.split == 1 && pw.split == 1 && px.rows == px.cols && px.rows == pw.rows && pw.rows == pw.cols && px.rows < 256)
+    // one launch for both, also of few tokens where dW is small: 8192 x 500 bf16, 4 tokens, 9.6 us, apart 7.4 and 6.6
+    const bool few = few_tokens_grad(t, sizeof(T)), small = (int64_t)n * in * out * (int64_t)sizeof(T) <= (8 << 20);
+    if (dx && dw && (!few || small) && px.split == 1 && pw.split == 1 && px.rows == px.cols && px.rows == pw.rows && pw.rows == pw.cols && px.rows < 256)
         return px.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
     if (dx)
         if (int rc = launch_gemm<T, true, false>(ax, px, product, s)) return rc;
-    if (dw)
+    if (dw && few) {
+        // 64 rows a wavefront, fewer where that leaves compute units without eight wavefronts
+        const int64_t across = parts_of(in, kWave * kPer<T>), all = across * n * out;
+        const int rows = all >= (int64_t)cus * 8 * 64 ? 64 : all >= (int64_t)cus * 8 * 16 ? 16 : 4;
+        const FewGradArgs f{dz, operand(x), operand(dw), t, in, out, rows};
+        const dim3 grid((unsigned)across, (unsigned)parts_of(out, 4 * rows), n);
+        if (grid.y > 65535) return fail(PSGD_EINVAL, "psgd_linear_grad: too many outputs");
+        if (t <= 2) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 2>), grid, dim3(256), 0, s, f);
+        else if (t <= 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 4>), grid, dim3(256), 0, s, f);
+        else if constexpr (sizeof(T) == 4) {
+            if (t <= 8) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 8>), grid, dim3(256), 0, s, f);
+            else hipLaunchKernelGGL((few_tokens_grad_kernel<T, 16>), grid, dim3(256), 0, s, f);
+        }
+    } else if (dw) {
         if (int rc = launch_gemm<T, false, false>(aw, pw, product, s)) return rc;
+    }
     return PSGD_OK;
 }
 
