@@ -866,8 +866,8 @@ inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cu
 }
 
 // Whether few_tokens_grad_kernel makes dW.  us, it / tiles: 4 tokens of eight learners 6400 x 4096 float 155 / 282, bf16 86 / 144, of one 4096 x 4096
-// 13 / 25 and 10 / 15; 16 float tokens 167 / 282 and 19 / 25.
-inline bool few_tokens_grad(int64_t t, int bytes) { return t >= 1 && t <= (bytes == 2 ? 4 : 16); }
+// 13 / 25 and 10 / 15; 16 float tokens 167 / 282 and 19 / 25, 8 bf16 92 / 145 and 14 / 16.
+inline bool few_tokens_grad(int64_t t, int bytes) { return t >= 1 && t <= (bytes == 2 ? 8 : 16); }
 
 struct GradRoom {
     size_t dz, sums, product, total;
@@ -962,10 +962,8 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
         if (grid.y > 65535) return fail(PSGD_EINVAL, "psgd_linear_grad: too many outputs");
         if (t <= 2) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 2>), grid, dim3(256), 0, s, f);
         else if (t <= 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 4>), grid, dim3(256), 0, s, f);
-        else if constexpr (sizeof(T) == 4) {
-            if (t <= 8) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 8>), grid, dim3(256), 0, s, f);
-            else hipLaunchKernelGGL((few_tokens_grad_kernel<T, 16>), grid, dim3(256), 0, s, f);
-        }
+        else if (t <= 8) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 8>), grid, dim3(256), 0, s, f);
+        else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 16>), grid, dim3(256), 0, s, f);
     } else if (dw) {
         if (int rc = launch_gemm<T, false, false>(aw, pw, product, s)) return rc;
     }
