@@ -170,7 +170,7 @@ template <typename T> __device__ __forceinline__ u32x4 chunk_of_few(const T* p, 
 template <typename T, int ROWS, int LANES> struct Bring {
     static constexpr int E = kPer<T>, COUNT = ROWS * kRowBytes / 16 / LANES, LINES = LANES / 8;      // chunks a lane brings; rows or blocks side by side
     static constexpr int WIDE = COUNT < E ? COUNT : E, BLOCKS = COUNT / WIDE, WORDS = WIDE * (int)sizeof(T) / 4;
-    static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0, "whole chunks and blocks a lane");
+    static_assert(COUNT > 0 && WORDS > 0 && COUNT % WIDE == 0 && BLOCKS <= 2, "whole chunks and blocks a lane");
 
     const T* base;             // of the tile's first row, or column
     int64_t pitch;
@@ -178,7 +178,7 @@ template <typename T, int ROWS, int LANES> struct Bring {
     int rows;                  // of the operand from the tile's first on, at most INT_MAX / 2
     int few;                   // rows of an operand that has fewer than a block, else 0
     int last;                  // ALONG: the last LINES rows of which there is one, and
-    uint32_t off[2 > BLOCKS ? 2 : BLOCKS];      // where the lane's chunk is in LINES rows, and in the last ones; else where its blocks are, and WIDE behind
+    uint32_t off[2];           // where the lane's chunk is in LINES rows, and in the last ones; else where its blocks are, and WIDE behind
     int place;                 // of the first chunk in the tile
     bool cut;                  // a block ends with the operand's last row instead of beginning at a multiple of WIDE
 
@@ -206,7 +206,10 @@ template <typename T, int ROWS, int LANES> struct Bring {
         } else {
             cut = rows < ROWS && rows % WIDE;
 #pragma unroll
-            for (int j = 0; j < BLOCKS; ++j) off[j] = (uint32_t)(c * E) * (uint32_t)pitch * size + (uint32_t)(row_of<false>(j) + WIDE) * size;
+            for (int k = 0; k < 2; ++k) {
+                const int j = k < BLOCKS ? k : 0;
+                off[k] = (uint32_t)(c * E) * (uint32_t)pitch * size + (uint32_t)(row_of<false>(j) + WIDE) * size;
+            }
             place = tile_place(line * WIDE, c);
         }
     }
@@ -227,7 +230,7 @@ template <typename T, int ROWS, int LANES> struct Bring {
     // The whole depth from k0 is there.  Chunks, or lines, first to end - 1.
     static constexpr int loads(bool along) { return along ? COUNT : BLOCKS * E; }
     template <bool ALONG> __device__ __forceinline__ void fetch(u32x4 (&raw)[COUNT], int64_t k0, int first = 0, int end = loads(ALONG)) {
-        if (ALONG) asm volatile("" : "+v"(off[0]), "+v"(off[1]));      // the choice between them is not made outside of the loop
+        asm volatile("" : "+v"(off[0]), "+v"(off[1]));      // no sums with them, and no choice between them, are made outside of the loop
 #pragma unroll
         for (int l = first; l < end; ++l) {
             if constexpr (ALONG) {
@@ -276,22 +279,31 @@ template <typename T, int ROWS, int LANES> struct Bring {
         if constexpr (ALONG) {
 #pragma unroll
             for (int n = first; n < end; ++n) *reinterpret_cast<u32x4*>(tile + (place ^ tile_place(n * LINES, 0))) = raw[n];
-        } else {
+        } else if (!cut && !few) {
 #pragma unroll
             for (int n = first; n < end; ++n) {
-                const int s = n / WIDE, e = n % WIDE;
-                u32x4 v;
+                *reinterpret_cast<u32x4*>(tile + (place ^ tile_place(n / WIDE * LINES * WIDE + n % WIDE, 0))) = turned(raw, n);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        } else {      // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if constexpr (sizeof(T) == 4)
-                        v[j] = word(raw, s * 4 + j, e);
-                    else      // the upper or lower halves of two words
-                        v[j] = __builtin_amdgcn_perm(word(raw, s * 8 + 2 * j + 1, e / 2), word(raw, s * 8 + 2 * j, e / 2), e % 2 ? 0x07060302u : 0x05040100u);
-                if (!cut && !few) *reinterpret_cast<u32x4*>(tile + (place ^ tile_place(s * LINES * WIDE + e, 0))) = v;
-                // a block that ends with the operand's last row may begin before the tile's first: to rows that are beyond the last
-                else *reinterpret_cast<u32x4*>(tile + tile_place(((few ? 0 : row_of<false>(s)) + e) & (ROWS - 1), c)) = v;
+            for (int n = first; n < end; ++n) {
+                *reinterpret_cast<u32x4*>(tile + tile_place(((few ? 0 : row_of<false>(n / WIDE)) + n % WIDE) & (ROWS - 1), c)) = turned(raw, n);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+    }
+    // Row n of the lane's blocks.
+    static __device__ __forceinline__ u32x4 turned(const u32x4 (&raw)[COUNT], int n) {
+        const int s = n / WIDE, e = n % WIDE;
+        u32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if constexpr (sizeof(T) == 4)
+                v[j] = word(raw, s * 4 + j, e);
+            else      // the upper or lower halves of two words
+                v[j] = __builtin_amdgcn_perm(word(raw, s * 8 + 2 * j + 1, e / 2), word(raw, s * 8 + 2 * j, e / 2), e % 2 ? 0x07060302u : 0x05040100u);
+        return v;
     }
     // Slot `slot` of `slots` in a tile's products: this lane's part of putting the next tile, which is in `raw`, into LDS, and of sending for the
     // one behind it, so that what is sent for travels for the time of a tile.  Chunks go one after the other, spread over the tile (2 % faster than
@@ -301,7 +313,7 @@ template <typename T, int ROWS, int LANES> struct Bring {
             const int first = slot * COUNT / slots, end = (slot + 1) * COUNT / slots;
             put<true>(raw, tile, first, end);
             if (more) fetch<true>(raw, k0, first, end);
-        } else if (slot == slots / 4) {
+        } else if (slot == slots / 3) {
             put<false>(raw, tile);
             if (more) fetch<false>(raw, k0);
         }
@@ -381,7 +393,8 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
     const T* q = reinterpret_cast<const T*>(a.q.p) + t.learner * a.q.learner;
     const int64_t m0 = (int64_t)t.tm * BM, n0 = (int64_t)t.tn * BN;
     // this part's stretch of k, in whole tiles
-    const int64_t tiles = (a.k + BK - 1) / BK, from = tiles * t.part / a.split, to = tiles * (t.part + 1) / a.split;
+    const int64_t tiles = (a.k + BK - 1) / BK;
+    const int from = (int)(tiles * t.part / a.split), to = (int)(tiles * (t.part + 1) / a.split);
     f32x16 acc[TN][TM];
 #pragma unroll
     for (int i = 0; i < TN; ++i)
@@ -407,18 +420,23 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
 #pragma unroll
         for (int i = 0; i < TN; ++i) f.q[i] = *reinterpret_cast<const u32x4*>(now + (at_q ^ (s << 5)) + 32 * i * kRowBytes);
     };
-    // A tile of k: each step's chunks are read while the one before is multiplied, and the next tile is brought in between (turn_over).  The fences
-    // keep the compiler from sinking loads to their uses.
-    auto multiply_tile = [&](const char* now, auto meanwhile) {
-        Step f[2];
-        read(now, 0, f[0]);
+    // A tile of k: each step's chunks are read while the one before is multiplied, and the next tile is brought in during the first three steps
+    // (turn_over).  The workgroup meets before the last step, so that the next tile's first chunks are read during it: met after it, the matrix
+    // cores would wait for them.  The fences keep the compiler from sinking loads to their uses.
+    Step f[2];
+    auto multiply_tile = [&](const char* now, auto more, const char* next, auto meanwhile) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            if (s < 3) read(now, s + 1, f[(s + 1) % 2]);
+            if (s < 3) {
+                read(now, s + 1, f[(s + 1) % 2]);
+            } else if constexpr (decltype(more)::value) {
+                __syncthreads();
+                read(next, 0, f[0]);
+            }
 #pragma unroll
             for (int i = 0; i < TN; ++i) {
                 __builtin_amdgcn_sched_barrier(0);
-                meanwhile(s * TN + i);
+                if (s < 3) meanwhile(s * TN + i);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int j = 0; j < TM; ++j) multiply(f[s % 2].q[i], f[s % 2].p[j], acc[i][j], T{});
@@ -427,34 +445,34 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
     };
     // Tiles of k that are there to their end, then what is cut off.
     auto walk = [&](auto& bring) {
-        const int64_t last = a.k / BK, whole = slow ? from : to < last ? to : last;
-        int64_t tile = from;
+        const int last = (int)(a.k / BK), whole = slow ? from : to < last ? to : last;
+        int tile = from;
         if (tile < whole) {
-            bring.fetch(tile * BK);
+            bring.fetch((int64_t)tile * BK);
             bring.put(0);
-            if (tile + 1 < whole) bring.fetch((tile + 1) * BK);
+            if (tile + 1 < whole) bring.fetch((int64_t)(tile + 1) * BK);
             __syncthreads();
+            read(lds, 0, f[0]);
             int side = 0;
             for (; tile + 2 < whole; ++tile) {
-                multiply_tile(lds + side, [&](int slot) { bring.turn_over(kBoth - side, true, (tile + 2) * BK, slot, 4 * TN); });
+                multiply_tile(lds + side, std::true_type{}, lds + (kBoth - side), [&](int slot) { bring.turn_over(kBoth - side, true, (int64_t)(tile + 2) * BK, slot, 3 * TN); });
                 side = kBoth - side;
-                __syncthreads();
             }
             if (tile + 1 < whole) {
-                multiply_tile(lds + side, [&](int slot) { bring.turn_over(kBoth - side, false, 0, slot, 4 * TN); });
+                multiply_tile(lds + side, std::true_type{}, lds + (kBoth - side), [&](int slot) { bring.turn_over(kBoth - side, false, 0, slot, 3 * TN); });
                 side = kBoth - side;
                 ++tile;
-                __syncthreads();
             }
-            multiply_tile(lds + side, [](int) {});
+            multiply_tile(lds + side, std::false_type{}, nullptr, [](int) {});
             ++tile;
             __syncthreads();
         }
         for (; tile < to; ++tile) {
-            bring.fetch_upto(tile * BK, a.k);
+            bring.fetch_upto((int64_t)tile * BK, a.k);
             bring.put(0);
             __syncthreads();
-            multiply_tile(lds, [](int) {});
+            read(lds, 0, f[0]);
+            multiply_tile(lds, std::false_type{}, nullptr, [](int) {});
             __syncthreads();
         }
     };
@@ -495,7 +513,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4*>(mine + lane % 32 * PITCH + 32 * i + 8 * g + lane / 32 * 4) =
                     (f32x4){acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // each wavefront has a place of its own
         if (left > 0) {
 #pragma unroll 2
             for (int r = lane / ACROSS; r < 32; r += kWave / ACROSS) {
@@ -519,7 +537,7 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
                 }
             }
         }
-        __syncthreads();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
