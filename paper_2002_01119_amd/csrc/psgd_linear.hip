@@ -9,6 +9,14 @@
 // so an operand comes with k along its rows or down its columns, and one kernel serves them all: it brings either into the same LDS tile,
 // rows of 128 bytes of k, and multiplies from there with the matrix instructions of the type (bf16 32x32x16, float 32x32x2, both summing
 // in fp32).  2 m n k operations against (m + n) k elements: bound by the matrix cores on batches, by reading W at a few tokens.
+//
+// Tiles of 256 x 256 (eight wavefronts), 128 x 128, 64 x 64 and for narrow float products 128 x 32 and 32 x 128 (four each) by 128 bytes of k, twice in
+// LDS: one is multiplied while the next is put beside it and the one behind is on its way in registers.  Large tiles read least; what then
+// keeps the matrix cores from their rate is the operands' way through registers and LDS (without it the same loop multiplies at 1200 to 1380
+// TFLOP/s in bf16; waiting for memory is not it: k read again and again from one place is 0 to 5 % faster).  Measured, TFLOP/s forward / dx / dW: bf16
+// 8192^3 1089 / 1182 / 1127, 4096^3 1150 / 1122 / 1070, 4 x 2048 x 2048 -> 8192 1066 / 1155 / 980 (a library's product of 8192^3 here: 1517 / 1384 / 1192);
+// float 4096^3 145 / 142 / 141 (154).  The epilogue of large tiles has the chip to itself, one workgroup to a compute unit: bias, GELU and a second
+// array of 134 MB are 43 of 301 us for 4 x 2048 x 2048 -> 8192.
 #include "psgd_rows.h"
 
 #include <initializer_list>
@@ -30,6 +38,7 @@ struct Operand {          // element (row, col) of learner i at p + i * learner 
 constexpr float kLog2E = 1.44269504088896341f;
 
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+// Rounded exponentials and reciprocals of the hardware, an ulp or two of float, are behind what an output in bf16 or a float sum of k products loses.
 // erf by Hastings' rational approximation (Abramowitz and Stegun 7.1.26), off by at most 1.5e-7 anywhere: a seventh of the instructions of one that is
 // exact to the last place, which the epilogue of a large tile waits for.  What it leaves in z Phi(z) is 8e-8 |z|.
 __device__ __forceinline__ float erf_of(float x) {
@@ -546,7 +555,7 @@ __global__ __launch_bounds__((TileShape<BM, BN>::LANES)) void gemm_kernel(GemmAr
     gemm_tile<T, BM, BN, P_ALONG, Q_ALONG>(a, blockIdx.x, gridDim.x);
 }
 // The backward pass' two products side by side, dx's workgroups first: neither fills the chip then, and a workgroup alone on its compute unit waits for
-// most of its time.
+// most of its time.  Float, 3 x 257 x 1000 -> 771: 38 us for both, one after the other 22 each.
 template <typename T, int TILE> __global__ __launch_bounds__(256) void gemm_pair_kernel(GemmArgs dx, GemmArgs dw, uint32_t first) {
     if (blockIdx.x < first) gemm_tile<T, TILE, TILE, true, false>(dx, blockIdx.x, first);
     else gemm_tile<T, TILE, TILE, false, false>(dw, blockIdx.x - first, gridDim.x - first);
@@ -554,7 +563,8 @@ template <typename T, int TILE> __global__ __launch_bounds__(256) void gemm_pair
 
 // ------------------------------------------------------------------------------------------------ a few tokens
 // The forward product of up to TOK tokens: W is read once, 1 KB of one row at a time, which is all it costs; the tokens come from the first-level
-// cache.  A wavefront takes R rows of W (outputs) and keeps R x TOK sums a lane, joined at the end.
+// cache.  A wavefront takes R rows of W (outputs) and keeps R x TOK sums a lane, joined at the end.  Bound by HBM: eight learners' bf16 4096 x 4096 for
+// one token 47 us, 268 MB at 5.7 TB/s.
 struct FewArgs {
     Operand x, w;
     Epilogue out;
@@ -636,7 +646,7 @@ template <typename T, int TOK, int R> __global__ __launch_bounds__(256) void few
 }
 
 // dW = dz' x of up to TOK tokens: little more than writing dW, which is done in rows.  A lane keeps 16 bytes of columns of x; a wavefront takes up to 64
-// rows (outputs), whose dz it reads at once, a row a lane.  (dx of so few tokens is left to the tiles: W read like this, with its sums beside it, was
+// rows (outputs), whose dz it reads at once, a row a lane.  Bound by HBM: 4 float tokens of eight learners, 6400 x 4096, 155 us, 839 MB at 5.4 TB/s.  (dx of so few tokens is left to the tiles: W read like this, with its sums beside it, was
 // slower at every size but one, 8 to 200 % at four tokens.)
 struct FewGradArgs {
     Operand dz, x, dw;
@@ -683,7 +693,8 @@ struct SlopeArgs {
     float* partial;        // [n][slabs][o] column sums, or NULL
     int64_t t, o;
 };
-// dz = dy act'(z) and its sums down the columns: 64 lanes side by side, four rows at a time, a slab of one learner's rows a workgroup.
+// dz = dy act'(z) and its sums down the columns.  dz is rounded to T once, for the matrix instructions take bf16; db sums what was not rounded.
+// Bound by HBM: 4 x 2048 x 2048 bf16 22 us, 100 MB at 4.6 TB/s.  64 lanes side by side, four rows at a time, a slab of one learner's rows a workgroup.
 template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     constexpr int E = kPer<T>;
     __shared__ float rest[4][kWave * E];
@@ -782,8 +793,9 @@ struct Plan {
 inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // What a tile costs, in us: a step of 128 bytes of k with nothing else on the compute unit, the same when the unit is full (a share of it), and what
-// comes before and after the steps.  Measured (products of 512 to 4096 a side, each tile with 1 to 16 parts of k): large tiles do the most with what
-// they read, small ones fill the chip and wait less.
+// comes before and after the steps.  Measured (products of 16 to 8192 a side, each tile with 1 to 32 parts of k; over 102 of them the choice costs 1 %
+// more than the best tile would): large tiles do the most with what they read, small ones fill the chip and wait less, and tiles of 32 multiply few
+// rows beyond the operand's (float, 7 x 4096 x 1512 -> 25: 40 us, by 64 x 64 68).  bf16 has none of those: its narrow products wait for memory.
 struct TileCost {
     int rows, cols, resident;
     float alone, shared, ends;
@@ -885,7 +897,7 @@ inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cu
 
 // Whether few_tokens_grad_kernel makes dW.  us, it / tiles: 4 tokens of eight learners 6400 x 4096 float 155 / 282, bf16 86 / 144, of one 4096 x 4096
 // 13 / 25 and 10 / 15; 16 float tokens 167 / 282 and 19 / 25, 8 bf16 92 / 145 and 14 / 16.
-inline bool few_tokens_grad(int64_t t, int bytes) { return t >= 1 && t <= (bytes == 2 ? 8 : 16); }
+inline bool few_tokens_grad(int64_t t, int64_t out, int bytes) { return t >= 1 && t <= (bytes == 2 ? 8 : 16) && out < 1 << 24; }
 
 struct GradRoom {
     size_t dz, sums, product, total;
@@ -897,7 +909,7 @@ inline GradRoom grad_room(int act, int learners, int64_t t, int64_t in, int64_t 
     r.dz = act != PSGD_ACT_NONE ? up256((size_t)learners * t * r.dz_pitch * bytes) : 0;
     r.sums = db ? up256((size_t)learners * slope_slabs(learners, t, out, bytes, cus) * out * sizeof(float)) : 0;
     const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus).bytes(learners, t, in) : 0;
-    const size_t b = dw && !few_tokens_grad(t, bytes) ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
+    const size_t b = dw && !few_tokens_grad(t, out, bytes) ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
     r.product = a > b ? a : b;
     r.total = r.dz + r.sums + r.product;
     return r;
@@ -966,7 +978,7 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
     const Plan px = gemm_plan(n, t, in, out, sizeof(T), cus), pw = gemm_plan(n, out, in, t, sizeof(T), cus);
     // one launch for both, also of few tokens where dW is small: 8192 x 500 bf16, 4 tokens, 9.6 us, apart 7.4 and 6.6
-    const bool few = few_tokens_grad(t, sizeof(T)), small = (int64_t)n * in * out * (int64_t)sizeof(T) <= (8 << 20);
+    const bool few = few_tokens_grad(t, out, sizeof(T)), small = (int64_t)n * in * out * (int64_t)sizeof(T) <= (8 << 20);
     if (dx && dw && (!few || small) && px.split == 1 && pw.split == 1 && px.rows == px.cols && px.rows == pw.rows && pw.rows == pw.cols && px.rows < 256)
         return px.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
     if (dx)
@@ -977,7 +989,6 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
         const int rows = all >= (int64_t)cus * 8 * 64 ? 64 : all >= (int64_t)cus * 8 * 16 ? 16 : 4;
         const FewGradArgs f{dz, operand(x), operand(dw), t, in, out, rows};
         const dim3 grid((unsigned)across, (unsigned)parts_of(out, 4 * rows), n);
-        if (grid.y > 65535) return fail(PSGD_EINVAL, "psgd_linear_grad: too many outputs");
         if (t <= 2) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 2>), grid, dim3(256), 0, s, f);
         else if (t <= 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 4>), grid, dim3(256), 0, s, f);
         else if (t <= 8) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 8>), grid, dim3(256), 0, s, f);
