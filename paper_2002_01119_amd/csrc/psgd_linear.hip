@@ -19,6 +19,7 @@
 // array of 134 MB are 43 of 301 us for 4 x 2048 x 2048 -> 8192.
 #include "psgd_rows.h"
 
+#include <algorithm>
 #include <initializer_list>
 #include <iterator>
 #include <type_traits>
@@ -480,8 +481,16 @@ __device__ __forceinline__ void gemm_tile(const GemmArgs& a, uint32_t id, uint32
             bring.fetch_upto((int64_t)tile * BK, a.k);
             bring.put(0);
             __syncthreads();
-            read(lds, 0, f[0]);
-            multiply_tile(lds, std::false_type{}, nullptr, [](int) {});
+            const int64_t left = a.k - (int64_t)tile * BK;      // no products of the zeros behind it
+            const int steps = left < BK ? (int)((left * (int)sizeof(T) + 31) / 32) : 4;
+#pragma unroll 1
+            for (int s = 0; s < steps; ++s) {
+                read(lds, s, f[0]);
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) multiply(f[0].q[i], f[0].p[j], acc[i][j], T{});
+            }
             __syncthreads();
         }
     };
@@ -804,6 +813,10 @@ constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.75f, 1.75f, 9.0f}, {128, 128,
 constexpr TileCost kCostsFloat[] = {{256, 256, 1, 8.0f, 8.0f, 10.0f}, {128, 128, 2, 2.4f, 2.4f, 6.0f}, {64, 64, 4, 0.7f, 0.55f, 2.5f},
                                     {128, 32, 4, 0.7f, 0.55f, 2.5f}, {32, 128, 4, 0.7f, 0.55f, 2.5f}};
 
+// One whole tile of k at most: there is no second one beside it in LDS, and one workgroup more fits a compute unit (not of the largest, for its
+// registers).  Such a product waits for C to be written: 4 x 2048 x 64 -> 8192 bf16 41 us before, now 35; 15 x 2120 x 16 -> 4096 120 and 84.
+inline bool short_k(int64_t k, int bytes) { return k < 2 * kRowBytes / bytes; }
+
 // The tile and the parts of k of the least cost.  Parts cost a second kernel and their sums' way through memory.
 inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
     Plan best{64, 64, 1};
@@ -816,7 +829,7 @@ inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, 
         const int64_t tiles = parts_of(m, c.rows) * parts_of(n, c.cols) * learners;
         for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (split > 1 && (steps < 2 * split || tiles * split > 8 * (int64_t)cus)) break;
-            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * c.resident;
+            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * (c.resident + (c.resident > 1 && short_k(k, bytes)));
             const float deep = (float)parts_of(groups, cus), rounds = (float)parts_of(groups, room);
             const float step = groups <= room ? (deep * c.shared > c.alone ? deep * c.shared : c.alone) : deep * c.shared;
             float us = (float)each * step + rounds * c.ends;
@@ -833,12 +846,14 @@ inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, 
 template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
     a.tiles_m = (int)parts_of(a.m, BM);
     a.tiles_n = (int)parts_of(a.n, BN);
-    constexpr size_t lds = (size_t)2 * (BM + BN) * kRowBytes;
+    using Shape = TileShape<BM, BN>;
+    constexpr size_t tile = (size_t)(BM + BN) * kRowBytes, rows = (size_t)Shape::LANES / kWave * 32 * (BN / Shape::ACROSS_N + 4) * sizeof(float);
     auto fn = gemm_kernel<T, BM, BN, P_ALONG, Q_ALONG>;
-    if (lds >= 64 * 1024) {
+    if (2 * tile >= 64 * 1024) {
         static LdsRecord record;
-        if (int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, record)) return rc;
+        if (int rc = allow_lds(reinterpret_cast<const void*>(fn), 2 * tile, record)) return rc;
     }
+    const size_t lds = short_k(a.k, sizeof(T)) ? std::max(tile, rows) : 2 * tile;
     const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
     if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(TileShape<BM, BN>::LANES), lds, s, a);
