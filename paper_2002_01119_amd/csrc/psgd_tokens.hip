@@ -219,7 +219,7 @@ __device__ void top_of_row(const LogArgs& a, TopRoom<B>& room, const float* batc
         }
     }
     if (listed) return;
-    uint64_t last = ~(uint64_t)0;
+    uint64_t last = 0;               // of the place before; the first takes any: NaN in column 0 has the largest rank there is
     for (int place = 0; place < a.k; ++place) {
         uint64_t most = 0;
         for (uint32_t q = tid; q < groups; q += B) {
@@ -229,7 +229,7 @@ __device__ void top_of_row(const LogArgs& a, TopRoom<B>& room, const float* batc
             for (int e = 0; e < E; ++e) {
                 const uint32_t col = q * E + e;
                 const uint64_t r = rank_of(order_of(z[e]), col);
-                if (col < v && r < last && r > most) most = r;
+                if (col < v && (place == 0 || r < last) && r > most) most = r;
             }
         }
 #pragma unroll

@@ -1,0 +1,50 @@
+"""Layers and losses where they went wrong once: rows that hold NaN, sizes of zero, activations far from zero, teachers and temperatures at the ends of float."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+from oracle import layers_oracle as orc  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+INF, NAN = math.inf, math.nan
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def layers():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2002_01119_amd import layers as m
+    m.load()
+    torch.cuda.set_device(0)
+    m.psgd.device_status()
+    return m
+
+
+def normal(shape, dtype, seed, sigma=1.0):
+    return torch.empty(shape).normal_(0.0, sigma, generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
+
+
+# v: one lane's groups, several lanes, every number of lanes a row takes, rows with the batches' maxima left out
+@pytest.mark.parametrize("v", [1, 5, 700, 5003, 40000, 400003])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_nan_in_the_first_column_is_an_alternative(layers, dtype, v):
+    """NaN counts as the largest, equal ones by ascending column: column 0 too, and a row of nothing but NaN."""
+    n, t, k = 1, 5, min(v, 7)
+    x = normal((n, t, v), dtype, v)
+    x[0, 0, 0] = NAN
+    x[0, 1] = NAN
+    x[0, 2, 0] = x[0, 2, v - 1] = NAN
+    x[0, 3, v // 2:] = -INF
+    x[0, 3, 0] = NAN
+    x[0, 4, 0] = INF
+    tokens = torch.zeros((n, t), dtype=torch.int32, device=DEV)
+    logp, ent = torch.empty((n, t), device=DEV), torch.empty((n, t), device=DEV)
+    top, idx = torch.full((n, t, k), 7.0, device=DEV), torch.full((n, t, k), -7, dtype=torch.int32, device=DEV)
+    layers.token_logprobs(x, tokens, logp, entropy=ent, top_logp=top, top_idx=idx)
+    (w_logp, w_ent, w_top, w_idx), _ = orc.logprobs(x, tokens, k)
+    assert torch.equal(idx.cpu().long(), w_idx)
+    assert idx[0, 0, 0] == 0 and idx[0, 1].tolist() == list(range(k))
+    assert torch.isnan(logp).all() and torch.isnan(ent).all() and torch.isnan(top).all()
