@@ -976,7 +976,8 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     float* sums = reinterpret_cast<float*>(room + r.dz);
     float* product = reinterpret_cast<float*>(room + r.dz + r.sums);
     Operand dz = operand(dy);
-    if (act != PSGD_ACT_NONE || db) {
+    // nobody asks for what it makes, or there is nothing to make it of: a grid of no workgroups is an error to the runtime
+    if (out > 0 && (db || (act != PSGD_ACT_NONE && (dx || dw)))) {
         const SlopeArgs a{operand(dy), operand(z), act != PSGD_ACT_NONE ? room : nullptr, r.dz_pitch, db ? sums : nullptr, t, out};
         const int64_t slabs = slope_slabs(n, t, out, sizeof(T), cus);
         const dim3 grid((unsigned)parts_of(out, kWave * kPer<T>), (unsigned)slabs, n);

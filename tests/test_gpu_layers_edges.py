@@ -48,3 +48,26 @@ def test_nan_in_the_first_column_is_an_alternative(layers, dtype, v):
     assert torch.equal(idx.cpu().long(), w_idx)
     assert idx[0, 0, 0] == 0 and idx[0, 1].tolist() == list(range(k))
     assert torch.isnan(logp).all() and torch.isnan(ent).all() and torch.isnan(top).all()
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("t,i,o", [(3, 4, 0), (3, 0, 5), (0, 4, 5), (3, 0, 0), (0, 0, 5), (0, 4, 0), (40, 70, 0)])
+def test_gradients_of_layers_with_sizes_of_zero(layers, act, dtype, t, i, o):
+    """What is summed over nothing is zero, what has no element is left alone."""
+    n = 2
+    x, w = normal((n, t, i), dtype, 1), normal((n, o, i), dtype, 2)
+    dy, z = normal((n, t, o), dtype, 3), normal((n, t, o), dtype, 4)
+    full = lambda *shape: torch.full(shape, 7.0, dtype=dtype, device=DEV)  # noqa: E731
+    y, zz, b = full(n, t, o), full(n, t, o), normal((n, o), dtype, 5)
+    layers.linear(x, w, y, bias=b, act=act, z=zz)
+    dx, dw, db = full(n, t, i), full(n, o, i), full(n, o)
+    for asked in (dict(dx=dx, dw=dw, db=db), dict(dx=dx), dict(dw=dw), dict(db=db), {}):
+        layers.linear_grad(dy, x, w, act=act, z=z if act != "none" else None, **asked)
+    torch.cuda.synchronize()
+    want, _ = orc.linear_grad(dy, x, w, act, z, dtype)
+    for got, v in ((dx, want[0]), (dw, want[1])):
+        assert torch.equal(orc.f64(got), v)
+    bound = orc.linear_grad(dy, x, w, act, z, dtype)[1][2]
+    orc.assert_within(db, want[2], bound, "db")
+    assert layers.psgd.device_status() == 0
