@@ -522,7 +522,8 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
     if (c == 0) return PSGD_OK;
     if (t > 0 && (!mean || !rstd)) return fail(PSGD_EINVAL, "%s: mean and rstd are needed", name);
     const Extent edy{"dy", dy, n, t, c}, ex{"x", x, n, t, c}, edx{"dx", dx, n, t, c}, eadd{"add", add ? add : dy, n, t, c};
-    const Extent eg{"gain", gain, n, 1, c}, edg{"dgain", dgain ? dgain : gain, n, 1, c}, edb{"dbias", dbias ? dbias : gain, n, 1, c};
+    const Extent eg{"gain", gain, n, 1, c};
+    const Extent edg{"dgain", dgain ? dgain : gain, n, 1, dgain ? c : 0}, edb{"dbias", dbias ? dbias : gain, n, 1, dbias ? c : 0};   // no column: nothing to overlap
     psgd_view vm, vr, vw;
     const Extent em = flat("mean", mean, n * t, &vm), er = flat("rstd", rstd, n * t, &vr);
     const size_t need = params ? psgd_layer_norm_grad_workspace(n, t, c) : 0;
@@ -538,7 +539,6 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
     for (const Extent* e : {&ex, &eg, &em, &er})
         if (int rc = refuse_overlap(name, edx, *e)) return rc;
     for (const Extent* e : {&edg, &edb}) {
-        if (e->v == gain) continue;
         if (int rc = check_operand(name, *e, true)) return rc;
         for (const Extent* o : {&edy, &ex, &eadd, &edx, &eg, &em, &er})
             if (int rc = refuse_overlap(name, *e, *o)) return rc;

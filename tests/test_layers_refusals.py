@@ -1,0 +1,22 @@
+"""CPU-only checks of refusals that a caller in C can come by and Python's views cannot.  Addresses here are numbers that nothing dereferences."""
+import pytest
+
+from paper_2002_01119_amd import layers, psgd
+
+F32, BF16 = layers.F32, layers.BF16
+
+
+def refused(rc, code, text):
+    assert rc == code, (rc, psgd.last_error())
+    assert text in psgd.last_error(), psgd.last_error()
+
+
+@pytest.mark.parametrize("given", [("dgain",), ("dbias",), ("dgain", "dbias")])
+def test_one_view_for_the_gain_and_its_gradient(given):
+    """The same struct, not one that is equal: the gain is read after its gradient may have been written."""
+    lib, n, t, c = layers.load(), 2, 3, 8
+    dy, x, dx = (layers.View((1 << 40) + (k << 30), t * c, c, F32) for k in range(3))
+    gain = layers.View(1 << 50, c, 0, F32)
+    outs = {name: gain if name in given else layers.View((1 << 51) + k * 4096, c, 0, F32) for k, name in enumerate(("dgain", "dbias"))}
+    rc = lib.psgd_layer_norm_grad(dy, x, gain, 1 << 60, (1 << 60) + 4096, None, dx, outs["dgain"], outs["dbias"], n, t, c, 1 << 61, 1 << 20, None)
+    refused(rc, psgd.EALIAS, "overlaps")
