@@ -41,7 +41,7 @@ typedef struct {
 } psgd_view;
 
 /* Activations of the linear layer. */
-enum { PSGD_ACT_NONE = 0, PSGD_ACT_RELU = 1, PSGD_ACT_GELU = 2 /* z Phi(z), by erf */, PSGD_ACT_SILU = 3 };
+enum { PSGD_ACT_NONE = 0, PSGD_ACT_RELU = 1, PSGD_ACT_GELU = 2 /* z Phi(z), the normal distribution's */, PSGD_ACT_SILU = 3 };
 
 enum { PSGD_MAX_TOP = 64, PSGD_MAX_SLOTS = 1024 };   /* psgd_token_logprobs: k; psgd_distill: k */
 

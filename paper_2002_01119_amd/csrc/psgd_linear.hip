@@ -38,29 +38,67 @@ struct Operand {          // element (row, col) of learner i at p + i * learner 
 
 constexpr float kLog2E = 1.44269504088896341f;
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
-// Rounded exponentials and reciprocals of the hardware, an ulp or two of float, are behind what an output in bf16 or a float sum of k products loses.
-// erf by Hastings' rational approximation (Abramowitz and Stegun 7.1.26), off by at most 1.5e-7 anywhere: a seventh of the instructions of one that is
-// exact to the last place, which the epilogue of a large tile waits for.  What it leaves in z Phi(z) is 8e-8 |z|.
-__device__ __forceinline__ float erf_of(float x) {
-    const float a = __builtin_fabsf(x), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, a, 1.0f));
-    float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
-    p = __builtin_fmaf(p, t, 1.421413741f);
-    p = __builtin_fmaf(p, t, -0.284496736f);
-    p = __builtin_fmaf(p, t, 0.254829592f);
-    return __builtin_copysignf(1.0f - p * t * exp_of(-a * a), x);
+// The activations z Phi(z) and z / (1 + exp(-z)) and their slopes, each as exact as its outputs' type can hold, however far z is from zero.  Phi by polynomials fitted to
+// the smallest relative error: with a = |z|, t = 1 / (1 + c a),
+//     Phi(-a) = exp(-a^2 / 2) t (c1 + t (c2 + ...)),      Phi(z) = 1/2 + z (d0 + d1 z^2 + ...).
+// bf16: the first alone, c = 0.375, five terms, off by 3.8e-5 of itself in float arithmetic on a <= 14.5 (beyond, the exponential is zero in float): a fiftieth of what
+// rounding the output costs, in no more instructions than an approximation of erf (1 + erf loses the digits of negative z), with the hardware's exponential and
+// reciprocal.  Float: the first with c = 0.25 and eight terms from 1.25 on, below it the second with six, both off by 1e-8; with their roundings Phi is off by at
+// most 12 units of 2^-24 of itself up to a = 3, and by a^2 / 2 more beyond, for the square's.  No branches: erfcf, the same to a few units, has them.  us, by
+// an approximation of erf (whose error stays while Phi falls) / erfcf / this: float 3 x 257 x 1000 -> 771 backward 42.1 / 45.8 / 43.3,
+// 4096 x 1024 -> 4096 forward 260 / 269 / 265, 4 x 8192 x 16 -> 4096 backward 554 / 570 / 554; bf16 4 x 8192 x 16 -> 4096 backward 286 / - / 270. SiLU of floats with the
+// exact exponential and quotient: 41.4 / 42.6 for the first.
+template <typename T> __device__ __forceinline__ float exp_of(float x) {
+    if constexpr (sizeof(T) == 4) return expf(x);
+    else return __builtin_amdgcn_exp2f(x * kLog2E);
 }
-template <int ACT> __device__ __forceinline__ float act_of(float z) {
+template <typename T> __device__ __forceinline__ float bell_of(float z) {       // exp(-z^2 / 2)
+    if constexpr (sizeof(T) == 4) return expf(-0.5f * z * z);
+    else return __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E));
+}
+template <int N> __device__ __forceinline__ float polynomial(float x, const float (&c)[N]) {
+    float p = c[N - 1];
+#pragma unroll
+    for (int i = N - 2; i >= 0; --i) p = __builtin_fmaf(p, x, c[i]);
+    return p;
+}
+// Phi(-|z|); float: |z| from 1.25 on.
+template <typename T> __device__ __forceinline__ float tail_of(float z, float bell) {
+    if constexpr (sizeof(T) == 4) {
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, __builtin_fabsf(z), 1.0f));
+        return t * polynomial(t, {0.0997423306f, 0.0995698348f, 0.0952199996f, 0.0711945444f, 0.0975557044f, -0.0292390473f, 0.114079773f, -0.0481649525f}) * bell;
+    } else {
+        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.375f, __builtin_fabsf(z), 1.0f));
+        return t * polynomial(t, {0.149079636f, 0.157558411f, 0.0841232985f, 0.199558422f, -0.0903177261f}) * bell;
+    }
+}
+template <typename T> __device__ __forceinline__ float normal_cdf(float z, float bell) {
+    const float tail = tail_of<T>(z, bell), far = z < 0.0f ? tail : 1.0f - tail;
+    if constexpr (sizeof(T) == 2) return far;
+    const float near = __builtin_fmaf(z, polynomial(z * z, {0.398942262f, -0.0664902106f, 0.00997228269f, -0.00118383719f, 0.000111041125f, -6.80949188e-06f}), 0.5f);
+    return __builtin_fabsf(z) < 1.25f ? near : far;
+}
+template <int ACT, typename T> __device__ __forceinline__ float act_of(float z) {
     if (ACT == PSGD_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (ACT == PSGD_ACT_GELU) return 0.5f * z * (1.0f + erf_of(z * 0.70710678118654752f));
-    if (ACT == PSGD_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+    if (ACT == PSGD_ACT_GELU) {
+        if constexpr (sizeof(T) == 4) return z * normal_cdf<T>(z, bell_of<T>(z));
+        // max(z, 0) - |z| Phi(-|z|); the least value keeps +inf times 0 out
+        else return __builtin_fmaf(-__builtin_fabsf(fminf(z, 1e30f)), tail_of<T>(z, bell_of<T>(z)), fmaxf(z, 0.0f));
+    }
+    if (ACT == PSGD_ACT_SILU) {
+        const float d = 1.0f + exp_of<T>(-z);
+        return sizeof(T) == 4 ? z / d : z * __builtin_amdgcn_rcpf(d);
+    }
     return z;
 }
-template <int ACT> __device__ __forceinline__ float slope_of(float z) {
+template <int ACT, typename T> __device__ __forceinline__ float slope_of(float z) {
     if (ACT == PSGD_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-    if (ACT == PSGD_ACT_GELU) return 0.5f * (1.0f + erf_of(z * 0.70710678118654752f)) + z * exp_of(-0.5f * z * z) * 0.39894228040143268f;
+    if (ACT == PSGD_ACT_GELU) {
+        const float bell = bell_of<T>(z);
+        return normal_cdf<T>(z, bell) + z * bell * 0.39894228040143268f;
+    }
     if (ACT == PSGD_ACT_SILU) {
-        const float p = __builtin_amdgcn_rcpf(1.0f + exp_of(-z));
+        const float d = 1.0f + exp_of<T>(-z), p = sizeof(T) == 4 ? 1.0f / d : __builtin_amdgcn_rcpf(d);
         return p * (1.0f + z * (1.0f - p));
     }
     return 1.0f;
@@ -103,13 +141,13 @@ __device__ __forceinline__ void finish(const Epilogue& a, int64_t learner, int64
     if (a.z.p) store_cols<T>(reinterpret_cast<T*>(const_cast<char*>(a.z.p)) + learner * a.z.learner + m * a.z.pitch + n, v, left);
     if (a.act == PSGD_ACT_RELU) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_RELU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_RELU, T>(v[e]);
     } else if (a.act == PSGD_ACT_GELU) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_GELU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_GELU, T>(v[e]);
     } else if (a.act == PSGD_ACT_SILU) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_SILU>(v[e]);
+        for (int e = 0; e < E; ++e) v[e] = act_of<PSGD_ACT_SILU, T>(v[e]);
     }
     if (a.residual.p) {
         float r[E];
@@ -646,9 +684,9 @@ template <typename T, int TOK, int R> __global__ __launch_bounds__(256) void few
     const Epilogue& o = a.out;
     if (o.bias.p) v += load_1(reinterpret_cast<const T*>(o.bias.p) + i * o.bias.learner + n);
     if (o.z.p) store_1(reinterpret_cast<T*>(const_cast<char*>(o.z.p)) + i * o.z.learner + t * o.z.pitch + n, v);
-    v = o.act == PSGD_ACT_RELU   ? act_of<PSGD_ACT_RELU>(v)
-        : o.act == PSGD_ACT_GELU ? act_of<PSGD_ACT_GELU>(v)
-        : o.act == PSGD_ACT_SILU ? act_of<PSGD_ACT_SILU>(v)
+    v = o.act == PSGD_ACT_RELU   ? act_of<PSGD_ACT_RELU, T>(v)
+        : o.act == PSGD_ACT_GELU ? act_of<PSGD_ACT_GELU, T>(v)
+        : o.act == PSGD_ACT_SILU ? act_of<PSGD_ACT_SILU, T>(v)
                                  : v;
     if (o.residual.p) v += load_1(reinterpret_cast<const T*>(o.residual.p) + i * o.residual.learner + t * o.residual.pitch + n);
     store_1(reinterpret_cast<T*>(const_cast<char*>(o.y.p)) + i * o.y.learner + t * o.y.pitch + n, v);
@@ -721,7 +759,7 @@ template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kern
                 float z[E];
                 widen<T>(load_cols(reinterpret_cast<const T*>(a.z.p) + i * a.z.learner + r * a.z.pitch + col, left), z);
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[e] *= slope_of<ACT>(z[e]);
+                for (int e = 0; e < E; ++e) v[e] *= slope_of<ACT, T>(z[e]);
                 store_cols<T>(reinterpret_cast<T*>(a.dz) + (i * a.t + r) * a.dz_pitch + col, v, left);
             }
 #pragma unroll

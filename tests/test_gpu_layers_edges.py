@@ -71,3 +71,54 @@ def test_gradients_of_layers_with_sizes_of_zero(layers, act, dtype, t, i, o):
     bound = orc.linear_grad(dy, x, w, act, z, dtype)[1][2]
     orc.assert_within(db, want[2], bound, "db")
     assert layers.psgd.device_status() == 0
+
+
+def grid(dtype, low, high):
+    """Every sixteenth of a binary order from 2^-20 up, both signs, and steps of 2^-8 through the range; in the type."""
+    k = torch.arange(16 * 20, dtype=torch.float64)
+    fine = 2.0 ** (k / 16 - 20)
+    z = torch.cat([fine, -fine, torch.arange(low, high, 2.0 ** -8, dtype=torch.float64), torch.zeros(1, dtype=torch.float64)])
+    return z.to(dtype).to(DEV)
+
+
+def of_kernels(layers, z, act, t):
+    """act(z) by the forward pass and its slope by db of dy = 1, one token (t = 1) or one of the tiles' rows."""
+    o = z.numel()
+    x, w = torch.zeros((1, t, 1), dtype=z.dtype, device=DEV), torch.zeros((1, o, 1), dtype=z.dtype, device=DEV)
+    y, db = torch.empty((1, t, o), dtype=z.dtype, device=DEV), torch.empty((1, o), dtype=z.dtype, device=DEV)
+    layers.linear(x, w, y, bias=z[None], act=act)
+    one = torch.ones((1, 1, o), dtype=z.dtype, device=DEV)
+    layers.linear_grad(one, x[:, :1], w, db=db, act=act, z=z[None, None])
+    torch.cuda.synchronize()
+    assert all(torch.equal(y[0, 0].nan_to_num(7.0), r.nan_to_num(7.0)) for r in y[0])
+    return orc.f64(y[0, 0]), orc.f64(db[0])
+
+
+@pytest.mark.parametrize("t", [1, 9])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gelu_is_exact_to_a_few_places_everywhere(layers, dtype, t):
+    """In float, from its operations: Phi to 12 U (a complementary error function of 8 U, its argument's two roundings, which z^2 multiplies), the
+    density to (z^2 + 12) U.  In bf16 the terms may be off by 2^-12 of themselves, a sixteenth of what rounding the output costs."""
+    z = grid(dtype, -14.0, 14.0)
+    y, slope = of_kernels(layers, z, "gelu", t)
+    z = orc.f64(z)
+    phi = 0.5 * torch.special.erfc(-z * math.sqrt(0.5))
+    density = z.abs() * torch.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+    off = orc.U if dtype == F32 else 0.0
+    part = 0.0 if dtype == F32 else 2.0 ** -12
+    b_phi, b_density = phi * (part + off * (12 + 2 * z * z)), density * (part + off * (12 + z * z))
+    want, want_slope = orc.act("gelu", z), orc.act_slope("gelu", z)
+    orc.assert_within(y, want, z.abs() * b_phi + 4 * off * want.abs() + orc.HALF[dtype] * want.abs() + 1e-36, "gelu")
+    orc.assert_within(slope, want_slope, b_phi + b_density + 4 * off * want_slope.abs() + orc.HALF[dtype] * want_slope.abs() + 1e-36, "its slope")
+
+
+@pytest.mark.parametrize("t", [1, 9])
+def test_silu_of_floats_is_exact_to_a_few_places_everywhere(layers, t):
+    """The exponential to 2 U, the sum, the quotient and the product to U each; what 1 - p of the slope loses is of p, not of itself."""
+    z = grid(F32, -100.0, 100.0)
+    y, slope = of_kernels(layers, z, "silu", t)
+    z = orc.f64(z)
+    p = torch.sigmoid(z)
+    want, want_slope = orc.act("silu", z), orc.act_slope("silu", z)
+    orc.assert_within(y, want, 8 * orc.U * want.abs() + 1e-36, "silu")
+    orc.assert_within(slope, want_slope, 8 * orc.U * (want_slope.abs() + 2 * p * (1 + z.abs() * (p + torch.sigmoid(-z)))) + 1e-36, "its slope")
