@@ -392,7 +392,7 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
         }
         for (int s = tid; s < a.k; s += B) {
             int32_t col = at<int32_t>(a.idx, i, r)[s];
-            const float l = at<float>(a.top, i, r)[s] * a.inv_tau;
+            const float l = at<float>(a.top, i, r)[s];       // divided by tau once the maximum is off: alone it may leave float
             if (col >= v) {
                 atomicOr(&g_token_status, kTokenFlag);
                 col = -1;
@@ -456,7 +456,7 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
         if (m == INFINITY) sum = NAN;
     }
     for (int s = tid; s < a.k; s += B)
-        if (at_col[s] >= 0) psum += exp_of(p[s] - amax);
+        if (at_col[s] >= 0) psum += exp_of((p[s] - amax) * a.inv_tau);
     group_all_2<Sum, W>(sum, psum, room2[1]);
     const float log_s = logf(sum), log_p = logf(psum), by_p = 1.0f / psum;
     float loss = 0.0f;
@@ -465,7 +465,7 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
             p[s] = 0.0f;
             continue;
         }
-        const float l = p[s] - amax, q = exp_of(l) * by_p;
+        const float l = (p[s] - amax) * a.inv_tau, q = exp_of(l) * by_p;
         if (q != 0.0f) loss += q * ((l - log_p) - ((z[s] - m) * a.inv_tau - log_s));
         p[s] = q;
     }

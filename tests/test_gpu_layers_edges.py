@@ -122,3 +122,42 @@ def test_silu_of_floats_is_exact_to_a_few_places_everywhere(layers, t):
     want, want_slope = orc.act("silu", z), orc.act_slope("silu", z)
     orc.assert_within(y, want, 8 * orc.U * want.abs() + 1e-36, "silu")
     orc.assert_within(slope, want_slope, 8 * orc.U * (want_slope.abs() + 2 * p * (1 + z.abs() * (p + torch.sigmoid(-z)))) + 1e-36, "its slope")
+
+
+def check_distill(layers, x, idx, top, weight, tau):
+    n, t, v = x.shape
+    loss, alone, grad = torch.full((n, t), 7.0, device=DEV), torch.full((n, t), 7.0, device=DEV), torch.full((n, t, v), 7.0, dtype=x.dtype, device=DEV)
+    layers.distill(x, idx, top, loss, tau=tau, weight=weight, dlogits=grad)
+    layers.distill(x, idx, top, alone, tau=tau, weight=weight)
+    torch.cuda.synchronize()
+    (w_loss, w_grad), (b_loss, b_grad) = orc.distill(x, idx, top, weight, tau, x.dtype)
+    return loss, alone, grad, w_loss, b_loss, w_grad, b_grad
+
+
+# one way of holding a row after the other; the last is read again
+@pytest.mark.parametrize("dtype,v", [(F32, 100), (BF16, 5003), (F32, 33001), (BF16, 140001)])
+@pytest.mark.parametrize("tau", [0.5, 0.7, 3.0])
+def test_a_teacher_at_the_ends_of_float(layers, dtype, v, tau):
+    """Slots of the lowest and of the largest float are slots, also where dividing them by the temperature leaves the type: a teacher of nothing
+    but the lowest value is uniform."""
+    n, t, k = 1, 4, 6
+    x = normal((n, t, v), dtype, 1)
+    idx = torch.arange(3, 3 + k, dtype=torch.int32, device=DEV).expand(n, t, k).contiguous()
+    top = normal((n, t, k), F32, 2)
+    low = torch.finfo(F32).min
+    top[0, 0] = low
+    top[0, 1] = -low
+    top[0, 2, 2:] = low
+    idx[0, 3, 1:] = -1
+    top[0, 3] = low
+    loss, alone, grad, _, _, _, _ = check_distill(layers, x, idx, top, None, tau)
+    # the same distributions from teachers in the middle of the range
+    mild = top.clone()
+    mild[0, 0] = mild[0, 1] = 0.0
+    mild[0, 2, 2:] = -1e4
+    mild[0, 3] = 0.0
+    _, _, _, w_loss, b_loss, w_grad, b_grad = check_distill(layers, x, idx, mild, None, tau)
+    orc.assert_within(loss, w_loss, b_loss, "loss")
+    orc.assert_within(alone, w_loss, b_loss, "loss alone")
+    orc.assert_within(grad, w_grad, b_grad, "dlogits")
+    assert loss[0, 0] > 0.0 and grad[0, 3, 3] < 0.0
