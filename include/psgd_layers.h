@@ -124,7 +124,8 @@ int psgd_token_logprobs(const psgd_view* logits, const psgd_view* tokens, float*
  *   weight              float [n * t] or NULL (all 1): 1 / tokens for a mean, 0 for a masked row
  *   loss                float [n * t]
  * A row with weight 0 or no slot given has loss 0 and gradient 0 whatever its logits hold.  An index >= v counts as a slot not given and
- * raises bit 1 of psgd_device_status().  tau > 0, v in 1..2^31-1, k in 1..PSGD_MAX_SLOTS.
+ * raises bit 1 of psgd_device_status().  tau > 0 and finite, log2(e) / tau too; v in 1..2^31-1, k in
+ * 1..PSGD_MAX_SLOTS.
  */
 int psgd_distill(const psgd_view* logits, const psgd_view* top_idx, const psgd_view* top_logit, const float* weight, float* loss,
                  const psgd_view* dlogits, float tau, int k, int n, int64_t t, int64_t v, void* stream);

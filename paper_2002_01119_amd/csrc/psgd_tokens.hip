@@ -31,6 +31,8 @@ template <typename T> constexpr uint32_t kMasked = sizeof(T) == 4 ? 0xFF800000u 
 constexpr float kLog2E = 1.44269504088896341f;
 constexpr float kNoLess = -200.0f;       // exp of it is 0 in float, and a product with it stays finite
 
+// 2^x of a difference that is at most 0, zero where it is not a number (-inf from -inf).
+__device__ __forceinline__ float exp_below(float x) { return __builtin_amdgcn_exp2f(fmaxf(x, kNoLess)); }
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 // Sums relative to a running maximum.  An empty one has m = -inf; differences that are not numbers (-inf from -inf) count as kNoLess.
@@ -419,13 +421,13 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
                     widen<T>(load_cols(x + col + u * B * E, v - col - u * B * E, kMasked<T>), c[u]);
                     to = Max::of(to, largest<T>(c[u]));
                 }
-                const float f = __builtin_amdgcn_exp2f(fmaxf(o.m - to, -1e30f) * scale);
+                const float f = exp_below((o.m - to) * scale);
                 o.s *= f;
                 o.m = to;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) o.s += __builtin_amdgcn_exp2f(fmaxf(c[u][e] - to, -1e30f) * scale);
+                    for (int e = 0; e < E; ++e) o.s += exp_below((c[u][e] - to) * scale);
             }
             m = o.m;
         }
@@ -452,7 +454,7 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
         }
     } else {
         // a lane without logits has m = -inf and s = 0; a row of nothing but -inf has no distribution: NaN, as the formula has it
-        sum = m == -INFINITY ? NAN : o.s * __builtin_amdgcn_exp2f(fmaxf(o.m - m, -1e30f) * scale);
+        sum = m == -INFINITY ? NAN : o.s * exp_below((o.m - m) * scale);
         if (m == INFINITY) sum = NAN;
     }
     for (int s = tid; s < a.k; s += B)
@@ -466,11 +468,12 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
             continue;
         }
         const float l = (p[s] - amax) * a.inv_tau, q = exp_of(l) * by_p;
-        if (q != 0.0f) loss += q * ((l - log_p) - ((z[s] - m) * a.inv_tau - log_s));
+        // tau (log p - log q): neither difference is divided by tau, with which it may leave float
+        if (q != 0.0f) loss += q * (((p[s] - amax) - (z[s] - m)) + a.tau * (log_s - log_p));
         p[s] = q;
     }
     loss = group_all<Sum, W>(loss, room);
-    if (tid == 0) a.loss[row] = weight * a.tau * a.tau * loss;
+    if (tid == 0) a.loss[row] = weight * a.tau * loss;
     if constexpr (GRAD) {
         const float share = weight * a.tau / sum;
         if constexpr (NV > 0) {
@@ -648,7 +651,7 @@ int psgd_distill(const psgd_view* logits, const psgd_view* top_idx, const psgd_v
         return fail(PSGD_EINVAL, "%s: logits and dlogits must be float or bf16 alike", name);
     if (top_idx->type != PSGD_I32 || top_logit->type != PSGD_F32) return fail(PSGD_EINVAL, "%s: top_idx must be int32, top_logit float", name);
     if (k < 1 || k > PSGD_MAX_SLOTS) return fail(PSGD_EINVAL, "%s: k=%d outside 1..%d", name, k, (int)PSGD_MAX_SLOTS);
-    if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.0f / tau)) return fail(PSGD_EINVAL, "%s: tau=%g", name, (double)tau);
+    if (!(tau > 0.0f) || !std::isfinite(tau) || !std::isfinite(1.0f / tau * kLog2E)) return fail(PSGD_EINVAL, "%s: tau=%g", name, (double)tau);
     if (t == 0) return PSGD_OK;
     if (!loss) return fail(PSGD_EINVAL, "%s: loss is needed", name);
     const int64_t rows = n * t;

@@ -161,3 +161,38 @@ def test_a_teacher_at_the_ends_of_float(layers, dtype, v, tau):
     orc.assert_within(alone, w_loss, b_loss, "loss alone")
     orc.assert_within(grad, w_grad, b_grad, "dlogits")
     assert loss[0, 0] > 0.0 and grad[0, 3, 3] < 0.0
+
+
+@pytest.mark.parametrize("dtype,v", [(F32, 100), (F32, 70001), (BF16, 140001)])
+@pytest.mark.parametrize("tau", [1e28, 1e30, 1e35])
+def test_masked_columns_at_a_very_high_temperature(layers, dtype, v, tau):
+    """All that is not masked is alike then; a masked column stays out."""
+    n, t, k = 1, 2, 4
+    x = normal((n, t, v), dtype, 1)
+    x[0, :, v // 3:] = -INF
+    idx = torch.arange(1, 1 + k, dtype=torch.int32, device=DEV).expand(n, t, k).contiguous()
+    top, weight = normal((n, t, k), F32, 2), torch.full((n, t), 1e-20, device=DEV)
+    loss, alone, grad, w_loss, b_loss, w_grad, b_grad = check_distill(layers, x, idx, top, weight, tau)
+    live = v // 3
+    assert torch.isposinf(w_loss).all() or torch.allclose(w_loss, torch.full_like(w_loss, float(weight[0, 0]) * tau * tau * math.log(live / k)), rtol=1e-6)
+    for got in (loss, alone):
+        got = orc.f64(got)
+        assert torch.equal(torch.isposinf(got), w_loss > torch.finfo(F32).max)
+        fine = torch.isfinite(got)
+        assert ((got - w_loss).abs() <= b_loss)[fine].all()
+    orc.assert_within(grad, w_grad, b_grad, "dlogits")
+    assert not grad[0, :, live:].any()
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -128, 4.0e-39, 2.0 ** -127])
+def test_temperatures_whose_reciprocal_leaves_float_with_its_logarithms_base(layers, tau):
+    """Refused, or right: 1 / tau may be a number where log2(e) / tau is none."""
+    x = normal((1, 1, 50), F32, 1)
+    idx, top = torch.tensor([[[3]]], dtype=torch.int32, device=DEV), torch.zeros((1, 1, 1), device=DEV)
+    loss, grad = torch.empty((1, 1), device=DEV), torch.empty_like(x)
+    try:
+        layers.distill(x, idx, top, loss, tau=tau, dlogits=grad)
+    except layers.psgd.PsgdError as e:
+        assert "tau" in str(e)
+        return
+    assert not torch.isnan(loss).any() and not torch.isnan(grad).any()
