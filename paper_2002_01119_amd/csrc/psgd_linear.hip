@@ -21,7 +21,6 @@
 
 #include <algorithm>
 #include <initializer_list>
-#include <iterator>
 #include <type_traits>
 
 namespace psgd {
@@ -119,7 +118,6 @@ struct GemmArgs {
     int tiles_m, tiles_n;
 };
 
-constexpr int kRowBytes = 128;                     // a row of the LDS tile: 64 bf16 or 32 floats of k, as eight chunks of 16 bytes
 template <typename T> constexpr int kDepth = kRowBytes / (int)sizeof(T);
 
 // Where chunk c of row r lies.  LDS serves 16 lanes of a 16-byte access at a time, from 64 banks: two rows.  Lanes that read one chunk of 16 rows
@@ -831,56 +829,6 @@ inline Operand operand(const psgd_view* v) {
     return v ? Operand{static_cast<const char*>(v->data), v->learner, v->row} : Operand{nullptr, 0, 0};
 }
 
-struct Plan {
-    int rows, cols, split;       // of a workgroup's tile; parts of k
-    size_t bytes(int learners, int64_t m, int64_t n) const {
-        return split > 1 ? up256((size_t)split * learners * m * n * sizeof(float)) : 0;
-    }
-};
-inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// What a tile costs, in us: a step of 128 bytes of k with nothing else on the compute unit, the same when the unit is full (a share of it), and what
-// comes before and after the steps.  Measured (products of 16 to 8192 a side, each tile with 1 to 32 parts of k; over 102 of them the choice costs 1 %
-// more than the best tile would): large tiles do the most with what they read, small ones fill the chip and wait less, and tiles of 32 multiply few
-// rows beyond the operand's (float, 7 x 4096 x 1512 -> 25: 40 us, by 64 x 64 68).  bf16 has none of those: its narrow products wait for memory.
-struct TileCost {
-    int rows, cols, resident;
-    float alone, shared, ends;
-};
-constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.75f, 1.75f, 9.0f}, {128, 128, 2, 0.7f, 0.45f, 5.0f}, {64, 64, 4, 0.53f, 0.25f, 2.2f}};
-constexpr TileCost kCostsFloat[] = {{256, 256, 1, 8.0f, 8.0f, 10.0f}, {128, 128, 2, 2.4f, 2.4f, 6.0f}, {64, 64, 4, 0.7f, 0.55f, 2.5f},
-                                    {128, 32, 4, 0.7f, 0.55f, 2.5f}, {32, 128, 4, 0.7f, 0.55f, 2.5f}};
-
-// One whole tile of k at most: there is no second one beside it in LDS, and one workgroup more fits a compute unit (not of the largest, for its
-// registers).  Such a product waits for C to be written: 4 x 2048 x 64 -> 8192 bf16 41 us before, now 35; 15 x 2120 x 16 -> 4096 120 and 84.
-inline bool short_k(int64_t k, int bytes) { return k < 2 * kRowBytes / bytes; }
-
-// The tile and the parts of k of the least cost.  Parts cost a second kernel and their sums' way through memory.
-inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
-    Plan best{64, 64, 1};
-    if (m < 1 || n < 1) return best;          // nothing to multiply
-    const int64_t steps = parts_of(k, kRowBytes / bytes);
-    float least = INFINITY;
-    const TileCost* const costs = bytes == 4 ? kCostsFloat : kCostsBf16;
-    for (const TileCost* at = costs; at < costs + (bytes == 4 ? std::size(kCostsFloat) : std::size(kCostsBf16)); ++at) {
-        const TileCost& c = *at;
-        const int64_t tiles = parts_of(m, c.rows) * parts_of(n, c.cols) * learners;
-        for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (split > 1 && (steps < 2 * split || tiles * split > 8 * (int64_t)cus)) break;
-            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * (c.resident + (c.resident > 1 && short_k(k, bytes)));
-            const float deep = (float)parts_of(groups, cus), rounds = (float)parts_of(groups, room);
-            const float step = groups <= room ? (deep * c.shared > c.alone ? deep * c.shared : c.alone) : deep * c.shared;
-            float us = (float)each * step + rounds * c.ends;
-            if (split > 1) us += 4.0f + (float)(split + 1) * (float)(m * n * learners) * 4.0f / 3.5e6f;
-            if (us < least) {
-                least = us;
-                best = Plan{c.rows, c.cols, split};
-            }
-        }
-    }
-    return best;
-}
-
 template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
     a.tiles_m = (int)parts_of(a.m, BM);
     a.tiles_n = (int)parts_of(a.n, BN);
@@ -940,34 +888,6 @@ template <typename T, int TILE> int launch_pair(GemmArgs dx, GemmArgs dw, hipStr
     return PSGD_OK;
 }
 
-inline int64_t slope_slabs(int learners, int64_t t, int64_t o, int bytes, int cus) {
-    const int64_t across = parts_of(o, kWave * 16 / bytes) * learners;
-    if (across < 1) return 1;
-    int64_t slabs = parts_of((int64_t)cus * 4, across);
-    if (slabs > parts_of(t, 16)) slabs = parts_of(t, 16);
-    return slabs < 1 ? 1 : slabs > 65535 ? 65535 : slabs;
-}
-
-// Whether few_tokens_grad_kernel makes dW.  us, it / tiles: 4 tokens of eight learners 6400 x 4096 float 155 / 282, bf16 86 / 144, of one 4096 x 4096
-// 13 / 25 and 10 / 15; 16 float tokens 167 / 282 and 19 / 25, 8 bf16 92 / 145 and 14 / 16.
-inline bool few_tokens_grad(int64_t t, int64_t out, int bytes) { return t >= 1 && t <= (bytes == 2 ? 8 : 16) && out < 1 << 24; }
-
-struct GradRoom {
-    size_t dz, sums, product, total;
-    int64_t dz_pitch;
-};
-inline GradRoom grad_room(int act, int learners, int64_t t, int64_t in, int64_t out, int bytes, int cus, bool dx, bool dw, bool db) {
-    GradRoom r{};
-    r.dz_pitch = parts_of(out, 16 / bytes) * (16 / bytes);
-    r.dz = act != PSGD_ACT_NONE ? up256((size_t)learners * t * r.dz_pitch * bytes) : 0;
-    r.sums = db ? up256((size_t)learners * slope_slabs(learners, t, out, bytes, cus) * out * sizeof(float)) : 0;
-    const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus).bytes(learners, t, in) : 0;
-    const size_t b = dw && !few_tokens_grad(t, out, bytes) ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
-    r.product = a > b ? a : b;
-    r.total = r.dz + r.sums + r.product;
-    return r;
-}
-
 inline int check_linear_sizes(const char* name, int n, int64_t t, int64_t in, int64_t out, int act) {
     if (int rc = check_counts(name, n, t, in)) return rc;
     if (int rc = check_counts(name, n, t, out)) return rc;
@@ -978,16 +898,6 @@ inline int check_room(const char* name, void* workspace, size_t have, size_t nee
     if (need && (!workspace || have < need || reinterpret_cast<uintptr_t>(workspace) % 256))
         return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
     return PSGD_OK;
-}
-
-// Four outputs a wavefront where that leaves eight wavefronts for each compute unit.
-inline bool four_outputs(int learners, int64_t out, int cus) { return out * learners >= (int64_t)cus * 32; }
-// Tokens that few_tokens_kernel takes: no tiles then, and no parts of k.  us, this kernel / tiles: float 1 token 4096 x 4096 12 / 19, of eight learners
-// 97 / 125, 4 tokens of eight learners 106 / 131; 8 tokens with an output a wavefront 4 x 1024 x 1024 7 / 12, with four 16 x 4489 x 4696 324 / 291 and
-// 16 x 4096 x 2048 125 / 126; bf16 1 token 4096 x 4096 5 / 12, 4 tokens 8 / 13 and of sixteen learners, 4489 x 4696, 165 / 235.
-inline int most_few(int learners, int64_t out, int bytes, int cus) { return bytes == 2 || four_outputs(learners, out, cus) ? 4 : 8; }
-inline Plan forward_plan(int learners, int64_t t, int64_t out, int64_t in, int bytes, int cus) {
-    return t <= most_few(learners, out, bytes, cus) ? Plan{64, 64, 1} : gemm_plan(learners, t, out, in, bytes, cus);
 }
 
 template <typename T> int linear_of(const GemmArgs& a, const Plan& plan, void* workspace, int cus, hipStream_t s) {
@@ -1030,25 +940,19 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     }
     GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
     GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
-    const Plan px = gemm_plan(n, t, in, out, sizeof(T), cus), pw = gemm_plan(n, out, in, t, sizeof(T), cus);
-    // one launch for both, also of few tokens where dW is small: 8192 x 500 bf16, 4 tokens, 9.6 us, apart 7.4 and 6.6
-    const bool few = few_tokens_grad(t, out, sizeof(T)), small = (int64_t)n * in * out * (int64_t)sizeof(T) <= (8 << 20);
-    if (dx && dw && (!few || small) && px.split == 1 && pw.split == 1 && px.rows == px.cols && px.rows == pw.rows && pw.rows == pw.cols && px.rows < 256)
-        return px.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
+    const GradPlan g = grad_plan(n, t, in, out, sizeof(T), cus, dx, dw);
+    if (g.pair) return g.dx.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
     if (dx)
-        if (int rc = launch_gemm<T, true, false>(ax, px, product, s)) return rc;
-    if (dw && few) {
-        // 64 rows a wavefront, fewer where that leaves compute units without eight wavefronts
-        const int64_t across = parts_of(in, kWave * kPer<T>), all = across * n * out;
-        const int rows = all >= (int64_t)cus * 8 * 64 ? 64 : all >= (int64_t)cus * 8 * 16 ? 16 : 4;
-        const FewGradArgs f{dz, operand(x), operand(dw), t, in, out, rows};
-        const dim3 grid((unsigned)across, (unsigned)parts_of(out, 4 * rows), n);
+        if (int rc = launch_gemm<T, true, false>(ax, g.dx, product, s)) return rc;
+    if (dw && g.few) {
+        const FewGradArgs f{dz, operand(x), operand(dw), t, in, out, g.few_rows};
+        const dim3 grid((unsigned)parts_of(in, kWave * kPer<T>), (unsigned)parts_of(out, 4 * g.few_rows), n);
         if (t <= 2) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 2>), grid, dim3(256), 0, s, f);
         else if (t <= 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 4>), grid, dim3(256), 0, s, f);
         else if (t <= 8) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 8>), grid, dim3(256), 0, s, f);
         else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_tokens_grad_kernel<T, 16>), grid, dim3(256), 0, s, f);
     } else if (dw) {
-        if (int rc = launch_gemm<T, false, false>(aw, pw, product, s)) return rc;
+        if (int rc = launch_gemm<T, false, false>(aw, g.dw, product, s)) return rc;
     }
     return PSGD_OK;
 }

@@ -10,6 +10,7 @@
 
 #include "psgd_internal.h"
 #include "psgd_layers.h"
+#include "psgd_layers_plan.h"
 
 namespace psgd {
 namespace {
@@ -19,8 +20,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-constexpr int kWave = 64;
 
 // ------------------------------------------------------------------------------------------------ elements
 // A lane's access is 16 bytes: four floats or eight bf16.  Rows start at any element: gfx950 takes such accesses unaligned.
@@ -285,8 +284,6 @@ inline int check_counts(const char* name, int n, int64_t t, int64_t c) {
 }
 
 inline bool float_type(int type) { return type == PSGD_F32 || type == PSGD_BF16; }
-
-inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 }  // namespace
 }  // namespace psgd

@@ -67,8 +67,7 @@ template <typename T> __device__ __forceinline__ float largest(const float (&v)[
     else return Max::of(Max::of(Max::of(a, v[3]), v[4]), Max::of(Max::of(v[5], v[6]), v[7]));
 }
 
-// Rows of a workgroup: one, or one for each of four wavefronts.
-template <int B> constexpr int kRowsOf = B == kWave ? 4 : 1;
+template <int B> constexpr int kRowsOf = rows_of_group(B);
 // Between the lanes of a row.  A wavefront's own accesses to LDS are in order, so there only the compiler has to keep them.
 template <int B> __device__ __forceinline__ void row_sync() {
     if constexpr (B == kWave) {
@@ -88,8 +87,6 @@ struct LogArgs {
     int32_t v;
 };
 
-constexpr int kUnroll = 4;               // 16-byte groups a lane has on their way: a batch
-
 // What finding the k largest takes of LDS, for rows of B lanes.  Lanes are joined to at most 256 groups.
 template <int B> struct TopRoom {
     static constexpr int GROUPS = B < 256 ? B : 256, LIST = B < 256 ? 512 : B < 1024 ? 1024 : 2048;
@@ -99,9 +96,6 @@ template <int B> struct TopRoom {
     uint64_t limit;
     int count, batches;
 };
-// Bytes of batches' maxima that a workgroup keeps; rows with more (beyond 393 216 floats) have all batches looked at.
-template <int B> constexpr int kBatchRoom = B == 1024 ? 96 * 1024 : 40 * 1024;
-
 // The k largest of a row, ties by ascending column.  Every lane knows the largest of its logits and the first 16-byte group that
 // holds it, and in LDS the largest of each of its batches.  Of up to 256 groups of lanes the k-th best is a threshold that at least k logits
 // reach, and no logit outside of the batches that reach it can be among the k: only those are read again, all lanes' at once, and what
@@ -518,15 +512,6 @@ inline Rows rows_of(const psgd_view* v) {
     return v ? Rows{static_cast<char*>(v->data), v->learner, v->row} : Rows{nullptr, 0, 0};
 }
 
-// Lanes for a row.  us, k = 20, rows x columns, 64 / 256 / 1024 lanes: 64 000 x 500 bf16 88 / 266 / 3549; 3200 x 1000 float 11 / 15 / 41; 4096 x 32 000
-// bf16 63 / 65 / 111, float 126 / 111 / 127; 4096 x 131 072 bf16 368 / 201 / 209; 256 x 200 000 float 288 / 105 / 66.  64 lanes have as many groups
-// of lanes, of which the 33rd best and beyond are no good threshold.  (Cutting a few long rows into parts that a second kernel joins was no faster: the
-// search's latency counts twice then.  1 x 131 072 bf16 20.5, uncut 16.9.)
-inline int lanes_of_row(int64_t rows, int64_t groups, int k, int cus) {
-    if (k <= 32 && (groups <= 256 || (groups <= 2048 && rows >= 4 * (int64_t)cus))) return 64;
-    return groups <= 1024 || rows >= 4 * (int64_t)cus ? 256 : 1024;
-}
-
 template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
     const int64_t groups = ((int64_t)a.v + kPer<T> - 1) / kPer<T>;
     const int lanes = lanes_of_row(a.rows, groups, a.k, cus);
@@ -534,14 +519,13 @@ template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
     do {                                                                                                                    \
         if (B == 1024 && TOP && lds > 40 * 1024) {                                                                          \
             static LdsRecord record;                                                                                        \
-            if (int rc = allow_lds(reinterpret_cast<const void*>(logprobs_kernel<T, B, EN, TOP>), kBatchRoom<B>, record)) return rc; \
+            if (int rc = allow_lds(reinterpret_cast<const void*>(logprobs_kernel<T, B, EN, TOP>), batch_room(B), record)) return rc; \
         }                                                                                                                   \
         hipLaunchKernelGGL((logprobs_kernel<T, B, EN, TOP>), dim3((unsigned)((a.rows + kRowsOf<B> - 1) / kRowsOf<B>)), dim3(B * kRowsOf<B>), lds, s, a); \
     } while (0)
 #define PSGD_LOG_B(B)                                                                                                       \
     do {                                                                                                                    \
-        const int64_t floats = (groups + B * kUnroll - 1) / (B * kUnroll) * B;                                              \
-        a.keep = a.k > 0 && floats * kRowsOf<B> * 4 <= kBatchRoom<B> ? (int)floats : 0;                                        \
+        a.keep = a.k > 0 ? batches_kept(groups, B) : 0;                                                                     \
         const size_t lds = (size_t)a.keep * kRowsOf<B> * sizeof(float);                                                     \
         if (a.entropy && a.k) PSGD_LOG(B, true, true);                                                                      \
         else if (a.entropy) PSGD_LOG(B, true, false);                                                                       \
@@ -556,28 +540,26 @@ template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
     return PSGD_OK;
 }
 
-// Rows of up to 64 KB go to 1024 lanes too, two rows a compute unit at a time, but for numbers of rows that would leave few of them for a second turn:
-// 592 x 10 007 float 15.4 us, by 256 lanes that hold sixteen groups each 13.6; 4096 rows 67 / 71.
 template <typename T> void launch_distill(const DistillArgs& a, int cus, hipStream_t s) {
+    const DistillHold h = distill_hold(a.rows, ((int64_t)a.v + kPer<T> - 1) / kPer<T>, a.dlogits.p, cus);
 #define PSGD_DISTILL(B, NV, GRAD)                                                                                           \
+    if (h.lanes == B && h.held == NV && (a.dlogits.p != nullptr) == GRAD)                                                   \
     hipLaunchKernelGGL((distill_kernel<T, B, NV, GRAD>), dim3((unsigned)((a.rows + kRowsOf<B> - 1) / kRowsOf<B>)), dim3(B * kRowsOf<B>), \
                        (size_t)a.k * 12 * kRowsOf<B>, s, a)
-    const int64_t groups = ((int64_t)a.v + kPer<T> - 1) / kPer<T>;
-    if (!a.dlogits.p) {
-        if (groups <= 256) PSGD_DISTILL(64, 0, false);
-        else if (groups <= 256 * 16) PSGD_DISTILL(256, 0, false);
-        else PSGD_DISTILL(1024, 0, false);
-    } else if (groups <= 64) PSGD_DISTILL(64, 1, true);
-    else if (groups <= 64 * 2) PSGD_DISTILL(64, 2, true);
-    else if (groups <= 64 * 4) PSGD_DISTILL(64, 4, true);
-    else if (groups <= 256 * 2) PSGD_DISTILL(256, 2, true);
-    else if (groups <= 256 * 4) PSGD_DISTILL(256, 4, true);
-    else if (groups <= 256 * 8) PSGD_DISTILL(256, 8, true);
-    else if (groups <= 256 * 16 && a.rows > 2 * (int64_t)cus && a.rows <= 4 * (int64_t)cus) PSGD_DISTILL(256, 16, true);
-    else if (groups <= 1024 * 4) PSGD_DISTILL(1024, 4, true);
-    else if (groups <= 1024 * 8) PSGD_DISTILL(1024, 8, true);
-    else if (groups <= 1024 * 16) PSGD_DISTILL(1024, 16, true);
-    else PSGD_DISTILL(1024, 0, true);
+    PSGD_DISTILL(64, 0, false);
+    PSGD_DISTILL(256, 0, false);
+    PSGD_DISTILL(1024, 0, false);
+    PSGD_DISTILL(64, 1, true);
+    PSGD_DISTILL(64, 2, true);
+    PSGD_DISTILL(64, 4, true);
+    PSGD_DISTILL(256, 2, true);
+    PSGD_DISTILL(256, 4, true);
+    PSGD_DISTILL(256, 8, true);
+    PSGD_DISTILL(256, 16, true);
+    PSGD_DISTILL(1024, 4, true);
+    PSGD_DISTILL(1024, 8, true);
+    PSGD_DISTILL(1024, 16, true);
+    PSGD_DISTILL(1024, 0, true);
 #undef PSGD_DISTILL
 }
 
