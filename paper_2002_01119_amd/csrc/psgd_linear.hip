@@ -37,15 +37,15 @@ struct Operand {          // element (row, col) of learner i at p + i * learner 
 
 constexpr float kLog2E = 1.44269504088896341f;
 
-// The activations z Phi(z) and z / (1 + exp(-z)) and their slopes, each as exact as its outputs' type can hold, however far z is from zero.  Phi by polynomials fitted to
-// the smallest relative error: with a = |z|, t = 1 / (1 + c a),
+// The activations z Phi(z) and z / (1 + exp(-z)) and their slopes, each as exact as its outputs' type can hold, however far z is from zero.  Phi by fitted polynomials: with
+// a = |z|, t = 1 / (1 + a / 4),
 //     Phi(-a) = exp(-a^2 / 2) t (c1 + t (c2 + ...)),      Phi(z) = 1/2 + z (d0 + d1 z^2 + ...).
-// bf16: the first alone, c = 0.375, five terms, off by 3.8e-5 of itself in float arithmetic on a <= 14.5 (beyond, the exponential is zero in float): a fiftieth of what
-// rounding the output costs, in no more instructions than an approximation of erf (1 + erf loses the digits of negative z), with the hardware's exponential and
-// reciprocal.  Float: the first with c = 0.25 and eight terms from 1.25 on, below it the second with six, both off by 1e-8; with their roundings Phi is off by at
-// most 12 units of 2^-24 of itself up to a = 3, and by a^2 / 2 more beyond, for the square's.  No branches: erfcf, the same to a few units, has them.  us, by
-// an approximation of erf (whose error stays while Phi falls) / erfcf / this: float 3 x 257 x 1000 -> 771 backward 42.1 / 45.8 / 43.3,
-// 4096 x 1024 -> 4096 forward 260 / 269 / 265, 4 x 8192 x 16 -> 4096 backward 554 / 570 / 554; bf16 4 x 8192 x 16 -> 4096 backward 286 / - / 270. SiLU of floats with the
+// bf16: the first alone, seven terms, fitted to 1e-7 and to 2e-5 of itself on a <= 14.5 (beyond, the exponential is zero in float), with the hardware's exponential and
+// reciprocal: 2e-7 in float arithmetic, which is what an output whose residual cancels z Phi(z) shows, and a hundredth of what rounding costs any other.  (Five terms, off by 4e-5
+// of itself, are no faster: 4 x 2048 x 2048 -> 8192 292.5 / 291.7 us, 4 x 8192 x 16 -> 4096 backward 269 / 267.)  Float: the first with eight terms from 1.25 on, below it the second with six, both off by
+// 1e-8 of themselves; with their roundings Phi is off by at most 12 units of 2^-24 of itself up to a = 3, and by a^2 / 2 more beyond, for the square's.  No branches:
+// erfcf, the same to a few units, has them.  us, by an approximation of erf (whose error stays while Phi falls) / erfcf / this: float
+// 3 x 257 x 1000 -> 771 backward 42.1 / 45.8 / 43.3, 4096 x 1024 -> 4096 forward 260 / 269 / 265, 4 x 8192 x 16 -> 4096 backward 554 / 570 / 554.  SiLU of floats with the
 // exact exponential and quotient: 41.4 / 42.6 for the first.
 template <typename T> __device__ __forceinline__ float exp_of(float x) {
     if constexpr (sizeof(T) == 4) return expf(x);
@@ -63,13 +63,11 @@ template <int N> __device__ __forceinline__ float polynomial(float x, const floa
 }
 // Phi(-|z|); float: |z| from 1.25 on.
 template <typename T> __device__ __forceinline__ float tail_of(float z, float bell) {
-    if constexpr (sizeof(T) == 4) {
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, __builtin_fabsf(z), 1.0f));
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, __builtin_fabsf(z), 1.0f));
+    if constexpr (sizeof(T) == 4)
         return t * polynomial(t, {0.0997423306f, 0.0995698348f, 0.0952199996f, 0.0711945444f, 0.0975557044f, -0.0292390473f, 0.114079773f, -0.0481649525f}) * bell;
-    } else {
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.375f, __builtin_fabsf(z), 1.0f));
-        return t * polynomial(t, {0.149079636f, 0.157558411f, 0.0841232985f, 0.199558422f, -0.0903177261f}) * bell;
-    }
+    else
+        return t * polynomial(t, {0.0990288705f, 0.109893471f, 0.0344877355f, 0.260672182f, -0.243641973f, 0.327903092f, -0.0883433446f}) * bell;
 }
 template <typename T> __device__ __forceinline__ float normal_cdf(float z, float bell) {
     const float tail = tail_of<T>(z, bell), far = z < 0.0f ? tail : 1.0f - tail;

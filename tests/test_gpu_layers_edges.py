@@ -196,3 +196,20 @@ def test_temperatures_whose_reciprocal_leaves_float_with_its_logarithms_base(lay
         assert "tau" in str(e)
         return
     assert not torch.isnan(loss).any() and not torch.isnan(grad).any()
+
+
+@pytest.mark.parametrize("t", [1, 9])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_a_residual_that_cancels_the_activation(layers, act, dtype, t):
+    """What is left is the activation's own error, which 32 bits hold to a few units of z whatever the output's type: 16 U |z|, as everywhere."""
+    z = grid(dtype, -8.0, 8.0)
+    o = z.numel()
+    x, w = torch.zeros((1, t, 1), dtype=dtype, device=DEV), torch.zeros((1, o, 1), dtype=dtype, device=DEV)
+    value = orc.act(act, orc.f64(z))
+    r = (-value).to(dtype).to(DEV)
+    y = torch.empty((1, t, o), dtype=dtype, device=DEV)
+    layers.linear(x, w, y, bias=z[None], act=act, residual=r.expand(1, t, o))
+    torch.cuda.synchronize()
+    want = value + orc.f64(r)
+    orc.assert_within(y[0, 0], want, orc.rounded(want, 16 * orc.U * orc.f64(z).abs(), dtype), "what is left")
