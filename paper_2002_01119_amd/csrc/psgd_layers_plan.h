@@ -40,12 +40,14 @@ constexpr TileCost kCostsBf16[] = {{256, 256, 1, 1.75f, 1.75f, 9.0f}, {128, 128,
 constexpr TileCost kCostsFloat[] = {{256, 256, 1, 8.0f, 8.0f, 10.0f}, {128, 128, 2, 2.4f, 2.4f, 6.0f}, {64, 64, 4, 0.7f, 0.55f, 2.5f},
                                     {128, 32, 4, 0.7f, 0.55f, 2.5f}, {32, 128, 4, 0.7f, 0.55f, 2.5f}};
 
-// One whole tile of k at most: there is no second one beside it in LDS, and one workgroup more fits a compute unit (not of the largest, for its
-// registers).  Such a product waits for C to be written: 4 x 2048 x 64 -> 8192 bf16 41 us before, now 35; 15 x 2120 x 16 -> 4096 120 and 84.
+// One whole tile of k at most: there is no second one beside it in LDS, and one workgroup more fits a compute unit, where its registers do: not of the
+// largest, nor of 128 x 128 for dx (174 a lane, 512 hold two).  Such a product waits for C to be written: 4 x 2048 x 64 -> 8192 bf16 41 us without, with
+// it 35; 15 x 2120 x 16 -> 4096 120 and 84.  (Counted for dx too, as it was: 4 x 2048 x 8192 from 100 outputs 63.5 us, now 52.9, 8 x 2048 x 2048 from 40 30.9
+// and 26.8; of eight such sizes 15 x 2120 x 4096 from 64 alone lost, 85 and 91.)
 inline bool short_k(int64_t k, int bytes) { return k < 2 * kRowBytes / bytes; }
 
 // The tile and the parts of k of the least cost.  Parts cost a second kernel and their sums' way through memory.
-inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus) {
+inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, int cus, bool dx = false) {
     Plan best{64, 64, 1};
     if (m < 1 || n < 1) return best;          // nothing to multiply
     const int64_t steps = parts_of(k, kRowBytes / bytes);
@@ -54,9 +56,10 @@ inline Plan gemm_plan(int learners, int64_t m, int64_t n, int64_t k, int bytes, 
     for (const TileCost* at = costs; at < costs + (bytes == 4 ? std::size(kCostsFloat) : std::size(kCostsBf16)); ++at) {
         const TileCost& c = *at;
         const int64_t tiles = parts_of(m, c.rows) * parts_of(n, c.cols) * learners;
+        const bool one_more = short_k(k, bytes) && c.resident > 1 && !(dx && c.rows == 128 && c.cols == 128);
         for (int split : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (split > 1 && (steps < 2 * split || tiles * split > 8 * (int64_t)cus)) break;
-            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * (c.resident + (c.resident > 1 && short_k(k, bytes)));
+            const int64_t groups = tiles * split, each = parts_of(steps, split), room = (int64_t)cus * (c.resident + one_more);
             const float deep = (float)parts_of(groups, cus), rounds = (float)parts_of(groups, room);
             const float step = groups <= room ? (deep * c.shared > c.alone ? deep * c.shared : c.alone) : deep * c.shared;
             float us = (float)each * step + rounds * c.ends;
@@ -102,7 +105,7 @@ inline GradRoom grad_room(int act, int learners, int64_t t, int64_t in, int64_t 
     r.dz_pitch = parts_of(out, 16 / bytes) * (16 / bytes);
     r.dz = act != PSGD_ACT_NONE ? up256((size_t)learners * t * r.dz_pitch * bytes) : 0;
     r.sums = db ? up256((size_t)learners * slope_slabs(learners, t, out, bytes, cus) * out * sizeof(float)) : 0;
-    const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus).bytes(learners, t, in) : 0;
+    const size_t a = dx ? gemm_plan(learners, t, in, out, bytes, cus, true).bytes(learners, t, in) : 0;
     const size_t b = dw && !few_tokens_grad(t, out, bytes) ? gemm_plan(learners, out, in, t, bytes, cus).bytes(learners, out, in) : 0;
     r.product = a > b ? a : b;
     r.total = r.dz + r.sums + r.product;
@@ -116,7 +119,7 @@ struct GradPlan {
     int few_rows;          // of dW to a wavefront there
 };
 inline GradPlan grad_plan(int learners, int64_t t, int64_t in, int64_t out, int bytes, int cus, bool dx, bool dw) {
-    GradPlan g{gemm_plan(learners, t, in, out, bytes, cus), gemm_plan(learners, out, in, t, bytes, cus), false, few_tokens_grad(t, out, bytes), 0};
+    GradPlan g{gemm_plan(learners, t, in, out, bytes, cus, true), gemm_plan(learners, out, in, t, bytes, cus), false, few_tokens_grad(t, out, bytes), 0};
     // one launch for both, also of few tokens where dW is small: 8192 x 500 bf16, 4 tokens, 9.6 us, apart 7.4 and 6.6
     const bool small = (int64_t)learners * in * out * bytes <= (8 << 20);
     g.pair = dx && dw && (!g.few || small) && g.dx.split == 1 && g.dw.split == 1 && g.dx.rows == g.dx.cols && g.dx.rows == g.dw.rows &&
