@@ -153,8 +153,13 @@ inline int batches_kept(int64_t groups, int lanes) {
 }
 
 // How distillation holds a row of so many 16-byte groups: so many lanes, `held` groups each; 0: none, the row is read again for the gradient.  Rows of
-// up to 64 KB go to 1024 lanes too, two rows a compute unit at a time, but for numbers of rows that would leave few of them for a second turn:
-// 592 x 10 007 float 15.4 us, by 256 lanes that hold sixteen groups each 13.6; 4096 rows 67 / 71.
+// 32 to 64 KB are held by 1024 lanes, two rows a compute unit at a time, or by 256 of sixteen groups each, four: the first are done with a row sooner, the
+// second take half as many turns, which counts from the third row of a compute unit to about the eighth.  us, 1024 / 256 lanes:
+//     rows                     512         520         1024        1536        2048        2560        4096
+//     10 007 float          10.0 / 10.5  13.0 / 10.9  19.3 / 16.5  26.0 / 25.5  32.0 / 30.6  38.0 / 38.5  66.1 / 67.4
+//     16 384 float          13.5 / 13.7  16.3 / 14.4  24.4 / 20.3  34.0 / 32.0  45.4 / 45.2  64.3 / 67.3   101 / 109
+//     20 000 bf16           13.8 / 14.0  17.6 / 16.7  24.7 / 23.4  32.6 / 29.4  40.7 / 37.6  48.5 / 44.4  78.7 / 70.3
+//     32 768 bf16           17.3 / 17.6  20.4 / 20.3  27.9 / 25.2  37.5 / 32.2  48.6 / 50.1  68.5 / 70.1   104 / 113
 struct DistillHold {
     int lanes, held;
 };
@@ -166,7 +171,7 @@ inline DistillHold distill_hold(int64_t rows, int64_t groups, bool gradient, int
     if (groups <= 256 * 2) return {256, 2};
     if (groups <= 256 * 4) return {256, 4};
     if (groups <= 256 * 8) return {256, 8};
-    if (groups <= 256 * 16 && rows > 2 * (int64_t)cus && rows <= 4 * (int64_t)cus) return {256, 16};
+    if (groups <= 256 * 16 && rows > 2 * (int64_t)cus && rows <= 8 * (int64_t)cus) return {256, 16};
     if (groups <= 1024 * 4) return {1024, 4};
     if (groups <= 1024 * 8) return {1024, 8};
     if (groups <= 1024 * 16) return {1024, 16};

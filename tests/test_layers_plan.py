@@ -52,6 +52,12 @@ def test_a_workgroup_more_is_counted_only_where_its_registers_fit(ask):
         assert ask(["grad 2 %d %d %d %d %d" % (n, t, i, o, CUS)])[0].startswith("dx=256x256/short")
 
 
+def test_rows_of_three_to_eight_a_compute_unit_are_held_by_fewer_lanes(ask):
+    for size, v in ((4, 10007), (4, 16384), (2, 20000), (2, 32768)):
+        got = ask(["distill %d %d %d 1 0 %d" % (size, rows, v, CUS) for rows in (512, 513, 1024, 1025, 1600, 2048, 2049)])
+        assert got == ["lanes=1024 held=4"] + ["lanes=256 held=16"] * 5 + ["lanes=1024 held=4"]
+
+
 def words(table, size):
     return {word for _, said in table[size] for word in said.split()}
 
