@@ -939,7 +939,11 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
     GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};
     GemmArgs aw{dz, operand(x), Epilogue{operand(dw), {}, {}, {}, PSGD_ACT_NONE}, nullptr, out, in, t, n, 1, 0, 0};
     const GradPlan g = grad_plan(n, t, in, out, sizeof(T), cus, dx, dw);
-    if (g.pair) return g.dx.rows == 128 ? launch_pair<T, 128>(ax, aw, s) : launch_pair<T, 64>(ax, aw, s);
+    if (g.pair) {
+        if constexpr (sizeof(T) == 2)
+            if (g.dx.rows == 128) return launch_pair<T, 128>(ax, aw, s);
+        return launch_pair<T, 64>(ax, aw, s);
+    }
     if (dx)
         if (int rc = launch_gemm<T, true, false>(ax, g.dx, product, s)) return rc;
     if (dw && g.few) {
