@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
+#include <utility>
 
 namespace psgd {
 namespace {
@@ -890,6 +891,9 @@ inline int check_linear_sizes(const char* name, int n, int64_t t, int64_t in, in
     if (int rc = check_counts(name, n, t, in)) return rc;
     if (int rc = check_counts(name, n, t, out)) return rc;
     if (act < PSGD_ACT_NONE || act > PSGD_ACT_SILU) return fail(PSGD_EINVAL, "%s: act=%d", name, act);
+    // arrays of all learners that have to be there, or that a workspace may hold, counted in elements
+    for (const auto& [rows, cols] : {std::pair<int64_t, int64_t>{t, in}, {t, out}, {out, in}})
+        if (rows > 0 && cols > kMostElements / n / rows) return fail(PSGD_EINVAL, "%s: the layer is too large", name);
     return PSGD_OK;
 }
 inline int check_room(const char* name, void* workspace, size_t have, size_t need) {
