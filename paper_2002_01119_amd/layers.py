@@ -74,10 +74,12 @@ def _bind():
 
 def _short(name, *args):
     """Whether the short way has made the call."""
-    if _ext is None:
+    if _ext is None or _lib is not psgd._lib:
         if _lib is None or psgd._call is None or not hasattr(psgd._call, "bind_layers"):
             return False
-        _bind()
+        load()                   # psgd may have loaded the library again
+        if _ext is None:
+            _bind()
     return psgd._answered(getattr(_ext, name)(*args))
 
 

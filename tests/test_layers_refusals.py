@@ -33,3 +33,15 @@ def test_products_whose_elements_no_address_reaches(n, t, i, o, act):
     y = layers.View(1 << 52, t * o, o, F32)
     refused(lib.psgd_linear(x, w, None, None, y, None, act, n, t, i, o, None, 0, None), psgd.EINVAL, "too large")
     assert lib.psgd_linear_workspace(x, w, n, t, i, o) == 0 and lib.psgd_linear_grad_workspace(dy, x, w, None, None, db, act, n, t, i, o) == 0
+
+
+def test_calls_go_to_the_library_that_is_loaded():
+    """A library built and loaded again is the one that psgd's errors and status are asked of; the layers' calls go there too."""
+    torch = pytest.importorskip("torch")
+    before = layers.load()
+    after = psgd.load(reload=True)
+    assert after is not before
+    x = torch.zeros(1, 1, 4)
+    with pytest.raises(ValueError, match="GPU"):
+        layers.layer_norm(x, torch.zeros(1, 4), None, torch.zeros(1, 1, 4))
+    assert layers._lib is after
