@@ -18,6 +18,13 @@ constexpr int kWave = 64;
 inline size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 inline int64_t parts_of(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Workgroups of a launch along x: its work items are counted in 32 bits, and what is beyond is not started, without an error.  Larger calls are launched in
+// slices of so many.
+constexpr int64_t kMostGroups = 1 << 21;
+template <typename F> void in_slices(int64_t groups, const F& launch) {      // launch(first, count)
+    for (int64_t first = 0; first < groups; first += kMostGroups) launch(first, (unsigned)(groups - first < kMostGroups ? groups - first : kMostGroups));
+}
+
 // ------------------------------------------------------------------------------------------------ linear layer
 constexpr int kRowBytes = 128;                     // a row of the LDS tile: 64 bf16 or 32 floats of k, as eight chunks of 16 bytes
 

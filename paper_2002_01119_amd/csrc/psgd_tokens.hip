@@ -83,7 +83,7 @@ struct LogArgs {
     float *logp, *entropy, *top_logp;
     int32_t* top_idx;
     int k, keep;            // keep: floats of LDS for a row's batches' maxima, 0 if they do not fit
-    int64_t t, rows;
+    int64_t t, rows, first;      // first: the row this launch begins with
     int32_t v;
 };
 
@@ -257,7 +257,7 @@ template <typename T, int B, bool ENTROPY, bool TOP> __global__ __launch_bounds_
     __shared__ float room[W], room2[2 * W];
     extern __shared__ float batches[];               // TOP: [row][batch][B], if a.keep says that they fit
     const int slot = ROWS > 1 ? threadIdx.x / B : 0;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + slot;
+    const int64_t row = a.first + (int64_t)blockIdx.x * ROWS + slot;
     if (ROWS > 1 && row >= a.rows) return;
     const int64_t i = row / a.t, r = row % a.t;
     const T* x = at<T>(a.logits, i, r);
@@ -338,7 +338,7 @@ struct DistillArgs {
     float* loss;
     float tau, inv_tau;
     int k;
-    int64_t t, rows;
+    int64_t t, rows, first;      // first: the row this launch begins with
     int32_t v;
 };
 
@@ -355,7 +355,7 @@ template <typename T, int B, int NV, bool GRAD> __global__ __launch_bounds__(B *
     __shared__ float room[W], room2[2][2 * W];
     extern __shared__ float slots[];                 // of each row: p, z and the columns
     const int slot = ROWS > 1 ? threadIdx.x / B : 0;
-    const int64_t row = (int64_t)blockIdx.x * ROWS + slot;
+    const int64_t row = a.first + (int64_t)blockIdx.x * ROWS + slot;
     if (ROWS > 1 && row >= a.rows) return;
     const int64_t i = row / a.t, r = row % a.t;
     float *p = slots + slot * 3 * a.k, *z = p + a.k;
@@ -521,7 +521,10 @@ template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
             static LdsRecord record;                                                                                        \
             if (int rc = allow_lds(reinterpret_cast<const void*>(logprobs_kernel<T, B, EN, TOP>), batch_room(B), record)) return rc; \
         }                                                                                                                   \
-        hipLaunchKernelGGL((logprobs_kernel<T, B, EN, TOP>), dim3((unsigned)((a.rows + kRowsOf<B> - 1) / kRowsOf<B>)), dim3(B * kRowsOf<B>), lds, s, a); \
+        in_slices(parts_of(a.rows, kRowsOf<B>), [&](int64_t first, unsigned count) {                                        \
+            a.first = first * kRowsOf<B>;                                                                                   \
+            hipLaunchKernelGGL((logprobs_kernel<T, B, EN, TOP>), dim3(count), dim3(B * kRowsOf<B>), lds, s, a);             \
+        });                                                                                                                 \
     } while (0)
 #define PSGD_LOG_B(B)                                                                                                       \
     do {                                                                                                                    \
@@ -540,12 +543,14 @@ template <typename T> int launch_logprobs(LogArgs a, int cus, hipStream_t s) {
     return PSGD_OK;
 }
 
-template <typename T> void launch_distill(const DistillArgs& a, int cus, hipStream_t s) {
+template <typename T> void launch_distill(DistillArgs a, int cus, hipStream_t s) {
     const DistillHold h = distill_hold(a.rows, ((int64_t)a.v + kPer<T> - 1) / kPer<T>, a.dlogits.p, cus);
 #define PSGD_DISTILL(B, NV, GRAD)                                                                                           \
     if (h.lanes == B && h.held == NV && (a.dlogits.p != nullptr) == GRAD)                                                   \
-    hipLaunchKernelGGL((distill_kernel<T, B, NV, GRAD>), dim3((unsigned)((a.rows + kRowsOf<B> - 1) / kRowsOf<B>)), dim3(B * kRowsOf<B>), \
-                       (size_t)a.k * 12 * kRowsOf<B>, s, a)
+    in_slices(parts_of(a.rows, kRowsOf<B>), [&](int64_t first, unsigned count) {                                            \
+        a.first = first * kRowsOf<B>;                                                                                       \
+        hipLaunchKernelGGL((distill_kernel<T, B, NV, GRAD>), dim3(count), dim3(B * kRowsOf<B>), (size_t)a.k * 12 * kRowsOf<B>, s, a); \
+    })
     PSGD_DISTILL(64, 0, false);
     PSGD_DISTILL(256, 0, false);
     PSGD_DISTILL(1024, 0, false);
@@ -615,7 +620,7 @@ int psgd_token_logprobs(const psgd_view* logits, const psgd_view* tokens, float*
     }
     int cus = 0;
     if (int rc = compute_units(&cus)) return rc;
-    const LogArgs a{rows_of(logits), rows_of(tokens), logp, entropy, top_logp, top_idx, k, 0, t, rows, (int32_t)v};
+    const LogArgs a{rows_of(logits), rows_of(tokens), logp, entropy, top_logp, top_idx, k, 0, t, rows, 0, (int32_t)v};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (int rc = logits->type == PSGD_F32 ? launch_logprobs<float>(a, cus, s) : launch_logprobs<uint16_t>(a, cus, s)) return rc;
     const hipError_t e = hipGetLastError();
@@ -654,7 +659,7 @@ int psgd_distill(const psgd_view* logits, const psgd_view* top_idx, const psgd_v
     }
     int cus = 0;
     if (int rc = compute_units(&cus)) return rc;
-    const DistillArgs a{rows_of(logits), rows_of(top_idx), rows_of(top_logit), rows_of(dlogits), weight, loss, tau, 1.0f / tau, k, t, rows, (int32_t)v};
+    const DistillArgs a{rows_of(logits), rows_of(top_idx), rows_of(top_logit), rows_of(dlogits), weight, loss, tau, 1.0f / tau, k, t, rows, 0, (int32_t)v};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (logits->type == PSGD_F32) launch_distill<float>(a, cus, s);
     else launch_distill<uint16_t>(a, cus, s);

@@ -213,3 +213,41 @@ def test_a_residual_that_cancels_the_activation(layers, act, dtype, t):
     torch.cuda.synchronize()
     want = value + orc.f64(r)
     orc.assert_within(y[0, 0], want, orc.rounded(want, 16 * orc.U * orc.f64(z).abs(), dtype), "what is left")
+
+
+# A launch counts its work items along one axis in 32 bits; what is beyond was never started, and nobody said so.
+def all_alike(out, first):
+    assert torch.equal(out, first.expand_as(out))
+
+
+def test_more_rows_of_logits_than_one_launch_counts(layers):
+    n, t, v = 512, (1 << 17) + 3, 8                             # 2^26 rows at four a workgroup of 256 are 2^32 work items
+    x = normal((1, t, v), BF16, 1)
+    tokens = (torch.arange(t, device=DEV) % v).int()[None]
+    one, all_of = (torch.full((k, t), 7.0, device=DEV) for k in (1, n))
+    layers.token_logprobs(x, tokens, one)
+    layers.token_logprobs(x.expand(n, t, v), tokens.expand(n, t), all_of)
+    all_alike(all_of, one)
+    idx, top = tokens[:, :, None], torch.zeros((1, t, 1), device=DEV)
+    grads = [torch.full((k, t, v), 7.0, dtype=BF16, device=DEV) for k in (1, n)]
+    for k, loss, grad in zip((1, n), (one, all_of), grads):
+        loss.fill_(7.0)
+        layers.distill(x.expand(k, t, v), idx.expand(k, t, 1), top.expand(k, t, 1), loss, dlogits=grad)
+    all_alike(all_of, one)
+    all_alike(grads[1], grads[0])
+    del grads
+    all_of.fill_(7.0)
+    layers.distill(x.expand(n, t, v), idx.expand(n, t, 1), top.expand(n, t, 1), all_of)
+    all_alike(all_of, one)
+
+
+def test_more_alternatives_rows_than_one_launch_counts(layers):
+    n, t, v, k = 512, (1 << 15) + 1, 1028, 33                   # 2^24 rows of a workgroup of 256 each
+    x, tokens = normal((1, t, v), BF16, 1), torch.zeros((1, t), dtype=torch.int32, device=DEV)
+    outs = []
+    for m in (1, n):
+        logp, top, idx = torch.full((m, t), 7.0, device=DEV), torch.full((m, t, k), 7.0, device=DEV), torch.full((m, t, k), -7, dtype=torch.int32, device=DEV)
+        layers.token_logprobs(x.expand(m, t, v), tokens.expand(m, t), logp, top_logp=top, top_idx=idx)
+        outs.append((logp, top, idx))
+    for one, all_of in zip(*outs):
+        all_alike(all_of, one)
