@@ -130,7 +130,8 @@ inline GradPlan grad_plan(int learners, int64_t t, int64_t in, int64_t out, int 
     // one launch for both, also of few tokens where dW is small: 8192 x 500 bf16, 4 tokens, 9.6 us, apart 7.4 and 6.6
     const bool small = (int64_t)learners * in * out * bytes <= (8 << 20);
     g.pair = dx && dw && (!g.few || small) && g.dx.split == 1 && g.dw.split == 1 && g.dx.rows == g.dx.cols && g.dx.rows == g.dw.rows &&
-             g.dw.rows == g.dw.cols && g.dx.rows < (bytes == 4 ? 128 : 256);       // (no two float products choose 128 x 128 together)
+             g.dw.rows == g.dw.cols && g.dx.rows < (bytes == 4 ? 128 : 256) &&       // (no two float products choose 128 x 128 together)
+             (parts_of(t, g.dx.rows) * parts_of(in, g.dx.rows) + parts_of(out, g.dx.rows) * parts_of(in, g.dx.rows)) * learners <= kMostGroups;
     // 64 rows a wavefront, fewer where that leaves compute units without eight wavefronts
     const int64_t all = parts_of(in, kWave * 16 / bytes) * learners * out;
     g.few_rows = all >= (int64_t)cus * 8 * 64 ? 64 : all >= (int64_t)cus * 8 * 16 ? 16 : 4;

@@ -774,11 +774,11 @@ template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kern
     }
 }
 
-// Adds the slabs of db up: 64 columns a workgroup, its sixteen wavefronts every sixteenth slab each.
+// Adds the slabs of db up: 64 columns a workgroup the first of them 64 `first`, its sixteen wavefronts every sixteenth slab each.
 constexpr int kSumWaves = 16;
-template <typename T> __global__ __launch_bounds__(kSumWaves* kWave) void sum_slabs_kernel(const float* partial, int64_t slabs, int64_t o, Operand db) {
+template <typename T> __global__ __launch_bounds__(kSumWaves* kWave) void sum_slabs_kernel(const float* partial, int64_t slabs, int64_t o, Operand db, int64_t first) {
     __shared__ float rest[kSumWaves][kWave];
-    const int64_t i = blockIdx.y, col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;
+    const int64_t i = blockIdx.y, col = (first + blockIdx.x) * kWave + threadIdx.x % kWave;
     const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
     float sum = 0.0f;
     if (col < o) {
@@ -828,9 +828,28 @@ inline Operand operand(const psgd_view* v) {
     return v ? Operand{static_cast<const char*>(v->data), v->learner, v->row} : Operand{nullptr, 0, 0};
 }
 
+inline Operand moved(Operand o, int64_t elements, int bytes) { return o.p ? Operand{o.p + elements * bytes, o.learner, o.pitch} : o; }
+inline Epilogue moved(const Epilogue& e, int64_t m, int64_t n, int bytes) {
+    return Epilogue{moved(e.y, m * e.y.pitch + n, bytes), moved(e.z, m * e.z.pitch + n, bytes), moved(e.residual, m * e.residual.pitch + n, bytes),
+                    moved(e.bias, n, bytes), e.act};
+}
+
 template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG> int launch_tiles(GemmArgs a, hipStream_t s) {
     a.tiles_m = (int)parts_of(a.m, BM);
     a.tiles_n = (int)parts_of(a.n, BN);
+    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
+    if (grid > kMostGroups) {       // more than a launch counts: one half of C after the other
+        if (a.split > 1 || (a.tiles_m == 1 && a.tiles_n == 1)) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
+        const int64_t m = a.tiles_m > 1 ? (int64_t)(a.tiles_m / 2) * BM : 0, n = a.tiles_m > 1 ? 0 : (int64_t)(a.tiles_n / 2) * BN;
+        GemmArgs low = a, high = a;
+        low.m = m ? m : a.m, low.n = n ? n : a.n;
+        high.m = a.m - m, high.n = a.n - n;
+        high.p = moved(a.p, P_ALONG ? m * a.p.pitch : m, sizeof(T));
+        high.q = moved(a.q, Q_ALONG ? n * a.q.pitch : n, sizeof(T));
+        high.out = moved(a.out, m, n, sizeof(T));
+        if (int rc = launch_tiles<T, BM, BN, P_ALONG, Q_ALONG>(low, s)) return rc;
+        return launch_tiles<T, BM, BN, P_ALONG, Q_ALONG>(high, s);
+    }
     using Shape = TileShape<BM, BN>;
     constexpr size_t tile = (size_t)(BM + BN) * kRowBytes, rows = (size_t)Shape::LANES / kWave * 32 * (BN / Shape::ACROSS_N + 4) * sizeof(float);
     auto fn = gemm_kernel<T, BM, BN, P_ALONG, Q_ALONG>;
@@ -839,8 +858,6 @@ template <typename T, int BM, int BN, bool P_ALONG, bool Q_ALONG> int launch_til
         if (int rc = allow_lds(reinterpret_cast<const void*>(fn), 2 * tile, record)) return rc;
     }
     const size_t lds = short_k(a.k, sizeof(T)) ? std::max(tile, rows) : 2 * tile;
-    const int64_t grid = (int64_t)a.tiles_m * a.tiles_n * a.learners * a.split;
-    if (grid > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear: too many tiles");
     hipLaunchKernelGGL(fn, dim3((unsigned)grid), dim3(TileShape<BM, BN>::LANES), lds, s, a);
     return PSGD_OK;
 }
@@ -876,7 +893,6 @@ template <typename T, int TILE> int launch_pair(GemmArgs dx, GemmArgs dw, hipStr
         a->tiles_n = (int)parts_of(a->n, TILE);
         count[k++] = (int64_t)a->tiles_m * a->tiles_n * a->learners;
     }
-    if (count[0] + count[1] > INT32_MAX) return fail(PSGD_EINVAL, "psgd_linear_grad: too many tiles");
     constexpr size_t bytes = (size_t)4 * TILE * kRowBytes;
     auto fn = gemm_pair_kernel<T, TILE>;
     if (bytes >= 64 * 1024) {
@@ -902,19 +918,29 @@ inline int check_room(const char* name, void* workspace, size_t have, size_t nee
     return PSGD_OK;
 }
 
+template <typename T, int TOK, int R> void launch_few(const FewArgs& all, int learners, hipStream_t s) {
+    in_slices(parts_of(all.n, 4 * R), [&](int64_t first, unsigned count) {
+        FewArgs f = all;
+        const int64_t n = first * 4 * R;
+        f.w = moved(all.w, n * all.w.pitch, sizeof(T));
+        f.out = moved(all.out, 0, n, sizeof(T));
+        f.n = all.n - n;
+        hipLaunchKernelGGL((few_tokens_kernel<T, TOK, R>), dim3(count, learners), dim3(256), 0, s, f);
+    });
+}
 template <typename T> int linear_of(const GemmArgs& a, const Plan& plan, void* workspace, int cus, hipStream_t s) {
     if (a.m > most_few(a.learners, a.n, sizeof(T), cus)) return launch_gemm<T, true, true>(a, plan, static_cast<float*>(workspace), s);
-    const FewArgs f{a.p, a.q, a.out, a.m, a.k, a.n};
+    const FewArgs all{a.p, a.q, a.out, a.m, a.k, a.n};
     const bool four = four_outputs(a.learners, a.n, cus);
 #define PSGD_FEW(TOK)                                                                                                       \
     do {                                                                                                                    \
-        if (four) hipLaunchKernelGGL((few_tokens_kernel<T, TOK, 4>), dim3((unsigned)parts_of(a.n, 16), a.learners), dim3(256), 0, s, f); \
-        else hipLaunchKernelGGL((few_tokens_kernel<T, TOK, 1>), dim3((unsigned)parts_of(a.n, 4), a.learners), dim3(256), 0, s, f);       \
+        if (four) launch_few<T, TOK, 4>(all, a.learners, s);                                                                \
+        else launch_few<T, TOK, 1>(all, a.learners, s);                                                                     \
     } while (0)
     if (a.m <= 1) PSGD_FEW(1);
     else if (a.m <= 2) PSGD_FEW(2);
     else if (a.m <= 4) PSGD_FEW(4);
-    else if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((few_tokens_kernel<T, 8, 1>), dim3((unsigned)parts_of(a.n, 4), a.learners), dim3(256), 0, s, f);
+    else if constexpr (sizeof(T) == 4) launch_few<T, 8, 1>(all, a.learners, s);
 #undef PSGD_FEW
     return PSGD_OK;
 }
@@ -937,7 +963,9 @@ int linear_grad_of(const psgd_view* dy, const psgd_view* z, const psgd_view* x, 
         else hipLaunchKernelGGL((slope_kernel<T, PSGD_ACT_SILU>), grid, dim3(256), 0, s, a);
         if (act != PSGD_ACT_NONE) dz = Operand{room, t * r.dz_pitch, r.dz_pitch};
         if (db) {
-            hipLaunchKernelGGL((sum_slabs_kernel<T>), dim3((unsigned)parts_of(out, kWave), n), dim3(kSumWaves * kWave), 0, s, sums, slabs, out, operand(db));
+            in_slices(parts_of(out, kWave), [&](int64_t first, unsigned count) {
+                hipLaunchKernelGGL((sum_slabs_kernel<T>), dim3(count, n), dim3(kSumWaves * kWave), 0, s, sums, slabs, out, operand(db), first);
+            });
         }
     }
     GemmArgs ax{dz, operand(w), Epilogue{operand(dx), {}, {}, {}, PSGD_ACT_NONE}, nullptr, t, in, out, n, 1, 0, 0};

@@ -251,3 +251,42 @@ def test_more_alternatives_rows_than_one_launch_counts(layers):
         outs.append((logp, top, idx))
     for one, all_of in zip(*outs):
         all_alike(all_of, one)
+
+
+
+def test_more_tiles_than_one_launch_counts(layers):
+    n, many, few = 512, (1 << 21) + 70, 20                      # 2^24 tiles of 64 x 64 and a workgroup of 256 each
+    x, w = normal((1, many, 8), BF16, 1), normal((1, 1, 8), BF16, 2)
+    bias = normal((1, 1), BF16, 3)
+    ys = [torch.full((k, many, 1), 7.0, dtype=BF16, device=DEV) for k in (1, n)]
+    for k, y in zip((1, n), ys):
+        layers.linear(x.expand(k, many, 8), w.expand(k, 1, 8), y, bias=bias.expand(k, 1), act="silu")
+    all_alike(ys[1], ys[0])
+    del ys
+    dy = normal((1, many, 1), BF16, 4)
+    dxs = [torch.full((k, many, 1), 7.0, dtype=BF16, device=DEV) for k in (1, n)]
+    for k, dx in zip((1, n), dxs):
+        layers.linear_grad(dy.expand(k, many, 1), x[:, :, :1].expand(k, many, 1), w[:, :, :1].expand(k, 1, 1), dx=dx)
+    all_alike(dxs[1], dxs[0])
+    del dxs
+    dy, x = normal((1, few, many), BF16, 5), normal((1, few, 1), BF16, 6)
+    dws = [torch.full((k, many, 1), 7.0, dtype=BF16, device=DEV) for k in (1, n)]
+    for k, dw in zip((1, n), dws):
+        layers.linear_grad(dy.expand(k, few, many), x.expand(k, few, 1), w[:, :, :1].expand(k, many, 1), dw=dw)
+    all_alike(dws[1], dws[0])
+
+
+def test_more_outputs_of_one_token_than_one_launch_counts(layers):
+    o = (1 << 28) + 100                                         # sixteen outputs a workgroup of 256; 64 sums of db a workgroup of 1024
+    x, w = normal((1, 1, 8), BF16, 1), normal((1, 1, 8), BF16, 2).expand(1, o, 8)
+    bias = normal((1, o), BF16, 3)
+    y = torch.full((1, 1, o), 7.0, dtype=BF16, device=DEV)
+    layers.linear(x, w, y, bias=bias)
+    start = o - (1 << 20)
+    for a, b in ((0, 1 << 20), (start, o)):                      # the first and the last, against a call for them alone
+        part = torch.empty((1, 1, b - a), dtype=BF16, device=DEV)
+        layers.linear(x, w[:, a:b], part, bias=bias[:, a:b])
+        assert torch.equal(y[:, :, a:b], part)
+    db = torch.full((1, o), 7.0, dtype=BF16, device=DEV)
+    layers.linear_grad(y, x, w, db=db)
+    assert torch.equal(db, y[:, 0])
