@@ -343,12 +343,12 @@ template <typename T> __global__ __launch_bounds__(256) void norm_slab_kernel(No
         }
 }
 
-// Adds the slabs up: 64 columns a workgroup, its sixteen wavefronts every sixteenth slab each.
+// Adds the slabs up: 64 columns a workgroup, the first of them 64 `first`, its sixteen wavefronts every sixteenth slab each.
 constexpr int kSumWaves = 16;
 template <typename G>
-__global__ __launch_bounds__(kSumWaves* kWave) void norm_params_kernel(const float* partial, int64_t slabs, Vecs dgain, Vecs dbias, int64_t c) {
+__global__ __launch_bounds__(kSumWaves* kWave) void norm_params_kernel(const float* partial, int64_t slabs, Vecs dgain, Vecs dbias, int64_t c, int64_t first) {
     __shared__ float rest[kSumWaves][kWave];
-    const int64_t i = blockIdx.y, col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;     // of 2 c: gain's, then bias's
+    const int64_t i = blockIdx.y, col = (first + blockIdx.x) * kWave + threadIdx.x % kWave;     // of 2 c: gain's, then bias's
     const int w = threadIdx.x / kWave, l = threadIdx.x % kWave;
     float sum = 0.0f;
     if (col < 2 * c) {
@@ -567,12 +567,11 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
 #undef PSGD_NORM_GRAD_TYPES
     }
     if (params) {
-        const dim3 grid((unsigned)((2 * c + kWave - 1) / kWave), n);
         const int64_t count = t > 0 ? slabs : 0;
-        if (params->type == PSGD_F32)
-            hipLaunchKernelGGL((norm_params_kernel<float>), grid, dim3(kSumWaves * kWave), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
-        else
-            hipLaunchKernelGGL((norm_params_kernel<uint16_t>), grid, dim3(kSumWaves * kWave), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c);
+        auto sum = params->type == PSGD_F32 ? norm_params_kernel<float> : norm_params_kernel<uint16_t>;
+        in_slices(parts_of(2 * c, kWave), [&](int64_t first, unsigned groups) {
+            hipLaunchKernelGGL(sum, dim3(groups, n), dim3(kSumWaves * kWave), 0, s, a.partial, count, vecs_of(dgain), vecs_of(dbias), c, first);
+        });
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);

@@ -290,3 +290,15 @@ def test_more_outputs_of_one_token_than_one_launch_counts(layers):
     db = torch.full((1, o), 7.0, dtype=BF16, device=DEV)
     layers.linear_grad(y, x, w, db=db)
     assert torch.equal(db, y[:, 0])
+
+
+
+def test_more_columns_of_a_norm_than_one_launch_counts(layers):
+    c = (1 << 27) + 72                                           # 64 sums of dgain or dbias a workgroup of 1024
+    x = normal((1, 1, 1024), BF16, 1).repeat(1, 1, c // 1024 + 1)[:, :, :c]
+    mean, rstd = torch.zeros((1, 1), device=DEV), torch.ones((1, 1), device=DEV)
+    gain = torch.ones((1, 1), dtype=BF16, device=DEV).expand(1, c).contiguous()
+    dx, dgain, dbias = torch.empty_like(x), torch.full((1, c), 7.0, dtype=BF16, device=DEV), torch.full((1, c), 7.0, dtype=BF16, device=DEV)
+    layers.layer_norm_grad(x, x, gain, mean, rstd, dx, dgain, dbias)
+    assert torch.equal(dbias, x[:, 0])
+    assert torch.equal(dgain, (x[:, 0].float() ** 2).to(BF16))
