@@ -3,8 +3,10 @@
  * X_out = mix(X) - lr * G of psgd.h takes (Sec. 2, Eq. 2: g(Phi_k, xi_k)).
  *
  * All n learners are computed by one call.  Activations are [n, t, c] arrays (t tokens of each learner), parameters are views of the
- * rows of an [n, d] array like X (learner i's layer lies at the same columns of row i), and gradients of parameters are written
- * into views of the rows of another, like G.  A single model is n = 1.
+ * rows of an [n, d] array (learner i's layer lies at the same columns of row i), and gradients of parameters are written into views of the
+ * rows of another.  A single model is n = 1.  In float the arrays are the averaging step's own X and G.  In bf16 G is (the step takes bf16 gradients), and a
+ * layer norm reads its gain and bias from X whatever its activations are, but the matrices of psgd_linear have the type of its activations: a learner that
+ * computes in bf16 keeps a bf16 copy of X's rows for them and makes it anew after each step.
  *
  * Conventions of psgd.h hold: device pointers of the current device, nothing kept after the enqueued work has run, PSGD_OK or a
  * negative psgd_status with the text in psgd_last_error(), work enqueued on `stream` only.  Beyond them:

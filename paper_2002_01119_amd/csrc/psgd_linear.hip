@@ -14,9 +14,9 @@
 // LDS: one is multiplied while the next is put beside it and the one behind is on its way in registers.  Large tiles read least; what then
 // keeps the matrix cores from their rate is the operands' way through registers and LDS (without it the same loop multiplies at 1200 to 1380
 // TFLOP/s in bf16; waiting for memory is not it: k read again and again from one place is 0 to 5 % faster).  Measured, TFLOP/s forward / dx / dW: bf16
-// 8192^3 1089 / 1182 / 1127, 4096^3 1150 / 1122 / 1070, 4 x 2048 x 2048 -> 8192 1066 / 1155 / 980 (a library's product of 8192^3 here: 1517 / 1384 / 1192);
-// float 4096^3 145 / 142 / 141 (154).  The epilogue of large tiles has the chip to itself, one workgroup to a compute unit: bias, GELU and a second
-// array of 134 MB are 43 of 301 us for 4 x 2048 x 2048 -> 8192.
+// 8192^3 1091 / 1157 / 1155 (a library's product of that size here: 1517 / 1384 / 1192), 4096^3 1143 / 1111 / 1089, 4 x 2048 x 2048 -> 8192
+// 1052 / 1118 / 1031, 4096 x 1024 -> 32 000 929 / 822 / 1016; float 4096^3 140 / 141 / 139 (154).  The epilogue of large tiles has the chip to itself, one
+// workgroup to a compute unit: bias, GELU and a second array of 134 MB are 42 of 303 us for 4 x 2048 x 2048 -> 8192.
 #include "psgd_rows.h"
 
 #include <algorithm>
@@ -38,16 +38,17 @@ struct Operand {          // element (row, col) of learner i at p + i * learner 
 
 constexpr float kLog2E = 1.44269504088896341f;
 
-// The activations z Phi(z) and z / (1 + exp(-z)) and their slopes, each as exact as its outputs' type can hold, however far z is from zero.  Phi by fitted polynomials: with
-// a = |z|, t = 1 / (1 + a / 4),
+// The activations z Phi(z) and z / (1 + exp(-z)) and their slopes, each as exact as its outputs' type can hold, however far z is from zero.  Phi by fitted
+// polynomials: with a = |z|, t = 1 / (1 + a / 4),
 //     Phi(-a) = exp(-a^2 / 2) t (c1 + t (c2 + ...)),      Phi(z) = 1/2 + z (d0 + d1 z^2 + ...).
-// bf16: the first alone, seven terms, fitted to 1e-7 and to 2e-5 of itself on a <= 14.5 (beyond, the exponential is zero in float), with the hardware's exponential and
-// reciprocal: 2e-7 in float arithmetic, which is what an output whose residual cancels z Phi(z) shows, and a hundredth of what rounding costs any other.  (Five terms, off by 4e-5
-// of itself, are no faster: 4 x 2048 x 2048 -> 8192 292.5 / 291.7 us, 4 x 8192 x 16 -> 4096 backward 269 / 267.)  Float: the first with eight terms from 1.25 on, below it the second with six, both off by
-// 1e-8 of themselves; with their roundings Phi is off by at most 12 units of 2^-24 of itself up to a = 3, and by a^2 / 2 more beyond, for the square's.  No branches:
-// erfcf, the same to a few units, has them.  us, by an approximation of erf (whose error stays while Phi falls) / erfcf / this: float
-// 3 x 257 x 1000 -> 771 backward 42.1 / 45.8 / 43.3, 4096 x 1024 -> 4096 forward 260 / 269 / 265, 4 x 8192 x 16 -> 4096 backward 554 / 570 / 554.  SiLU of floats with the
-// exact exponential and quotient: 41.4 / 42.6 for the first.
+// bf16: the first alone, seven terms, fitted to 1e-7 and to 2e-5 of itself on a <= 14.5 (beyond, the exponential is zero in float), with the hardware's
+// exponential and reciprocal: 2e-7 in float arithmetic, which is what an output whose residual cancels z Phi(z) shows, and a hundredth of what rounding
+// costs any other.  (Five terms, off by 4e-5 of itself, are no faster: 4 x 2048 x 2048 -> 8192 292.5 / 291.7 us.)
+// Float: the first with eight terms from 1.25 on, below it the second with six, both off by 1e-8 of themselves; with their roundings Phi is off by at most
+// 12 units of 2^-24 of itself up to a = 3, and by a^2 / 2 more beyond, for the square's.  No branches: erfcf, the same to a few units, has them.  us, by
+// an approximation of erf (whose error stays while Phi falls) / erfcf / this: 3 x 257 x 1000 -> 771 backward 42.1 / 45.8 / 43.3, 4096 x 1024 -> 4096
+// forward 260 / 269 / 265, 4 x 64 x 512 -> 2048 15.2 / - / 15.9.  SiLU by the exact exponential and quotient, the hardware's before: the first 41.4 / 42.7,
+// the last 14.8 / 15.5.
 template <typename T> __device__ __forceinline__ float exp_of(float x) {
     if constexpr (sizeof(T) == 4) return expf(x);
     else return __builtin_amdgcn_exp2f(x * kLog2E);
@@ -66,14 +67,16 @@ template <int N> __device__ __forceinline__ float polynomial(float x, const floa
 template <typename T> __device__ __forceinline__ float tail_of(float z, float bell) {
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, __builtin_fabsf(z), 1.0f));
     if constexpr (sizeof(T) == 4)
-        return t * polynomial(t, {0.0997423306f, 0.0995698348f, 0.0952199996f, 0.0711945444f, 0.0975557044f, -0.0292390473f, 0.114079773f, -0.0481649525f}) * bell;
+        return t * polynomial(t, {0.0997423306f, 0.0995698348f, 0.0952199996f, 0.0711945444f, 0.0975557044f, -0.0292390473f, 0.114079773f,
+                                  -0.0481649525f}) * bell;
     else
         return t * polynomial(t, {0.0990288705f, 0.109893471f, 0.0344877355f, 0.260672182f, -0.243641973f, 0.327903092f, -0.0883433446f}) * bell;
 }
 template <typename T> __device__ __forceinline__ float normal_cdf(float z, float bell) {
     const float tail = tail_of<T>(z, bell), far = z < 0.0f ? tail : 1.0f - tail;
     if constexpr (sizeof(T) == 2) return far;
-    const float near = __builtin_fmaf(z, polynomial(z * z, {0.398942262f, -0.0664902106f, 0.00997228269f, -0.00118383719f, 0.000111041125f, -6.80949188e-06f}), 0.5f);
+    const float slope = polynomial(z * z, {0.398942262f, -0.0664902106f, 0.00997228269f, -0.00118383719f, 0.000111041125f, -6.80949188e-06f});
+    const float near = __builtin_fmaf(z, slope, 0.5f);
     return __builtin_fabsf(z) < 1.25f ? near : far;
 }
 template <int ACT, typename T> __device__ __forceinline__ float act_of(float z) {
@@ -690,8 +693,9 @@ template <typename T, int TOK, int R> __global__ __launch_bounds__(256) void few
 }
 
 // dW = dz' x of up to TOK tokens: little more than writing dW, which is done in rows.  A lane keeps 16 bytes of columns of x; a wavefront takes up to 64
-// rows (outputs), whose dz it reads at once, a row a lane.  Bound by HBM: 4 float tokens of eight learners, 6400 x 4096, 155 us, 839 MB at 5.4 TB/s.  (dx of so few tokens is left to the tiles: W read like this, with its sums beside it, was
-// slower at every size but one, 8 to 200 % at four tokens.)
+// rows (outputs), whose dz it reads at once, a row a lane.  Bound by HBM: 4 float tokens of eight learners, 6400 x 4096, 155 us, 839 MB at 5.4 TB/s.
+// (dx of so few tokens is left to the tiles: 1 to 8 tokens of eight learners, 4096 x 4096, 44 us in bf16, W at 6.1 TB/s, and 98 to 102 in float, 5.3 to 5.5;
+// of one learner 13 and 20.  W read in rows, with its sums beside it, was slower at every size but one, 8 to 200 % at four tokens.)
 struct FewGradArgs {
     Operand dz, x, dw;
     int64_t t, in, out;
@@ -737,7 +741,10 @@ struct SlopeArgs {
     float* partial;        // [n][slabs][o] column sums, or NULL
     int64_t t, o;
 };
-// dz = dy act'(z) and its sums down the columns.  dz is rounded to T once, for the matrix instructions take bf16; db sums what was not rounded.
+// dz = dy act'(z) and its sums down the columns.  In bf16 dz is rounded once, for the matrix instructions take bf16; db sums what was not rounded.  The
+// rounding is as large as the one of the outputs: dx and dW are 0.0023 of themselves from the formula's instead of 0.0017 (4 x 2048 x 8192 -> 2048), and
+// equal the product of the rounded dz but for 0.05 % of their values.  Kept whole as the sum of two bf16, dz would make both products twice, 540 us more
+// on 570 there; without an activation nothing is rounded but the outputs, and float layers have no such choice to make.
 // Bound by HBM: 4 x 2048 x 2048 bf16 22 us, 100 MB at 4.6 TB/s.  64 lanes side by side, four rows at a time, a slab of one learner's rows a workgroup.
 template <typename T, int ACT> __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a) {
     constexpr int E = kPer<T>;

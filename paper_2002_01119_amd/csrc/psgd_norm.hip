@@ -523,7 +523,8 @@ int psgd_layer_norm_grad(const psgd_view* dy, const psgd_view* x, const psgd_vie
     if (t > 0 && (!mean || !rstd)) return fail(PSGD_EINVAL, "%s: mean and rstd are needed", name);
     const Extent edy{"dy", dy, n, t, c}, ex{"x", x, n, t, c}, edx{"dx", dx, n, t, c}, eadd{"add", add ? add : dy, n, t, c};
     const Extent eg{"gain", gain, n, 1, c};
-    const Extent edg{"dgain", dgain ? dgain : gain, n, 1, dgain ? c : 0}, edb{"dbias", dbias ? dbias : gain, n, 1, dbias ? c : 0};   // no column: nothing to overlap
+    // what is not asked for has no column to overlap
+    const Extent edg{"dgain", dgain ? dgain : gain, n, 1, dgain ? c : 0}, edb{"dbias", dbias ? dbias : gain, n, 1, dbias ? c : 0};
     psgd_view vm, vr, vw;
     const Extent em = flat("mean", mean, n * t, &vm), er = flat("rstd", rstd, n * t, &vr);
     const size_t need = params ? psgd_layer_norm_grad_workspace(n, t, c) : 0;

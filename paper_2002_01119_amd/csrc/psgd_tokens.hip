@@ -10,7 +10,9 @@
 //
 // Measured: log probabilities, entropy and 20 alternatives of 4096 rows of 32 000 floats 119 us (524 MB, 4.4 TB/s), of one row of 131 072 bf16 with 8
 // alternatives 15 (one compute unit reads it, then the search); distillation of 8192 rows of 131 072 bf16 880 us (4.3 GB, 4.9 TB/s; a copy of that
-// size reaches 4.74), of 592 rows of 10 007 floats 12.7.
+// size reaches 4.74), of 592 rows of 10 007 floats 12.8; its loss alone of 2048 rows of 131 072 bf16 90 (537 MB, 6.0 TB/s).  Rows that no workgroup's
+// registers hold, beyond 131 072 bf16 or 65 536 floats, are read twice for the gradient: 2048 rows of 200 000 bf16 434 us, 3.8 TB/s of what they cannot do
+// without.
 #include "psgd_rows.h"
 
 namespace psgd {
@@ -33,6 +35,8 @@ constexpr float kNoLess = -200.0f;       // exp of it is 0 in float, and a produ
 
 // 2^x of a difference that is at most 0, zero where it is not a number (-inf from -inf).
 __device__ __forceinline__ float exp_below(float x) { return __builtin_amdgcn_exp2f(fmaxf(x, kNoLess)); }
+// The product's rounding is |x| 2^-24 of the exponential, as much as the difference of two logits that x is: where it enters sums, of terms that are at
+// most 0.37 / |x|; where it is an output, the gradient's q, no more than its logit was known to.
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
 
 // Sums relative to a running maximum.  An empty one has m = -inf; differences that are not numbers (-inf from -inf) count as kNoLess.

@@ -7,6 +7,7 @@ views of the rows of an [n, d] tensor like X, gradients of parameters are writte
     layers.linear(x, w, y, bias=X[:, b0:b1], act="gelu", z=z)
     layers.linear_grad(dy, x, w, dx=dx, dw=dw, db=db, act="gelu", z=z)
 
+Matrices have the type of the activations: in bf16 w and b are views of a bf16 copy of X, made after each step (`Xb.copy_(X)`), and dw and db of a bf16 G.
 A single model is n = 1.  Every operand has unit stride along its last dimension and any strides along the others (0 shares an input between
 learners); outputs are the caller's tensors.  Work is enqueued on `stream` (None: torch's current stream).  A workspace that a call needs is
 taken from torch's allocator on that stream, or is the caller's `workspace` (a contiguous uint8 tensor of at least the bytes that the
