@@ -1,0 +1,616 @@
+"""Performance cases of the learners' attention blocks: what lies between the linear layers that make queries, keys and values and the one that
+takes attention's output, for all n learners at once, and its form for one new token of each sequence.
+
+Activations are [n, t, heads * head], slices of the columns of one [n, t, (heads + 2 kv) * head] array as a linear layer leaves them.  Kinds:
+
+  qk              norm of every head of the queries and keys (RMS, a gain of each learner's own) and the rotation by position, in one pass
+  qk_grad         its backward pass: gradients of the queries and keys that went in, and of the two gains
+  attention       causal attention in packed sequences, with a sliding window and first tokens that stay visible where the case has them; also the
+                  logarithm of each row's sum, which the backward pass takes
+  attention_grad  its backward pass: the gradients of queries, keys and values
+  step            one new token of each of b sequences against their caches, which take its key and value; caches of a window are rings
+  dropout         y = residual + dropped x, the mask regenerated from (seed, step) wherever it is needed; the backward pass is the same call
+
+Common fields: n learners, t tokens each (step: b sequences each), heads, kv (heads of the keys), head (a head's columns), type, window (0: none),
+sinks, seqs (sequences that the t tokens are split into, 0: one of all), pitch the columns that lie between an activation's rows.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+F32, BF16 = "f32", "bf16"
+DTYPE = {F32: torch.float32, BF16: torch.bfloat16}
+DEV = "cuda:0"
+EPS = 1e-6
+BASE = 10000.0
+
+
+def _qk(kind, n, t, heads, kv, head, name=None, type=BF16, gtype=F32, rotary=0, pairs="halves", norm=True, far=4096, pitch=0):
+    c = dict(kind=kind, n=n, t=t, heads=heads, kv=kv, head=head, type=type, gtype=gtype, rotary=rotary or head, pairs=pairs, norm=norm, far=far, pitch=pitch)
+    return dict(c, name=name) if name else c
+
+
+def _attention(kind, n, t, heads, kv, head, name=None, type=BF16, window=0, sinks=0, seqs=0, pitch=0):
+    c = dict(kind=kind, n=n, t=t, heads=heads, kv=kv, head=head, type=type, window=window, sinks=sinks, seqs=seqs, pitch=pitch)
+    return dict(c, name=name) if name else c
+
+
+def _step(n, b, longest, heads, kv, head, name=None, type=BF16, window=0, sinks=0, even=False, pitch=0):
+    c = dict(kind="step", n=n, b=b, longest=longest, heads=heads, kv=kv, head=head, type=type, window=window, sinks=sinks, even=even, pitch=pitch)
+    return dict(c, name=name) if name else c
+
+
+def _dropout(n, t, c, name=None, type=BF16, p=0.1, residual=True, pitch=0):
+    d = dict(kind="dropout", n=n, t=t, c=c, type=type, p=p, residual=residual, pitch=pitch)
+    return dict(d, name=name) if name else d
+
+
+def listed():
+    return [
+        # One new token for each of eight learners: a call that costs its launch.
+        _qk("qk", 8, 1, 8, 2, 64, "qk_n8_t1_h8x64", type=F32),
+        # A training batch of four learners.
+        _qk("qk", 4, 4096, 32, 8, 128, "qk_n4_t4096_h32x128_bf16"),
+        # Its backward pass, gains' gradients into fp32 rows of G.
+        _qk("qk_grad", 4, 4096, 32, 8, 128, "qk_grad_n4_t4096_h32x128_bf16"),
+        # Odd sizes, a part of each head rotated, neighbouring columns as pairs, positions far out.
+        _qk("qk_grad", 3, 517, 6, 2, 80, "qk_grad_n3_t517_h6x80_odd", type=F32, rotary=32, pairs="neighbours", far=1_000_000, pitch=5),
+        # A training batch of packed sequences, all of a sequence's past visible.
+        _attention("attention", 4, 4096, 32, 8, 128, "attention_n4_t4096_h32x128_packed_bf16", seqs=5),
+        # One long document through a window with four first tokens that stay visible.
+        _attention("attention", 1, 32768, 8, 2, 128, "attention_n1_t32768_h8x128_window4096_bf16", window=4096, sinks=4),
+        # The backward pass of the training batch.
+        _attention("attention_grad", 4, 4096, 32, 8, 128, "attention_grad_n4_t4096_h32x128_packed_bf16", seqs=5),
+        # Odd sizes in full precision, a narrow window.
+        _attention("attention_grad", 3, 517, 6, 3, 72, "attention_grad_n3_t517_h6x72_window100_odd", type=F32, window=100, sinks=3, seqs=3, pitch=7),
+        # A single sequence with a long past: the cache is read once, by the whole chip.
+        _step(1, 1, 131072, 32, 8, 128, "step_n1_b1_131072_h32x128_bf16", even=True),
+        # Serving a batch of different lengths, most of them past the window, their caches rings.
+        _step(2, 48, 9000, 32, 8, 128, "step_n2_b48_window4096_h32x128_bf16", window=4096, sinks=4),
+        # One token of each learner.
+        _dropout(8, 1, 4096, "dropout_n8_t1_4096", type=F32),
+        # A training batch, added to the stream beside it.
+        _dropout(4, 4096, 4096, "dropout_n4_t4096_4096_bf16"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(1, int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi)))))))
+
+
+def _size(rng, lo, hi):
+    """A size of the range: odd ones, multiples of eight and powers of two among them."""
+    v = _log_int(rng, lo, hi)
+    how = rng.random()
+    if how < 0.35:
+        return v | 1
+    if how < 0.7:
+        return max(8, v // 8 * 8) if hi >= 8 else v
+    return min(hi, 1 << max(0, round(math.log2(v))))
+
+
+def draw(rng):
+    """A call of the same ranges: 1 .. 64 learners, one token to 32 768, pasts to 131 072, heads of 16 to 256 columns shared by 1 to 16 query heads."""
+    kind = rng.choice(["qk", "qk_grad", "attention", "attention", "attention_grad", "attention_grad", "step", "step", "dropout"])
+    type = rng.choice([F32, BF16, BF16])
+    pitch = rng.choice([0, 0, 0, 8, 24, 3])
+    n = _log_int(rng, 1, 64)
+    if kind == "dropout":
+        c = _size(rng, 16, 16384)
+        t = _size(rng, 1, max(1, min(16384, (1 << 26) // (n * c))))
+        return _dropout(n, t, c, type=type, p=rng.choice([0.0, 0.1, 0.1, 0.25, 0.5, 0.013]), residual=rng.random() < 0.6, pitch=pitch)
+    kv = rng.choice([1, 2, 2, 4, 8, 3])
+    heads = kv * rng.choice([1, 1, 2, 4, 4, 8, 16, 5])
+    head = rng.choice([64, 64, 128, 128, 128, 256, 32, 16, 80, 96, 72, 50])
+    while heads * head > 8192:
+        heads -= kv * max(1, heads // kv // 2)
+    width = heads * head
+    if kind in ("qk", "qk_grad"):
+        t = _size(rng, 1, max(1, min(16384, (1 << 26) // (n * width))))
+        rotary = rng.choice([head, head, head, head // 4 * 2])
+        return _qk(kind, n, t, heads, kv, head, type=type, gtype=rng.choice([F32, BF16]), rotary=rotary, pairs=rng.choice(["halves", "halves", "neighbours"]),
+                   norm=rng.random() < 0.75, far=rng.choice([4096, 131072, 1_000_000]), pitch=pitch)
+    window = rng.choice([0, 0, _log_int(rng, 1, 4096), _log_int(rng, 64, 4096)])
+    sinks = rng.choice([0, 1, 4, 4, 37]) if window else 0
+    if kind == "step":
+        n = min(n, 8)
+        b = _log_int(rng, 1, 128)
+        seen = (1 << 29) // (n * b * kv * head * (4 if type == F32 else 2))
+        longest = _size(rng, 1, max(1, min(131072, seen)))
+        return _step(n, b, longest, heads, kv, head, type=type, window=window, sinks=sinks, even=rng.random() < 0.3, pitch=pitch)
+    n = min(n, 16)
+    most = (1.2e12 if type == BF16 else 2e11) / (1 if kind == "attention" else 3) / (4 * n * width)        # of t times the tokens that a row sees
+    if kind == "attention_grad":                   # where every row sees one token, softmax has no gradient: what is left of it is rounding
+        window = window and max(8, window)
+    t = _size(rng, 1 if kind == "attention" else 16, max(16, min(32768, int(math.sqrt(most)))))
+    seqs = rng.choice([0, 0, _log_int(rng, 1, 64), 3]) if t > 64 else 0
+    return _attention(kind, n, t, heads, kv, head, type=type, window=window, sinks=sinks, seqs=min(seqs, t), pitch=pitch)
+
+
+# ------------------------------------------------------------------------------------------------ inputs
+class _Draws:
+    def __init__(self, seed):
+        self.g = torch.Generator(device=DEV)
+        self.g.manual_seed(seed)
+
+    def normal(self, shape, type, mean=0.0, sigma=1.0):
+        return torch.empty(shape, dtype=DTYPE[type], device=DEV).normal_(mean, sigma, generator=self.g)
+
+    def ints(self, lo, hi, shape):
+        return torch.randint(lo, hi, shape, generator=self.g, device=DEV, dtype=torch.int32)
+
+
+def _rows(n, t, c, pitch, type, draws=None, sigma=1.0):
+    """An [n, t, c] activation whose rows lie `pitch` columns apart; drawn, or an output to be written."""
+    shape = (n, t, c + pitch)
+    whole = draws.normal(shape, type, 0.0, sigma) if draws else torch.zeros(shape, dtype=DTYPE[type], device=DEV)
+    return whole[:, :, :c]
+
+
+def _projected(case, t, type, draws=None, sigma=1.0):
+    """Queries, keys and values side by side, as a linear layer leaves them."""
+    q, k = case["heads"] * case["head"], case["kv"] * case["head"]
+    a = _rows(case["n"], t, q + 2 * k, case["pitch"], type, draws, sigma)
+    return a[:, :, :q], a[:, :, q:q + k], a[:, :, q + k:]
+
+
+def _prepare_qk(case, draws):
+    n, t, head = case["n"], case["t"], case["head"]
+    q, k, _ = _projected(case, t, case["type"], draws, 1.3)
+    first = draws.ints(0, max(1, case["far"] - t), (n, 1))
+    s = dict(case=case, q=q, k=k, positions=first + torch.arange(t, device=DEV, dtype=torch.int32))
+    s["q_gain"] = draws.normal((n, head), F32, 1.0, 0.1) if case["norm"] else None
+    s["k_gain"] = draws.normal((n, head), F32, 1.0, 0.1) if case["norm"] else None
+    qo, ko, _ = _projected(case, t, case["type"], draws if case["kind"] == "qk_grad" else None, 1e-2)
+    if case["kind"] == "qk":
+        return dict(s, q_out=qo, k_out=ko)
+    dq, dk, _ = _projected(case, t, case["type"])
+    grads = torch.zeros((n, 2 * head), dtype=DTYPE[case["gtype"]], device=DEV)
+    return dict(s, dq_out=qo, dk_out=ko, dq=dq, dk=dk, dq_gain=grads[:, :head] if case["norm"] else None, dk_gain=grads[:, head:] if case["norm"] else None)
+
+
+def _prepare_attention(case, draws):
+    n, t, heads, head = case["n"], case["t"], case["heads"], case["head"]
+    q, k, v = _projected(case, t, case["type"], draws)
+    q *= 1.5                                                       # some rows look at few tokens
+    s = dict(case=case, q=q, k=k, v=v, starts=None)
+    if case["seqs"]:
+        cuts = draws.ints(0, t + 1, (n, case["seqs"] + 1)).sort(1).values
+        cuts[:, 0] = 0                                             # rows behind the last sequence are padding
+        cuts[:, -1] = t - t // 50
+        s["starts"] = cuts.clamp(max=t - t // 50).contiguous()
+    s["out"] = _rows(n, t, heads * head, case["pitch"], case["type"])
+    s["lse"] = torch.zeros((n, heads, t), device=DEV)
+    if case["kind"] == "attention":
+        return s
+    made = _plain_attention(s)
+    s["out"].copy_(made["out"])
+    s["lse"].copy_(made["lse"])
+    s["dout"] = _rows(n, t, heads * head, case["pitch"], case["type"], draws, 1e-2)
+    s["dq"], s["dk"], s["dv"] = _projected(case, t, case["type"])
+    return s
+
+
+def _prepare_step(case, draws):
+    n, b, longest = case["n"], case["b"], case["longest"]
+    width = case["kv"] * case["head"]
+    room = min(longest, case["window"] + case["sinks"]) if case["window"] else longest
+    q, k, v = _projected(case, b, case["type"], draws)
+    q *= 1.5
+    lengths = draws.ints(longest // 8, longest, (n, b)) if not case["even"] else torch.full((n, b), longest - 1, dtype=torch.int32, device=DEV)
+    caches = [draws.normal((n, b, room, width), case["type"]) for _ in range(2)]
+    return dict(case=case, q=q, k=k, v=v, cache_k=caches[0], cache_v=caches[1], lengths=lengths,
+                out=_rows(n, b, case["heads"] * case["head"], case["pitch"], case["type"]))
+
+
+def _prepare_dropout(case, draws):
+    n, t, c, pitch, type = case["n"], case["t"], case["c"], case["pitch"], case["type"]
+    return dict(case=case, x=_rows(n, t, c, pitch, type, draws), residual=_rows(n, t, c, pitch, type, draws) if case["residual"] else None,
+                y=_rows(n, t, c, pitch, type), seed=int(draws.ints(0, 2 ** 31 - 1, (1,)).item()), step=int(draws.ints(0, 100_000, (1,)).item()))
+
+
+def prepare(case, seed):
+    draws = _Draws(seed)
+    if case["kind"].startswith("qk"):
+        return _prepare_qk(case, draws)
+    if case["kind"].startswith("attention"):
+        return _prepare_attention(case, draws)
+    return _prepare_step(case, draws) if case["kind"] == "step" else _prepare_dropout(case, draws)
+
+
+# ------------------------------------------------------------------------------------------------ plain forms, in 32 bits
+def _turns(case, positions):
+    """cos and sin of [n, t, 1, rotary / 2] angles, taken in 64 bits: far positions turn many times."""
+    half = case["rotary"] // 2
+    rate = BASE ** (torch.arange(half, device=DEV, dtype=torch.float64) * (-1.0 / max(1, half)))
+    angle = positions.double()[:, :, None, None] * rate
+    return angle.cos().float(), angle.sin().float()
+
+
+def _rotated(case, x, cos, sin):
+    """[n, t, heads, head] with the first `rotary` columns of each head rotated."""
+    r = case["rotary"]
+    a, b = (x[..., :r // 2], x[..., r // 2:r]) if case["pairs"] == "halves" else (x[..., 0:r:2], x[..., 1:r:2])
+    a, b = a * cos - b * sin, b * cos + a * sin
+    both = torch.cat((a, b), -1) if case["pairs"] == "halves" else torch.stack((a, b), -1).flatten(-2)
+    return torch.cat((both, x[..., r:]), -1)
+
+
+def _plain_qk(s):
+    case, out = s["case"], {}
+    cos, sin = _turns(case, s["positions"])
+    for name in ("q", "k"):
+        x = s[name].float().unflatten(2, (-1, case["head"]))
+        if case["norm"]:
+            x = x * (x.square().mean(3, keepdim=True) + EPS).rsqrt() * s[name + "_gain"][:, None, None]
+        out[name + "_out"] = _rotated(case, x, cos, sin).flatten(2).to(s[name].dtype)
+    return out
+
+
+def _plain_qk_grad(s):
+    case, out = s["case"], {}
+    cos, sin = _turns(case, s["positions"])
+    for name in ("q", "k"):
+        u = _rotated(case, s["d%s_out" % name].float().unflatten(2, (-1, case["head"])), cos, -sin)
+        if case["norm"]:
+            x = s[name].float().unflatten(2, (-1, case["head"]))
+            r = (x.square().mean(3, keepdim=True) + EPS).rsqrt()
+            h = x * r
+            out["d%s_gain" % name] = (u * h).sum((1, 2)).to(DTYPE[case["gtype"]])
+            u = u * s[name + "_gain"][:, None, None]
+            u = r * (u - h * (u * h).mean(3, keepdim=True))
+        out["d" + name] = u.flatten(2).to(s[name].dtype)
+    return out
+
+
+def _visible(case, starts, t):
+    """[t, t]: whether row i sees row j; one learner's."""
+    r = torch.arange(t, device=DEV)
+    near = r[None, :] <= r[:, None]
+    if starts is None:
+        first = torch.zeros_like(r)
+    else:
+        seq = (starts[None, :] <= r[:, None]).sum(1) - 1           # -1 in front of the first sequence, the last one's number plus one behind it
+        within = (seq >= 0) & (seq < case["seqs"])
+        first = starts[seq.clamp(min=0)].long()
+        near &= (seq[:, None] == seq[None, :]) & within[:, None]
+    if case["window"]:
+        near &= (r[:, None] - r[None, :] < case["window"]) | (r[None, :] - first[:, None] < case["sinks"])
+    return near
+
+
+def _head_chunks(case):
+    """Query heads that are computed together, all of one key head."""
+    group = case["heads"] // case["kv"]
+    at_once = max(1, min(group, (1 << 30) // (case["t"] * case["t"])))
+    return [(h, min(h + at_once, (h // group + 1) * group), h // group) for g in range(case["kv"]) for h in range(g * group, (g + 1) * group, at_once)]
+
+
+def _of_head(x, i, h, head):
+    return x[i, :, h * head:(h + 1) * head].float()
+
+
+def _of_heads(x, i, h0, h1, head):
+    return x[i, :, h0 * head:h1 * head].float().unflatten(1, (h1 - h0, head)).transpose(0, 1)
+
+
+def _plain_attention(s):
+    case = s["case"]
+    n, t, heads, head = case["n"], case["t"], case["heads"], case["head"]
+    out, lse = torch.zeros((n, t, heads * head), device=DEV, dtype=s["q"].dtype), torch.zeros((n, heads, t), device=DEV)
+    for i in range(n):
+        seen = _visible(case, s["starts"][i] if s["starts"] is not None else None, t)
+        there = seen.any(1)
+        for h0, h1, g in _head_chunks(case):
+            z = torch.matmul(_of_heads(s["q"], i, h0, h1, head), _of_head(s["k"], i, g, head).t()) * head ** -0.5
+            z = torch.where(seen, z, -math.inf)
+            m = torch.where(there, z.amax(2), 0.0)
+            z = torch.exp(z - m[:, :, None])
+            total = torch.where(there, z.sum(2), 1.0)
+            y = torch.matmul(z, _of_head(s["v"], i, g, head)) / total[:, :, None]
+            out[i, :, h0 * head:h1 * head] = y.transpose(0, 1).flatten(1).to(out.dtype)
+            lse[i, h0:h1] = torch.where(there, m + torch.log(total), 0.0)
+    return {"out": out, "lse": lse}
+
+
+def _plain_attention_grad(s):
+    case = s["case"]
+    n, t, heads, kv, head = case["n"], case["t"], case["heads"], case["kv"], case["head"]
+    scale = head ** -0.5
+    dq = torch.zeros((n, t, heads * head), device=DEV, dtype=s["q"].dtype)
+    dk, dv = (torch.zeros((n, t, kv * head), device=DEV) for _ in range(2))
+    for i in range(n):
+        seen = _visible(case, s["starts"][i] if s["starts"] is not None else None, t)
+        there = seen.any(1)[:, None]
+        for h0, h1, g in _head_chunks(case):
+            q, k, v = _of_heads(s["q"], i, h0, h1, head), _of_head(s["k"], i, g, head), _of_head(s["v"], i, g, head)
+            dy = torch.where(there, _of_heads(s["dout"], i, h0, h1, head), 0.0)
+            z = torch.matmul(q, k.t()) * scale - s["lse"][i, h0:h1, :, None]
+            p = torch.where(seen, torch.exp(z), 0.0)
+            along = (dy * _of_heads(s["out"], i, h0, h1, head)).sum(2, keepdim=True)
+            z = p * (torch.matmul(dy, v.t()) - along) * scale
+            here = slice(g * head, (g + 1) * head)
+            for j in range(h1 - h0):
+                dv[i, :, here] += torch.matmul(p[j].t(), dy[j])
+                dk[i, :, here] += torch.matmul(z[j].t(), q[j])
+            dq[i, :, h0 * head:h1 * head] = torch.matmul(z, k).transpose(0, 1).flatten(1).to(dq.dtype)
+    return {"dq": dq, "dk": dk.to(dq.dtype), "dv": dv.to(dq.dtype)}
+
+
+def _plain_step(s):
+    case = s["case"]
+    n, b, heads, kv, head, window, sinks = (case[f] for f in ("n", "b", "heads", "kv", "head", "window", "sinks"))
+    ck, cv, p = s["cache_k"], s["cache_v"], s["lengths"].long()
+    room, width = ck.shape[2], kv * head
+    ring = max(1, room - sinks)
+    slot = torch.where(p < sinks, p, sinks + (p - sinks) % ring)
+    at = slot[:, :, None, None].expand(n, b, 1, width)
+    ck.scatter_(2, at, s["k"][:, :, None, :])
+    cv.scatter_(2, at, s["v"][:, :, None, :])
+    j = torch.arange(room, device=DEV)
+    held = torch.where(j < sinks, j, j + (p[:, :, None] - j).div(ring, rounding_mode="floor") * ring)      # the position that a slot holds
+    seen = (held <= p[:, :, None]) & (j <= p[:, :, None])
+    if window:
+        seen &= (p[:, :, None] - held < window) | (held < sinks)
+    out = torch.zeros((n, b, heads * head), device=DEV, dtype=s["q"].dtype)
+    q = s["q"].float().unflatten(2, (kv, heads // kv, head))
+    at_once = max(1, (1 << 28) // (room * width))
+    for i in range(n):
+        for b0 in range(0, b, at_once):
+            b1 = min(b, b0 + at_once)
+            k = ck[i, b0:b1].float().unflatten(2, (kv, head)).transpose(1, 2)
+            v = cv[i, b0:b1].float().unflatten(2, (kv, head)).transpose(1, 2)
+            z = torch.matmul(q[i, b0:b1], k.transpose(2, 3)) * head ** -0.5
+            z = torch.where(seen[i, b0:b1, None, None], z, -math.inf)
+            z = torch.exp(z - z.amax(3, keepdim=True))
+            out[i, b0:b1] = (torch.matmul(z, v) / z.sum(3, keepdim=True)).flatten(1).to(out.dtype)
+    return {"out": out, "cache_k": ck, "cache_v": cv}
+
+
+def _signed(x):
+    return x - (1 << 64) if x >= 1 << 63 else x
+
+
+GOLDEN = 0x9E3779B97F4A7C15
+M64 = (1 << 64) - 1
+
+
+def _splitmix(z):
+    """SplitMix64's output function over int64 tensors, whose products wrap."""
+    z = (z ^ (z >> 30 & (1 << 34) - 1)) * _signed(0xBF58476D1CE4E5B9)
+    z = (z ^ (z >> 27 & (1 << 37) - 1)) * _signed(0x94D049BB133111EB)
+    return z ^ (z >> 31 & (1 << 33) - 1)
+
+
+def _plain_dropout(s):
+    case = s["case"]
+    n, t, c = case["n"], case["t"], case["c"]
+    keep = 65536 - int(math.floor(case["p"] * 65536 + 0.5))
+    words = (c + 3) // 4
+    state = s["seed"] ^ ((s["step"] + 1) * GOLDEN & M64)
+    z = torch.arange(1, n * t * words + 1, device=DEV) * _signed(GOLDEN) + _signed(state)
+    z = _splitmix(z)[:, None] >> torch.tensor([0, 16, 32, 48], device=DEV) & 65535
+    kept = (z < keep).view(n, t, words * 4)[:, :, :c]
+    y = torch.where(kept, s["x"].float() * (65536.0 / keep), 0.0)
+    if s["residual"] is not None:
+        y = y + s["residual"].float()
+    return {"y": y.to(s["x"].dtype)}
+
+
+_PLAIN = dict(qk=_plain_qk, qk_grad=_plain_qk_grad, attention=_plain_attention, attention_grad=_plain_attention_grad, step=_plain_step, dropout=_plain_dropout)
+
+
+def run(s):
+    case, kind = s["case"], s["case"]["kind"]
+    if not own:
+        return _PLAIN[kind](s)
+    from paper_2002_01119_amd import attention
+    if kind in ("qk", "qk_grad"):
+        how = dict(positions=s["positions"], q_gain=s["q_gain"], k_gain=s["k_gain"], eps=EPS, rotary=case["rotary"], base=BASE, pairs=case["pairs"])
+        if kind == "qk":
+            attention.qk_norm_rope(s["q"], s["k"], s["q_out"], s["k_out"], case["heads"], case["kv"], **how)
+            return {"q_out": s["q_out"], "k_out": s["k_out"]}
+        attention.qk_norm_rope_grad(s["dq_out"], s["dk_out"], s["q"], s["k"], s["dq"], s["dk"], case["heads"], case["kv"], dq_gain=s["dq_gain"],
+                                    dk_gain=s["dk_gain"], **how)
+        out = {"dq_gain": s["dq_gain"], "dq": s["dq"], "dk_gain": s["dk_gain"], "dk": s["dk"]}
+        return {name: out[name] for name in out if out[name] is not None}
+    if kind == "attention":
+        attention.attention(s["q"], s["k"], s["v"], s["out"], case["heads"], case["kv"], lse=s["lse"], starts=s["starts"], window=case["window"],
+                            sinks=case["sinks"])
+        return {"out": s["out"], "lse": s["lse"]}
+    if kind == "attention_grad":
+        attention.attention_grad(s["dout"], s["q"], s["k"], s["v"], s["out"], s["lse"], s["dq"], s["dk"], s["dv"], case["heads"], case["kv"],
+                                 starts=s["starts"], window=case["window"], sinks=case["sinks"])
+        return {"dq": s["dq"], "dk": s["dk"], "dv": s["dv"]}
+    if kind == "step":
+        attention.attention_step(s["q"], s["k"], s["v"], s["cache_k"], s["cache_v"], s["lengths"], s["out"], case["heads"], case["kv"],
+                                 window=case["window"], sinks=case["sinks"])
+        return {"out": s["out"], "cache_k": s["cache_k"], "cache_v": s["cache_v"]}
+    attention.dropout(s["x"], s["y"], case["p"], s["seed"], step=s["step"], residual=s["residual"])
+    return {"y": s["y"]}
+
+
+# ------------------------------------------------------------------------------------------------ what a pass cannot do without
+def _size_of(type):
+    return 4 if type == F32 else 2
+
+
+def _pairs_seen(case):
+    """Pairs of a row and a row that it sees, of one learner and head: sequences of equal length stand for the drawn ones."""
+    t = case["t"] - case["t"] // 50 if case["seqs"] else case["t"]
+    count = max(1, case["seqs"])
+    length = t / count
+    near = min(length, case["window"]) if case["window"] else length
+    seen = near * (near + 1) / 2 + (length - near) * (near + min(case["sinks"], length - near))
+    return count * seen
+
+
+def work(case):
+    n, kind, e = case["n"], case["kind"], _size_of(case["type"])
+    if kind == "dropout":
+        count = n * case["t"] * case["c"]
+        return {"bytes": (3 if case["residual"] else 2) * count * e, "flops": 10 * count}
+    heads, kv, head = case["heads"], case["kv"], case["head"]
+    if kind in ("qk", "qk_grad"):
+        count = n * case["t"] * (heads + kv) * head
+        if kind == "qk":
+            return {"bytes": 2 * count * e + 4 * n * case["t"] + (8 * n * head if case["norm"] else 0), "flops": 8 * count}
+        return {"bytes": (3 if case["norm"] else 2) * count * e + 4 * n * case["t"] + (n * head * (8 + 2 * _size_of(case["gtype"])) if case["norm"] else 0),
+                "flops": 14 * count}
+    if kind == "step":
+        rows = case["longest"] if case["even"] else case["longest"] * 9 / 16
+        if case["window"]:
+            rows = min(rows, case["window"] + case["sinks"])
+        return {"bytes": int(n * case["b"] * (2 * rows * kv + 4 * kv + 2 * heads) * head * e), "flops": int(4 * n * case["b"] * heads * rows * head)}
+    width = n * case["t"] * head * e
+    pairs = _pairs_seen(case)
+    if kind == "attention":
+        return {"bytes": width * (2 * heads + 2 * kv) + 4 * n * heads * case["t"], "flops": int(4 * n * heads * pairs * head)}
+    return {"bytes": width * (4 * heads + 4 * kv) + 4 * n * heads * case["t"], "flops": int(10 * n * heads * pairs * head)}
+
+
+# ------------------------------------------------------------------------------------------------ the definitions in 64 bits
+def _exact_turn(case, s, x, back=False):
+    """Each pair of columns as one complex number, turned."""
+    r = case["rotary"]
+    half = r // 2
+    if not half:
+        return x.clone()
+    rate = torch.exp(-math.log(BASE) / half * torch.arange(half, device=DEV, dtype=torch.float64))
+    angle = s["positions"].double().unsqueeze(2) * rate
+    turn = torch.polar(torch.ones_like(angle), -angle if back else angle).unsqueeze(2)
+    y = x.clone()
+    if case["pairs"] == "halves":
+        z = torch.complex(x[..., :half].contiguous(), x[..., half:r].contiguous()) * turn
+        y[..., :half], y[..., half:r] = z.real, z.imag
+    else:
+        y[..., :r] = torch.view_as_real(torch.view_as_complex(x[..., :r].unflatten(-1, (half, 2)).contiguous()) * turn).flatten(-2)
+    return y
+
+
+def _exact_qk(s):
+    case, out = s["case"], {}
+    n, t, head = case["n"], case["t"], case["head"]
+    grad = case["kind"] == "qk_grad"
+    for name in ("q", "k"):
+        x = s[name].double().reshape(n, t, -1, head)
+        size = torch.sqrt(torch.linalg.vecdot(x, x) / head + EPS).unsqueeze(3)
+        gain = s[name + "_gain"].double().view(n, 1, 1, head) if case["norm"] else None
+        if not grad:
+            out[name + "_out"] = _exact_turn(case, s, x / size * gain if case["norm"] else x).reshape(n, t, -1)
+            continue
+        u = _exact_turn(case, s, s["d%s_out" % name].double().reshape(n, t, -1, head), back=True)
+        if case["norm"]:
+            out["d%s_gain" % name] = (x / size * u).sum(2).sum(1)
+            u = u * gain
+            u = u / size - x * (torch.linalg.vecdot(u, x) / head).unsqueeze(3) / size ** 3
+        out["d" + name] = u.reshape(n, t, -1)
+    return out
+
+
+def _sequences(s, i):
+    if s["starts"] is None:
+        return [(0, s["case"]["t"])]
+    cuts = s["starts"][i].tolist()
+    return [(a, b) for a, b in zip(cuts, cuts[1:]) if b > a]
+
+
+_BLOCK = 2048
+
+
+def _exact_blocks(case, lo, hi):
+    """Blocks of a sequence's rows with the columns that they can see and which of them each row does."""
+    for r0 in range(lo, hi, _BLOCK):
+        r1 = min(hi, r0 + _BLOCK)
+        from_ = max(lo, r0 - case["window"] + 1) if case["window"] else lo
+        cols = torch.arange(from_, r1, device=DEV)
+        if case["window"] and case["sinks"]:
+            cols = torch.cat((torch.arange(lo, min(lo + case["sinks"], from_), device=DEV), cols))
+        back = torch.arange(r0, r1, device=DEV).unsqueeze(1) - cols
+        ok = back >= 0
+        if case["window"]:
+            ok = ok & ((back < case["window"]) | (cols < lo + case["sinks"]))
+        yield slice(r0, r1), cols, ~ok
+
+
+def _exact_attention(s):
+    case = s["case"]
+    n, t, heads, head = case["n"], case["t"], case["heads"], case["head"]
+    per = heads // case["kv"]
+    q, k, v = (s[x].double().reshape(n, t, -1, head) for x in ("q", "k", "v"))
+    grad = case["kind"] == "attention_grad"
+    if grad:
+        dy, y = s["dout"].double().reshape(n, t, heads, head), s["out"].double().reshape(n, t, heads, head)
+        dq, dk, dv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    else:
+        y = torch.zeros_like(q)
+        lse = torch.zeros((n, heads, t), device=DEV, dtype=torch.float64)
+    for i in range(n):
+        for lo, hi in _sequences(s, i):
+            for rows, cols, gone in _exact_blocks(case, lo, hi):
+                for h in range(heads):
+                    g = h // per
+                    kk, vv = k[i, cols, g], v[i, cols, g]
+                    z = (q[i, rows, h] @ kk.T).div_(math.sqrt(head)).masked_fill_(gone, -math.inf)
+                    if not grad:
+                        lse[i, h, rows] = torch.logsumexp(z, 1)
+                        y[i, rows, h] = torch.softmax(z, 1) @ vv
+                        continue
+                    p = torch.exp(z - s["lse"][i, h, rows].double().unsqueeze(1))
+                    up = dy[i, rows, h]
+                    dz = p * (up @ vv.T - torch.linalg.vecdot(up, y[i, rows, h]).unsqueeze(1)) / math.sqrt(head)
+                    dv[i, :, g].index_add_(0, cols, p.T @ up)
+                    dk[i, :, g].index_add_(0, cols, dz.T @ q[i, rows, h])
+                    dq[i, rows, h] = dz @ kk
+    if grad:
+        return {"dq": dq.reshape(n, t, -1), "dk": dk.reshape(n, t, -1), "dv": dv.reshape(n, t, -1)}
+    return {"out": y.reshape(n, t, -1), "lse": lse}
+
+
+def _exact_step(s):
+    case = s["case"]
+    n, b, heads, kv, head, window, sinks = (case[f] for f in ("n", "b", "heads", "kv", "head", "window", "sinks"))
+    room = s["cache_k"].shape[2]
+    out = torch.zeros((n, b, heads * head), device=DEV, dtype=torch.float64)
+    ck, cv = s["cache_k"].clone(), s["cache_v"].clone()
+    for i, lengths in enumerate(s["lengths"].tolist()):
+        for j, p in enumerate(lengths):
+            place = lambda x: x if x < sinks or x < room else sinks + (x - sinks) % (room - sinks)
+            ck[i, j, place(p)], cv[i, j, place(p)] = s["k"][i, j], s["v"][i, j]
+            from_ = max(0, p + 1 - window) if window else 0
+            past = torch.arange(from_, p + 1, device=DEV)
+            past = torch.cat((torch.arange(0, min(sinks, from_), device=DEV), past))
+            at = torch.where((past < sinks) | (past < room), past, sinks + (past - sinks) % max(1, room - sinks))
+            k, v = (c[i, j, at].double().reshape(-1, kv, 1, head) for c in (ck, cv))
+            q = s["q"][i, j].double().reshape(kv, heads // kv, head)
+            p_ = torch.softmax((k * q).sum(3) / math.sqrt(head), 0) if k.shape[0] * heads * head < 1 << 22 else \
+                torch.softmax(torch.stack([k[:, g, 0] @ q[g].T for g in range(kv)], 1) / math.sqrt(head), 0)
+            out[i, j] = torch.stack([p_[:, g].T @ v[:, g, 0] for g in range(kv)]).reshape(-1)
+    return {"out": out, "cache_k": ck.double(), "cache_v": cv.double()}
+
+
+def _exact_dropout(s):
+    case = s["case"]
+    n, t, c = case["n"], case["t"], case["c"]
+    words = (c + 3) // 4
+    state = np.uint64((s["seed"] ^ (s["step"] + 1) * GOLDEN) & M64)
+    z = np.arange(1, n * t * words + 1, dtype=np.uint64) * np.uint64(GOLDEN) + state
+    for by, m in ((30, 0xBF58476D1CE4E5B9), (27, 0x94D049BB133111EB)):
+        z = (z ^ z >> np.uint64(by)) * np.uint64(m)
+    z ^= z >> np.uint64(31)
+    drawn = torch.from_numpy(z.astype("<u8").view("<u2").astype(np.int32)).to(DEV).view(n, t, 4 * words)[:, :, :c]
+    share = 65536 - math.floor(case["p"] * 65536 + 0.5)
+    y = drawn.lt(share) * (s["x"].double() * (65536 / share))
+    return {"y": y if s["residual"] is None else y + s["residual"].double()}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"].startswith("qk"):
+        return _exact_qk(s)
+    if case["kind"].startswith("attention"):
+        return _exact_attention(s)
+    return _exact_step(s) if case["kind"] == "step" else _exact_dropout(s)
