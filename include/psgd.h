@@ -353,7 +353,8 @@ int psgd_interleaved_free(void* ptr);
 /*
  * psgd_device_status - waits for the current device, then returns the sticky flag word that
  * kernels raise (bit 0: a mixing table held an entry outside [0, n) and the step wrote
- * nothing; bit 1: a token's index in psgd_layers.h was beyond its row).  `clear` != 0 resets it.  Negative psgd_status on failure.
+ * nothing; bit 1: a token's index in psgd_layers.h was beyond its row, or a start or
+ * length in psgd_attention.h out of its range).  `clear` != 0 resets it.  Negative psgd_status on failure.
  */
 int psgd_device_status(int clear);
 

@@ -1,0 +1,131 @@
+/*
+ * psgd_attention.h - C boundary of the learners' attention blocks: what lies between the linear layers of psgd_layers.h that make queries, keys and
+ * values and the one that takes attention's output, for all n learners in one call, forward and backward, and its form for one new token of each sequence.
+ *
+ * Conventions of psgd_layers.h hold: operands are psgd_view, device pointers of the current device, work enqueued on `stream` only, nothing
+ * allocated, workspaces of the caller (256-byte aligned, one for each call that may run at the same time), sums and statistics in fp32 and in a fixed
+ * order, each output rounded once.  Beyond them:
+ *   - queries are [n, t, heads * head], keys and values [n, t, kv * head]: a head's columns side by side, the heads one after the other.  kv divides
+ *     heads; query head h uses key head h / (heads / kv).  They may be column slices of one [n, t, (heads + 2 kv) * head] array, as a linear layer
+ *     leaves them, and so may their gradients.  head in 1..PSGD_MAX_HEAD.
+ *   - `starts` cuts the t rows of a learner into sequences: int32 [n, sequences + 1] (`row` is ignored), ascending; sequence s is rows starts[s] up to but not
+ *     including starts[s + 1], and may be empty.  Rows in front of the first and behind the last sequence belong to none: what they hold is not read, and
+ *     outputs' rows there are left as they were.  NULL with sequences = 0: all t rows are one sequence.  A start that is not in 0..t or below the one
+ *     before it raises bit 1 of psgd_device_status(), and the learner's outputs are then unspecified.
+ *   - nothing passes from one sequence to another: NaN or infinity in a row reaches no row of another sequence (of its own sequence it may reach any).
+ *   - row i of a sequence sees row j of it where j <= i and, with window > 0, i - j < window or j < sinks.  window = 0: no window, and sinks = 0.
+ */
+#ifndef PSGD_ATTENTION_H
+#define PSGD_ATTENTION_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "psgd_layers.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { PSGD_MAX_HEAD = 256 };
+
+/* Which columns of a head turn together, of the first `rotary`: c and c + rotary / 2, or 2 c and 2 c + 1. */
+enum { PSGD_PAIRS_HALVES = 0, PSGD_PAIRS_NEIGHBOURS = 1 };
+
+/*
+ * psgd_qk_norm_rope - norm of each head of queries and keys, and the rotation by position, in one pass.  For a head's columns x with gain g:
+ *
+ *     u = x r g, r = (mean(x^2) + eps)^-1/2   (without gains u = x),      (y_a, y_b) = (u_a cos f - u_b sin f, u_b cos f + u_a sin f)
+ *
+ * for the pair p of columns (a, b), f = position * base^(-2 p / rotary); columns from `rotary` on are u.  Angles are taken in 64 bits.
+ *
+ *   q, q_out [n, t, heads * head], k, k_out [n, t, kv * head], one type, float or bf16; q_out may be q and k_out k (same pointer and strides)
+ *   positions  int32 [n, t] (`row` is the stride between tokens) or NULL: the row's number
+ *   q_gain, k_gain  [n, head], float or bf16 alike, or both NULL: no norm, the rotation alone
+ * rotary even, in 0..head; base > 0 and finite; eps >= 0.  heads or kv may be 0 (its operands are then ignored).
+ */
+int psgd_qk_norm_rope(const psgd_view* q, const psgd_view* k, const psgd_view* positions, const psgd_view* q_gain, const psgd_view* k_gain,
+                      const psgd_view* q_out, const psgd_view* k_out, int heads, int kv, int head, int rotary, int pairs, double base, float eps,
+                      int n, int64_t t, void* stream);
+
+/*
+ * psgd_qk_norm_rope_grad - its backward pass.  With v the gradient of the output turned back, h = x r and w = v g:
+ *     dx = r (w - h mean(w h)),   dg = sum over tokens and heads of v h   (without gains dx = v).
+ *
+ *   dq_out, dk_out  gradients of q_out and k_out;  q, k  what went in;  dq, dk  written (dq may be dq_out, dk dk_out)
+ *   dq_gain, dk_gain  [n, head], float or bf16 alike, or NULL (each)
+ * q, k and the gains' gradients are not looked at without gains.  With t = 0 the gains' gradients are zero.
+ */
+size_t psgd_qk_norm_rope_grad_workspace(int n, int64_t t, int head);
+int psgd_qk_norm_rope_grad(const psgd_view* dq_out, const psgd_view* dk_out, const psgd_view* q, const psgd_view* k, const psgd_view* positions,
+                           const psgd_view* q_gain, const psgd_view* k_gain, const psgd_view* dq, const psgd_view* dk, const psgd_view* dq_gain,
+                           const psgd_view* dk_gain, int heads, int kv, int head, int rotary, int pairs, double base, float eps, int n, int64_t t,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * psgd_attention - out_i = sum_j p_ij v_j, p_ij = exp(s_ij - lse_i), s_ij = scale q_i . k_j, lse_i = log sum_j exp(s_ij) over the rows j that row i sees.
+ *
+ *   q, k, v, out  one type, float or bf16;  lse  float [n, heads, t], written, or NULL (the backward pass wants it)
+ * scale finite.  In bf16 the products are exact and summed in fp32, and p is rounded to bf16 where it enters the second one (lse sums it before that).
+ */
+int psgd_attention(const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_view* starts, const psgd_view* out, float* lse, int heads,
+                   int kv, int head, int window, int sinks, float scale, int sequences, int n, int64_t t, void* stream);
+
+/*
+ * psgd_attention_grad - its backward pass.  With D_i = dout_i . out_i, dp_ij = dout_i . v_j and ds_ij = p_ij (dp_ij - D_i):
+ *     dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij dout_i,  the last two also over the heads that share the key head.
+ *
+ *   dout, q, k, v, out, dq, dk, dv  one type;  lse as psgd_attention wrote it.
+ * In bf16, p and ds are rounded to bf16 where they enter a product.
+ */
+size_t psgd_attention_grad_workspace(int heads, int kv, int head, int window, int sinks, int sequences, int n, int64_t t);
+int psgd_attention_grad(const psgd_view* dout, const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_view* out, const float* lse,
+                        const psgd_view* starts, const psgd_view* dq, const psgd_view* dk, const psgd_view* dv, int heads, int kv, int head, int window,
+                        int sinks, float scale, int sequences, int n, int64_t t, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A cache of keys or values: column c of the row at `slot` of sequence s of learner i lies at data[i * learner + s * sequence + slot * row + c].
+ * No two rows may share a byte.
+ */
+typedef struct {
+    void* data;
+    int64_t learner;
+    int64_t sequence;
+    int64_t row;
+    int32_t type;
+} psgd_cache;
+
+/*
+ * psgd_attention_step - attention of one new token of each of b sequences of each learner, whose key and value are put into the caches.
+ *
+ *   q [n, b, heads * head], k, v [n, b, kv * head], out [n, b, heads * head];  cache_k, cache_v  `slots` rows of kv * head a sequence; one type
+ *   lengths  int32 [n, b] (`row` is the stride between sequences): the tokens that the sequence's cache has seen, which is the new one's position p.
+ *            Negative: no such sequence; nothing of it is read and its row of out is left as it was
+ * The token at position p lies in slot p where p < sinks, else in slot sinks + (p - sinks) mod (slots - sinks): a cache of at least sinks + window rows is
+ * a ring and takes sequences of any length (up to 2^30 tokens), one with fewer rows, or without a window, takes `slots` tokens (sinks is 0 without a window).  A length beyond
+ * that raises bit 1 of psgd_device_status(), makes the row of out NaN and leaves the caches as they were.  The call does not change lengths.
+ */
+size_t psgd_attention_step_workspace(int heads, int kv, int head, int window, int sinks, int n, int64_t b, int64_t slots);
+int psgd_attention_step(const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_cache* cache_k, const psgd_cache* cache_v,
+                        const psgd_view* lengths, const psgd_view* out, int heads, int kv, int head, int window, int sinks, float scale, int n,
+                        int64_t b, int64_t slots, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * psgd_dropout - y = x m / P(m = 1) [+ residual], m = 0 with probability p, 1 otherwise, from a counter: nothing of the mask is stored, and the backward
+ * pass is the same call with y's gradient for x (the residual's is y's own).
+ *
+ *   x, y, residual (or NULL) [n, t, c], one type, float or bf16; y may be x or residual
+ *   seed, step, step_dev  what the mask depends on, beside the element's place: step is added to *step_dev where that (device, or NULL) is given, so a
+ *            captured graph draws a new mask for each of its replays
+ * SplitMix64 (Steele, Lea and Flood 2014; the mixing tables' generator), state seed XOR (step + 1) 0x9E3779B97F4A7C15 plus a multiple of that constant for each four columns of a row: the multiple
+ * is (i t + r) ceil(c / 4) + column / 4 + 1 for learner i and row r, and the column's 16 bits of the output, the lowest first, are kept where they
+ * are below 65536 - round(65536 p).  So p is taken in steps of 2^-16, and y is scaled by the inverse of what is kept of 65536.  A dropped element is 0 whatever x holds.
+ * p in 0..1; with p = 1 y is the residual, or 0.
+ */
+int psgd_dropout(const psgd_view* x, const psgd_view* residual, const psgd_view* y, float p, uint64_t seed, uint64_t step, const uint64_t* step_dev,
+                 int n, int64_t t, int64_t c, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* PSGD_ATTENTION_H */

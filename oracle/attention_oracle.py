@@ -1,0 +1,193 @@
+"""Plain 64-bit CPU forms of the learners' attention blocks, and how far a kernel that sums in fp32 may be from them.
+
+As in layers_oracle: each function returns (values, bounds), the bound of an element being what the roundings of the kernel's arithmetic can add up to, from the
+magnitudes of the terms that enter it.
+"""
+import math
+
+import numpy as np
+import torch
+
+from oracle.layers_oracle import FEW, HALF, U, f64, rounded
+
+ANGLE = 2 * math.pi * 2.0 ** -27 + 4 * U     # of a cosine or sine: an eighth of a turn in 32 bits, and the function's own roundings
+
+
+def split(x, head):
+    return x.unflatten(2, (-1, head))
+
+
+def turn(x, positions, rotary, pairs, base, back=False):
+    """[n, t, heads, head] with pairs of columns turned, and for each element the sum of magnitudes that entered it."""
+    y, size = x.clone(), x.abs().clone()
+    half = rotary // 2
+    for p in range(half):
+        a, b = (p, p + half) if pairs == "halves" else (2 * p, 2 * p + 1)
+        f = positions.double()[:, :, None] * base ** (-2.0 * p / rotary)
+        c, s = torch.cos(f), -torch.sin(f) if back else torch.sin(f)
+        y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+        size[..., a] = size[..., b] = x[..., a].abs() + x[..., b].abs()
+    return y, size
+
+
+def qk_norm_rope(x, gain, positions, head, rotary, pairs, base, eps, dtype):
+    x, gain = split(f64(x), head), f64(gain)
+    u = x
+    if gain is not None:
+        u = x * (x.square().mean(3, keepdim=True) + eps).rsqrt() * gain[:, None, None]
+    y, size = turn(u, positions.cpu(), rotary, pairs, base)
+    b = size * (ANGLE + (FEW + head) * U)
+    return y.flatten(2), rounded(y, b, dtype).flatten(2)
+
+
+def qk_norm_rope_grad(dy, x, gain, positions, head, rotary, pairs, base, eps, dtype, gtype=None):
+    """(dx, dgain), (bounds); dgain None without a gain."""
+    dy, gain = split(f64(dy), head), f64(gain)
+    v, size = turn(dy, positions.cpu(), rotary, pairs, base, back=True)
+    b_v = size * (ANGLE + FEW * U)
+    if gain is None:
+        return (v.flatten(2), None), (rounded(v, b_v, dtype).flatten(2), None)
+    x = split(f64(x), head)
+    r = (x.square().mean(3, keepdim=True) + eps).rsqrt()
+    h, w = x * r, v * gain[:, None, None]
+    b_h, b_w = (FEW + head) * U * h.abs(), b_v * gain.abs()[:, None, None] + U * w.abs()
+    m = (w * h).mean(3, keepdim=True)
+    b_m = ((FEW + head) * U * (w * h).abs() + b_w * h.abs() + w.abs() * b_h).mean(3, keepdim=True)
+    dx = r * (w - h * m)
+    b_dx = r * (b_w + h.abs() * b_m + b_h * m.abs() + (FEW + head) * U * (w.abs() + (h * m).abs()))
+    dg = (v * h).sum((1, 2))
+    terms = x.shape[1] * x.shape[2]
+    b_dg = ((terms + FEW) * U * (v * h).abs() + b_v * h.abs() + v.abs() * b_h).sum((1, 2))
+    return (dx.flatten(2), dg), (rounded(dx, b_dx, dtype).flatten(2), rounded(dg, b_dg, gtype))
+
+
+def visible(t, window, sinks):
+    i, j = torch.arange(t)[:, None], torch.arange(t)[None, :]
+    return (j <= i) & ((i - j < window) | (j < sinks)) if window else j <= i
+
+
+def sequences(starts, t):
+    return [(0, t)] if starts is None else [(a, b) for a, b in zip(starts[:-1], starts[1:]) if b > a]
+
+
+def _scores(q, k, scale, head):
+    return q @ k.T * scale, (head + FEW) * U * abs(scale) * (q.abs() @ k.abs().T)
+
+
+def _product_half(dtype):
+    return HALF[dtype] if dtype == torch.bfloat16 else 0.0
+
+
+def one_head(q, k, v, seen, scale, dtype):
+    """Rows of queries over rows of keys: (out, lse), (bounds)."""
+    head = q.shape[1]
+    s, e = _scores(q, k, scale, head)
+    s = s.masked_fill(~seen, -math.inf)
+    lse = torch.logsumexp(s, 1, keepdim=True)
+    p = torch.exp(s - lse)
+    e = torch.where(seen, e + FEW * U * (s.abs() + lse.abs() + 1.0), 0.0)             # what p is off by, of itself
+    out, keys = p @ v, seen.shape[1]
+    b = (p * e) @ v.abs() + (p * e).sum(1, keepdim=True) * out.abs() + ((keys + FEW) * U + _product_half(dtype)) * (p @ v.abs())
+    b_lse = (p * e).sum(1, keepdim=True) + (keys + FEW) * U + FEW * U * lse.abs()
+    return (out, lse[:, 0]), (b, b_lse[:, 0])
+
+
+def attention(q, k, v, starts, heads, kv, window, sinks, scale, dtype):
+    """(out, lse), (bounds); rows of no sequence are NaN."""
+    n, t, c = q.shape
+    head = c // heads
+    q, k, v = (split(f64(x), head) for x in (q, k, v))
+    out, lse = torch.full((n, t, heads, head), math.nan, dtype=torch.float64), torch.full((n, heads, t), math.nan, dtype=torch.float64)
+    b_out, b_lse = out.clone(), lse.clone()
+    for i in range(n):
+        for lo, hi in sequences(None if starts is None else starts[i].tolist(), t):
+            seen = visible(hi - lo, window, sinks)
+            for h in range(heads):
+                g = h * kv // heads
+                (o, l), (bo, bl) = one_head(q[i, lo:hi, h], k[i, lo:hi, g], v[i, lo:hi, g], seen, scale, dtype)
+                out[i, lo:hi, h], lse[i, h, lo:hi], b_out[i, lo:hi, h], b_lse[i, h, lo:hi] = o, l, bo, bl
+    return (out.flatten(2), lse), (rounded(out, b_out, dtype).flatten(2), b_lse)
+
+
+def attention_grad(dout, q, k, v, out, lse, starts, heads, kv, window, sinks, scale, dtype):
+    """(dq, dk, dv), (bounds), from out and lse as they are given; rows of no sequence are NaN."""
+    n, t, c = q.shape
+    head, half = c // heads, _product_half(dtype)
+    dout, q, k, v, out = (split(f64(x), head) for x in (dout, q, k, v, out))
+    lse = f64(lse)
+    dq, dk, dv = torch.full_like(q, math.nan), torch.full_like(k, math.nan), torch.full_like(v, math.nan)
+    b_dq, b_dk, b_dv = dq.clone(), dk.clone(), dv.clone()
+    for i in range(n):
+        for lo, hi in sequences(None if starts is None else starts[i].tolist(), t):
+            seen = visible(hi - lo, window, sinks)
+            for x in (dk, dv, b_dk, b_dv):
+                x[i, lo:hi] = 0.0
+            rows = (hi - lo) * heads // kv
+            for h in range(heads):
+                g = h * kv // heads
+                qq, kk, vv, dd, oo, ll = q[i, lo:hi, h], k[i, lo:hi, g], v[i, lo:hi, g], dout[i, lo:hi, h], out[i, lo:hi, h], lse[i, h, lo:hi, None]
+                s, e = _scores(qq, kk, scale, head)
+                p = torch.where(seen, torch.exp(s - ll), 0.0)
+                e = e + FEW * U * (s.abs() + ll.abs() + 1.0)
+                dp, along = dd @ vv.T, (dd * oo).sum(1, keepdim=True)
+                off = (head + FEW) * U * (dd.abs() @ vv.abs().T + (dd * oo).abs().sum(1, keepdim=True))
+                ds = p * (dp - along)
+                b_ds = p * off + ds.abs() * (e + half) + FEW * U * p * (dp.abs() + along.abs())
+                dq[i, lo:hi, h] = scale * ds @ kk
+                b_dq[i, lo:hi, h] = abs(scale) * (b_ds + (hi - lo + FEW) * U * ds.abs()) @ kk.abs()
+                dk[i, lo:hi, g] += scale * ds.T @ qq
+                b_dk[i, lo:hi, g] += abs(scale) * (b_ds + (rows + FEW) * U * ds.abs()).T @ qq.abs()
+                dv[i, lo:hi, g] += p.T @ dd
+                b_dv[i, lo:hi, g] += (p * (e + half + (rows + FEW) * U)).T @ dd.abs()
+    return tuple(x.flatten(2) for x in (dq, dk, dv)), tuple(rounded(x, b, dtype).flatten(2) for x, b in ((dq, b_dq), (dk, b_dk), (dv, b_dv)))
+
+
+def slot_of(p, sinks, slots):
+    return p if p < sinks else sinks + (p - sinks) % (slots - sinks)
+
+
+def attention_step(q, k, v, cache_k, cache_v, lengths, heads, kv, window, sinks, scale, dtype):
+    """out, its bound and the caches after it; rows of no sequence are NaN."""
+    n, b, c = q.shape
+    head, slots = c // heads, cache_k.shape[2]
+    cache_k, cache_v = cache_k.cpu().clone(), cache_v.cpu().clone()
+    out = torch.full((n, b, heads, head), math.nan, dtype=torch.float64)
+    bound = out.clone()
+    for i in range(n):
+        for r in range(b):
+            p = int(lengths[i, r])
+            if p < 0:
+                continue
+            cache_k[i, r, slot_of(p, sinks, slots)], cache_v[i, r, slot_of(p, sinks, slots)] = k[i, r].cpu(), v[i, r].cpu()
+            near = [j for j in range(p + 1) if not window or p - j < window or j < sinks]
+            at = [slot_of(j, sinks, slots) for j in near]
+            keys, values = (f64(x[i, r, at]).unflatten(1, (kv, head)) for x in (cache_k, cache_v))
+            for h in range(heads):
+                (o, _), (bo, _) = one_head(f64(q[i, r]).view(heads, head)[h:h + 1], keys[:, h * kv // heads], values[:, h * kv // heads],
+                                           torch.ones(1, len(near), dtype=torch.bool), scale, dtype)
+                out[i, r, h], bound[i, r, h] = o[0], bo[0]
+    return out.flatten(2), rounded(out, bound, dtype).flatten(2), cache_k, cache_v
+
+
+def dropped(n, t, c, p, seed, step):
+    """[n, t, c]: which elements are kept, and what they are multiplied by."""
+    keep = 65536 - int(math.floor(float(np.float32(p)) * 65536 + 0.5))
+    words, golden = (c + 3) // 4, 0x9E3779B97F4A7C15
+    mask = (1 << 64) - 1
+    state = np.uint64((seed ^ ((step + 1) * golden & mask)) & mask)
+    with np.errstate(over="ignore"):
+        z = (np.arange(n * t * words, dtype=np.uint64) + np.uint64(1)) * np.uint64(golden) + state
+        z = (z ^ (z >> np.uint64(30))) * np.uint64(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> np.uint64(27))) * np.uint64(0x94D049BB133111EB)
+        z = z ^ (z >> np.uint64(31))
+    bits = np.stack([(z >> np.uint64(16 * e)) & np.uint64(65535) for e in range(4)], 1).astype(np.int64)
+    return torch.from_numpy(bits < keep).view(n, t, 4 * words)[:, :, :c], 65536.0 / keep if keep else 0.0
+
+
+def dropout(x, residual, p, seed, step, dtype):
+    kept, scale = dropped(*x.shape, p, seed, step)
+    y = torch.where(kept, f64(x) * scale, 0.0)
+    b = FEW * U * y.abs()
+    if residual is not None:
+        y, b = y + f64(residual), b + FEW * U * (y.abs() + f64(residual).abs())
+    return y, rounded(y, b, dtype)

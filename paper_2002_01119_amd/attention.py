@@ -1,0 +1,214 @@
+"""Attention blocks of all learners at once: ctypes binding of include/psgd_attention.h, argument marshalling only.
+
+What lies between the linear layers of `layers`: a linear layer leaves queries, keys and values side by side, and the next one takes what attention makes:
+
+    layers.linear(x, w_qkv, a)                                                   # a [n, t, (heads + 2 kv) head]
+    q, k, v = a.split((heads * head, kv * head, kv * head), 2)                   # column slices, no copies
+    attention.qk_norm_rope(q, k, q, k, heads, kv, q_gain=gq, k_gain=gk, positions=pos)
+    attention.attention(q, k, v, y, heads, kv, lse=lse, starts=starts, window=4096, sinks=4)
+    attention.dropout(z, x_next, 0.1, seed, step=step, residual=x)               # z: the output layer's
+
+The backward pass takes the same views.  A training step keeps the queries and keys as they went into qk_norm_rope, so it writes them to another place there.
+For serving, attention_step is one new token of each sequence against its cache.  Conventions are those of `layers`: unit stride along the last dimension, any
+strides along the others, outputs are the caller's tensors, work is enqueued on `stream` (None: torch's current stream), a workspace comes from torch's allocator
+or is the caller's.  What the library refuses raises `psgd.PsgdError`, a tensor that is not what a call takes raises ValueError.
+"""
+import ctypes
+
+from . import layers, psgd
+from .layers import I32, View, _shape, _vector, _view, _workspace
+
+PAIRS = {"halves": 0, "neighbours": 1}
+MAX_HEAD = 256
+
+EXPORTS = ("psgd_qk_norm_rope", "psgd_qk_norm_rope_grad", "psgd_qk_norm_rope_grad_workspace", "psgd_attention", "psgd_attention_grad",
+           "psgd_attention_grad_workspace", "psgd_attention_step", "psgd_attention_step_workspace", "psgd_dropout")
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("learner", ctypes.c_int64), ("sequence", ctypes.c_int64), ("row", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+_lib = None
+
+
+def load():
+    """The library of psgd.load() with these functions' signatures declared."""
+    global _lib
+    lib = psgd.load()
+    if _lib is lib:
+        return lib
+    layers.load()
+    view, cache, vp = ctypes.POINTER(View), ctypes.POINTER(Cache), ctypes.c_void_p
+    i32, i64, u64, f32, f64, size = ctypes.c_int, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float, ctypes.c_double, ctypes.c_size_t
+    turned, masked, tokens, work = [i32] * 5 + [f64, f32], [i32] * 5, [i32, i64], [vp, size]
+    signatures = {
+        "psgd_qk_norm_rope": (i32, [view] * 7 + turned + tokens + [vp]),
+        "psgd_qk_norm_rope_grad": (i32, [view] * 11 + turned + tokens + work + [vp]),
+        "psgd_qk_norm_rope_grad_workspace": (size, tokens + [i32]),
+        "psgd_attention": (i32, [view] * 5 + [vp] + masked + [f32, i32] + tokens + [vp]),
+        "psgd_attention_grad": (i32, [view] * 5 + [vp] + [view] * 4 + masked + [f32, i32] + tokens + work + [vp]),
+        "psgd_attention_grad_workspace": (size, masked + [i32] + tokens),
+        "psgd_attention_step": (i32, [view] * 3 + [cache] * 2 + [view] * 2 + masked + [f32] + tokens + [i64] + work + [vp]),
+        "psgd_attention_step_workspace": (size, masked + tokens + [i64]),
+        "psgd_dropout": (i32, [view] * 3 + [f32, u64, u64, vp] + tokens + [i64, vp]),
+    }
+    for name, (res, args) in signatures.items():
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
+    _lib = lib
+    return lib
+
+
+def _head(what, t, heads):
+    """(n, t, a head's columns) of an [n, t, heads * head] tensor."""
+    n, rows, c = _shape(what, t, 3)
+    if heads < 1 or c % heads:
+        raise ValueError("%s: %d columns are not those of %d heads" % (what, c, heads))
+    return n, rows, c // heads
+
+
+def _numbers(what, t, shape):
+    """An int32 tensor of two dimensions, any strides along both."""
+    if t is None:
+        return None
+    import torch
+    if _shape(what, t, 2) != shape or t.dtype != torch.int32:
+        raise ValueError("%s must be int32 of shape %s" % (what, list(shape)))
+    return View(t.data_ptr(), t.stride(0) if shape[0] > 1 else 0, t.stride(1) if shape[1] > 1 else 0, I32)
+
+
+def _starts(t, n):
+    """(view, number of sequences) of int32 [n, sequences + 1]."""
+    if t is None:
+        return None, 0
+    import torch
+    shape = _shape("starts", t, 2)
+    if shape[0] != n or shape[1] < 2 or t.dtype != torch.int32:
+        raise ValueError("starts must be int32 of shape [%d, sequences + 1]" % n)
+    return _view("starts", t, shape), shape[1] - 1
+
+
+def _pairs(pairs):
+    if pairs not in PAIRS:
+        raise ValueError("pairs must be one of %s" % ", ".join(PAIRS))
+    return PAIRS[pairs]
+
+
+def qk_norm_rope(q, k, q_out, k_out, heads, kv, positions=None, q_gain=None, k_gain=None, eps=1e-6, rotary=None, base=10000.0, pairs="halves", stream=None):
+    """Enqueue the norm of every head of q [n, t, heads * head] and k [n, t, kv * head] (RMS, gains [n, head]; without gains none) and the rotation of the first
+    `rotary` columns of each (None: all) by positions [n, t] int32 (None: the row's number).  q_out may be q, k_out may be k."""
+    n, t, head = _head("q", q, heads)
+    vq, vk = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head))
+    vqo, vko = _view("q_out", q_out, (n, t, heads * head)), _view("k_out", k_out, (n, t, kv * head))
+    vp, vgq, vgk = _numbers("positions", positions, (n, t)), _view("q_gain", q_gain, (n, head)), _view("k_gain", k_gain, (n, head))
+    psgd._on_current_device(q, k, positions, q_gain, k_gain, q_out, k_out)
+    psgd._check(load().psgd_qk_norm_rope(vq, vk, vp, vgq, vgk, vqo, vko, heads, kv, head, head if rotary is None else rotary, _pairs(pairs), float(base), float(eps),
+                                         n, t, psgd._stream_handle(stream)))
+
+
+def qk_norm_rope_grad_workspace(n, t, head):
+    return load().psgd_qk_norm_rope_grad_workspace(n, t, head)
+
+
+def qk_norm_rope_grad(dq_out, dk_out, q, k, dq, dk, heads, kv, positions=None, q_gain=None, k_gain=None, dq_gain=None, dk_gain=None, eps=1e-6, rotary=None,
+                      base=10000.0, pairs="halves", workspace=None, stream=None):
+    """Enqueue the backward pass of qk_norm_rope: dq, dk and the gains' gradients ([n, head], float32 or bfloat16 alike) from those of q_out and k_out and
+    what went in.  dq may be dq_out, dk may be dk_out.  Without gains q and k may be None."""
+    n, t, head = _head("dq_out", dq_out, heads)
+    vdqo, vdko = _view("dq_out", dq_out, (n, t, heads * head)), _view("dk_out", dk_out, (n, t, kv * head))
+    vq, vk = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head))
+    vdq, vdk = _view("dq", dq, (n, t, heads * head)), _view("dk", dk, (n, t, kv * head))
+    vp, vgq, vgk = _numbers("positions", positions, (n, t)), _view("q_gain", q_gain, (n, head)), _view("k_gain", k_gain, (n, head))
+    vdgq, vdgk = _view("dq_gain", dq_gain, (n, head)), _view("dk_gain", dk_gain, (n, head))
+    if q_gain is None and (dq_gain is not None or dk_gain is not None):
+        raise ValueError("dq_gain and dk_gain are of q_gain and k_gain")
+    psgd._on_current_device(dq_out, dk_out, q, k, positions, q_gain, k_gain, dq, dk, dq_gain, dk_gain)
+    lib = load()
+    need = lib.psgd_qk_norm_rope_grad_workspace(n, t, head) if vdgq or vdgk else 0
+    room, pw, bw = _workspace(workspace, need, stream)
+    psgd._check(lib.psgd_qk_norm_rope_grad(vdqo, vdko, vq, vk, vp, vgq, vgk, vdq, vdk, vdgq, vdgk, heads, kv, head, head if rotary is None else rotary, _pairs(pairs),
+                                           float(base), float(eps), n, t, pw, bw, psgd._stream_handle(stream)))
+
+
+def attention(q, k, v, out, heads, kv, lse=None, starts=None, window=0, sinks=0, scale=None, stream=None):
+    """Enqueue causal attention of q [n, t, heads * head] over k and v [n, t, kv * head] into out, and where `lse` ([n, heads, t] float32) is given the logarithm of
+    each row's sum.  starts int32 [n, sequences + 1]: where the sequences begin and the last one ends (None: one of all rows).  window > 0: a row
+    sees the last `window` rows up to itself and the first `sinks` of its sequence.  scale None: head ** -0.5."""
+    n, t, head = _head("q", q, heads)
+    vq, vk, vv = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head)), _view("v", v, (n, t, kv * head))
+    vo, (vs, sequences) = _view("out", out, (n, t, heads * head)), _starts(starts, n)
+    import torch
+    pl = _vector("lse", lse, n * heads * t, torch.float32)
+    psgd._on_current_device(q, k, v, starts, out, lse)
+    psgd._check(load().psgd_attention(vq, vk, vv, vs, vo, pl, heads, kv, head, window, sinks, head ** -0.5 if scale is None else float(scale), sequences, n, t,
+                                      psgd._stream_handle(stream)))
+
+
+def attention_grad_workspace(heads, kv, head, n, t, window=0, sinks=0, sequences=0):
+    return load().psgd_attention_grad_workspace(heads, kv, head, window, sinks, sequences, n, t)
+
+
+def attention_grad(dout, q, k, v, out, lse, dq, dk, dv, heads, kv, starts=None, window=0, sinks=0, scale=None, workspace=None, stream=None):
+    """Enqueue the backward pass of attention: dq, dk and dv from dout and what attention took and wrote (out and lse)."""
+    n, t, head = _head("q", q, heads)
+    vd, vq, vk, vv = _view("dout", dout, (n, t, heads * head)), _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head)), _view("v", v, (n, t, kv * head))
+    vo, (vs, sequences) = _view("out", out, (n, t, heads * head)), _starts(starts, n)
+    vdq, vdk, vdv = _view("dq", dq, (n, t, heads * head)), _view("dk", dk, (n, t, kv * head)), _view("dv", dv, (n, t, kv * head))
+    import torch
+    pl = _vector("lse", lse, n * heads * t, torch.float32)
+    psgd._on_current_device(dout, q, k, v, out, lse, starts, dq, dk, dv)
+    lib = load()
+    room, pw, bw = _workspace(workspace, lib.psgd_attention_grad_workspace(heads, kv, head, window, sinks, sequences, n, t), stream)
+    psgd._check(lib.psgd_attention_grad(vd, vq, vk, vv, vo, pl, vs, vdq, vdk, vdv, heads, kv, head, window, sinks, head ** -0.5 if scale is None else float(scale),
+                                        sequences, n, t, pw, bw, psgd._stream_handle(stream)))
+
+
+def _cache(what, t, shape):
+    """A cache [n, b, slots, kv * head] with unit stride along its last dimension."""
+    import torch
+    got = _shape(what, t, 4)
+    if (got[0], got[1], got[3]) != shape or got[2] < 1:
+        raise ValueError("%s must be of shape [%d, %d, slots, %d], not %s" % ((what,) + shape + (list(got),)))
+    kind = {torch.float32: layers.F32, torch.bfloat16: layers.BF16}.get(t.dtype)
+    if kind is None:
+        raise ValueError("%s must be float32 or bfloat16" % what)
+    if got[3] > 1 and t.stride(3) != 1:
+        raise ValueError("%s must have unit stride along its last dimension" % what)
+    return Cache(t.data_ptr(), *(t.stride(d) if got[d] > 1 else 0 for d in range(3)), kind), got[2]
+
+
+def attention_step_workspace(heads, kv, head, n, b, slots, window=0, sinks=0):
+    return load().psgd_attention_step_workspace(heads, kv, head, window, sinks, n, b, slots)
+
+
+def attention_step(q, k, v, cache_k, cache_v, lengths, out, heads, kv, window=0, sinks=0, scale=None, workspace=None, stream=None):
+    """Enqueue attention of one new token of each of b sequences of each learner (q [n, b, heads * head], k and v [n, b, kv * head]) over the caches
+    [n, b, slots, kv * head], which take its key and value, into out [n, b, heads * head].  lengths int32 [n, b]: the tokens that each cache has seen, the new
+    token's position (negative: no such sequence).  With a window and slots >= sinks + window the caches are rings.  lengths stay as they are."""
+    n, b, head = _head("q", q, heads)
+    vq, vk, vv = _view("q", q, (n, b, heads * head)), _view("k", k, (n, b, kv * head)), _view("v", v, (n, b, kv * head))
+    vo, vl = _view("out", out, (n, b, heads * head)), _numbers("lengths", lengths, (n, b))
+    (vck, slots), (vcv, slots_v) = _cache("cache_k", cache_k, (n, b, kv * head)), _cache("cache_v", cache_v, (n, b, kv * head))
+    if slots != slots_v:
+        raise ValueError("cache_k and cache_v must have as many slots")
+    psgd._on_current_device(q, k, v, cache_k, cache_v, lengths, out)
+    lib = load()
+    room, pw, bw = _workspace(workspace, lib.psgd_attention_step_workspace(heads, kv, head, window, sinks, n, b, slots), stream)
+    psgd._check(lib.psgd_attention_step(vq, vk, vv, vck, vcv, vl, vo, heads, kv, head, window, sinks, head ** -0.5 if scale is None else float(scale), n, b, slots,
+                                        pw, bw, psgd._stream_handle(stream)))
+
+
+def dropout(x, y, p, seed, step=0, residual=None, step_dev=None, stream=None):
+    """Enqueue y = x m / P(m = 1) + residual, m = 0 with probability p, from (seed, step) and the element's place in [n, t, c]; x, y and residual of one type, y
+    may be x or residual.  The backward pass is dropout(dy, dx, p, seed, step).  step_dev (device int64 / uint64 tensor, >= 1 element) is added to step."""
+    n, t, c = _shape("x", x, 3)
+    vx, vr, vy = _view("x", x, (n, t, c)), _view("residual", residual, (n, t, c)), _view("y", y, (n, t, c))
+    psgd._on_current_device(x, residual, y, step_dev)
+    sp = None
+    if step_dev is not None:
+        import torch
+        if step_dev.dtype not in (torch.int64, torch.uint64) or step_dev.numel() < 1:
+            raise ValueError("step_dev must be a 64-bit integer device tensor")
+        sp = step_dev.data_ptr()
+    psgd._check(load().psgd_dropout(vx, vr, vy, float(p), seed & (2 ** 64 - 1), step & (2 ** 64 - 1), sp, n, t, c, psgd._stream_handle(stream)))

@@ -1,0 +1,191 @@
+// What the attention kernels share (gfx950): operands of the matrix instructions and the tiles in LDS that they come from.
+//
+// All products are of 16 x 16 blocks, D[m, n] = sum_k A[m, k] B[n, k], 32 of k at a time: lane l holds eight k of row l % 16 of A and as many of row
+// l % 16 of B, and of D the elements m = 4 (l / 16) + 0..3 of column n = l % 16.  bf16 takes one instruction for 32 of k, float eight.  Which of the 32 a
+// lane's eight are does not matter as long as A and B agree, and that is used twice: a float's eight are two groups of 16 bytes next to each other; and a
+// result D of one product is B of the next as it stands, its m being that one's k (two blocks of 16 make 32: slot e < 4 of lane l is k = 4 (l / 16) + e,
+// slot e >= 4 is 16 more), so p = exp(s) never leaves its registers.
+//
+// That product's A is a tile of rows k read across: in bf16 by the transposing LDS read (16 lanes read 4 rows of 16 columns, each lane gets its
+// column's four rows), in float element by element.
+#ifndef PSGD_ATTENTION_CORE_H
+#define PSGD_ATTENTION_CORE_H
+
+#include "psgd_attention.h"
+#include "psgd_attention_plan.h"
+#include "psgd_rows.h"
+
+namespace psgd {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+
+// Eight values of one row.
+template <typename T> struct Eight;
+template <> struct Eight<uint16_t> {
+    u32x4 v;
+};
+template <> struct Eight<float> {
+    float v[8];
+};
+
+__device__ __forceinline__ f32x4 mma(const Eight<uint16_t>& a, const Eight<uint16_t>& b, f32x4 d) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.v), __builtin_bit_cast(bf16x8, b.v), d, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma(const Eight<float>& a, const Eight<float>& b, f32x4 d) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) d = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], d, 0, 0, 0);
+    return d;
+}
+
+template <typename T> __device__ __forceinline__ Eight<T> no_values() {
+    Eight<T> r;
+    if constexpr (sizeof(T) == 2) {
+        r.v = (u32x4){0, 0, 0, 0};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = 0.0f;
+    }
+    return r;
+}
+// Two blocks of a result as the operand of the next product.
+template <typename T> __device__ __forceinline__ Eight<T> as_operand(f32x4 low, f32x4 high) {
+    Eight<T> r;
+    if constexpr (sizeof(T) == 2) {
+        r.v = (u32x4){two_bf16(low[0], low[1]), two_bf16(low[2], low[3]), two_bf16(high[0], high[1]), two_bf16(high[2], high[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            r.v[e] = low[e];
+            r.v[4 + e] = high[e];
+        }
+    }
+    return r;
+}
+__device__ __forceinline__ float dot(const Eight<uint16_t>& a, const Eight<uint16_t>& b) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_fmaf(low_bf16(a.v[i]), low_bf16(b.v[i]), __builtin_fmaf(high_bf16(a.v[i]), high_bf16(b.v[i]), s));
+    return s;
+}
+__device__ __forceinline__ float dot(const Eight<float>& a, const Eight<float>& b) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(a.v[i], b.v[i], s);
+    return s;
+}
+
+// 16 bytes of a row of `left` elements more; `whole`: rows are a whole number of them.  Nothing is read where left <= 0.
+template <typename T> __device__ __forceinline__ u32x4 load_group(const T* p, int left, bool whole) {
+    if (whole) {
+        u32x4 r = {0, 0, 0, 0};
+        if (left > 0) r = load_raw(p);
+        return r;
+    }
+    return load_cols(p, left);
+}
+// The values of k block kc (columns 32 kc ...) that lane group g holds, of a row of `left` elements (0: none) in memory.
+template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T* row, int kc, int g, int left, bool whole) {
+    const int col = 32 * kc + 8 * g;
+    Eight<T> r;
+    if constexpr (sizeof(T) == 2) {
+        r.v = load_group(row + col, left - col, whole);
+    } else {
+        const u32x4 a = load_group(row + col, left - col, whole), b = load_group(row + col + 4, left - col - 4, whole);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            r.v[e] = __uint_as_float(a[e]);
+            r.v[4 + e] = __uint_as_float(b[e]);
+        }
+    }
+    return r;
+}
+
+// A tile of ROWS rows of H columns in LDS.  Its 16-byte groups are permuted within a row by the row's number, so that 16 rows' groups of one column,
+// and eight rows' pairs of groups next to each other (what the transposing read takes at a time), lie in different banks.
+template <typename T, int H, int ROWS> struct Tile {
+    static constexpr int kGroups = H * (int)sizeof(T) / 16;          // of a row
+    static constexpr int kBytes = ROWS * kGroups * 16;
+    static __device__ __forceinline__ int turn(int row) {
+        return kGroups == 8 ? (row >> 1 & 3) << 1 | (row >> 3 & 1) : (row & 7) << 1 | (row >> 3 & 1);
+    }
+    static __device__ __forceinline__ int place(int row, int group) { return (row * kGroups + (group ^ turn(row))) * 16; }
+
+    static __device__ __forceinline__ void put(char* tile, int row, int group, u32x4 v) { *reinterpret_cast<u32x4*>(tile + place(row, group)) = v; }
+
+    // A of rows 16 block ..., columns 32 kc ...
+    static __device__ __forceinline__ Eight<T> along(const char* tile, int block, int kc, int lane) {
+        const int row = 16 * block + lane % 16, g = lane / 16;
+        Eight<T> r;
+        if constexpr (sizeof(T) == 2) {
+            r.v = *reinterpret_cast<const u32x4*>(tile + place(row, 4 * kc + g));
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(tile + place(row, 8 * kc + 2 * g)), b = *reinterpret_cast<const f32x4*>(tile + place(row, 8 * kc + 2 * g + 1));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                r.v[e] = a[e];
+                r.v[4 + e] = b[e];
+            }
+        }
+        return r;
+    }
+    // A of columns 16 block ... of the tile, its rows 32 kc ... in the order of as_operand's.
+    static __device__ __forceinline__ Eight<T> across(const char* tile, int block, int kc, int lane) {
+        Eight<T> r;
+        if constexpr (sizeof(T) == 2) {
+            const int row = 32 * kc + 4 * (lane / 16) + lane % 16 / 4, group = 2 * block + (lane % 4) / 2;
+            typedef __attribute__((address_space(3))) i16x4* lds;
+            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + place(row, group) + lane % 2 * 8));
+            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + place(row + 16, group) + lane % 2 * 8));
+            const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+            r.v = (u32x4){x[0], x[1], y[0], y[1]};
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                r.v[e] = *reinterpret_cast<const float*>(tile + place(32 * kc + e / 4 * 16 + 4 * (lane / 16) + e % 4, 4 * block + lane % 16 / 4) + lane % 4 * 4);
+        }
+        return r;
+    }
+};
+
+// The four lanes that hold parts of one column of a result, together.
+template <typename OP> __device__ __forceinline__ float column_all(float v) {
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = OP::of(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return OP::of(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+struct Larger {      // the other one where one is NaN: sums carry it on
+    static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
+};
+
+// Four columns next to each other, from `col` on, of a row of `head`.
+template <typename T> __device__ __forceinline__ void store_four(T* row, int col, int head, f32x4 v) {
+    if (col + 4 <= head) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any*>(row + col) = (u32x2){two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+        else *reinterpret_cast<u32x4_any*>(row + col) = __builtin_bit_cast(u32x4, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < head) store_1(row + col + e, v[e]);
+    }
+}
+
+__device__ __forceinline__ float exp_2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct HeadsView {      // [n, t, heads * head] in the kernels
+    char* p;
+    int64_t learner, row;      // in elements
+};
+inline HeadsView heads_view(const psgd_view* v) { return {static_cast<char*>(v->data), v->learner, v->row}; }
+template <typename T> __device__ __forceinline__ T* at(const HeadsView& a, int64_t i, int64_t r, int64_t col) {
+    return reinterpret_cast<T*>(a.p) + i * a.learner + r * a.row + col;
+}
+
+}  // namespace
+}  // namespace psgd
+#endif

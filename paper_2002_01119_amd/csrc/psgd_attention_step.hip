@@ -1,0 +1,386 @@
+// Attention of one new token of each sequence against its cache, which takes the token's key and value (gfx950).
+//
+// What counts is that the cache is read once: 2 kv head values a position against 4 heads head operations.  A workgroup has one key head of one sequence
+// and a part of its positions; its four wavefronts take 32 positions each in turn and meet only at the end.  The query heads that share the key head
+// are the columns of the matrix products, 16 at most at a time.  Keys come from memory as the first product's operand; values go through the wavefront's own
+// tile in LDS, to be read across.  Where a sequence is cut into parts, each leaves its maximum, sum and output and a second kernel joins them in order.
+//
+// The new key and value are taken from where they come from, not from the cache, which one workgroup of the last part writes: nobody waits for it, and what the
+// slot held before is a position that the window has left.
+#include "psgd_attention_core.h"
+
+#include <algorithm>
+
+namespace psgd {
+namespace {
+
+__device__ int g_step_status = 0;
+constexpr int kStepFlag = 2;            // bit 1 of psgd_device_status()
+
+struct CacheView {
+    char* p;
+    int64_t learner, sequence, row;
+};
+struct StepArgs {
+    HeadsView q, k, v, o;                // [n, b, ...]
+    CacheView ck, cv;
+    const int32_t* lengths;
+    int64_t lengths_learner, lengths_row, b, first;
+    float *part_o, *part_ml;             // [n b heads][parts][head], [n b heads][parts][2]
+    int heads, kv, head, window, sinks, slots, blocks, parts, most;      // blocks: of 16 query heads of a key head; most: the longest that a cache takes
+    float scale;
+};
+
+// The positions that the new token sees, numbered from 0: first tokens, then from the window on to itself.
+struct Seen {
+    int sinks, from, count, at, ring, base;
+    __device__ __forceinline__ Seen(const StepArgs& a, int p) {
+        at = p;
+        from = a.window ? std::max(0, p - a.window + 1) : 0;
+        sinks = std::min(a.sinks, from);
+        count = sinks + p - from + 1;
+        ring = std::max(1, a.slots - a.sinks);
+        base = from >= a.sinks ? (from - a.sinks) % ring - from + a.sinks : 0;       // slot of `from`, less `from`
+        first = a.sinks;
+    }
+    int first;
+    __device__ __forceinline__ int position(int u) const { return u < sinks ? u : from + u - sinks; }
+    __device__ __forceinline__ int slot(int position) const {
+        if (position < first) return position;
+        if (from < first) {                             // the window begins in front of the first slot of the ring: it has not turned beyond it
+            return first + (position - first) % ring;
+        }
+        const int s = position + base;
+        return s >= first + ring ? s - ring : s;
+    }
+};
+
+template <typename T, int H> struct StepShape {
+    static constexpr int kSteps = H / 32, kCols = H / 16;
+    using Lds = Tile<T, H, kStepKeys>;
+    static constexpr int kMoves = kStepKeys * Lds::kGroups / kWave;      // 16-byte groups of a tile of values that a lane moves
+    static constexpr size_t kTiles = (size_t)kStepWaves * Lds::kBytes, kJoin = (size_t)kStepWaves * 16 * (H + 2) * sizeof(float);
+    static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
+};
+
+template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) void step_kernel(StepArgs a) {
+    using S = StepShape<T, H>;
+    using Lds = typename S::Lds;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int64_t id = a.first + blockIdx.x, unit = id / a.parts;
+    const int part = (int)(id % a.parts), block = (int)(unit % a.blocks), kv = (int)(unit / a.blocks % a.kv);
+    const int64_t pair = unit / a.blocks / a.kv, i = pair / a.b, r = pair % a.b;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane % 16, g = lane / 16;
+    const int members = a.heads / a.kv, member = 16 * block + col, h = kv * members + member;
+    const bool whole = a.head % kPer<T> == 0;
+    const int length = a.lengths[i * a.lengths_learner + r * a.lengths_row];
+    if (length < 0) return;
+    T* const out = at<T>(a.o, i, r, (int64_t)h * a.head);
+    if (length >= a.most) {
+        if (part == 0 && wave == 0) {
+            if (lane == 0) atomicOr(&g_step_status, kStepFlag);
+            if (member < members)
+                for (int c = g; c < a.head; c += 4) store_1(out + c, NAN);
+        }
+        return;
+    }
+    const Seen seen(a, length);
+    const int each = (seen.count + a.parts - 1) / a.parts, u0 = std::min(part * each, seen.count), u1 = std::min(u0 + each, seen.count);
+    const T *nk = at<T>(a.k, i, r, (int64_t)kv * a.head), *nv = at<T>(a.v, i, r, (int64_t)kv * a.head);
+    T* const ck = reinterpret_cast<T*>(a.ck.p) + i * a.ck.learner + r * a.ck.sequence + (int64_t)kv * a.head;
+    T* const cv = reinterpret_cast<T*>(a.cv.p) + i * a.cv.learner + r * a.cv.sequence + (int64_t)kv * a.head;
+    if (block == 0 && part == a.parts - 1) {
+        const int64_t slot = seen.slot(length);
+        for (int c = threadIdx.x; c < a.head; c += kStepWaves * kWave) {
+            ck[slot * a.ck.row + c] = nk[c];
+            cv[slot * a.cv.row + c] = nv[c];
+        }
+    }
+    auto key_row = [&](int u) { const int p = seen.position(u); return p == length ? nk : ck + (int64_t)seen.slot(p) * a.ck.row; };
+    auto value_row = [&](int u) { const int p = seen.position(u); return p == length ? nv : cv + (int64_t)seen.slot(p) * a.cv.row; };
+
+    Eight<T> q[S::kSteps];
+    f32x4 o[S::kCols];
+    const T* const pq = at<T>(a.q, i, r, (int64_t)h * a.head);
+#pragma unroll
+    for (int kc = 0; kc < S::kSteps; ++kc) q[kc] = load_eight(pq, kc, g, member < members ? a.head : 0, whole);
+#pragma unroll
+    for (int c = 0; c < S::kCols; ++c) o[c] = (f32x4){0, 0, 0, 0};
+    float top = -INFINITY, sum = 0.0f;
+    const float to_log2 = a.scale * kLog2E;
+    char* const tile = lds + wave * Lds::kBytes;
+
+    for (int u = u0 + wave * kStepKeys; u < u1; u += kStepWaves * kStepKeys) {
+        Eight<T> k[2][S::kSteps];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int at = u + 16 * kb + col;
+            const T* row = at < u1 ? key_row(at) : nk;
+#pragma unroll
+            for (int kc = 0; kc < S::kSteps; ++kc) k[kb][kc] = load_eight(row, kc, g, at < u1 ? a.head : 0, whole);
+        }
+        u32x4 v[S::kMoves];
+#pragma unroll
+        for (int j = 0; j < S::kMoves; ++j) {
+            const int at = u + (lane + 64 * j) / Lds::kGroups, c = (lane + 64 * j) % Lds::kGroups * kPer<T>;
+            v[j] = load_group((at < u1 ? value_row(at) : nv) + c, at < u1 ? a.head - c : 0, whole);
+        }
+        f32x4 s[2];
+        float m = -INFINITY;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            s[kb] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int kc = 0; kc < S::kSteps; ++kc) s[kb] = mma(k[kb][kc], q[kc], s[kb]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[kb][e] = u + 16 * kb + 4 * g + e < u1 ? s[kb][e] * to_log2 : -INFINITY;
+                m = fmaxf(m, s[kb][e]);
+            }
+        }
+        m = fmaxf(top, column_all<Larger>(m));
+        const float safe = m == -INFINITY ? 0.0f : m, less = exp_2(top - safe);
+        top = m;
+        sum *= less;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[kb][e] = exp_2(s[kb][e] - safe);
+                sum += s[kb][e];
+            }
+        const Eight<T> p = as_operand<T>(s[0], s[1]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // the tile before this one has been read
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < S::kMoves; ++j) Lds::put(tile, (lane + 64 * j) / Lds::kGroups, (lane + 64 * j) % Lds::kGroups, v[j]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) o[c] = mma(Lds::across(tile, c, 0, lane), p, o[c] * less);
+    }
+    sum = column_all<Sum>(sum);
+    // the wavefronts' parts, in order: [wave][16 heads][H], then maxima and sums
+    __syncthreads();
+    float *const all = reinterpret_cast<float*>(lds), *const ml = all + kStepWaves * 16 * H;
+#pragma unroll
+    for (int c = 0; c < S::kCols; ++c) *reinterpret_cast<f32x4*>(all + ((wave * 16 + col) * H + 16 * c + 4 * g)) = o[c];
+    if (g == 0) {
+        ml[(wave * 16 + col) * 2] = top;
+        ml[(wave * 16 + col) * 2 + 1] = sum;
+    }
+    __syncthreads();
+    const int here = std::min(16, members - 16 * block);
+    for (int e = threadIdx.x; e < here * H; e += kStepWaves * kWave) {
+        const int m = e / H, c = e % H;
+        float most = ml[m * 2];
+#pragma unroll
+        for (int w = 1; w < kStepWaves; ++w) most = fmaxf(most, ml[(w * 16 + m) * 2]);
+        const float safe = most == -INFINITY ? 0.0f : most;
+        float total = 0.0f, value = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kStepWaves; ++w) {
+            const float less = exp_2(ml[(w * 16 + m) * 2] - safe);
+            total += less * ml[(w * 16 + m) * 2 + 1];
+            value += less * all[(w * 16 + m) * H + c];
+        }
+        const int head = kv * members + 16 * block + m;
+        if (a.parts == 1) {
+            if (c < a.head) store_1(at<T>(a.o, i, r, (int64_t)head * a.head) + c, value / total);
+        } else {
+            const int64_t at = ((i * a.b + r) * a.heads + head) * a.parts + part;
+            if (c < a.head) a.part_o[at * a.head + c] = value;
+            if (c == 0) {
+                a.part_ml[at * 2] = most;
+                a.part_ml[at * 2 + 1] = total;
+            }
+        }
+    }
+}
+
+// Joins a head's parts, in order: one workgroup a head of a sequence.
+template <typename T> __global__ __launch_bounds__(256) void step_join_kernel(StepArgs a) {
+    const int64_t id = a.first + blockIdx.x, pair = id / a.heads, i = pair / a.b, r = pair % a.b;
+    const int h = (int)(id % a.heads);
+    const int length = a.lengths[i * a.lengths_learner + r * a.lengths_row];
+    if (length < 0 || length >= a.most) return;
+    const float *ml = a.part_ml + id * a.parts * 2, *o = a.part_o + id * a.parts * a.head;
+    float most = -INFINITY;
+    for (int s = 0; s < a.parts; ++s) most = fmaxf(most, ml[2 * s]);
+    const float safe = most == -INFINITY ? 0.0f : most;
+    float total = 0.0f, value = 0.0f;
+    const int c = threadIdx.x;
+    for (int s = 0; s < a.parts; ++s) {
+        const float less = exp_2(ml[2 * s] - safe);
+        total += less * ml[2 * s + 1];
+        if (c < a.head) value += less * o[(int64_t)s * a.head + c];
+    }
+    if (c < a.head) store_1(at<T>(a.o, i, r, (int64_t)h * a.head) + c, value / total);
+}
+
+using StepKernel = void (*)(StepArgs);
+template <typename T, int H> int launch_step(const char* name, StepArgs a, int64_t units, int64_t rows, hipStream_t s) {
+    static LdsRecord record = {};
+    const StepKernel fn = step_kernel<T, H>, join = step_join_kernel<T>;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(fn), StepShape<T, H>::kLds, record)) return rc;
+    in_slices(units * a.parts, [&](int64_t first, unsigned groups) {
+        a.first = first;
+        hipLaunchKernelGGL(fn, dim3(groups), dim3(kStepWaves * kWave), (StepShape<T, H>::kLds), s, a);
+    });
+    if (a.parts > 1)
+        in_slices(rows, [&](int64_t first, unsigned groups) {
+            a.first = first;
+            hipLaunchKernelGGL(join, dim3(groups), dim3(256), 0, s, a);
+        });
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+template <typename T> int step_of(const char* name, const StepArgs& a, int64_t units, int64_t rows, hipStream_t s) {
+    switch (held_head(a.head)) {
+        case 64: return launch_step<T, 64>(name, a, units, rows, s);
+        case 128: return launch_step<T, 128>(name, a, units, rows, s);
+        default: return launch_step<T, 256>(name, a, units, rows, s);
+    }
+}
+
+inline int64_t most_seen(int window, int sinks, int64_t slots) { return window && (int64_t)window + sinks < slots ? (int64_t)window + sinks : slots; }
+
+// A cache as an output: no two of its rows share an address.
+inline int check_cache(const char* name, const char* what, const psgd_cache& c, int n, int64_t b, int64_t slots, int64_t width) {
+    if (!c.data) return fail(PSGD_EINVAL, "%s: %s is a null pointer", name, what);
+    if (reinterpret_cast<uintptr_t>(c.data) % elem_bytes(c.type)) return fail(PSGD_EALIGN, "%s: %s is not aligned to its element size", name, what);
+    if (c.learner < 0 || c.sequence < 0 || c.row < 0) return fail(PSGD_EINVAL, "%s: a stride of %s is negative", name, what);
+    if (c.learner > kMostElements / n || c.sequence > kMostElements / b || c.row > kMostElements / slots) return fail(PSGD_EINVAL, "%s: %s is too large", name, what);
+    // the three counts by stride: each has to step over what those of smaller strides cover
+    struct {
+        int64_t stride, count;
+    } d[3] = {{c.learner, n}, {c.sequence, b}, {c.row, slots}};
+    std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    int64_t covered = width;
+    for (const auto& x : d) {
+        if (x.count == 1) continue;
+        if (x.stride < covered) return fail(PSGD_EALIAS, "%s: rows of %s overlap", name, what);
+        covered += (x.count - 1) * x.stride;
+    }
+    return PSGD_OK;
+}
+// Whether the caches share a byte: unless their rows, sequences or learners are as far apart and interleave.
+inline bool caches_meet(const psgd_cache& a, const psgd_cache& b, int n, int64_t s, int64_t slots, int64_t width) {
+    const int64_t unit = elem_bytes(a.type), span = ((n - 1) * a.learner + (s - 1) * a.sequence + (slots - 1) * a.row + width) * unit;
+    const int64_t span_b = ((n - 1) * b.learner + (s - 1) * b.sequence + (slots - 1) * b.row + width) * unit;
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.data), y = reinterpret_cast<uintptr_t>(b.data);
+    if (x + span <= y || y + span_b <= x) return false;
+    if (a.learner != b.learner || a.sequence != b.sequence || a.row != b.row) return true;
+    const int64_t in_sequence = ((slots - 1) * a.row + width) * unit, in_learner = in_sequence + (s - 1) * a.sequence * unit;
+    if (n > 1 && !combs_meet(x, in_learner, y, in_learner, a.learner * unit)) return false;
+    if (s > 1 && (n == 1 || a.learner % a.sequence == 0) && !combs_meet(x, in_sequence, y, in_sequence, a.sequence * unit)) return false;
+    return slots == 1 || (s > 1 && a.sequence % a.row) || (n > 1 && a.learner % a.row) || combs_meet(x, width * unit, y, width * unit, a.row * unit);
+}
+// Its bytes from the first to behind the last, as one operand.
+inline Extent cache_extent(const char* what, const psgd_cache& c, int n, int64_t b, int64_t slots, int64_t width, psgd_view* room) {
+    return flat(what, c.data, (n - 1) * c.learner + (b - 1) * c.sequence + (slots - 1) * c.row + width, room, c.type);
+}
+
+inline int check_step(const char* name, int heads, int kv, int head, int window, int sinks, int n, int64_t b, int64_t slots) {
+    if (heads < 1 || kv < 1 || heads % kv) return fail(PSGD_EINVAL, "%s: kv=%d does not divide heads=%d", name, kv, heads);
+    if (head < 1 || head > PSGD_MAX_HEAD) return fail(PSGD_EINVAL, "%s: head=%d outside 1..%d", name, head, (int)PSGD_MAX_HEAD);
+    if (int rc = check_counts(name, n, b, (int64_t)heads * head)) return rc;
+    if (window < 0 || sinks < 0 || (sinks && !window)) return fail(PSGD_EINVAL, "%s: window=%d with sinks=%d", name, window, sinks);
+    if (slots < 1 || slots > 1 << 30) return fail(PSGD_EINVAL, "%s: slots=%lld outside 1..2^30", name, (long long)slots);
+    if ((int64_t)n * b > INT32_MAX || (int64_t)n * b * heads > INT32_MAX) return fail(PSGD_EINVAL, "%s: n * b * heads beyond 2^31 - 1", name);
+    return PSGD_OK;
+}
+
+}  // namespace
+
+int attention_step_status(int clear, int* word) {
+    hipError_t e = hipMemcpyFromSymbol(word, HIP_SYMBOL(g_step_status), sizeof(int));
+    if (e != hipSuccess) return hip_error(e, "hipMemcpyFromSymbol");
+    if (clear && *word) {
+        const int zero = 0;
+        e = hipMemcpyToSymbol(HIP_SYMBOL(g_step_status), &zero, sizeof(int));
+        if (e != hipSuccess) return hip_error(e, "hipMemcpyToSymbol");
+    }
+    return PSGD_OK;
+}
+
+}  // namespace psgd
+
+extern "C" {
+
+size_t psgd_attention_step_workspace(int heads, int kv, int head, int window, int sinks, int n, int64_t b, int64_t slots) {
+    using namespace psgd;
+    clear_error();
+    int cus = 0;
+    if (b < 1 || check_step("psgd_attention_step_workspace", heads, kv, head, window, sinks, n, b, slots) || compute_units(&cus)) return 0;
+    const int parts = step_parts((int64_t)n * b * kv * parts_of(heads / kv, 16), most_seen(window, sinks, slots), cus);
+    return parts > 1 ? up256((size_t)n * b * heads * parts * (head + 2) * sizeof(float)) : 0;
+}
+
+int psgd_attention_step(const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_cache* cache_k, const psgd_cache* cache_v,
+                        const psgd_view* lengths, const psgd_view* out, int heads, int kv, int head, int window, int sinks, float scale, int n,
+                        int64_t b, int64_t slots, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_attention_step";
+    clear_error();
+    if (!q || !k || !v || !cache_k || !cache_v || !lengths || !out) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (int rc = check_step(name, heads, kv, head, window, sinks, n, b, slots)) return rc;
+    if (!std::isfinite(scale)) return fail(PSGD_EINVAL, "%s: scale=%g", name, (double)scale);
+    for (int type : {k->type, v->type, out->type, cache_k->type, cache_v->type})
+        if (!float_type(type) || type != q->type) return fail(PSGD_EINVAL, "%s: q, k, v, out and the caches must be float or bf16 alike", name);
+    if (lengths->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: lengths must be int32", name);
+    if (b == 0) return PSGD_OK;
+    const int64_t cq = (int64_t)heads * head, cw = (int64_t)kv * head;
+    psgd_view vk, vv, vw;
+    const Extent eq{"q", q, n, b, cq}, ek{"k", k, n, b, cw}, ev{"v", v, n, b, cw}, eo{"out", out, n, b, cq}, el{"lengths", lengths, n, b, 1};
+    for (const Extent* e : {&eq, &ek, &ev, &el})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    if (int rc = check_operand(name, eo, true)) return rc;
+    if (int rc = check_cache(name, "cache_k", *cache_k, n, b, slots, cw)) return rc;
+    if (int rc = check_cache(name, "cache_v", *cache_v, n, b, slots, cw)) return rc;
+    const Extent eck = cache_extent("cache_k", *cache_k, n, b, slots, cw, &vk), ecv = cache_extent("cache_v", *cache_v, n, b, slots, cw, &vv);
+    for (const Extent* o : {&eo, &eck, &ecv})
+        for (const Extent* e : {&eq, &ek, &ev, &el})
+            if (int rc = refuse_overlap(name, *o, *e)) return rc;
+    if (caches_meet(*cache_k, *cache_v, n, b, slots, cw)) return fail(PSGD_EALIAS, "%s: cache_k overlaps cache_v", name);
+    for (const Extent* e : {&eck, &ecv})
+        if (int rc = refuse_overlap(name, *e, eo)) return rc;
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    const int blocks = (int)parts_of(heads / kv, 16);
+    const int64_t units = (int64_t)n * b * kv * blocks;
+    const int parts = step_parts(units, most_seen(window, sinks, slots), cus);
+    const size_t rows = (size_t)n * b * heads, need = parts > 1 ? up256(rows * parts * (head + 2) * sizeof(float)) : 0;
+    if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256))
+        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
+    const Extent ew = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&eq, &ek, &ev, &el, &eo, &eck, &ecv})
+        if (int rc = refuse_overlap(name, ew, *e)) return rc;
+    StepArgs a{};
+    a.q = heads_view(q);
+    a.k = heads_view(k);
+    a.v = heads_view(v);
+    a.o = heads_view(out);
+    a.ck = CacheView{static_cast<char*>(cache_k->data), cache_k->learner, cache_k->sequence, cache_k->row};
+    a.cv = CacheView{static_cast<char*>(cache_v->data), cache_v->learner, cache_v->sequence, cache_v->row};
+    a.lengths = static_cast<const int32_t*>(lengths->data);
+    a.lengths_learner = lengths->learner;
+    a.lengths_row = lengths->row;
+    a.b = b;
+    a.heads = heads;
+    a.kv = kv;
+    a.head = head;
+    a.most = window && slots >= (int64_t)window + sinks ? 1 << 30 : (int)slots;
+    a.window = window;
+    a.sinks = sinks;
+    a.slots = (int)slots;
+    a.blocks = blocks;
+    a.parts = parts;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o ? a.part_o + rows * parts * head : nullptr;
+    a.scale = scale;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return q->type == PSGD_F32 ? step_of<float>(name, a, units, (int64_t)rows, s) : step_of<uint16_t>(name, a, units, (int64_t)rows, s);
+}
+
+}  // extern "C"

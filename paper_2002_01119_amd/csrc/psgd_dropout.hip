@@ -1,0 +1,136 @@
+// Dropout from a counter (gfx950): y = x m / P(m = 1) [+ residual], the mask made again wherever it is needed, so nothing of it is stored and the
+// backward pass is the same call.
+//
+// Four columns of a row share one output of SplitMix64, 16 bits each: three 64-bit xors of shifts and two products, 12 instructions at a quarter of the
+// rate and about as many others, which is 15 a column against 4 bytes or more of memory: bound by HBM (16 bits a column, not 32, because those would
+// double the products and make the multipliers the bound in bf16).  A lane takes 16 bytes, four or eight columns, of each array.
+#include "psgd_attention.h"
+#include "psgd_rows.h"
+
+namespace psgd {
+namespace {
+
+// Division of numbers below 2^31 by one divisor: a product and a shift.
+struct Divider {
+    uint32_t by, mul, shift;
+};
+inline Divider divider(uint32_t by) {
+    uint32_t s = 0;
+    while ((1ull << s) < by) ++s;
+    return {by, (uint32_t)(((1ull << (31 + s)) + by - 1) / by), s};
+}
+__device__ __forceinline__ uint32_t divided(uint32_t x, Divider d) { return (uint32_t)((uint64_t)x * d.mul >> (31 + d.shift)); }
+
+struct DropArgs {
+    const char *x, *residual;
+    char* y;
+    int64_t x_learner, x_row, r_learner, r_row, y_learner, y_row;
+    const uint64_t* step_dev;
+    uint64_t seed, step;
+    int64_t c, words, first_row;       // words: of a row; the launch's first row, of n t
+    uint32_t items, keep;
+    Divider groups, tokens;            // 16-byte groups of a row; t
+    float scale;
+};
+
+__device__ __forceinline__ uint64_t split_mix(uint64_t z) {
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
+
+constexpr int kDropThreads = 256;
+
+template <typename T, bool RES> __global__ __launch_bounds__(kDropThreads) void dropout_kernel(DropArgs a) {
+    constexpr int E = kPer<T>;
+    constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
+    const uint64_t step = a.step + (a.step_dev ? *a.step_dev : 0), state = a.seed ^ ((step + 1) * kGolden);
+    const uint32_t stride = gridDim.x * kDropThreads;
+    for (uint32_t item = blockIdx.x * kDropThreads + threadIdx.x; item < a.items; item += stride) {
+        const uint32_t row_here = divided(item, a.groups);
+        const int64_t col = (int64_t)(item - row_here * a.groups.by) * E, left = a.c - col;
+        const int64_t row = a.first_row + row_here;
+        const uint32_t i = divided((uint32_t)row, a.tokens), r = (uint32_t)row - i * a.tokens.by;
+        float v[E], w[E];
+        widen<T>(load_cols(reinterpret_cast<const T*>(a.x) + i * a.x_learner + r * a.x_row + col, left), v);
+        if (RES) widen<T>(load_cols(reinterpret_cast<const T*>(a.residual) + i * a.r_learner + r * a.r_row + col, left), w);
+        const uint64_t word = (uint64_t)(row * a.words + (col >> 2) + 1);
+#pragma unroll
+        for (int k = 0; k < E; k += 4) {
+            const uint64_t z = split_mix(state + (word + k / 4) * kGolden);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool kept = (uint32_t)(z >> (16 * e) & 0xFFFF) < a.keep;
+                const float u = kept ? v[k + e] * a.scale : 0.0f;
+                v[k + e] = RES ? u + w[k + e] : u;
+            }
+        }
+        store_cols<T>(reinterpret_cast<T*>(a.y) + i * a.y_learner + r * a.y_row + col, v, left);
+    }
+}
+
+}  // namespace
+}  // namespace psgd
+
+extern "C" int psgd_dropout(const psgd_view* x, const psgd_view* residual, const psgd_view* y, float p, uint64_t seed, uint64_t step,
+                            const uint64_t* step_dev, int n, int64_t t, int64_t c, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_dropout";
+    clear_error();
+    if (!x || !y) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (int rc = check_counts(name, n, t, c)) return rc;
+    if ((int64_t)n * t > INT32_MAX) return fail(PSGD_EINVAL, "%s: n * t beyond 2^31 - 1", name);
+    if (!float_type(x->type) || y->type != x->type || (residual && residual->type != x->type))
+        return fail(PSGD_EINVAL, "%s: x, y and residual must be float or bf16 alike", name);
+    if (!(p >= 0.0f && p <= 1.0f)) return fail(PSGD_EINVAL, "%s: p=%g is not in 0..1", name, (double)p);
+    if (t == 0 || c == 0) return PSGD_OK;
+    psgd_view vs;
+    const Extent ex{"x", x, n, t, c}, ey{"y", y, n, t, c}, er{"residual", residual ? residual : x, n, t, residual ? c : 0},
+        es = flat("step_dev", step_dev, step_dev ? 2 : 0, &vs);
+    if (int rc = check_operand(name, ex, false)) return rc;
+    if (int rc = check_operand(name, er, false)) return rc;
+    if (int rc = check_operand(name, ey, true)) return rc;
+    if (reinterpret_cast<uintptr_t>(step_dev) % 8) return fail(PSGD_EALIGN, "%s: step_dev is not aligned to its element size", name);
+    if (int rc = refuse_overlap(name, ey, ex, true)) return rc;
+    if (int rc = refuse_overlap(name, ey, er, true)) return rc;
+    if (int rc = refuse_overlap(name, ey, es)) return rc;
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    const int64_t drop = (int64_t)std::floor((double)p * 65536.0 + 0.5), groups = parts_of(c, 16 / elem_bytes(x->type));
+    DropArgs a{};
+    a.x = static_cast<const char*>(x->data);
+    a.x_learner = x->learner;
+    a.x_row = x->row;
+    if (residual) {
+        a.residual = static_cast<const char*>(residual->data);
+        a.r_learner = residual->learner;
+        a.r_row = residual->row;
+    }
+    a.y = static_cast<char*>(y->data);
+    a.y_learner = y->learner;
+    a.y_row = y->row;
+    a.step_dev = step_dev;
+    a.seed = seed;
+    a.step = step;
+    a.c = c;
+    a.words = parts_of(c, 4);
+    a.keep = (uint32_t)(65536 - drop);
+    a.scale = a.keep ? (float)(65536.0 / a.keep) : 0.0f;
+    a.groups = divider((uint32_t)groups);
+    a.tokens = divider((uint32_t)t);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    // a launch counts its items below 2^30: a step of all its threads beyond that is still below 2^31
+    const int64_t rows = (int64_t)n * t, most = (1 << 30) / groups;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int64_t here = rows - first < most ? rows - first : most;
+        a.first_row = first;
+        a.items = (uint32_t)(here * groups);
+        const int64_t full = parts_of(a.items, kDropThreads), chip = (int64_t)cus * 8;
+        const dim3 grid((unsigned)(full < chip ? full : chip));
+        void (*fn)(DropArgs) = x->type == PSGD_F32 ? (residual ? dropout_kernel<float, true> : dropout_kernel<float, false>)
+                                                   : (residual ? dropout_kernel<uint16_t, true> : dropout_kernel<uint16_t, false>);
+        hipLaunchKernelGGL(fn, grid, dim3(kDropThreads), 0, s, a);
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}

@@ -1,0 +1,590 @@
+// Norm of each head of queries and keys with the rotation by position, forward and backward (gfx950).
+//
+//     u = x r g,  r = (mean x^2 + eps)^-1/2,      (y_a, y_b) = (u_a cos f - u_b sin f, u_b cos f + u_a sin f),   f = position base^(-2 p / rotary)
+//     v = dy turned back,  h = x r,  w = v g:     dx = r (w - h mean(w h)),   dg = sum v h
+//
+// About ten vector operations an element against 4 bytes (forward, bf16) to 12 (backward, float): bound by HBM, so every array is touched once.  A
+// wavefront takes a token: its lanes make the token's cosines and sines, one pair of columns each, exchange them through LDS, and every head of the
+// token uses them.  A head takes as many lanes as its columns make of pairs of 16-byte groups, so a lane holds both columns of each of its pairs (a
+// group of the first half and one of the second, or two neighbouring ones) and a wavefront works on 64 / lanes heads at once.
+//
+// An angle is position times rate in turns, in 64 bits: whole quarters are taken off there and the rest, an eighth of a turn at most, is rounded to 32
+// bits, so it is off by 2^-27 turns, 5e-8 of a radian, wherever the token is.
+#include "psgd_attention.h"
+#include "psgd_rows.h"
+
+namespace psgd {
+namespace {
+
+constexpr int kMostPairs = PSGD_MAX_HEAD / 2;
+constexpr int kHeadWaves = 4;
+
+struct HeadRows {       // [n, t, heads * head]
+    char* p;
+    int64_t learner, row;   // in elements
+};
+struct Gains {          // [n, head]
+    const char* p;
+    int64_t learner;
+};
+struct QkArgs {
+    HeadRows in[2], out[2];      // queries, keys; backward: the gradients that come and those that go
+    HeadRows x[2];               // backward: what went in
+    Gains gain[2];
+    const int32_t* positions;
+    int64_t pos_learner, pos_row, t;
+    float* partial;              // backward: [n][gridDim.x][2][head], or NULL
+    int heads[2], head, rotary, lanes;      // lanes: of a head, a power of two
+    int gain_bf16, neighbours;
+    float eps, inv_head;
+    double turn[kMostPairs];     // turns a position, of each pair
+};
+
+// E values next to each other, as floats: 16 bytes, or four bf16.
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+template <typename T, int E> __device__ __forceinline__ void load_group(const T* p, float (&v)[E]) {
+    if constexpr (E * sizeof(T) == 16) {
+        widen<T>(load_raw(p), v);
+    } else {
+        const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            v[2 * i] = low_bf16(r[i]);
+            v[2 * i + 1] = high_bf16(r[i]);
+        }
+    }
+}
+template <typename T, int E> __device__ __forceinline__ void store_group(T* p, const float (&v)[E]) {
+    if constexpr (E * sizeof(T) == 16) *reinterpret_cast<u32x4_any*>(p) = narrow(v, T{});
+    else *reinterpret_cast<u32x2_any*>(p) = (u32x2){two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+}
+
+// What a lane holds of a head: E pairs of columns.  VEC: as two groups of E columns next to each other, which takes rotary and the columns behind it
+// to be multiples of 2 E; else column by column, any head.
+template <typename T, int E, bool VEC> struct Columns {
+    int a, b;            // VEC: of the two groups
+    int first, head, half;
+    bool here, turned, neighbours;
+    __device__ __forceinline__ Columns(const QkArgs& q, int j) {
+        first = j * E;
+        head = q.head;
+        half = q.rotary / 2;
+        neighbours = q.neighbours;
+        here = 2 * first < head;
+        turned = first < half;
+        const bool apart = turned && !neighbours;
+        a = apart ? first : 2 * first;
+        b = apart ? first + half : 2 * first + E;
+    }
+    __device__ __forceinline__ void column_of(int e, int& ca, int& cb) const {
+        const int p = first + e;
+        const bool apart = p < half && !neighbours;
+        ca = apart ? p : 2 * p;
+        cb = apart ? p + half : 2 * p + 1;
+    }
+    __device__ __forceinline__ void load(const T* p, bool live, float (&va)[E], float (&vb)[E]) const {
+        if constexpr (VEC) {
+            if (live) {
+                load_group<T, E>(p + a, va);
+                load_group<T, E>(p + b, vb);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) va[e] = vb[e] = 0.0f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                int ca, cb;
+                column_of(e, ca, cb);
+                va[e] = live && ca < head ? load_1(p + ca) : 0.0f;
+                vb[e] = live && cb < head ? load_1(p + cb) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T* p, bool live, const float (&va)[E], const float (&vb)[E]) const {
+        if (!live) return;
+        if constexpr (VEC) {
+            store_group<T, E>(p + a, va);
+            store_group<T, E>(p + b, vb);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                int ca, cb;
+                column_of(e, ca, cb);
+                if (ca < head) store_1(p + ca, va[e]);
+                if (cb < head) store_1(p + cb, vb[e]);
+            }
+        }
+    }
+    // Turns each pair by its angle, or back by it.  Columns that are not turned stay as they are, NaN beside them or not.
+    __device__ __forceinline__ void turn(const float (&c)[E], const float (&s)[E], float (&va)[E], float (&vb)[E]) const {
+        if (VEC && neighbours) {
+            if (!turned) return;
+#pragma unroll
+            for (int e = 0; e < E / 2; ++e) {
+                const float a0 = va[2 * e], a1 = va[2 * e + 1], b0 = vb[2 * e], b1 = vb[2 * e + 1];
+                va[2 * e] = a0 * c[e] - a1 * s[e];
+                va[2 * e + 1] = a1 * c[e] + a0 * s[e];
+                vb[2 * e] = b0 * c[E / 2 + e] - b1 * s[E / 2 + e];
+                vb[2 * e + 1] = b1 * c[E / 2 + e] + b0 * s[E / 2 + e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const bool yes = VEC ? turned : first + e < half;
+                const float x = va[e], y = vb[e];
+                va[e] = yes ? x * c[e] - y * s[e] : x;
+                vb[e] = yes ? y * c[e] + x * s[e] : y;
+            }
+        }
+    }
+    // The column that element e of each half of the lane's values is.
+    __device__ __forceinline__ void place(int e, int& ca, int& cb) const {
+        if constexpr (VEC) {
+            ca = a + e;
+            cb = b + e;
+        } else {
+            column_of(e, ca, cb);
+        }
+    }
+    template <typename P> __device__ __forceinline__ void gather(const P* p, float (&ga)[E], float (&gb)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            int ca, cb;
+            place(e, ca, cb);
+            ga[e] = ca < head ? load_1(p + ca) : 0.0f;
+            gb[e] = cb < head ? load_1(p + cb) : 0.0f;
+        }
+    }
+    __device__ __forceinline__ void gains(const Gains& g, bool bf16, int64_t i, float (&ga)[E], float (&gb)[E]) const {
+        if (bf16) gather(reinterpret_cast<const uint16_t*>(g.p) + i * g.learner, ga, gb);
+        else gather(reinterpret_cast<const float*>(g.p) + i * g.learner, ga, gb);
+    }
+};
+
+// Over a head's lanes, 1 to 64, in every one of them.
+__device__ __forceinline__ float head_sum(float v, int lanes) {
+    if (lanes > 1) v += dpp<0xB1>(v);
+    if (lanes > 2) v += dpp<0x4E>(v);
+    if (lanes > 4) v += dpp<0x141>(v);
+    if (lanes > 8) v += dpp<0x140>(v);
+    if (lanes > 16) {
+        auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    }
+    if (lanes > 32) {
+        auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(b[0]) + __uint_as_float(b[1]);
+    }
+    return v;
+}
+
+__device__ __forceinline__ void wave_meets() {       // LDS that lanes of one wavefront exchange
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// cos and sin of so many turns.
+__device__ __forceinline__ void cos_sin(double turns, float& c, float& s) {
+    const double quarters = rint(4.0 * turns);
+    const float rest = (float)(turns - 0.25 * quarters);
+    float s0, c0;
+    sincospif(2.0f * rest, &s0, &c0);
+    const int q = (int)((int64_t)quarters & 3);
+    const float cc = q & 1 ? s0 : c0, ss = q & 1 ? c0 : s0;
+    c = q == 1 || q == 2 ? -cc : cc;
+    s = q >= 2 ? -ss : ss;
+}
+
+// The token's cosines and sines into the wavefront's LDS.
+__device__ __forceinline__ void angles(const QkArgs& q, const double (&turn)[2], int64_t i, int64_t r, int lane, float* cs) {
+    const double at = q.positions ? (double)q.positions[i * q.pos_learner + r * q.pos_row] : (double)r;
+    wave_meets();           // the token before this one has been read
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if (lane + 64 * k < q.rotary / 2) cos_sin(at * turn[k], cs[lane + 64 * k], cs[kMostPairs + lane + 64 * k]);
+    wave_meets();
+}
+template <int E> __device__ __forceinline__ void pair_angles(const float* cs, int first, int half, float (&c)[E], float (&s)[E]) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const bool yes = first + e < half;
+        c[e] = yes ? cs[first + e] : 1.0f;
+        s[e] = yes ? cs[kMostPairs + first + e] : 0.0f;
+    }
+}
+
+template <typename T, int E, bool VEC> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_kernel(QkArgs a) {
+    __shared__ float trig[kHeadWaves][2 * kMostPairs];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane / a.lanes, at_once = kWave / a.lanes;
+    const int64_t i = blockIdx.y;
+    const Columns<T, E, VEC> cols(a, lane % a.lanes);
+    const double turn[2] = {a.turn[lane], a.turn[lane + 64]};
+    const bool norm = a.gain[0].p != nullptr || a.gain[1].p != nullptr;
+    for (int64_t r = (int64_t)blockIdx.x * kHeadWaves + wave; r < a.t; r += (int64_t)gridDim.x * kHeadWaves) {
+        angles(a, turn, i, r, lane, trig[wave]);
+        float c[E], s[E];
+        pair_angles<E>(trig[wave], cols.first, cols.half, c, s);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (a.heads[which] == 0) continue;
+            float ga[E], gb[E];
+            if (norm) cols.gains(a.gain[which], a.gain_bf16, i, ga, gb);
+            const T* in = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row;
+            T* out = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row;
+            for (int h0 = 0; h0 < a.heads[which]; h0 += at_once) {
+                const int h = h0 + sub;
+                const bool live = cols.here && h < a.heads[which];
+                float va[E], vb[E];
+                cols.load(in + (int64_t)h * a.head, live, va, vb);
+                if (norm) {
+                    float sq = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sq = __builtin_fmaf(va[e], va[e], __builtin_fmaf(vb[e], vb[e], sq));
+                    const float rs = 1.0f / sqrtf(head_sum(sq, a.lanes) * a.inv_head + a.eps);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        va[e] = va[e] * rs * ga[e];
+                        vb[e] = vb[e] * rs * gb[e];
+                    }
+                }
+                cols.turn(c, s, va, vb);
+                cols.store(out + (int64_t)h * a.head, live, va, vb);
+            }
+        }
+    }
+}
+
+template <typename T, int E, bool VEC> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_grad_kernel(QkArgs a) {
+    __shared__ float trig[kHeadWaves][2 * kMostPairs];
+    __shared__ float sums[kHeadWaves][2][PSGD_MAX_HEAD];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane / a.lanes, at_once = kWave / a.lanes;
+    const int64_t i = blockIdx.y;
+    const Columns<T, E, VEC> cols(a, lane % a.lanes);
+    const double turn[2] = {a.turn[lane], a.turn[lane + 64]};
+    const bool norm = a.gain[0].p != nullptr || a.gain[1].p != nullptr;
+    float da[2][E], db[2][E];
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int e = 0; e < E; ++e) da[which][e] = db[which][e] = 0.0f;
+    for (int64_t r = (int64_t)blockIdx.x * kHeadWaves + wave; r < a.t; r += (int64_t)gridDim.x * kHeadWaves) {
+        angles(a, turn, i, r, lane, trig[wave]);
+        float c[E], s[E];
+        pair_angles<E>(trig[wave], cols.first, cols.half, c, s);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] = -s[e];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (a.heads[which] == 0) continue;
+            float ga[E], gb[E];
+            if (norm) cols.gains(a.gain[which], a.gain_bf16, i, ga, gb);
+            const T* in = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row;
+            const T* px = norm ? reinterpret_cast<const T*>(a.x[which].p) + i * a.x[which].learner + r * a.x[which].row : nullptr;
+            T* out = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row;
+            for (int h0 = 0; h0 < a.heads[which]; h0 += at_once) {
+                const int h = h0 + sub;
+                const bool live = cols.here && h < a.heads[which];
+                float va[E], vb[E];
+                cols.load(in + (int64_t)h * a.head, live, va, vb);
+                if (!norm) {
+                    cols.turn(c, s, va, vb);
+                    cols.store(out + (int64_t)h * a.head, live, va, vb);
+                    continue;
+                }
+                float xa[E], xb[E];
+                cols.load(px + (int64_t)h * a.head, live, xa, xb);
+                cols.turn(c, s, va, vb);
+                float sq = 0.0f, wx = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    sq = __builtin_fmaf(xa[e], xa[e], __builtin_fmaf(xb[e], xb[e], sq));
+                    wx = __builtin_fmaf(va[e] * ga[e], xa[e], __builtin_fmaf(vb[e] * gb[e], xb[e], wx));
+                }
+                sq = head_sum(sq, a.lanes);
+                wx = head_sum(wx, a.lanes);
+                const float rs = 1.0f / sqrtf(sq * a.inv_head + a.eps), along = wx * rs * a.inv_head;      // mean(w h)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float ha = xa[e] * rs, hb = xb[e] * rs;
+                    da[which][e] = __builtin_fmaf(va[e], ha, da[which][e]);
+                    db[which][e] = __builtin_fmaf(vb[e], hb, db[which][e]);
+                    va[e] = rs * __builtin_fmaf(-ha, along, va[e] * ga[e]);
+                    vb[e] = rs * __builtin_fmaf(-hb, along, vb[e] * gb[e]);
+                }
+                cols.store(out + (int64_t)h * a.head, live, va, vb);
+            }
+        }
+    }
+    if (!a.partial) return;
+    // the heads that the wavefront worked on at once, then its wavefronts, in a fixed order
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            float u = da[which][e], v = db[which][e];
+            for (int m = a.lanes; m < kWave; m *= 2) {
+                u += __shfl_xor(u, m);
+                v += __shfl_xor(v, m);
+            }
+            int ca, cb;
+            cols.place(e, ca, cb);
+            if (sub == 0 && ca < a.head) sums[wave][which][ca] = u;
+            if (sub == 0 && cb < a.head) sums[wave][which][cb] = v;
+        }
+    __syncthreads();
+    float* part = a.partial + (i * gridDim.x + blockIdx.x) * 2 * a.head;
+    for (int e = threadIdx.x; e < 2 * a.head; e += kHeadWaves * kWave) {
+        const int which = e >= a.head, col = e - which * a.head;
+        float v = sums[0][which][col];
+#pragma unroll
+        for (int w = 1; w < kHeadWaves; ++w) v += sums[w][which][col];
+        part[e] = v;
+    }
+}
+
+// Adds the slabs up: 64 columns a workgroup, its sixteen wavefronts every sixteenth slab each.
+constexpr int kGainWaves = 16;
+template <typename G>
+__global__ __launch_bounds__(kGainWaves* kWave) void qk_gains_kernel(const float* partial, int64_t slabs, G* dq, int64_t lq, G* dk, int64_t lk, int head) {
+    __shared__ float rest[kGainWaves][kWave];
+    const int64_t i = blockIdx.y;
+    const int col = blockIdx.x * kWave + threadIdx.x % kWave, w = threadIdx.x / kWave, l = threadIdx.x % kWave;
+    float sum = 0.0f;
+    if (col < 2 * head) {
+        const float* p = partial + i * slabs * 2 * head + col;
+#pragma unroll 4
+        for (int64_t s = w; s < slabs; s += kGainWaves) sum += p[s * 2 * head];
+    }
+    rest[w][l] = sum;
+    __syncthreads();
+    if (w == 0 && col < 2 * head) {
+        float v = rest[0][l];
+#pragma unroll
+        for (int k = 1; k < kGainWaves; ++k) v += rest[k][l];
+        if (col < head) {
+            if (dq) store_1(dq + i * lq + col, v);
+        } else if (dk) {
+            store_1(dk + i * lk + (col - head), v);
+        }
+    }
+}
+
+inline HeadRows head_rows(const psgd_view* v) { return v ? HeadRows{static_cast<char*>(v->data), v->learner, v->row} : HeadRows{nullptr, 0, 0}; }
+inline Gains gains_of(const psgd_view* v) { return v ? Gains{static_cast<const char*>(v->data), v->learner} : Gains{nullptr, 0}; }
+
+// Workgroups for each learner, four tokens at a time each.
+inline int64_t forward_groups(int n, int64_t t, int cus) {
+    const int64_t most = parts_of(t, kHeadWaves), fair = parts_of((int64_t)cus * 8, n);
+    return most < fair ? most : fair;
+}
+// Backward they leave a partial row each behind.  The same for any device, since the workspace's size is asked for without one.
+inline int64_t grad_slabs(int n, int64_t t) {
+    const int64_t most = parts_of(t, kHeadWaves), fair = parts_of(2048, n);
+    const int64_t g = most < fair ? most : fair;
+    return g < 1 ? 1 : g;
+}
+
+// How a lane holds a head: two groups of 16 bytes, two of four bf16, or column by column.
+enum { kGroups16, kGroups8, kColumns };
+inline int head_way(int head, int rotary, int bytes) {
+    if (rotary % (32 / bytes) == 0 && (head - rotary) % (32 / bytes) == 0) return kGroups16;
+    return bytes == 2 && rotary % 8 == 0 && (head - rotary) % 8 == 0 ? kGroups8 : kColumns;
+}
+inline int pairs_of_lane(int way, int bytes) { return way == kGroups16 ? 16 / bytes : 4; }
+
+inline int fill_args(const char* name, QkArgs& a, int heads, int kv, int head, int rotary, int pairs, double base, float eps, int n, int64_t t) {
+    if (int rc = check_counts(name, n, t, head)) return rc;
+    if (heads < 0 || kv < 0 || head < 1 || head > PSGD_MAX_HEAD)
+        return fail(PSGD_EINVAL, "%s: heads=%d, kv=%d, head=%d (1..%d)", name, heads, kv, head, (int)PSGD_MAX_HEAD);
+    if ((int64_t)heads * head > INT32_MAX || (int64_t)kv * head > INT32_MAX) return fail(PSGD_EINVAL, "%s: a size beyond 2^31 - 1", name);
+    if (rotary < 0 || rotary > head || rotary % 2) return fail(PSGD_EINVAL, "%s: rotary=%d is not an even number in 0..%d", name, rotary, head);
+    if (pairs != PSGD_PAIRS_HALVES && pairs != PSGD_PAIRS_NEIGHBOURS) return fail(PSGD_EINVAL, "%s: pairs=%d", name, pairs);
+    if (!(base > 0.0) || !std::isfinite(base)) return fail(PSGD_EINVAL, "%s: base=%g", name, base);
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(PSGD_EINVAL, "%s: eps=%g", name, (double)eps);
+    a.t = t;
+    a.heads[0] = heads;
+    a.heads[1] = kv;
+    a.head = head;
+    a.rotary = rotary;
+    a.neighbours = pairs == PSGD_PAIRS_NEIGHBOURS;
+    a.eps = eps;
+    a.inv_head = 1.0f / (float)head;
+    for (int p = 0; p < kMostPairs; ++p) a.turn[p] = p < rotary / 2 ? std::pow(base, -2.0 * p / rotary) / (2.0 * M_PI) : 0.0;
+    for (int p = 0; p < rotary / 2; ++p)
+        if (!std::isfinite(a.turn[p])) return fail(PSGD_EINVAL, "%s: base=%g", name, base);
+    return PSGD_OK;
+}
+
+inline int check_positions(const char* name, const Extent& e) {
+    if (e.v->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: positions must be int32", name);
+    return check_operand(name, e, false);
+}
+
+}  // namespace
+}  // namespace psgd
+
+extern "C" {
+
+int psgd_qk_norm_rope(const psgd_view* q, const psgd_view* k, const psgd_view* positions, const psgd_view* q_gain, const psgd_view* k_gain,
+                      const psgd_view* q_out, const psgd_view* k_out, int heads, int kv, int head, int rotary, int pairs, double base, float eps,
+                      int n, int64_t t, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_qk_norm_rope";
+    clear_error();
+    QkArgs a{};
+    if (int rc = fill_args(name, a, heads, kv, head, rotary, pairs, base, eps, n, t)) return rc;
+    if ((heads && (!q || !q_out)) || (kv && (!k || !k_out))) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (heads == 0) q = q_out = nullptr;
+    if (kv == 0) k = k_out = nullptr;
+    if ((q_gain == nullptr) != (k_gain == nullptr)) return fail(PSGD_EINVAL, "%s: q_gain and k_gain go together", name);
+    const psgd_view* one = q ? q : k;
+    if (!one || t == 0) return PSGD_OK;
+    for (const psgd_view* v : {q, k, q_out, k_out})
+        if (v && (!float_type(v->type) || v->type != one->type)) return fail(PSGD_EINVAL, "%s: q, k, q_out and k_out must be float or bf16 alike", name);
+    if (q_gain && (!float_type(q_gain->type) || k_gain->type != q_gain->type)) return fail(PSGD_EINVAL, "%s: q_gain and k_gain must be float or bf16 alike", name);
+    const psgd_view none{nullptr, 0, 0, one->type};
+    const int64_t cq = (int64_t)heads * head, ck = (int64_t)kv * head;
+    const Extent eq{"q", q ? q : &none, n, t, cq}, ek{"k", k ? k : &none, n, t, ck}, eqo{"q_out", q_out ? q_out : &none, n, t, cq},
+        eko{"k_out", k_out ? k_out : &none, n, t, ck}, egq{"q_gain", q_gain ? q_gain : &none, n, 1, q_gain ? head : 0},
+        egk{"k_gain", k_gain ? k_gain : &none, n, 1, k_gain ? head : 0}, ep{"positions", positions ? positions : &none, n, t, positions ? 1 : 0};
+    for (const Extent* e : {&eq, &ek, &egq, &egk})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    if (positions)
+        if (int rc = check_positions(name, ep)) return rc;
+    for (const Extent* e : {&eqo, &eko})
+        if (int rc = check_operand(name, *e, true)) return rc;
+    if (int rc = refuse_overlap(name, eqo, eq, true)) return rc;
+    if (int rc = refuse_overlap(name, eko, ek, true)) return rc;
+    if (int rc = refuse_overlap(name, eqo, ek)) return rc;
+    if (int rc = refuse_overlap(name, eko, eq)) return rc;
+    if (int rc = refuse_overlap(name, eqo, eko)) return rc;
+    for (const Extent* o : {&eqo, &eko})
+        for (const Extent* e : {&egq, &egk, &ep})
+            if (int rc = refuse_overlap(name, *o, *e)) return rc;
+    int cus = 0;
+    if (int rc = compute_units(&cus)) return rc;
+    a.in[0] = head_rows(q);
+    a.in[1] = head_rows(k);
+    a.out[0] = head_rows(q_out);
+    a.out[1] = head_rows(k_out);
+    a.gain[0] = gains_of(q_gain);
+    a.gain[1] = gains_of(k_gain);
+    a.gain_bf16 = q_gain && q_gain->type == PSGD_BF16;
+    if (positions) {
+        a.positions = static_cast<const int32_t*>(positions->data);
+        a.pos_learner = positions->learner;
+        a.pos_row = positions->row;
+    }
+    const int bytes = elem_bytes(one->type), way = head_way(head, rotary, bytes);
+    a.lanes = 1;
+    while (2 * a.lanes * pairs_of_lane(way, bytes) < head) a.lanes *= 2;
+    void (*fn)(QkArgs) = one->type == PSGD_F32 ? (way == kGroups16 ? qk_kernel<float, 4, true> : qk_kernel<float, 4, false>)
+                                               : (way == kGroups16 ? qk_kernel<uint16_t, 8, true> : way == kGroups8 ? qk_kernel<uint16_t, 4, true> : qk_kernel<uint16_t, 4, false>);
+    hipLaunchKernelGGL(fn, dim3((unsigned)forward_groups(n, t, cus), n), dim3(kHeadWaves * kWave), 0, static_cast<hipStream_t>(stream), a);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+
+size_t psgd_qk_norm_rope_grad_workspace(int n, int64_t t, int head) {
+    if (n < 1 || n > PSGD_MAX_N || t < 0 || t > INT32_MAX || head < 1 || head > PSGD_MAX_HEAD) return 0;
+    return psgd::up256((size_t)n * psgd::grad_slabs(n, t) * 2 * head * sizeof(float));
+}
+
+int psgd_qk_norm_rope_grad(const psgd_view* dq_out, const psgd_view* dk_out, const psgd_view* q, const psgd_view* k, const psgd_view* positions,
+                           const psgd_view* q_gain, const psgd_view* k_gain, const psgd_view* dq, const psgd_view* dk, const psgd_view* dq_gain,
+                           const psgd_view* dk_gain, int heads, int kv, int head, int rotary, int pairs, double base, float eps, int n, int64_t t,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_qk_norm_rope_grad";
+    clear_error();
+    QkArgs a{};
+    if (int rc = fill_args(name, a, heads, kv, head, rotary, pairs, base, eps, n, t)) return rc;
+    if ((q_gain == nullptr) != (k_gain == nullptr)) return fail(PSGD_EINVAL, "%s: q_gain and k_gain go together", name);
+    const bool norm = q_gain != nullptr;
+    if ((heads && (!dq_out || !dq || (norm && !q))) || (kv && (!dk_out || !dk || (norm && !k)))) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (heads == 0) dq_out = dq = q = nullptr;
+    if (kv == 0) dk_out = dk = k = nullptr;
+    if (!norm) q = k = dq_gain = dk_gain = nullptr;
+    const psgd_view* one = dq_out ? dq_out : dk_out;
+    const int type = one ? one->type : (int)PSGD_F32;
+    for (const psgd_view* v : {dq_out, dk_out, q, k, dq, dk})
+        if (v && (!float_type(v->type) || v->type != type)) return fail(PSGD_EINVAL, "%s: dq_out, dk_out, q, k, dq and dk must be float or bf16 alike", name);
+    if (norm && (!float_type(q_gain->type) || k_gain->type != q_gain->type)) return fail(PSGD_EINVAL, "%s: q_gain and k_gain must be float or bf16 alike", name);
+    const psgd_view* params = dq_gain ? dq_gain : dk_gain;
+    if (params && (!float_type(params->type) || (dq_gain && dk_gain && dk_gain->type != dq_gain->type)))
+        return fail(PSGD_EINVAL, "%s: dq_gain and dk_gain must be float or bf16 alike", name);
+    if (!params && (!one || t == 0)) return PSGD_OK;
+    const psgd_view none{nullptr, 0, 0, type};
+    psgd_view vw;
+    const int64_t cq = (int64_t)heads * head, ck = (int64_t)kv * head;
+    const size_t need = params ? psgd_qk_norm_rope_grad_workspace(n, t, head) : 0;
+    const Extent eqo{"dq_out", dq_out ? dq_out : &none, n, t, cq}, eko{"dk_out", dk_out ? dk_out : &none, n, t, ck}, eq{"q", q ? q : &none, n, t, q ? cq : 0},
+        ek{"k", k ? k : &none, n, t, k ? ck : 0}, edq{"dq", dq ? dq : &none, n, t, cq}, edk{"dk", dk ? dk : &none, n, t, ck},
+        egq{"q_gain", norm ? q_gain : &none, n, 1, norm ? head : 0}, egk{"k_gain", norm ? k_gain : &none, n, 1, norm ? head : 0},
+        edgq{"dq_gain", dq_gain ? dq_gain : &none, n, 1, dq_gain ? head : 0}, edgk{"dk_gain", dk_gain ? dk_gain : &none, n, 1, dk_gain ? head : 0},
+        ep{"positions", positions ? positions : &none, n, t, positions ? 1 : 0}, ew = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&eqo, &eko, &eq, &ek, &egq, &egk})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    if (positions)
+        if (int rc = check_positions(name, ep)) return rc;
+    for (const Extent* e : {&edq, &edk, &edgq, &edgk})
+        if (int rc = check_operand(name, *e, true)) return rc;
+    if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256))
+        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
+    if (int rc = refuse_overlap(name, edq, eqo, true)) return rc;
+    if (int rc = refuse_overlap(name, edk, eko, true)) return rc;
+    if (int rc = refuse_overlap(name, edq, eko)) return rc;
+    if (int rc = refuse_overlap(name, edk, eqo)) return rc;
+    if (int rc = refuse_overlap(name, edq, edk)) return rc;
+    if (int rc = refuse_overlap(name, edgq, edgk)) return rc;
+    for (const Extent* o : {&edq, &edk, &edgq, &edgk})
+        for (const Extent* e : {&eq, &ek, &egq, &egk, &ep})
+            if (int rc = refuse_overlap(name, *o, *e)) return rc;
+    for (const Extent* o : {&edgq, &edgk})
+        for (const Extent* e : {&eqo, &eko, &edq, &edk})
+            if (int rc = refuse_overlap(name, *o, *e)) return rc;
+    if (need)
+        for (const Extent* e : {&eqo, &eko, &eq, &ek, &edq, &edk, &egq, &egk, &edgq, &edgk, &ep})
+            if (int rc = refuse_overlap(name, ew, *e)) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    a.in[0] = head_rows(dq_out);
+    a.in[1] = head_rows(dk_out);
+    a.x[0] = head_rows(q);
+    a.x[1] = head_rows(k);
+    a.out[0] = head_rows(dq);
+    a.out[1] = head_rows(dk);
+    a.gain[0] = gains_of(q_gain);
+    a.gain[1] = gains_of(k_gain);
+    a.gain_bf16 = norm && q_gain->type == PSGD_BF16;
+    if (positions) {
+        a.positions = static_cast<const int32_t*>(positions->data);
+        a.pos_learner = positions->learner;
+        a.pos_row = positions->row;
+    }
+    a.partial = params ? static_cast<float*>(workspace) : nullptr;
+    const int bytes = elem_bytes(type), way = head_way(head, rotary, bytes);
+    a.lanes = 1;
+    while (2 * a.lanes * pairs_of_lane(way, bytes) < head) a.lanes *= 2;
+    const int64_t slabs = grad_slabs(n, t);
+    if (one && t > 0) {
+        void (*fn)(QkArgs) = type == PSGD_F32
+                                 ? (way == kGroups16 ? qk_grad_kernel<float, 4, true> : qk_grad_kernel<float, 4, false>)
+                                 : (way == kGroups16 ? qk_grad_kernel<uint16_t, 8, true> : way == kGroups8 ? qk_grad_kernel<uint16_t, 4, true> : qk_grad_kernel<uint16_t, 4, false>);
+        hipLaunchKernelGGL(fn, dim3((unsigned)slabs, n), dim3(kHeadWaves * kWave), 0, s, a);
+    }
+    if (params) {
+        const int64_t count = one && t > 0 ? slabs : 0;
+        const dim3 grid((unsigned)parts_of(2 * head, kWave), n);
+        const int64_t lq = dq_gain ? dq_gain->learner : 0, lk = dk_gain ? dk_gain->learner : 0;
+        void *pq = dq_gain ? dq_gain->data : nullptr, *pk = dk_gain ? dk_gain->data : nullptr;
+        if (params->type == PSGD_F32)
+            hipLaunchKernelGGL(qk_gains_kernel<float>, grid, dim3(kGainWaves * kWave), 0, s, a.partial, count, static_cast<float*>(pq), lq, static_cast<float*>(pk), lk, head);
+        else
+            hipLaunchKernelGGL(qk_gains_kernel<uint16_t>, grid, dim3(kGainWaves * kWave), 0, s, a.partial, count, static_cast<uint16_t*>(pq), lq, static_cast<uint16_t*>(pk), lk, head);
+    }
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+
+}  // extern "C"

@@ -999,9 +999,12 @@ int psgd_device_status(int clear) {
         e = hipMemcpyToSymbol(HIP_SYMBOL(g_status_word), &zero, sizeof(int));
         if (e != hipSuccess) return hip_fail(e, "hipMemcpyToSymbol");
     }
-    int tokens = 0;
-    if (int rc = token_status(clear, &tokens)) return rc;
-    return word | tokens;
+    for (auto status : {token_status, attention_status, attention_step_status}) {
+        int flags = 0;
+        if (int rc = status(clear, &flags)) return rc;
+        word |= flags;
+    }
+    return word;
 }
 
 }  // extern "C"
