@@ -50,6 +50,15 @@ template <typename T> __device__ __forceinline__ Eight<T> no_values() {
     }
     return r;
 }
+__device__ __forceinline__ Eight<uint16_t> negative(Eight<uint16_t> a) {
+    a.v ^= 0x80008000u;
+    return a;
+}
+__device__ __forceinline__ Eight<float> negative(Eight<float> a) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a.v[e] = -a.v[e];
+    return a;
+}
 // Two blocks of a result as the operand of the next product.
 template <typename T> __device__ __forceinline__ Eight<T> as_operand(f32x4 low, f32x4 high) {
     Eight<T> r;
@@ -103,6 +112,11 @@ template <typename T> __device__ __forceinline__ Eight<T> load_eight(const T* ro
     return r;
 }
 
+// LDS by its 32-bit address.
+template <typename V> using InLds = __attribute__((address_space(3))) V*;
+template <typename V> __device__ __forceinline__ InLds<V> lds_at(uint32_t at) { return (InLds<V>)(uintptr_t)at; }
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(InLds<const char>)p; }
+
 // A tile of ROWS rows of H columns in LDS.  Its 16-byte groups are permuted within a row by the row's number, so that 16 rows' groups of one column,
 // and eight rows' pairs of groups next to each other (what the transposing read takes at a time), lie in different banks.
 template <typename T, int H, int ROWS> struct Tile {
@@ -115,14 +129,16 @@ template <typename T, int H, int ROWS> struct Tile {
 
     static __device__ __forceinline__ void put(char* tile, int row, int group, u32x4 v) { *reinterpret_cast<u32x4*>(tile + place(row, group)) = v; }
 
-    // A of rows 16 block ..., columns 32 kc ...
-    static __device__ __forceinline__ Eight<T> along(const char* tile, int block, int kc, int lane) {
-        const int row = 16 * block + lane % 16, g = lane / 16;
+    // A of rows 16 block ..., columns 32 kc ....  `from`: the tile's place in LDS plus the lane's in it; the rest is an exclusive or, since a row's bits are below
+    // those of rows, and an offset in the instruction.
+    static __device__ __forceinline__ uint32_t along_lane(int lane) { return place(lane % 16, (sizeof(T) == 2 ? 1 : 2) * (lane / 16)); }
+    static __device__ __forceinline__ Eight<T> along(uint32_t from, int block, int kc) {
         Eight<T> r;
+        const uint32_t rows = 16 * block * kGroups * 16;
         if constexpr (sizeof(T) == 2) {
-            r.v = *reinterpret_cast<const u32x4*>(tile + place(row, 4 * kc + g));
+            r.v = *lds_at<u32x4>((from ^ (kc * 64)) + rows);
         } else {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(tile + place(row, 8 * kc + 2 * g)), b = *reinterpret_cast<const f32x4*>(tile + place(row, 8 * kc + 2 * g + 1));
+            const f32x4 a = *lds_at<f32x4>((from ^ (kc * 128)) + rows), b = *lds_at<f32x4>((from ^ (kc * 128 + 16)) + rows);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 r.v[e] = a[e];
@@ -132,19 +148,21 @@ template <typename T, int H, int ROWS> struct Tile {
         return r;
     }
     // A of columns 16 block ... of the tile, its rows 32 kc ... in the order of as_operand's.
-    static __device__ __forceinline__ Eight<T> across(const char* tile, int block, int kc, int lane) {
+    static __device__ __forceinline__ uint32_t across_lane(int lane) {
+        if constexpr (sizeof(T) == 2) return place(lane / 16 * 4 + lane % 16 / 4, lane % 4 / 2) + lane % 2 * 8;
+        else return place(lane / 16 * 4, lane % 16 / 4) + lane % 4 * 4;
+    }
+    static __device__ __forceinline__ Eight<T> across(uint32_t from, int block, int kc) {
         Eight<T> r;
+        const uint32_t rows = 32 * kc * kGroups * 16;
         if constexpr (sizeof(T) == 2) {
-            const int row = 32 * kc + 4 * (lane / 16) + lane % 16 / 4, group = 2 * block + (lane % 4) / 2;
-            typedef __attribute__((address_space(3))) i16x4* lds;
-            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + place(row, group) + lane % 2 * 8));
-            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds)(tile + place(row + 16, group) + lane % 2 * 8));
-            const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+            const uint32_t at = (from ^ (block * 32)) + rows;
+            const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4>(at)));
+            const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<i16x4>(at + 16 * kGroups * 16)));
             r.v = (u32x4){x[0], x[1], y[0], y[1]};
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                r.v[e] = *reinterpret_cast<const float*>(tile + place(32 * kc + e / 4 * 16 + 4 * (lane / 16) + e % 4, 4 * block + lane % 16 / 4) + lane % 4 * 4);
+            for (int e = 0; e < 8; ++e) r.v[e] = *lds_at<float>((from ^ (block * 64 ^ e % 4 * 32)) + rows + (e / 4 * 16 + e % 4) * kGroups * 16);
         }
         return r;
     }

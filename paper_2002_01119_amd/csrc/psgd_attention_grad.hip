@@ -1,0 +1,416 @@
+// Causal attention in packed sequences, with a sliding window and first tokens that stay visible: the backward pass (gfx950).
+//
+//     D_i = do_i . o_i,   ds_ij = p_ij (do_i . v_j - D_i),   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij do_i
+//
+// In two kernels, so that every sum has one owner and a fixed order: the first owns queries and makes dq (and D, which the second reads), the second owns keys,
+// walks the queries that see them, of all heads that share the key head, and makes dk and dv.  Both compute s and p again from lse: seven products, of which
+// five are what the gradients cannot do without.
+#include "psgd_attention_walk.h"
+
+namespace psgd {
+namespace {
+
+// dq and D.  Queries and their gradients stay in registers, keys and values are walked as above, 32 rows of a tile at a time.
+template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (Shape<T, H>::kTwice)) void attention_dq_kernel(AttentionArgs a) {
+    using S = Shape<T, H>;
+    using Lds = typename S::Lds;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int members = a.heads / a.kv;
+    const Work w = find_work<S::kOwn>(a, members, true);
+    if (!w.there) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo;
+    const int h = w.kv_head * members + w.member, row0 = w.tile * S::kOwn, row1 = std::min(row0 + S::kOwn, len);
+    const bool whole = a.head % kPer<T> == 0;
+    const int mine = row0 + wave * 16 * S::kOwnBlocks;
+    constexpr bool kStart = sizeof(T) == 2;                           // as in the other kernel
+    const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f), lse_by = kStart ? kLog2E / to_log2 : kLog2E;
+    const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo;
+
+    Eight<T> q[S::kOwnBlocks][S::kSteps], dy[S::kOwnBlocks][S::kSteps];
+    f32x4 dq[S::kOwnBlocks][S::kCols];
+    float lse[S::kOwnBlocks], along[S::kOwnBlocks];
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const int row = mine + 16 * b + col, left = row < len ? a.head : 0;
+        const T *pq = at<T>(a.q, w.learner, w.lo + row, (int64_t)h * a.head), *pd = at<T>(a.dout, w.learner, w.lo + row, (int64_t)h * a.head),
+                *po = at<T>(a.o, w.learner, w.lo + row, (int64_t)h * a.head);
+        float d = 0.0f;
+#pragma unroll
+        for (int kc = 0; kc < S::kSteps; ++kc) {
+            q[b][kc] = load_eight(pq, kc, g, left, whole);
+            dy[b][kc] = load_eight(pd, kc, g, left, whole);
+            d += dot(dy[b][kc], load_eight(po, kc, g, left, whole));
+        }
+        d = column_all<Sum>(d);
+        along[b] = -d;
+        lse[b] = row < len ? -a.lse[stat + row] * lse_by : -INFINITY;     // rows that are not there: p = 0
+        if (row < len && g == 0) a.along[stat + row] = d;
+        if (a.scale < 0.0f) {
+#pragma unroll
+            for (int kc = 0; kc < S::kSteps; ++kc) q[b][kc] = negative(q[b][kc]);
+        }
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) dq[b][c] = (f32x4){0, 0, 0, 0};
+    }
+    const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
+    const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
+    Mover<T, H, S::kWalked, S::kThreads, DIRECT> mk, mv;
+    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
+    mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
+    mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
+    mk.land(lds);
+    mv.land(lds + Lds::kBytes);
+    __syncthreads();
+    uint32_t along_at = lds_address(lds) + Lds::along_lane(lane), across_at = lds_address(lds) + Lds::across_lane(lane);
+    for (int step = 0; step < walk.count; ++step) {
+        const int key0 = walk.tile(step) * S::kWalked;
+        asm("" : "+v"(along_at), "+v"(across_at));      // each read's own address is made from these where it is wanted: kept, they would take a third of the registers
+        const uint32_t buffer = (step & 1) * 2 * Lds::kBytes;
+        char* const next = lds + (~step & 1) * 2 * Lds::kBytes;
+        if (DIRECT && step + 1 < walk.count) {
+            mk.fetch(next, keys, a.k.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
+            mv.fetch(next + Lds::kBytes, values, a.v.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
+        }
+        if (mine < len && any_sees(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks)) {
+            const bool full = all_see(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks);
+#pragma unroll
+            for (int half = 0; half < S::kBlocks / 2; ++half) {
+                f32x4 s[S::kOwnBlocks][2], dp[S::kOwnBlocks][2];
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b) {
+                        s[b][kb] = kStart ? (f32x4){lse[b], lse[b], lse[b], lse[b]} : (f32x4){0, 0, 0, 0};
+                        dp[b][kb] = kStart ? (f32x4){along[b], along[b], along[b], along[b]} : (f32x4){0, 0, 0, 0};
+                    }
+#pragma unroll
+                    for (int kc = 0; kc < S::kSteps; ++kc) {
+                        const Eight<T> k = Lds::along(along_at + buffer, 2 * half + kb, kc), v = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + kb, kc);
+#pragma unroll
+                        for (int b = 0; b < S::kOwnBlocks; ++b) {
+                            s[b][kb] = mma(k, q[b][kc], s[b][kb]);
+                            dp[b][kb] = mma(v, dy[b][kc], dp[b][kb]);
+                        }
+                    }
+                }
+                if (!full) {
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b)
+#pragma unroll
+                        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[b][kb][e] = sees(mine + 16 * b + col, key0 + 16 * (2 * half + kb) + 4 * g + e, a.window, a.sinks) ? s[b][kb][e] : -INFINITY;
+                }
+                Eight<T> ds[S::kOwnBlocks];
+#pragma unroll
+                for (int b = 0; b < S::kOwnBlocks; ++b) {
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = exp_2(kStart ? s[b][kb][e] * to_log2 : __builtin_fmaf(s[b][kb][e], to_log2, lse[b]));
+                            s[b][kb][e] = p * (kStart ? dp[b][kb][e] : dp[b][kb][e] + along[b]);
+                        }
+                    ds[b] = as_operand<T>(s[b][0], s[b][1]);
+                }
+#pragma unroll
+                for (int c = 0; c < S::kCols; ++c) {
+                    const Eight<T> k = Lds::across(across_at + buffer, c, half);
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b) dq[b][c] = mma(k, ds[b], dq[b][c]);
+                }
+            }
+        }
+        if (step + 1 < walk.count) {
+            if (!DIRECT) {
+                mk.fetch(next, keys, a.k.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
+                mv.fetch(next + Lds::kBytes, values, a.v.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
+            }
+            mk.land(next);
+            mv.land(next + Lds::kBytes);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const int row = mine + 16 * b + col;
+        if (row >= len) continue;
+        T* p = at<T>(a.dq, w.learner, w.lo + row, (int64_t)h * a.head);
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) store_four(p, 16 * c + 4 * g, a.head, dq[b][c] * a.scale);
+    }
+}
+
+// dk and dv.  Keys stay in registers and values there or in LDS; the queries that see them and their gradients are walked, one head that shares the key
+// head after the other, with lse and D of a tile's rows beside it.
+template <typename T, int H> struct KeyShape : Shape<T, H> {
+    // 128 columns in bf16: keys and both gradients are 160 registers, and with the values' 32 two workgroups would not fit a compute unit
+    static constexpr bool kValuesInLds = sizeof(T) == 2 && H == 128;
+    static constexpr int kRows = kValuesInLds ? 32 : Shape<T, H>::kWalked;
+    static constexpr int kTwice = sizeof(T) == 2 && H <= 128 ? 2 : 1;
+    using Lds = Tile<T, H, kRows>;
+    using Own = Tile<T, H, Shape<T, H>::kOwn>;
+    static constexpr size_t kTiles = 4 * (size_t)Lds::kBytes, kStats = kTiles + (kValuesInLds ? Own::kBytes : 0), kBytes = kStats + 4 * kRows * sizeof(float);
+};
+
+template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (KeyShape<T, H>::kTwice)) void attention_dkv_kernel(AttentionArgs a) {
+    using S = KeyShape<T, H>;
+    using Lds = typename S::Lds;
+    extern __shared__ __attribute__((aligned(16))) char lds[];       // two of queries and gradients, values, two of [2][rows] statistics
+    const Work w = find_work<S::kOwn>(a, 1, false);
+    if (!w.there) return;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo, members = a.heads / a.kv;
+    const int key0 = w.tile * S::kOwn, key1 = std::min(key0 + S::kOwn, len);
+    const bool whole = a.head % kPer<T> == 0;
+    const int mine = key0 + wave * 16 * S::kOwnBlocks;               // the wavefront's first key
+    // In bf16 p = exp2(to_log2 (q . k - lse / scale)): the products' sums start from -lse / scale, and those of dout . v from -D, which leaves two operations
+    // less for each pair.  (In float those sums would be rounded as often as they have terms at the size of what they start from.)  A negative scale's sign
+    // goes to the keys; one of 0 is next to nothing, beside which the products are lost.
+    constexpr bool kStart = sizeof(T) == 2;
+    const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f), lse_by = kStart ? kLog2E / to_log2 : kLog2E;
+    float* const stats = reinterpret_cast<float*>(lds + S::kStats);
+
+    Eight<T> k[S::kOwnBlocks][S::kSteps], v[S::kValuesInLds ? 1 : S::kOwnBlocks][S::kSteps];
+    f32x4 dk[S::kOwnBlocks][S::kCols], dv[S::kOwnBlocks][S::kCols];
+    Mover<T, H, S::kRows, S::kThreads, DIRECT> mq, md;
+    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, S::kStats);
+    if constexpr (S::kValuesInLds) {
+        Mover<T, H, S::kOwn, S::kThreads, DIRECT> mv;
+        mv.fetch(lds + S::kTiles, at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head), a.v.row, key0, len, a.head, whole);
+        mv.land(lds + S::kTiles);
+    }
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const int row = mine + 16 * b + col, left = row < len ? a.head : 0;
+        const T *pk = at<T>(a.k, w.learner, w.lo + row, (int64_t)w.kv_head * a.head), *pv = at<T>(a.v, w.learner, w.lo + row, (int64_t)w.kv_head * a.head);
+#pragma unroll
+        for (int kc = 0; kc < S::kSteps; ++kc) {
+            k[b][kc] = load_eight(pk, kc, g, left, whole);
+            if constexpr (!S::kValuesInLds) v[b][kc] = load_eight(pv, kc, g, left, whole);
+            if (a.scale < 0.0f) k[b][kc] = negative(k[b][kc]);
+        }
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) dk[b][c] = dv[b][c] = (f32x4){0, 0, 0, 0};
+    }
+    // the tiles of queries: from the keys' own on, to the last that the window leaves them
+    const int first = key0 / S::kRows;
+    const int64_t behind = key0 < a.sinks ? len : std::min((int64_t)len, (int64_t)key1 - 1 + a.window);
+    const int tiles = (int)((behind + S::kRows - 1) / S::kRows) - first, count = tiles * members;
+    float held[2];
+    auto fetch = [&](int step) {
+        char* const tile = lds + (step & 1) * 2 * Lds::kBytes;
+        const int h = w.kv_head * members + step / tiles, row0 = (first + step % tiles) * S::kRows, row = row0 + threadIdx.x;
+        mq.fetch(tile, at<T>(a.q, w.learner, w.lo, (int64_t)h * a.head), a.q.row, row0, len, a.head, whole);
+        md.fetch(tile + Lds::kBytes, at<T>(a.dout, w.learner, w.lo, (int64_t)h * a.head), a.dout.row, row0, len, a.head, whole);
+        const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo + row;
+        const bool there = threadIdx.x < S::kRows && row < len;
+        held[0] = there ? -a.lse[stat] * lse_by : -INFINITY;
+        held[1] = there ? -a.along[stat] : 0.0f;
+    };
+    auto land = [&](int buffer) {
+        mq.land(lds + buffer * 2 * Lds::kBytes);
+        md.land(lds + buffer * 2 * Lds::kBytes + Lds::kBytes);
+        if (threadIdx.x < S::kRows) {
+            stats[buffer * 2 * S::kRows + threadIdx.x] = held[0];
+            stats[(buffer * 2 + 1) * S::kRows + threadIdx.x] = held[1];
+        }
+    };
+    fetch(0);
+    land(0);
+    __syncthreads();
+    uint32_t along_at = lds_address(lds) + Lds::along_lane(lane), across_at = lds_address(lds) + Lds::across_lane(lane);
+    uint32_t value_at = lds_address(lds) + S::kTiles + S::Own::along_lane(lane) + wave * 16 * S::kOwnBlocks * S::Own::kGroups * 16;
+    for (int step = 0; step < count; ++step) {
+        const int row0 = (first + step % tiles) * S::kRows;
+        asm("" : "+v"(along_at), "+v"(across_at), "+v"(value_at));      // each read's own address is made from these where it is wanted: kept, they would take a third of the registers
+        const uint32_t buffer = (step & 1) * 2 * Lds::kBytes;
+        const float* st = stats + (step & 1) * 2 * S::kRows;
+        if (DIRECT && step + 1 < count) fetch(step + 1);
+        if (mine < len && any_sees(row0, row0 + S::kRows - 1, mine, mine + 16 * S::kOwnBlocks - 1, a.window, a.sinks)) {
+            const bool full = all_see(row0, row0 + S::kRows - 1, mine, mine + 16 * S::kOwnBlocks - 1, a.window, a.sinks);
+#pragma unroll
+            for (int half = 0; half < S::kRows / 32; ++half) {
+                f32x4 s[S::kOwnBlocks][2], dp[S::kOwnBlocks][2], lse[2], along[2];
+#pragma unroll
+                for (int qb = 0; qb < 2; ++qb) {
+                    const int row = 16 * (2 * half + qb) + 4 * g;
+                    lse[qb] = *reinterpret_cast<const f32x4*>(st + row);
+                    along[qb] = *reinterpret_cast<const f32x4*>(st + S::kRows + row);
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b) {
+                        s[b][qb] = kStart ? lse[qb] : (f32x4){0, 0, 0, 0};
+                        dp[b][qb] = kStart ? along[qb] : (f32x4){0, 0, 0, 0};
+                    }
+                }
+#pragma unroll
+                for (int kc = 0; kc < S::kSteps; ++kc) {
+                    if constexpr (S::kValuesInLds) {
+#pragma unroll
+                        for (int b = 0; b < S::kOwnBlocks; ++b) v[0][b] = S::Own::along(value_at, b, kc);
+                    }
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb) {
+                        const Eight<T> q = Lds::along(along_at + buffer, 2 * half + qb, kc), dy = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + qb, kc);
+#pragma unroll
+                        for (int b = 0; b < S::kOwnBlocks; ++b) {
+                            s[b][qb] = mma(q, k[b][kc], s[b][qb]);
+                            if constexpr (S::kValuesInLds) dp[b][qb] = mma(dy, v[0][b], dp[b][qb]);
+                            else dp[b][qb] = mma(dy, v[b][kc], dp[b][qb]);
+                        }
+                    }
+                }
+                if (!full) {
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b)
+#pragma unroll
+                        for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                s[b][qb][e] = sees(row0 + 16 * (2 * half + qb) + 4 * g + e, mine + 16 * b + col, a.window, a.sinks) ? s[b][qb][e] : -INFINITY;
+                }
+                Eight<T> p[S::kOwnBlocks], ds[S::kOwnBlocks];
+#pragma unroll
+                for (int b = 0; b < S::kOwnBlocks; ++b) {
+#pragma unroll
+                    for (int qb = 0; qb < 2; ++qb)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = exp_2(kStart ? s[b][qb][e] * to_log2 : __builtin_fmaf(s[b][qb][e], to_log2, lse[qb][e]));
+                            s[b][qb][e] = x;
+                            dp[b][qb][e] = x * (kStart ? dp[b][qb][e] : dp[b][qb][e] + along[qb][e]);
+                        }
+                    p[b] = as_operand<T>(s[b][0], s[b][1]);
+                    ds[b] = as_operand<T>(dp[b][0], dp[b][1]);
+                }
+#pragma unroll
+                for (int c = 0; c < S::kCols; ++c) {
+                    const Eight<T> dy = Lds::across(across_at + buffer + Lds::kBytes, c, half), q = Lds::across(across_at + buffer, c, half);
+#pragma unroll
+                    for (int b = 0; b < S::kOwnBlocks; ++b) {
+                        dv[b][c] = mma(dy, p[b], dv[b][c]);
+                        dk[b][c] = mma(q, ds[b], dk[b][c]);
+                    }
+                }
+            }
+        }
+        if (step + 1 < count) {
+            if (!DIRECT) fetch(step + 1);
+            land(~step & 1);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int b = 0; b < S::kOwnBlocks; ++b) {
+        const int row = mine + 16 * b + col;
+        if (row >= len) continue;
+        T *pk = at<T>(a.dk, w.learner, w.lo + row, (int64_t)w.kv_head * a.head), *pv = at<T>(a.dv, w.learner, w.lo + row, (int64_t)w.kv_head * a.head);
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) {
+            store_four(pk, 16 * c + 4 * g, a.head, dk[b][c] * a.scale);
+            store_four(pv, 16 * c + 4 * g, a.head, dv[b][c]);
+        }
+    }
+}
+
+template <typename T, int H> int launch_backward(const char* name, AttentionArgs a, hipStream_t s) {
+    static LdsRecord record_q[2] = {}, record_kv[2] = {};
+    const bool dq = straight<T, H>(a.head, {a.k, a.v}), dkv = straight<T, H>(a.head, {a.q, a.dout, a.v});
+    const AttentionKernel fq = dq ? attention_dq_kernel<T, H, true> : attention_dq_kernel<T, H, false>;
+    const AttentionKernel fkv = dkv ? attention_dkv_kernel<T, H, true> : attention_dkv_kernel<T, H, false>;
+    const size_t lds = kTileLds<T, H>, more = KeyShape<T, H>::kBytes;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(fq), lds, record_q[dq])) return rc;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(fkv), more, record_kv[dkv])) return rc;
+    a.places = tile_places(a.t, a.sequences, own_rows(H, sizeof(T)));
+    in_slices(a.places * a.n * a.heads, [&](int64_t first, unsigned groups) {
+        a.first = first;
+        hipLaunchKernelGGL(fq, dim3(groups), dim3(kAttentionWaves * kWave), lds, s, a);
+    });
+    in_slices(a.places * a.n * a.kv, [&](int64_t first, unsigned groups) {
+        a.first = first;
+        hipLaunchKernelGGL(fkv, dim3(groups), dim3(kAttentionWaves * kWave), more, s, a);
+    });
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+template <typename T> int backward_of(const char* name, const AttentionArgs& a, hipStream_t s) {
+    switch (held_head(a.head)) {
+        case 64: return launch_backward<T, 64>(name, a, s);
+        case 128: return launch_backward<T, 128>(name, a, s);
+        default: return launch_backward<T, 256>(name, a, s);
+    }
+}
+
+}  // namespace
+}  // namespace psgd
+
+extern "C" {
+
+size_t psgd_attention_grad_workspace(int heads, int kv, int head, int window, int sinks, int sequences, int n, int64_t t) {
+    (void)kv, (void)head, (void)window, (void)sinks, (void)sequences;
+    if (n < 1 || n > PSGD_MAX_N || t < 1 || t > INT32_MAX || heads < 1) return 0;
+    return psgd::up256((size_t)n * heads * t * sizeof(float));
+}
+
+int psgd_attention_grad(const psgd_view* dout, const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_view* out, const float* lse,
+                        const psgd_view* starts, const psgd_view* dq, const psgd_view* dk, const psgd_view* dv, int heads, int kv, int head, int window,
+                        int sinks, float scale, int sequences, int n, int64_t t, void* workspace, size_t workspace_bytes, void* stream) {
+    using namespace psgd;
+    const char* name = "psgd_attention_grad";
+    clear_error();
+    if (!dout || !q || !k || !v || !out || !dq || !dk || !dv) return fail(PSGD_EINVAL, "%s: null operand", name);
+    if (int rc = check_shape(name, heads, kv, head, window, sinks, scale, sequences, starts, n, t)) return rc;
+    for (const psgd_view* x : {dout, q, k, v, out, dq, dk, dv})
+        if (!float_type(x->type) || x->type != q->type) return fail(PSGD_EINVAL, "%s: dout, q, k, v, out, dq, dk and dv must be float or bf16 alike", name);
+    if (t == 0) return PSGD_OK;
+    if (!lse) return fail(PSGD_EINVAL, "%s: lse is needed", name);
+    const size_t need = psgd_attention_grad_workspace(heads, kv, head, window, sinks, sequences, n, t);
+    psgd_view vl, vw;
+    const int64_t cq = (int64_t)heads * head, ck = (int64_t)kv * head;
+    const Extent ed{"dout", dout, n, t, cq}, eq{"q", q, n, t, cq}, ek{"k", k, n, t, ck}, ev{"v", v, n, t, ck}, eo{"out", out, n, t, cq},
+        es{"starts", starts ? starts : q, n, 1, starts ? (int64_t)sequences + 1 : 0}, el = flat("lse", lse, (int64_t)n * heads * t, &vl),
+        edq{"dq", dq, n, t, cq}, edk{"dk", dk, n, t, ck}, edv{"dv", dv, n, t, ck}, ew = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&ed, &eq, &ek, &ev, &eo, &es, &el})
+        if (int rc = check_operand(name, *e, false)) return rc;
+    for (const Extent* e : {&edq, &edk, &edv})
+        if (int rc = check_operand(name, *e, true)) return rc;
+    if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
+    for (const Extent* o : {&edq, &edk, &edv, &ew})
+        for (const Extent* e : {&ed, &eq, &ek, &ev, &eo, &es, &el})
+            if (int rc = refuse_overlap(name, *o, *e)) return rc;
+    if (int rc = refuse_overlap(name, edq, edk)) return rc;
+    if (int rc = refuse_overlap(name, edq, edv)) return rc;
+    if (int rc = refuse_overlap(name, edk, edv)) return rc;
+    for (const Extent* e : {&edq, &edk, &edv})
+        if (int rc = refuse_overlap(name, ew, *e)) return rc;
+    AttentionArgs a{};
+    a.dout = heads_view(dout);
+    a.q = heads_view(q);
+    a.k = heads_view(k);
+    a.v = heads_view(v);
+    a.o = heads_view(out);
+    a.dq = heads_view(dq);
+    a.dk = heads_view(dk);
+    a.dv = heads_view(dv);
+    a.lse = const_cast<float*>(lse);
+    a.along = static_cast<float*>(workspace);
+    if (starts) {
+        if (int rc = attention_flags(&a.status)) return rc;
+        a.starts = static_cast<const int32_t*>(starts->data);
+        a.starts_learner = starts->learner;
+    }
+    a.t = t;
+    a.sequences = sequences;
+    a.heads = heads;
+    a.kv = kv;
+    a.head = head;
+    a.window = window > 0 && window < t ? window : INT32_MAX;      // a window that leaves nothing out is none
+    a.sinks = (int)std::min<int64_t>(sinks, t);
+    a.n = n;
+    a.scale = scale;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return q->type == PSGD_F32 ? backward_of<float>(name, a, s) : backward_of<uint16_t>(name, a, s);
+}
+
+}  // extern "C"

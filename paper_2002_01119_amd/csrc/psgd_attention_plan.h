@@ -16,7 +16,7 @@ inline int held_head(int head) { return head <= 64 ? 64 : head <= 128 ? 128 : 25
 
 // Rows of a workgroup's own, a matrix instruction's 16 columns or two times that for each of its wavefronts, and rows of the tiles that it walks.
 constexpr int kAttentionWaves = 4;
-constexpr int own_blocks(int held, int bytes) { return held * bytes <= 256 ? 2 : 1; }
+constexpr int own_blocks(int held, int bytes) { return bytes == 2 && held <= 128 ? 2 : 1; }
 constexpr int own_rows(int held, int bytes) { return kAttentionWaves * 16 * own_blocks(held, bytes); }
 constexpr int walked_rows(int held, int bytes) { return held * bytes <= 256 ? 64 : 32; }
 

@@ -109,6 +109,7 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
     float top = -INFINITY, sum = 0.0f;
     const float to_log2 = a.scale * kLog2E;
     char* const tile = lds + wave * Lds::kBytes;
+    const uint32_t across_at = lds_address(tile) + Lds::across_lane(lane);
 
     for (int u = u0 + wave * kStepKeys; u < u1; u += kStepWaves * kStepKeys) {
         Eight<T> k[2][S::kSteps];
@@ -157,7 +158,7 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int c = 0; c < S::kCols; ++c) o[c] = mma(Lds::across(tile, c, 0, lane), p, o[c] * less);
+        for (int c = 0; c < S::kCols; ++c) o[c] = mma(Lds::across(across_at, c, 0), p, o[c] * less);
     }
     sum = column_all<Sum>(sum);
     // the wavefronts' parts, in order: [wave][16 heads][H], then maxima and sums

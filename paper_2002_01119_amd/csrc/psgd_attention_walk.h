@@ -1,0 +1,181 @@
+// What attention's forward and backward kernels share (gfx950): a call's arguments, which tile a workgroup has, and how the tiles that it walks get to LDS.
+#ifndef PSGD_ATTENTION_WALK_H
+#define PSGD_ATTENTION_WALK_H
+
+#include <algorithm>
+#include <initializer_list>
+#include <type_traits>
+
+#include "psgd_attention_core.h"
+
+namespace psgd {
+
+// The device's word that kernels raise bit 1 of psgd_device_status() in.
+int attention_flags(int** word);
+
+namespace {
+
+constexpr int kAttentionFlag = 2;
+
+struct AttentionArgs {
+    HeadsView q, k, v, o, dout, dq, dk, dv;
+    float *lse, *along;          // [n, heads, t]; along: D
+    const int32_t* starts;
+    int64_t starts_learner, t, first, total, places;      // first, total: workgroups of this launch and of all
+    int* status;
+    int sequences, heads, kv, head, window, sinks, n;      // no window: the largest number
+    float scale;
+};
+
+// Which learner, head and tile a workgroup has.  Workgroups that read the same keys follow each other on one die: dies take workgroups in turn, so where
+// the pairs of learner and key head are a multiple of eight each die keeps its own.
+struct Work {
+    int learner, kv_head, member, lo, hi, tile;      // member: of the heads that share the key head; lo, hi: the sequence's rows
+    bool there;
+};
+template <int ROWS> __device__ __forceinline__ Work find_work(const AttentionArgs& a, int members, bool last_first) {
+    const int64_t id = a.first + blockIdx.x, inner = members * a.places;
+    const int units = a.n * a.kv;
+    int64_t unit, in;
+    if (units % 8 == 0) {
+        unit = id / (8 * inner) * 8 + id % 8;
+        in = id / 8 % inner;
+    } else {
+        unit = id / inner;
+        in = id % inner;
+    }
+    Work w{(int)(unit / a.kv), (int)(unit % a.kv), (int)(in % members), 0, (int)a.t, 0, true};
+    int64_t place = in / members;
+    if (last_first) place = a.places - 1 - place;
+    if (!a.starts) {
+        w.tile = (int)place;
+    } else {
+        const int32_t* starts = a.starts + w.learner * a.starts_learner;
+        const int lane = threadIdx.x % kWave, t = (int)a.t;
+        if (place == 0 && in % members == 0 && w.kv_head == 0) {
+            bool bad = false;
+            for (int s = threadIdx.x; s <= a.sequences; s += blockDim.x) bad |= starts[s] < 0 || starts[s] > t || (s > 0 && starts[s] < starts[s - 1]);
+            if (bad) atomicOr(a.status, kAttentionFlag);
+        }
+        // the last sequence whose places start here or before: 64 candidates at a time
+        int lo = 0, hi = a.sequences;          // it is in [lo, hi), if any is
+        while (hi - lo > kWave) {
+            const int mid = lo + (hi - lo) / 2;
+            const int at = std::min(std::max(starts[mid], 0), t);
+            if (at / ROWS + mid <= place) lo = mid;
+            else hi = mid;
+        }
+        const int s = lo + lane, at = s < hi ? std::min(std::max(starts[s], 0), t) : 0;
+        const int found = __popcll(__ballot(s < hi && at / ROWS + s <= place)) - 1;
+        if (found < 0) {
+            w.there = false;
+            return w;
+        }
+        const int seq = lo + found;
+        w.lo = std::min(std::max(starts[seq], 0), t);
+        w.hi = std::min(std::max(starts[seq + 1], 0), t);
+        w.tile = (int)(place - (w.lo / ROWS + seq));
+    }
+    w.there = w.tile >= 0 && (int64_t)w.tile * ROWS < w.hi - w.lo;
+    return w;
+}
+
+// Brings a tile, rows row0 ... of a sequence (its first row `seq`, `len` rows), from memory to LDS.  DIRECT: straight there, 16 bytes a lane, which takes rows
+// and heads that start and end on 16 bytes; rows behind the sequence's last are that one again, which p = 0 leaves out.  Else through registers, any element
+// alignment, rows behind the last as zero.  `fetch` starts what a tile needs, `land` ends it: after the workgroup's next meeting the tile is there.
+template <typename T, int H, int ROWS, int THREADS, bool DIRECT> struct Mover {
+    using Lds = Tile<T, H, ROWS>;
+    static constexpr int kEach = ROWS * Lds::kGroups / THREADS;
+    static_assert(ROWS * Lds::kGroups % THREADS == 0, "every lane moves as much");
+    u32x4 held[DIRECT ? 1 : kEach];
+    __device__ __forceinline__ void fetch(char* tile, const T* seq, int64_t row_stride, int row0, int len, int head, bool whole) {
+        if constexpr (DIRECT) {
+            const char* const from = reinterpret_cast<const char*>(seq + row0 * row_stride);
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), stride = (int)row_stride * (int)sizeof(T), last = len - 1 - row0;
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(tile)) + wave * kWave * 16;
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int slot = threadIdx.x + j * THREADS, row = slot / Lds::kGroups, group = slot % Lds::kGroups ^ Lds::turn(row);
+                const uint32_t off = std::min(row, last) * stride + group * 16;
+                // written out, since the compiler would wait for it before the next read across a tile, whichever tile that is
+                if (group * kPer<T> < head) asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to + j * THREADS * 16), "v"(off), "s"(from) : "memory");
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int at = threadIdx.x + j * THREADS, row = row0 + at / Lds::kGroups, col = at % Lds::kGroups * kPer<T>;
+                held[j] = load_group(seq + row * row_stride + col, row < len ? head - col : 0, whole);
+            }
+        }
+    }
+    __device__ __forceinline__ void land(char* tile) const {
+        if constexpr (DIRECT) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        } else {
+#pragma unroll
+            for (int j = 0; j < kEach; ++j) {
+                const int at = threadIdx.x + j * THREADS;
+                Lds::put(tile, at / Lds::kGroups, at % Lds::kGroups, held[j]);
+            }
+        }
+    }
+};
+// Columns behind the head's, which DIRECT never writes, are zero.
+template <int THREADS> __device__ __forceinline__ void clear_lds(char* lds, int bytes) {
+    for (int i = threadIdx.x * 16; i < bytes; i += THREADS * 16) *reinterpret_cast<u32x4*>(lds + i) = (u32x4){0, 0, 0, 0};
+    __syncthreads();
+}
+
+// Tiles of keys that a tile of queries sees: those of the first tokens, then from the window on.
+struct KeyWalk {
+    int sink_tiles, first, count;
+    __device__ __forceinline__ KeyWalk(int row0, int row1, int window, int sinks, int rows) {      // queries [row0, row1)
+        const int from = std::max(0, row0 - window + 1) / rows, to = (row1 + rows - 1) / rows;
+        sink_tiles = std::min((sinks + rows - 1) / rows, from);
+        first = from;
+        count = sink_tiles + to - from;
+    }
+    __device__ __forceinline__ int tile(int step) const { return step < sink_tiles ? step : first + step - sink_tiles; }
+};
+__device__ __forceinline__ bool sees(int i, int j, int window, int sinks) { return ((uint32_t)(i - j) < (uint32_t)window) | ((j < sinks) & (j <= i)); }
+// Whether rows [i0, i1] see all, and whether any of them sees one, of [j0, j1].
+__device__ __forceinline__ bool all_see(int i0, int i1, int j0, int j1, int window, int sinks) { return j1 <= i0 && (i1 - j0 < window || j1 < sinks); }
+__device__ __forceinline__ bool any_sees(int i0, int i1, int j0, int j1, int window, int sinks) { return j0 <= i1 && (i0 - j1 < window || j0 < sinks); }
+
+constexpr float kLag = 8.0f;
+
+template <typename T, int H> struct Shape {
+    static constexpr int kOwnBlocks = own_blocks(H, sizeof(T)), kOwn = own_rows(H, sizeof(T)), kWalked = walked_rows(H, sizeof(T));
+    static constexpr int kThreads = kAttentionWaves * kWave, kBlocks = kWalked / 16, kSteps = H / 32, kCols = H / 16;
+    static constexpr int kTwice = H * sizeof(T) < 1024 ? 2 : 1;      // workgroups of a compute unit, which its registers are shared out to
+    using Lds = Tile<T, H, kWalked>;
+};
+
+template <typename T, int H> constexpr size_t kTileLds = 4 * (size_t)Tile<T, H, walked_rows(H, sizeof(T))>::kBytes;
+using AttentionKernel = void (*)(AttentionArgs);
+
+// Whether tiles of these operands can go straight to LDS: heads and rows on 16 bytes, a tile within 31 bits.
+template <typename T, int H> bool straight(int head, std::initializer_list<HeadsView> operands) {
+    if (head % kPer<T>) return false;
+    for (const HeadsView& v : operands)
+        if (reinterpret_cast<uintptr_t>(v.p) % 16 || v.learner % kPer<T> || v.row % kPer<T> || v.row * 256 > INT32_MAX / 4) return false;
+    return true;
+}
+
+inline int check_shape(const char* name, int heads, int kv, int head, int window, int sinks, float scale, int sequences, const psgd_view* starts, int n, int64_t t) {
+    if (heads < 1 || kv < 1 || heads % kv) return fail(PSGD_EINVAL, "%s: kv=%d does not divide heads=%d", name, kv, heads);
+    if (head < 1 || head > PSGD_MAX_HEAD) return fail(PSGD_EINVAL, "%s: head=%d outside 1..%d", name, head, (int)PSGD_MAX_HEAD);
+    if (int rc = check_counts(name, n, t, (int64_t)heads * head)) return rc;
+    if (window < 0 || sinks < 0 || (sinks && !window)) return fail(PSGD_EINVAL, "%s: window=%d with sinks=%d", name, window, sinks);
+    if (!std::isfinite(scale)) return fail(PSGD_EINVAL, "%s: scale=%g", name, (double)scale);
+    if (sequences < 0 || (sequences > 0) != (starts != nullptr)) return fail(PSGD_EINVAL, "%s: sequences=%d %s starts", name, sequences, starts ? "with" : "without");
+    if (starts && starts->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: starts must be int32", name);
+    // a row's number and a tile's end are counted in 32 bits, and so are all learners' heads
+    if (t > INT32_MAX - 1024 || (int64_t)n * heads > INT32_MAX || sequences > INT32_MAX - 1024 || (double)n * heads * ((double)t + sequences) > 1e15)
+        return fail(PSGD_EINVAL, "%s: a size beyond 2^31 - 1", name);
+    return PSGD_OK;
+}
+
+}  // namespace
+}  // namespace psgd
+#endif
