@@ -20,7 +20,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     using Lds = typename S::Lds;
     extern __shared__ __attribute__((aligned(16))) char lds[];       // two of keys, two of values
     const int members = a.heads / a.kv;
-    const Work w = find_work<S::kOwn>(a, members, true);
+    const Work w = find_work<S::kOwn>(a, a.first + blockIdx.x, members, true);
     if (!w.there) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo;
     const int h = w.kv_head * members + w.member, row0 = w.tile * S::kOwn, row1 = std::min(row0 + S::kOwn, len);

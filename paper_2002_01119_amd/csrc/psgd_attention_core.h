@@ -191,6 +191,10 @@ template <typename T> __device__ __forceinline__ void store_four(T* row, int col
     }
 }
 
+__device__ __forceinline__ void wave_meets() {       // LDS that lanes of one wavefront exchange
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 __device__ __forceinline__ float exp_2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;

@@ -16,7 +16,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     using Lds = typename S::Lds;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int members = a.heads / a.kv;
-    const Work w = find_work<S::kOwn>(a, members, true);
+    const Work w = find_work<S::kOwn>(a, a.first + blockIdx.x, members, true);
     if (!w.there) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo;
     const int h = w.kv_head * members + w.member, row0 = w.tile * S::kOwn, row1 = std::min(row0 + S::kOwn, len);
@@ -144,10 +144,46 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
 
 // dk and dv.  Keys stay in registers and values there or in LDS; the queries that see them and their gradients are walked, one head that shares the key
 // head after the other, with lse and D of a tile's rows beside it.
+
+// The tiles of queries that a tile of keys is walked over, from its own on to the last that the window leaves it, for each head that shares the key head;
+// and the parts that they are cut into.
+struct QueryWalk {
+    int first, tiles, count, parts, each;
+    __device__ __forceinline__ QueryWalk(const AttentionArgs& a, int key0, int key1, int len, int tile, int rows) {
+        first = key0 / rows;
+        const int64_t behind = key0 < a.sinks ? len : std::min((int64_t)len, (int64_t)key1 - 1 + a.window);
+        tiles = (int)((behind + rows - 1) / rows) - first;
+        count = tiles * (a.heads / a.kv);
+        const bool one_of_first = tile < a.first_tiles;
+        parts = std::min(one_of_first ? a.first_parts : a.most_parts, (count - 1) / (one_of_first ? a.first_steps : a.part_steps) + 1);
+        each = (count + parts - 1) / parts;
+        parts = (count + each - 1) / each;
+    }
+};
+// A part's sums: dk's rows of H columns, then dv's.
+template <int H, int OWN> __device__ __forceinline__ float* part_of(const AttentionArgs& a, const Work& w, int part) {
+    const int64_t unit = (int64_t)w.learner * a.kv + w.kv_head;
+    const int64_t slot = w.tile < a.first_tiles ? (a.n * a.kv) * a.part_slots + unit * a.first_slots + ((int64_t)w.sequence * a.first_tiles + w.tile) * a.first_parts + part
+                                                : unit * a.part_slots + w.place * a.most_parts + part;
+    return a.parts + slot * (2 * OWN * H);
+}
+// Tile and part of workgroup `id` of those that have the first tiles of each sequence.
+template <int OWN> __device__ __forceinline__ Work first_work(const AttentionArgs& a, int64_t id, int parts) {
+    const int64_t each = (int64_t)a.first_tiles * parts, of_unit = each * std::max(1, a.sequences), unit = id / of_unit;
+    Work w{(int)(unit / a.kv), (int)(unit % a.kv), (int)(id % parts), 0, (int)a.t, (int)(id / parts % a.first_tiles), true, (int)(id % of_unit / each), 0};
+    if (a.starts) {
+        const int32_t* const starts = a.starts + w.learner * a.starts_learner + w.sequence;
+        w.lo = std::min(std::max(starts[0], 0), (int)a.t);
+        w.hi = std::min(std::max(starts[1], 0), (int)a.t);
+    }
+    w.there = w.tile * OWN < w.hi - w.lo;
+    return w;
+}
+
 template <typename T, int H> struct KeyShape : Shape<T, H> {
     // 128 columns in bf16: keys and both gradients are 160 registers, and with the values' 32 two workgroups would not fit a compute unit
-    static constexpr bool kValuesInLds = sizeof(T) == 2 && H == 128;
-    static constexpr int kRows = kValuesInLds ? 32 : Shape<T, H>::kWalked;
+    static constexpr bool kValuesInLds = values_in_lds(H, sizeof(T));
+    static constexpr int kRows = query_rows(H, sizeof(T));
     static constexpr int kTwice = sizeof(T) == 2 && H <= 128 ? 2 : 1;
     using Lds = Tile<T, H, kRows>;
     using Own = Tile<T, H, Shape<T, H>::kOwn>;
@@ -158,10 +194,14 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     using S = KeyShape<T, H>;
     using Lds = typename S::Lds;
     extern __shared__ __attribute__((aligned(16))) char lds[];       // two of queries and gradients, values, two of [2][rows] statistics
-    const Work w = find_work<S::kOwn>(a, 1, false);
-    if (!w.there) return;
+    const int64_t id = a.first + blockIdx.x;
+    const Work w = id < a.firsts ? first_work<S::kOwn>(a, id, a.first_parts) : find_work<S::kOwn, true>(a, id - a.firsts, a.most_parts, false);
+    if (!w.there || (id >= a.firsts && w.tile < a.first_tiles)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo, members = a.heads / a.kv;
     const int key0 = w.tile * S::kOwn, key1 = std::min(key0 + S::kOwn, len);
+    const QueryWalk walk(a, key0, key1, len, w.tile, S::kRows);
+    if (w.member >= walk.parts) return;
+    const int step0 = w.member * walk.each, step1 = std::min(step0 + walk.each, walk.count);
     const bool whole = a.head % kPer<T> == 0;
     const int mine = key0 + wave * 16 * S::kOwnBlocks;               // the wavefront's first key
     // In bf16 p = exp2(to_log2 (q . k - lse / scale)): the products' sums start from -lse / scale, and those of dout . v from -D, which leaves two operations
@@ -193,14 +233,10 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
 #pragma unroll
         for (int c = 0; c < S::kCols; ++c) dk[b][c] = dv[b][c] = (f32x4){0, 0, 0, 0};
     }
-    // the tiles of queries: from the keys' own on, to the last that the window leaves them
-    const int first = key0 / S::kRows;
-    const int64_t behind = key0 < a.sinks ? len : std::min((int64_t)len, (int64_t)key1 - 1 + a.window);
-    const int tiles = (int)((behind + S::kRows - 1) / S::kRows) - first, count = tiles * members;
     float held[2];
     auto fetch = [&](int step) {
         char* const tile = lds + (step & 1) * 2 * Lds::kBytes;
-        const int h = w.kv_head * members + step / tiles, row0 = (first + step % tiles) * S::kRows, row = row0 + threadIdx.x;
+        const int h = w.kv_head * members + step / walk.tiles, row0 = (walk.first + step % walk.tiles) * S::kRows, row = row0 + threadIdx.x;
         mq.fetch(tile, at<T>(a.q, w.learner, w.lo, (int64_t)h * a.head), a.q.row, row0, len, a.head, whole);
         md.fetch(tile + Lds::kBytes, at<T>(a.dout, w.learner, w.lo, (int64_t)h * a.head), a.dout.row, row0, len, a.head, whole);
         const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo + row;
@@ -216,17 +252,17 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
             stats[(buffer * 2 + 1) * S::kRows + threadIdx.x] = held[1];
         }
     };
-    fetch(0);
-    land(0);
+    fetch(step0);
+    land(step0 & 1);
     __syncthreads();
     uint32_t along_at = lds_address(lds) + Lds::along_lane(lane), across_at = lds_address(lds) + Lds::across_lane(lane);
     uint32_t value_at = lds_address(lds) + S::kTiles + S::Own::along_lane(lane) + wave * 16 * S::kOwnBlocks * S::Own::kGroups * 16;
-    for (int step = 0; step < count; ++step) {
-        const int row0 = (first + step % tiles) * S::kRows;
+    for (int step = step0; step < step1; ++step) {
+        const int row0 = (walk.first + step % walk.tiles) * S::kRows;
         asm("" : "+v"(along_at), "+v"(across_at), "+v"(value_at));      // each read's own address is made from these where it is wanted: kept, they would take a third of the registers
         const uint32_t buffer = (step & 1) * 2 * Lds::kBytes;
         const float* st = stats + (step & 1) * 2 * S::kRows;
-        if (DIRECT && step + 1 < count) fetch(step + 1);
+        if (DIRECT && step + 1 < step1) fetch(step + 1);
         if (mine < len && any_sees(row0, row0 + S::kRows - 1, mine, mine + 16 * S::kOwnBlocks - 1, a.window, a.sinks)) {
             const bool full = all_see(row0, row0 + S::kRows - 1, mine, mine + 16 * S::kOwnBlocks - 1, a.window, a.sinks);
 #pragma unroll
@@ -294,11 +330,24 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                 }
             }
         }
-        if (step + 1 < count) {
+        if (step + 1 < step1) {
             if (!DIRECT) fetch(step + 1);
             land(~step & 1);
         }
         __syncthreads();
+    }
+    if (walk.parts > 1) {
+        float* const part = part_of<H, S::kOwn>(a, w, w.member);
+#pragma unroll
+        for (int b = 0; b < S::kOwnBlocks; ++b) {
+            float* const to = part + (wave * 16 * S::kOwnBlocks + 16 * b + col) * H + 4 * g;
+#pragma unroll
+            for (int c = 0; c < S::kCols; ++c) {
+                *reinterpret_cast<f32x4*>(to + 16 * c) = dk[b][c];
+                *reinterpret_cast<f32x4*>(to + S::kOwn * H + 16 * c) = dv[b][c];
+            }
+        }
+        return;
     }
 #pragma unroll
     for (int b = 0; b < S::kOwnBlocks; ++b) {
@@ -311,6 +360,25 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
             store_four(pv, 16 * c + 4 * g, a.head, dv[b][c]);
         }
     }
+}
+
+// Joins the parts of a tile, in order: a workgroup for 1024 of a tile's numbers, which is one load of each lane's from each part.
+template <typename T, int H> __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
+    constexpr int OWN = own_rows(H, sizeof(T));
+    const int64_t id = a.first + blockIdx.x;
+    const Work w = id < a.firsts ? first_work<OWN>(a, id, a.split) : find_work<OWN>(a, id - a.firsts, a.split, false);
+    if (!w.there || (id >= a.firsts && w.tile < a.first_tiles)) return;
+    const int key0 = w.tile * OWN, len = w.hi - w.lo;
+    const QueryWalk walk(a, key0, std::min(key0 + OWN, len), len, w.tile, query_rows(H, sizeof(T)));
+    if (walk.parts < 2) return;
+    const int e = (w.member * 256 + threadIdx.x) * 4, which = e / (OWN * H), row = e / H % OWN, col = e % H;
+    if (key0 + row >= len || col >= a.head) return;
+    const float* const from = part_of<H, OWN>(a, w, 0) + e;
+    f32x4 v = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int part = 0; part < walk.parts; ++part) v += *reinterpret_cast<const f32x4*>(from + (int64_t)part * (2 * OWN * H));
+    if (which) store_four(at<T>(a.dv, w.learner, w.lo + key0 + row, (int64_t)w.kv_head * a.head), col, a.head, v);
+    else store_four(at<T>(a.dk, w.learner, w.lo + key0 + row, (int64_t)w.kv_head * a.head), col, a.head, v * a.scale);
 }
 
 template <typename T, int H> int launch_backward(const char* name, AttentionArgs a, hipStream_t s) {
@@ -326,9 +394,17 @@ template <typename T, int H> int launch_backward(const char* name, AttentionArgs
         a.first = first;
         hipLaunchKernelGGL(fq, dim3(groups), dim3(kAttentionWaves * kWave), lds, s, a);
     });
-    in_slices(a.places * a.n * a.kv, [&](int64_t first, unsigned groups) {
+    const int64_t tiles = a.places * a.n * a.kv, first_tiles = (int64_t)std::max(1, a.sequences) * a.first_tiles * a.n * a.kv;
+    a.firsts = first_tiles * a.first_parts;
+    in_slices(a.firsts + tiles * a.most_parts, [&](int64_t first, unsigned groups) {
         a.first = first;
         hipLaunchKernelGGL(fkv, dim3(groups), dim3(kAttentionWaves * kWave), more, s, a);
+    });
+    a.split = 2 * own_rows(H, sizeof(T)) * H / 1024;
+    a.firsts = first_tiles * a.split;
+    in_slices(a.firsts + (a.most_parts > 1 ? tiles * a.split : 0), [&](int64_t first, unsigned groups) {
+        a.first = first;
+        hipLaunchKernelGGL((attention_join_kernel<T, H>), dim3(groups), dim3(256), 0, s, a);
     });
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);
@@ -347,9 +423,11 @@ template <typename T> int backward_of(const char* name, const AttentionArgs& a, 
 extern "C" {
 
 size_t psgd_attention_grad_workspace(int heads, int kv, int head, int window, int sinks, int sequences, int n, int64_t t) {
-    (void)kv, (void)head, (void)window, (void)sinks, (void)sequences;
-    if (n < 1 || n > PSGD_MAX_N || t < 1 || t > INT32_MAX || heads < 1) return 0;
-    return psgd::up256((size_t)n * heads * t * sizeof(float));
+    using namespace psgd;
+    if (n < 1 || n > PSGD_MAX_N || t < 1 || t > INT32_MAX || heads < 1 || kv < 1 || heads % kv || head < 1 || head > PSGD_MAX_HEAD || sequences < 0) return 0;
+    size_t most = 0;             // of either type
+    for (int bytes : {2, 4}) most = std::max(most, key_parts(heads, kv, head, bytes, window, sinks, sequences, n, t).bytes(n * kv));
+    return up256((size_t)n * heads * t * sizeof(float)) + most;
 }
 
 int psgd_attention_grad(const psgd_view* dout, const psgd_view* q, const psgd_view* k, const psgd_view* v, const psgd_view* out, const float* lse,
@@ -364,27 +442,37 @@ int psgd_attention_grad(const psgd_view* dout, const psgd_view* q, const psgd_vi
         if (!float_type(x->type) || x->type != q->type) return fail(PSGD_EINVAL, "%s: dout, q, k, v, out, dq, dk and dv must be float or bf16 alike", name);
     if (t == 0) return PSGD_OK;
     if (!lse) return fail(PSGD_EINVAL, "%s: lse is needed", name);
-    const size_t need = psgd_attention_grad_workspace(heads, kv, head, window, sinks, sequences, n, t);
     psgd_view vl, vw;
     const int64_t cq = (int64_t)heads * head, ck = (int64_t)kv * head;
     const Extent ed{"dout", dout, n, t, cq}, eq{"q", q, n, t, cq}, ek{"k", k, n, t, ck}, ev{"v", v, n, t, ck}, eo{"out", out, n, t, cq},
         es{"starts", starts ? starts : q, n, 1, starts ? (int64_t)sequences + 1 : 0}, el = flat("lse", lse, (int64_t)n * heads * t, &vl),
-        edq{"dq", dq, n, t, cq}, edk{"dk", dk, n, t, ck}, edv{"dv", dv, n, t, ck}, ew = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+        edq{"dq", dq, n, t, cq}, edk{"dk", dk, n, t, ck}, edv{"dv", dv, n, t, ck};
     for (const Extent* e : {&ed, &eq, &ek, &ev, &eo, &es, &el})
         if (int rc = check_operand(name, *e, false)) return rc;
     for (const Extent* e : {&edq, &edk, &edv})
         if (int rc = check_operand(name, *e, true)) return rc;
-    if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)
-        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
-    for (const Extent* o : {&edq, &edk, &edv, &ew})
+    for (const Extent* o : {&edq, &edk, &edv})
         for (const Extent* e : {&ed, &eq, &ek, &ev, &eo, &es, &el})
             if (int rc = refuse_overlap(name, *o, *e)) return rc;
     if (int rc = refuse_overlap(name, edq, edk)) return rc;
     if (int rc = refuse_overlap(name, edq, edv)) return rc;
     if (int rc = refuse_overlap(name, edk, edv)) return rc;
-    for (const Extent* e : {&edq, &edk, &edv})
+    const KeyParts parts = key_parts(heads, kv, head, elem_bytes(q->type), window, sinks, sequences, n, t);
+    const size_t stats = up256((size_t)n * heads * t * sizeof(float)), need = stats + parts.bytes(n * kv);
+    if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256)
+        return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);
+    const Extent ew = flat("the workspace", workspace, (int64_t)(need / 4), &vw);
+    for (const Extent* e : {&ed, &eq, &ek, &ev, &eo, &es, &el, &edq, &edk, &edv})
         if (int rc = refuse_overlap(name, ew, *e)) return rc;
     AttentionArgs a{};
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats);
+    a.most_parts = parts.most;
+    a.part_steps = parts.steps;
+    a.part_slots = parts.slots;
+    a.first_tiles = parts.first_tiles;
+    a.first_parts = parts.first_most;
+    a.first_steps = parts.first_steps;
+    a.first_slots = parts.first_slots;
     a.dout = heads_view(dout);
     a.q = heads_view(q);
     a.k = heads_view(k);

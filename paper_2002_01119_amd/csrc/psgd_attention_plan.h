@@ -11,6 +11,9 @@
 
 namespace psgd {
 
+// Compute units that parts are made for: the whole accelerator's, whatever the device has, so that a workspace's size and the order of sums are the same on any.
+constexpr int kChipUnits = 256;
+
 // A head's columns as the kernels hold them: the rest is zero.
 inline int held_head(int head) { return head <= 64 ? 64 : head <= 128 ? 128 : 256; }
 
@@ -24,12 +27,62 @@ constexpr int walked_rows(int held, int bytes) { return held * bytes <= 256 ? 64
 // tiles whatever their lengths, so that a workgroup finds its sequence by itself and no launch depends on device memory.
 inline int64_t tile_places(int64_t t, int sequences, int rows) { return t / rows + (sequences > 0 ? sequences : 1); }
 
+// ------------------------------------------------------------------------------------------------ dk and dv
+// A tile of keys is walked by one workgroup, query head after query head; how many steps (tiles of queries) that are is seen on the device.  Where that leaves
+// compute units idle a tile's steps are cut into parts, whose sums a second kernel joins in order: all tiles' where there are few of them, and the first
+// tokens' that stay visible, which every query sees while the window spares the others most.
+constexpr bool values_in_lds(int held, int bytes) { return bytes == 2 && held == 128; }
+constexpr int query_rows(int held, int bytes) { return values_in_lds(held, bytes) ? 32 : walked_rows(held, bytes); }
+
+struct KeyParts {
+    int most, steps;                               // parts of a tile at most, and steps that a part has at least
+    int first_tiles, first_most, first_steps;      // of the first tiles of a sequence (so many), if they are cut apart from the others
+    int64_t slots, first_slots;                    // of parts, of each learner's key head
+    size_t slot_bytes;
+    size_t bytes(int64_t units) const { return up256((size_t)(slots + first_slots) * units * slot_bytes); }
+};
+inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window, int64_t sinks, int sequences, int n, int64_t t) {
+    constexpr int cus = kChipUnits;
+    const int held = held_head(head), own = own_rows(held, bytes), rows = query_rows(held, bytes), members = heads / kv;
+    const int64_t units = (int64_t)n * kv;
+    const bool narrow = window > 0 && window < t;
+    const int64_t tiles = parts_of(t, own) * units, places = tile_places(t, sequences, own);
+    const int64_t most_steps = (parts_of(narrow && window + own < t ? window + own : t, rows) + 1) * members;      // of a tile that is not a first one
+    const int64_t all = tiles * (narrow ? most_steps : (most_steps + 1) / 2);
+    KeyParts p{1, 1, 0, 1, 1, 0, 0, 2 * (size_t)own * held * sizeof(float)};
+    // Two rounds of what is resident, and no less than 16 steps: writing a part and reading it again takes as long as five.
+    if (tiles < (narrow ? 2 : 4) * (int64_t)cus) {
+        const int64_t fair = parts_of(all, 4 * (int64_t)cus), steps = fair > 16 ? fair : 16;
+        int64_t most = parts_of(most_steps, steps);
+        while (most > 1 && places * units * most > 16 * (int64_t)cus) --most;
+        p.most = (int)most;
+        p.steps = (int)(steps < 1 << 30 ? steps : 1 << 30);
+        p.slots = most > 1 ? places * most : 0;
+    }
+    if (narrow && sinks > 0) {
+        // an eighth of what the others take, since they are few and the last to end; no more than 256 MB
+        const int64_t first_steps = (parts_of(t, rows) + 1) * members, steps = most_steps / 8 > 16 ? most_steps / 8 : 16;
+        const int64_t first_tiles = parts_of(sinks < t ? sinks : t, own), slots = (sequences > 0 ? sequences : 1) * first_tiles;
+        const int64_t room = ((int64_t)256 << 20) / ((int64_t)p.slot_bytes * units * slots), most = parts_of(first_steps, steps);
+        p.first_most = (int)(most < room ? most : room > 1 ? room : 1);
+        if (p.first_most > 1) {
+            p.first_tiles = (int)first_tiles;
+            p.first_steps = (int)(steps < 1 << 30 ? steps : 1 << 30);
+            p.first_slots = slots * p.first_most;
+        }
+    }
+    return p;
+}
+
 // ------------------------------------------------------------------------------------------------ one new token
-constexpr int kStepWaves = 4;
 constexpr int kStepKeys = 32;               // of a wavefront at a time
-// Parts that a sequence's keys are cut into.
-inline int step_parts(int64_t units, int64_t most_keys, int cus) {
-    const int64_t most = parts_of(most_keys, kStepWaves * kStepKeys * 2), fair = parts_of((int64_t)cus * 4, units);
+// A wavefront has `stages` tiles of 32 keys and values in LDS, 128 KB of them in a workgroup: one workgroup a compute unit, with 64 KB or more on their way,
+// three times what the memory's latency takes.
+constexpr int step_waves(int held, int bytes) { return held * bytes <= 256 ? 4 : held * bytes == 512 ? 2 : 1; }
+constexpr int step_stages(int held, int bytes) { return held * bytes == 128 ? 4 : 2; }
+// Parts that a sequence's keys are cut into: two workgroups a compute unit, and no fewer keys than two tiles a wavefront.
+inline int step_parts(int64_t units, int64_t most_keys, int head, int bytes) {
+    const int64_t most = parts_of(most_keys, step_waves(held_head(head), bytes) * kStepKeys * 2), fair = parts_of(2 * kChipUnits, units);
     const int64_t p = most < fair ? most : fair;
     return (int)(p < 1 ? 1 : p > 1024 ? 1024 : p);
 }

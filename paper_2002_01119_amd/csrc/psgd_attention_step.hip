@@ -1,9 +1,10 @@
 // Attention of one new token of each sequence against its cache, which takes the token's key and value (gfx950).
 //
 // What counts is that the cache is read once: 2 kv head values a position against 4 heads head operations.  A workgroup has one key head of one sequence
-// and a part of its positions; its four wavefronts take 32 positions each in turn and meet only at the end.  The query heads that share the key head
-// are the columns of the matrix products, 16 at most at a time.  Keys come from memory as the first product's operand; values go through the wavefront's own
-// tile in LDS, to be read across.  Where a sequence is cut into parts, each leaves its maximum, sum and output and a second kernel joins them in order.
+// and a part of its positions; its wavefronts take 32 positions each in turn and meet only at the end.  Keys and values go straight from memory to the
+// wavefront's own tiles in LDS, the next ones while these are worked on, so no register waits for them.  The query heads that share the key head
+// are the columns of the matrix products, 16 at most at a time.  Where a sequence is cut into parts, each leaves its maximum, sum and output and a second kernel
+// joins them in order.
 //
 // The new key and value are taken from where they come from, not from the cache, which one workgroup of the last part writes: nobody waits for it, and what the
 // slot held before is a position that the window has left.
@@ -56,21 +57,23 @@ struct Seen {
 };
 
 template <typename T, int H> struct StepShape {
-    static constexpr int kSteps = H / 32, kCols = H / 16;
+    static constexpr int kSteps = H / 32, kCols = H / 16, kWaves = step_waves(H, sizeof(T)), kStages = step_stages(H, sizeof(T));
     using Lds = Tile<T, H, kStepKeys>;
-    static constexpr int kMoves = kStepKeys * Lds::kGroups / kWave;      // 16-byte groups of a tile of values that a lane moves
-    static constexpr size_t kTiles = (size_t)kStepWaves * Lds::kBytes, kJoin = (size_t)kStepWaves * 16 * (H + 2) * sizeof(float);
+    static constexpr int kMoves = kStepKeys * Lds::kGroups / kWave;      // 16-byte groups of a tile that a lane moves
+    static constexpr size_t kTiles = (size_t)kWaves * kStages * 2 * Lds::kBytes, kJoin = (size_t)kWaves * 16 * (H + 2) * sizeof(float);
     static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
 };
 
-template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) void step_kernel(StepArgs a) {
+// DIRECT: tiles go straight to LDS, which takes heads and rows that start and end on 16 bytes; else through registers, one tile at a time.
+template <typename T, int H, bool DIRECT> __global__ __launch_bounds__((StepShape<T, H>::kWaves * kWave)) void step_kernel(StepArgs a) {
     using S = StepShape<T, H>;
     using Lds = typename S::Lds;
+    constexpr int THREADS = S::kWaves * kWave, STRIDE = S::kWaves * kStepKeys;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t id = a.first + blockIdx.x, unit = id / a.parts;
     const int part = (int)(id % a.parts), block = (int)(unit % a.blocks), kv = (int)(unit / a.blocks % a.kv);
     const int64_t pair = unit / a.blocks / a.kv, i = pair / a.b, r = pair % a.b;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col = lane % 16, g = lane / 16;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16;
     const int members = a.heads / a.kv, member = 16 * block + col, h = kv * members + member;
     const bool whole = a.head % kPer<T> == 0;
     const int length = a.lengths[i * a.lengths_learner + r * a.lengths_row];
@@ -91,40 +94,73 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
     T* const cv = reinterpret_cast<T*>(a.cv.p) + i * a.cv.learner + r * a.cv.sequence + (int64_t)kv * a.head;
     if (block == 0 && part == a.parts - 1) {
         const int64_t slot = seen.slot(length);
-        for (int c = threadIdx.x; c < a.head; c += kStepWaves * kWave) {
+        for (int c = threadIdx.x; c < a.head; c += THREADS) {
             ck[slot * a.ck.row + c] = nk[c];
             cv[slot * a.cv.row + c] = nv[c];
         }
     }
-    auto key_row = [&](int u) { const int p = seen.position(u); return p == length ? nk : ck + (int64_t)seen.slot(p) * a.ck.row; };
-    auto value_row = [&](int u) { const int p = seen.position(u); return p == length ? nv : cv + (int64_t)seen.slot(p) * a.cv.row; };
 
     Eight<T> q[S::kSteps];
     f32x4 o[S::kCols];
     const T* const pq = at<T>(a.q, i, r, (int64_t)h * a.head);
 #pragma unroll
-    for (int kc = 0; kc < S::kSteps; ++kc) q[kc] = load_eight(pq, kc, g, member < members ? a.head : 0, whole);
+    for (int kc = 0; kc < S::kSteps; ++kc) {
+        q[kc] = load_eight(pq, kc, g, member < members ? a.head : 0, whole);
+        if (a.scale < 0.0f) q[kc] = negative(q[kc]);              // as in the forward pass
+    }
 #pragma unroll
     for (int c = 0; c < S::kCols; ++c) o[c] = (f32x4){0, 0, 0, 0};
     float top = -INFINITY, sum = 0.0f;
-    const float to_log2 = a.scale * kLog2E;
-    char* const tile = lds + wave * Lds::kBytes;
-    const uint32_t across_at = lds_address(tile) + Lds::across_lane(lane);
+    const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f);
+    char* const tiles = lds + wave * S::kStages * 2 * Lds::kBytes;
+    if (DIRECT && a.head < H) {
+        for (int c = threadIdx.x * 16; c < (int)S::kTiles; c += THREADS * 16) *reinterpret_cast<u32x4*>(lds + c) = (u32x4){0, 0, 0, 0};
+        __syncthreads();
+    }
+    const uint32_t base = __builtin_amdgcn_readfirstlane(lds_address(tiles));
 
-    for (int u = u0 + wave * kStepKeys; u < u1; u += kStepWaves * kStepKeys) {
-        Eight<T> k[2][S::kSteps];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int at = u + 16 * kb + col;
-            const T* row = at < u1 ? key_row(at) : nk;
-#pragma unroll
-            for (int kc = 0; kc < S::kSteps; ++kc) k[kb][kc] = load_eight(row, kc, g, at < u1 ? a.head : 0, whole);
-        }
-        u32x4 v[S::kMoves];
+    // The tile of keys and values from u on into a stage.  Rows behind the part's last are that one again: their p is 0.
+    auto fetch = [&](int u, int stage) {
 #pragma unroll
         for (int j = 0; j < S::kMoves; ++j) {
-            const int at = u + (lane + 64 * j) / Lds::kGroups, c = (lane + 64 * j) % Lds::kGroups * kPer<T>;
-            v[j] = load_group((at < u1 ? value_row(at) : nv) + c, at < u1 ? a.head - c : 0, whole);
+            const int slot = lane + 64 * j, row = slot / Lds::kGroups, group = DIRECT ? slot % Lds::kGroups ^ Lds::turn(row) : slot % Lds::kGroups;
+            const int p = seen.position(std::min(u + row, u1 - 1)), c = group * kPer<T>;
+            const int64_t at = seen.slot(p);
+            const T *fk = (p == length ? nk : ck + at * a.ck.row) + c, *fv = (p == length ? nv : cv + at * a.cv.row) + c;
+            if constexpr (DIRECT) {
+                const uint32_t to = base + stage * 2 * Lds::kBytes + j * 1024;
+                if (c < a.head)
+                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %3, off" ::"s"(to), "v"(fk),
+                                 "s"(to + Lds::kBytes), "v"(fv)
+                                 : "memory");
+            } else {
+                Lds::put(tiles, row, group, load_group(fk, a.head - c, whole));
+                Lds::put(tiles + Lds::kBytes, row, group, load_group(fv, a.head - c, whole));
+            }
+        }
+    };
+    const uint32_t along_at = base + Lds::along_lane(lane), across_at = base + Lds::across_lane(lane);
+    if (DIRECT) {
+#pragma unroll
+        for (int st = 0; st + 1 < S::kStages; ++st)
+            if (u0 + wave * kStepKeys + st * STRIDE < u1) fetch(u0 + wave * kStepKeys + st * STRIDE, st);
+    }
+    int stage = 0;
+    for (int u = u0 + wave * kStepKeys; u < u1; u += STRIDE) {
+        const int buffer = DIRECT ? stage * 2 * Lds::kBytes : 0;
+        if constexpr (DIRECT) {
+            const int ahead = u + (S::kStages - 1) * STRIDE, next = stage == 0 ? S::kStages - 1 : stage - 1;
+            // what was fetched last may still be on its way, but no tile before it.  (The stage that is written was read a turn ago, by products that have ended.)
+            if (ahead < u1) {
+                fetch(ahead, next);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(std::min(63, (S::kStages - 1) * 2 * S::kMoves)) : "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            }
+        } else {
+            wave_meets();
+            fetch(u, 0);
+            wave_meets();
         }
         f32x4 s[2];
         float m = -INFINITY;
@@ -132,7 +168,7 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
         for (int kb = 0; kb < 2; ++kb) {
             s[kb] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-            for (int kc = 0; kc < S::kSteps; ++kc) s[kb] = mma(k[kb][kc], q[kc], s[kb]);
+            for (int kc = 0; kc < S::kSteps; ++kc) s[kb] = mma(Lds::along(along_at + buffer, kb, kc), q[kc], s[kb]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 s[kb][e] = u + 16 * kb + 4 * g + e < u1 ? s[kb][e] * to_log2 : -INFINITY;
@@ -151,19 +187,14 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
                 sum += s[kb][e];
             }
         const Eight<T> p = as_operand<T>(s[0], s[1]);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");       // the tile before this one has been read
-        __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int j = 0; j < S::kMoves; ++j) Lds::put(tile, (lane + 64 * j) / Lds::kGroups, (lane + 64 * j) % Lds::kGroups, v[j]);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int c = 0; c < S::kCols; ++c) o[c] = mma(Lds::across(across_at, c, 0), p, o[c] * less);
+        for (int c = 0; c < S::kCols; ++c) o[c] = mma(Lds::across(across_at + buffer + Lds::kBytes, c, 0), p, o[c] * less);
+        stage = stage + 1 == S::kStages ? 0 : stage + 1;
     }
     sum = column_all<Sum>(sum);
     // the wavefronts' parts, in order: [wave][16 heads][H], then maxima and sums
     __syncthreads();
-    float *const all = reinterpret_cast<float*>(lds), *const ml = all + kStepWaves * 16 * H;
+    float *const all = reinterpret_cast<float*>(lds), *const ml = all + S::kWaves * 16 * H;
 #pragma unroll
     for (int c = 0; c < S::kCols; ++c) *reinterpret_cast<f32x4*>(all + ((wave * 16 + col) * H + 16 * c + 4 * g)) = o[c];
     if (g == 0) {
@@ -172,15 +203,15 @@ template <typename T, int H> __global__ __launch_bounds__(kStepWaves* kWave) voi
     }
     __syncthreads();
     const int here = std::min(16, members - 16 * block);
-    for (int e = threadIdx.x; e < here * H; e += kStepWaves * kWave) {
+    for (int e = threadIdx.x; e < here * H; e += THREADS) {
         const int m = e / H, c = e % H;
         float most = ml[m * 2];
 #pragma unroll
-        for (int w = 1; w < kStepWaves; ++w) most = fmaxf(most, ml[(w * 16 + m) * 2]);
+        for (int w = 1; w < S::kWaves; ++w) most = fmaxf(most, ml[(w * 16 + m) * 2]);
         const float safe = most == -INFINITY ? 0.0f : most;
         float total = 0.0f, value = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kStepWaves; ++w) {
+        for (int w = 0; w < S::kWaves; ++w) {
             const float less = exp_2(ml[(w * 16 + m) * 2] - safe);
             total += less * ml[(w * 16 + m) * 2 + 1];
             value += less * all[(w * 16 + m) * H + c];
@@ -220,13 +251,21 @@ template <typename T> __global__ __launch_bounds__(256) void step_join_kernel(St
 }
 
 using StepKernel = void (*)(StepArgs);
+template <typename T> bool step_direct(const StepArgs& a) {
+    for (int64_t x : {(int64_t)a.head, a.k.learner, a.k.row, a.v.learner, a.v.row, a.ck.learner, a.ck.sequence, a.ck.row, a.cv.learner, a.cv.sequence, a.cv.row})
+        if (x % kPer<T>) return false;
+    for (const char* p : {a.k.p, a.v.p, a.ck.p, a.cv.p})
+        if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+    return true;
+}
 template <typename T, int H> int launch_step(const char* name, StepArgs a, int64_t units, int64_t rows, hipStream_t s) {
-    static LdsRecord record = {};
-    const StepKernel fn = step_kernel<T, H>, join = step_join_kernel<T>;
-    if (int rc = allow_lds(reinterpret_cast<const void*>(fn), StepShape<T, H>::kLds, record)) return rc;
+    static LdsRecord record[2] = {};
+    const bool direct = step_direct<T>(a);
+    const StepKernel fn = direct ? step_kernel<T, H, true> : step_kernel<T, H, false>, join = step_join_kernel<T>;
+    if (int rc = allow_lds(reinterpret_cast<const void*>(fn), StepShape<T, H>::kLds, record[direct])) return rc;
     in_slices(units * a.parts, [&](int64_t first, unsigned groups) {
         a.first = first;
-        hipLaunchKernelGGL(fn, dim3(groups), dim3(kStepWaves * kWave), (StepShape<T, H>::kLds), s, a);
+        hipLaunchKernelGGL(fn, dim3(groups), dim3(StepShape<T, H>::kWaves * kWave), (StepShape<T, H>::kLds), s, a);
     });
     if (a.parts > 1)
         in_slices(rows, [&](int64_t first, unsigned groups) {
@@ -312,9 +351,9 @@ extern "C" {
 size_t psgd_attention_step_workspace(int heads, int kv, int head, int window, int sinks, int n, int64_t b, int64_t slots) {
     using namespace psgd;
     clear_error();
-    int cus = 0;
-    if (b < 1 || check_step("psgd_attention_step_workspace", heads, kv, head, window, sinks, n, b, slots) || compute_units(&cus)) return 0;
-    const int parts = step_parts((int64_t)n * b * kv * parts_of(heads / kv, 16), most_seen(window, sinks, slots), cus);
+    if (b < 1 || check_step("psgd_attention_step_workspace", heads, kv, head, window, sinks, n, b, slots)) return 0;
+    int parts = 1;               // of either type
+    for (int bytes : {2, 4}) parts = std::max(parts, step_parts((int64_t)n * b * kv * parts_of(heads / kv, 16), most_seen(window, sinks, slots), head, bytes));
     return parts > 1 ? up256((size_t)n * b * heads * parts * (head + 2) * sizeof(float)) : 0;
 }
 
@@ -346,11 +385,9 @@ int psgd_attention_step(const psgd_view* q, const psgd_view* k, const psgd_view*
     if (caches_meet(*cache_k, *cache_v, n, b, slots, cw)) return fail(PSGD_EALIAS, "%s: cache_k overlaps cache_v", name);
     for (const Extent* e : {&eck, &ecv})
         if (int rc = refuse_overlap(name, *e, eo)) return rc;
-    int cus = 0;
-    if (int rc = compute_units(&cus)) return rc;
     const int blocks = (int)parts_of(heads / kv, 16);
     const int64_t units = (int64_t)n * b * kv * blocks;
-    const int parts = step_parts(units, most_seen(window, sinks, slots), cus);
+    const int parts = step_parts(units, most_seen(window, sinks, slots), head, elem_bytes(q->type));
     const size_t rows = (size_t)n * b * heads, need = parts > 1 ? up256(rows * parts * (head + 2) * sizeof(float)) : 0;
     if (need && (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 256))
         return fail(PSGD_EINVAL, "%s: %zu bytes of workspace are needed, at a multiple of 256", name, need);

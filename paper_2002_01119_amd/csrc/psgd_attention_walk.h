@@ -25,34 +25,46 @@ struct AttentionArgs {
     int* status;
     int sequences, heads, kv, head, window, sinks, n;      // no window: the largest number
     float scale;
+    // dk's and dv's parts (key_parts); firsts: workgroups that have the first tiles' of each sequence; split: workgroups that join a tile
+    float* parts;
+    int most_parts, part_steps, first_tiles, first_parts, first_steps, split;
+    int64_t part_slots, first_slots, firsts;
 };
 
-// Which learner, head and tile a workgroup has.  Workgroups that read the same keys follow each other on one die: dies take workgroups in turn, so where
-// the pairs of learner and key head are a multiple of eight each die keeps its own.
+// Which learner, head and tile a workgroup has.  Workgroups that read the same keys are on one die: dies take workgroups in turn, so where the pairs of
+// learner and key head are a multiple of eight each die keeps its own, and else each takes eight workgroups that follow each other.
 struct Work {
-    int learner, kv_head, member, lo, hi, tile;      // member: of the heads that share the key head; lo, hi: the sequence's rows
+    int learner, kv_head, member, lo, hi, tile;      // member: of the heads that share the key head, or of a tile's parts; lo, hi: the sequence's rows
     bool there;
+    int sequence;
+    int64_t place;
 };
-template <int ROWS> __device__ __forceinline__ Work find_work(const AttentionArgs& a, int members, bool last_first) {
-    const int64_t id = a.first + blockIdx.x, inner = members * a.places;
+// The members of a tile follow each other too, unless they are parts, of which most tiles have only the first: those would all be one die's.
+template <int ROWS, bool PARTS = false> __device__ __forceinline__ Work find_work(const AttentionArgs& a, int64_t id, int members, bool last_first) {
+    const int64_t inner = members * a.places;
     const int units = a.n * a.kv;
     int64_t unit, in;
-    if (units % 8 == 0) {
-        unit = id / (8 * inner) * 8 + id % 8;
-        in = id / 8 % inner;
+    if (PARTS && units % 8 == 0) {
+        unit = id / 8 % (units / 8) * 8 + id % 8;
+        in = id / units;
+    } else if (units % 8 == 0) {
+        unit = id / (8 * members) % (units / 8) * 8 + id % 8;
+        in = id / (units * members) * members + id / 8 % members;
     } else {
-        unit = id / inner;
-        in = id % inner;
+        const int64_t even = inner * units / 64 * 64, at = id < even ? id / 64 * 64 + id % 8 * 8 + id / 8 % 8 : id;
+        unit = at / inner;
+        in = at % inner;
     }
-    Work w{(int)(unit / a.kv), (int)(unit % a.kv), (int)(in % members), 0, (int)a.t, 0, true};
-    int64_t place = in / members;
+    const int member = (int)(PARTS ? in / a.places : in % members);
+    int64_t place = PARTS ? in % a.places : in / members;
     if (last_first) place = a.places - 1 - place;
+    Work w{(int)(unit / a.kv), (int)(unit % a.kv), member, 0, (int)a.t, 0, true, 0, place};
     if (!a.starts) {
         w.tile = (int)place;
     } else {
         const int32_t* starts = a.starts + w.learner * a.starts_learner;
         const int lane = threadIdx.x % kWave, t = (int)a.t;
-        if (place == 0 && in % members == 0 && w.kv_head == 0) {
+        if (place == 0 && member == 0 && w.kv_head == 0) {
             bool bad = false;
             for (int s = threadIdx.x; s <= a.sequences; s += blockDim.x) bad |= starts[s] < 0 || starts[s] > t || (s > 0 && starts[s] < starts[s - 1]);
             if (bad) atomicOr(a.status, kAttentionFlag);
@@ -71,7 +83,7 @@ template <int ROWS> __device__ __forceinline__ Work find_work(const AttentionArg
             w.there = false;
             return w;
         }
-        const int seq = lo + found;
+        const int seq = w.sequence = lo + found;
         w.lo = std::min(std::max(starts[seq], 0), t);
         w.hi = std::min(std::max(starts[seq + 1], 0), t);
         w.tile = (int)(place - (w.lo / ROWS + seq));
