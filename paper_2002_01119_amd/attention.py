@@ -12,6 +12,7 @@ The backward pass takes the same views.  A training step keeps the queries and k
 For serving, attention_step is one new token of each sequence against its cache.  Conventions are those of `layers`: unit stride along the last dimension, any
 strides along the others, outputs are the caller's tensors, work is enqueued on `stream` (None: torch's current stream), a workspace comes from torch's allocator
 or is the caller's.  What the library refuses raises `psgd.PsgdError`, a tensor that is not what a call takes raises ValueError.
+Calls that are plainly in order take the short way of the _call extension, as `layers`' do.
 """
 import ctypes
 
@@ -30,6 +31,7 @@ class Cache(ctypes.Structure):
 
 
 _lib = None
+_ext = None              # the extension, once bound to the library's functions
 
 
 def load():
@@ -57,7 +59,33 @@ def load():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
     _lib = lib
+    _bind()
     return lib
+
+
+def _bind():
+    """Hand the extension, if psgd.py has it, the addresses of the loaded library's functions."""
+    global _ext
+    _ext = None
+    if psgd._call is not None and hasattr(psgd._call, "bind_attention"):
+        psgd._call.bind_attention(*(ctypes.cast(getattr(_lib, name), ctypes.c_void_p).value for name in EXPORTS))
+        _ext = psgd._call
+
+
+def _short(name, *args):
+    """Whether the short way has made the call."""
+    if _ext is None or _lib is not psgd._lib:
+        if _lib is None or psgd._call is None or not hasattr(psgd._call, "bind_attention"):
+            return False
+        load()                   # psgd may have loaded the library again
+        if _ext is None:
+            _bind()
+    return psgd._answered(getattr(_ext, name)(*args))
+
+
+def _rotary(q, heads, rotary):
+    """None: all of a head's columns."""
+    return q.shape[2] // heads if rotary is None and hasattr(q, "shape") and len(q.shape) == 3 and isinstance(heads, int) and heads > 0 else rotary
 
 
 def _head(what, t, heads):
@@ -98,6 +126,8 @@ def _pairs(pairs):
 def qk_norm_rope(q, k, q_out, k_out, heads, kv, positions=None, q_gain=None, k_gain=None, eps=1e-6, rotary=None, base=10000.0, pairs="halves", stream=None):
     """Enqueue the norm of every head of q [n, t, heads * head] and k [n, t, kv * head] (RMS, gains [n, head]; without gains none) and the rotation of the first
     `rotary` columns of each (None: all) by positions [n, t] int32 (None: the row's number).  q_out may be q, k_out may be k."""
+    if _short("qk_norm_rope", q, k, q_out, k_out, heads, kv, positions, q_gain, k_gain, eps, _rotary(q, heads, rotary), base, PAIRS.get(pairs), stream):
+        return
     n, t, head = _head("q", q, heads)
     vq, vk = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head))
     vqo, vko = _view("q_out", q_out, (n, t, heads * head)), _view("k_out", k_out, (n, t, kv * head))
@@ -115,6 +145,9 @@ def qk_norm_rope_grad(dq_out, dk_out, q, k, dq, dk, heads, kv, positions=None, q
                       base=10000.0, pairs="halves", workspace=None, stream=None):
     """Enqueue the backward pass of qk_norm_rope: dq, dk and the gains' gradients ([n, head], float32 or bfloat16 alike) from those of q_out and k_out and
     what went in.  dq may be dq_out, dk may be dk_out.  Without gains q and k may be None."""
+    if workspace is None and _short("qk_norm_rope_grad", dq_out, dk_out, q, k, dq, dk, heads, kv, positions, q_gain, k_gain, dq_gain, dk_gain, eps,
+                                    _rotary(dq_out, heads, rotary), base, PAIRS.get(pairs), stream):
+        return
     n, t, head = _head("dq_out", dq_out, heads)
     vdqo, vdko = _view("dq_out", dq_out, (n, t, heads * head)), _view("dk_out", dk_out, (n, t, kv * head))
     vq, vk = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head))
@@ -135,6 +168,8 @@ def attention(q, k, v, out, heads, kv, lse=None, starts=None, window=0, sinks=0,
     """Enqueue causal attention of q [n, t, heads * head] over k and v [n, t, kv * head] into out, and where `lse` ([n, heads, t] float32) is given the logarithm of
     each row's sum.  starts int32 [n, sequences + 1]: where the sequences begin and the last one ends (None: one of all rows).  window > 0: a row
     sees the last `window` rows up to itself and the first `sinks` of its sequence.  scale None: head ** -0.5."""
+    if _short("attention", q, k, v, out, heads, kv, lse, starts, window, sinks, scale, stream):
+        return
     n, t, head = _head("q", q, heads)
     vq, vk, vv = _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head)), _view("v", v, (n, t, kv * head))
     vo, (vs, sequences) = _view("out", out, (n, t, heads * head)), _starts(starts, n)
@@ -151,6 +186,8 @@ def attention_grad_workspace(heads, kv, head, n, t, window=0, sinks=0, sequences
 
 def attention_grad(dout, q, k, v, out, lse, dq, dk, dv, heads, kv, starts=None, window=0, sinks=0, scale=None, workspace=None, stream=None):
     """Enqueue the backward pass of attention: dq, dk and dv from dout and what attention took and wrote (out and lse)."""
+    if workspace is None and _short("attention_grad", dout, q, k, v, out, lse, dq, dk, dv, heads, kv, starts, window, sinks, scale, stream):
+        return
     n, t, head = _head("q", q, heads)
     vd, vq, vk, vv = _view("dout", dout, (n, t, heads * head)), _view("q", q, (n, t, heads * head)), _view("k", k, (n, t, kv * head)), _view("v", v, (n, t, kv * head))
     vo, (vs, sequences) = _view("out", out, (n, t, heads * head)), _starts(starts, n)
@@ -186,6 +223,8 @@ def attention_step(q, k, v, cache_k, cache_v, lengths, out, heads, kv, window=0,
     """Enqueue attention of one new token of each of b sequences of each learner (q [n, b, heads * head], k and v [n, b, kv * head]) over the caches
     [n, b, slots, kv * head], which take its key and value, into out [n, b, heads * head].  lengths int32 [n, b]: the tokens that each cache has seen, the new
     token's position (negative: no such sequence).  With a window and slots >= sinks + window the caches are rings.  lengths stay as they are."""
+    if workspace is None and _short("attention_step", q, k, v, cache_k, cache_v, lengths, out, heads, kv, window, sinks, scale, stream):
+        return
     n, b, head = _head("q", q, heads)
     vq, vk, vv = _view("q", q, (n, b, heads * head)), _view("k", k, (n, b, kv * head)), _view("v", v, (n, b, kv * head))
     vo, vl = _view("out", out, (n, b, heads * head)), _numbers("lengths", lengths, (n, b))
@@ -202,6 +241,8 @@ def attention_step(q, k, v, cache_k, cache_v, lengths, out, heads, kv, window=0,
 def dropout(x, y, p, seed, step=0, residual=None, step_dev=None, stream=None):
     """Enqueue y = x m / P(m = 1) + residual, m = 0 with probability p, from (seed, step) and the element's place in [n, t, c]; x, y and residual of one type, y
     may be x or residual.  The backward pass is dropout(dy, dx, p, seed, step).  step_dev (device int64 / uint64 tensor, >= 1 element) is added to step."""
+    if _short("dropout", x, y, p, seed, step, residual, step_dev, stream):
+        return
     n, t, c = _shape("x", x, 3)
     vx, vr, vy = _view("x", x, (n, t, c)), _view("residual", residual, (n, t, c)), _view("y", y, (n, t, c))
     psgd._on_current_device(x, residual, y, step_dev)

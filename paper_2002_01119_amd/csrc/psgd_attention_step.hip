@@ -57,7 +57,7 @@ struct Seen {
 };
 
 template <typename T, int H> struct StepShape {
-    static constexpr int kSteps = H / 32, kCols = H / 16, kWaves = step_waves(H, sizeof(T)), kStages = step_stages(H, sizeof(T));
+    static constexpr int kSteps = H / 32, kCols = H / 16, kWaves = step_waves(H, sizeof(T)), kStages = kStepStages;
     using Lds = Tile<T, H, kStepKeys>;
     static constexpr int kMoves = kStepKeys * Lds::kGroups / kWave;      // 16-byte groups of a tile that a lane moves
     static constexpr size_t kTiles = (size_t)kWaves * kStages * 2 * Lds::kBytes, kJoin = (size_t)kWaves * 16 * (H + 2) * sizeof(float);

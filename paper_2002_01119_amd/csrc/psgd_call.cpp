@@ -9,10 +9,12 @@
 #include <c10/core/Allocator.h>
 #include <c10/hip/HIPStream.h>
 
+#include <cmath>
 #include <cstdint>
 #include <initializer_list>
 
 #include "psgd.h"
+#include "psgd_attention.h"
 #include "psgd_layers.h"
 
 namespace {
@@ -494,11 +496,254 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return answer(0);
 }
 
+// ------------------------------------------------------------------------------------------------ attention blocks (psgd_attention.h)
+struct Attention {
+    decltype(&psgd_qk_norm_rope) qk_norm_rope = nullptr;
+    decltype(&psgd_qk_norm_rope_grad) qk_norm_rope_grad = nullptr;
+    decltype(&psgd_qk_norm_rope_grad_workspace) qk_norm_rope_grad_workspace = nullptr;
+    decltype(&psgd_attention) attention = nullptr;
+    decltype(&psgd_attention_grad) attention_grad = nullptr;
+    decltype(&psgd_attention_grad_workspace) attention_grad_workspace = nullptr;
+    decltype(&psgd_attention_step) attention_step = nullptr;
+    decltype(&psgd_attention_step_workspace) attention_step_workspace = nullptr;
+    decltype(&psgd_dropout) dropout = nullptr;
+} blocks;
+int blocks_device() { return blocks.dropout ? static_cast<int>(c10::hip::current_device()) : -1; }
+
+// What the calls have in common: n learners of t tokens, heads of the queries and of the keys.
+struct Heads {
+    int64_t n = -1, t = -1, cq = -1, ck = -1, heads, kv, head;
+    // After the queries have said what n, t and cq are.
+    bool of(PyObject* h, PyObject* k) {
+        if (!integer(h, heads) || !integer(k, kv) || heads < 1 || kv < 1 || cq % heads || n > PSGD_MAX_N) return false;
+        head = cq / heads;
+        ck = kv * head;
+        return heads <= INT32_MAX && kv <= INT32_MAX && head <= PSGD_MAX_HEAD;
+    }
+};
+// [rows, cols] int32 of any strides.
+bool numbers(PyObject* o, int dev, int64_t rows, int64_t cols, Operand& x, bool optional = false) {
+    if (o == Py_None) return optional;
+    const at::Tensor* t = plain(o, dev);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols) return false;
+    x.v = psgd_view{t->data_ptr(), rows > 1 ? t->stride(0) : 0, cols > 1 ? t->stride(1) : 0, PSGD_I32};
+    x.there = true;
+    return true;
+}
+bool starts_of(PyObject* o, int dev, int64_t n, Operand& x, int64_t& sequences) {
+    sequences = 0;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o, dev);
+    if (!t || t->scalar_type() != at::kInt || t->dim() != 2 || t->size(0) != n || t->size(1) < 2 || t->stride(1) != 1) return false;
+    x.v = psgd_view{t->data_ptr(), n > 1 ? t->stride(0) : 0, 0, PSGD_I32};
+    x.there = true;
+    sequences = t->size(1) - 1;
+    return sequences <= INT32_MAX;
+}
+bool small(PyObject* o, int& v) {
+    int64_t x;
+    if (!integer(o, x) || x < INT32_MIN || x > INT32_MAX) return false;
+    v = static_cast<int>(x);
+    return true;
+}
+bool real(PyObject* o, double& v) {
+    if (!PyFloat_CheckExact(o)) return false;
+    v = PyFloat_AS_DOUBLE(o);
+    return true;
+}
+// None: head ** -0.5, in 64 bits as Python has it
+bool scale_of(PyObject* o, int64_t head, float& v) {
+    if (o != Py_None) return number(o, v);
+    v = static_cast<float>(std::pow(static_cast<double>(head), -0.5));
+    return true;
+}
+bool word_of(PyObject* o, uint64_t& v) {
+    if (!PyLong_CheckExact(o)) return false;
+    v = PyLong_AsUnsignedLongLongMask(o);
+    return true;
+}
+
+// qk_norm_rope(q, k, q_out, k_out, heads, kv, positions, q_gain, k_gain, eps, rotary, base, pairs, stream)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        Heads s;
+        Operand q, k, qo, ko, pos, gq, gk;
+        float eps;
+        double base;
+        int rotary, pairs;
+        void* st;
+        if (count != 14 || dev < 0 || !operand(a[0], dev, {&s.n, &s.t, &s.cq}, q) || !s.of(a[4], a[5]) || !operand(a[1], dev, {&s.n, &s.t, &s.ck}, k) ||
+            !operand(a[2], dev, {&s.n, &s.t, &s.cq}, qo) || !operand(a[3], dev, {&s.n, &s.t, &s.ck}, ko) || !numbers(a[6], dev, s.n, s.t, pos, true) ||
+            !operand(a[7], dev, {&s.n, &s.head}, gq, true) || !operand(a[8], dev, {&s.n, &s.head}, gk, true) || !number(a[9], eps) || !small(a[10], rotary) ||
+            !real(a[11], base) || !small(a[12], pairs) || !stream_of(a[13], dev, st))
+            return NOT_MINE;
+        Unlocked run;
+        return blocks.qk_norm_rope(q.get(), k.get(), pos.get(), gq.get(), gk.get(), qo.get(), ko.get(), static_cast<int>(s.heads), static_cast<int>(s.kv),
+                                   static_cast<int>(s.head), rotary, pairs, base, eps, static_cast<int>(s.n), s.t, st);
+    });
+}
+
+// qk_norm_rope_grad(dq_out, dk_out, q, k, dq, dk, heads, kv, positions, q_gain, k_gain, dq_gain, dk_gain, eps, rotary, base, pairs, stream)
+PyObject* qk_norm_rope_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        Heads s;
+        Operand qo, ko, q, k, dq, dk, pos, gq, gk, dgq, dgk;
+        float eps;
+        double base;
+        int rotary, pairs;
+        void* st;
+        c10::DataPtr room;
+        if (count != 18 || dev < 0 || !operand(a[0], dev, {&s.n, &s.t, &s.cq}, qo) || !s.of(a[6], a[7]) || !operand(a[1], dev, {&s.n, &s.t, &s.ck}, ko) ||
+            !operand(a[2], dev, {&s.n, &s.t, &s.cq}, q, true) || !operand(a[3], dev, {&s.n, &s.t, &s.ck}, k, true) || !operand(a[4], dev, {&s.n, &s.t, &s.cq}, dq) ||
+            !operand(a[5], dev, {&s.n, &s.t, &s.ck}, dk) || !numbers(a[8], dev, s.n, s.t, pos, true) || !operand(a[9], dev, {&s.n, &s.head}, gq, true) ||
+            !operand(a[10], dev, {&s.n, &s.head}, gk, true) || !operand(a[11], dev, {&s.n, &s.head}, dgq, true) || !operand(a[12], dev, {&s.n, &s.head}, dgk, true) ||
+            (!gq.there && (dgq.there || dgk.there)) || !number(a[13], eps) || !small(a[14], rotary) || !real(a[15], base) || !small(a[16], pairs) ||
+            !stream_of(a[17], dev, st))
+            return NOT_MINE;
+        const size_t need = dgq.there || dgk.there ? blocks.qk_norm_rope_grad_workspace(static_cast<int>(s.n), s.t, static_cast<int>(s.head)) : 0;
+        if (!workspace(dev, need, st, room)) return NOT_MINE;
+        Unlocked run;
+        return blocks.qk_norm_rope_grad(qo.get(), ko.get(), q.get(), k.get(), pos.get(), gq.get(), gk.get(), dq.get(), dk.get(), dgq.get(), dgk.get(),
+                                        static_cast<int>(s.heads), static_cast<int>(s.kv), static_cast<int>(s.head), rotary, pairs, base, eps,
+                                        static_cast<int>(s.n), s.t, room.get(), need, st);
+    });
+}
+
+// attention(q, k, v, out, heads, kv, lse, starts, window, sinks, scale, stream)
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        Heads s;
+        Operand q, k, v, o, st;
+        float *lse, scale;
+        int window, sinks;
+        int64_t sequences;
+        void* stream;
+        if (count != 12 || dev < 0 || !operand(a[0], dev, {&s.n, &s.t, &s.cq}, q) || !s.of(a[4], a[5]) || !operand(a[1], dev, {&s.n, &s.t, &s.ck}, k) ||
+            !operand(a[2], dev, {&s.n, &s.t, &s.ck}, v) || !operand(a[3], dev, {&s.n, &s.t, &s.cq}, o) || !vector(a[6], dev, s.n * s.heads * s.t, at::kFloat, lse) ||
+            !starts_of(a[7], dev, s.n, st, sequences) || !small(a[8], window) || !small(a[9], sinks) || !scale_of(a[10], s.head, scale) || !stream_of(a[11], dev, stream))
+            return NOT_MINE;
+        Unlocked run;
+        return blocks.attention(q.get(), k.get(), v.get(), st.get(), o.get(), lse, static_cast<int>(s.heads), static_cast<int>(s.kv), static_cast<int>(s.head), window,
+                                sinks, scale, static_cast<int>(sequences), static_cast<int>(s.n), s.t, stream);
+    });
+}
+
+// attention_grad(dout, q, k, v, out, lse, dq, dk, dv, heads, kv, starts, window, sinks, scale, stream)
+PyObject* attention_grad(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        Heads s;
+        Operand d, q, k, v, o, st, dq, dk, dv;
+        float *lse, scale;
+        int window, sinks;
+        int64_t sequences;
+        void* stream;
+        c10::DataPtr room;
+        if (count != 16 || dev < 0 || !operand(a[1], dev, {&s.n, &s.t, &s.cq}, q) || !s.of(a[9], a[10]) || !operand(a[0], dev, {&s.n, &s.t, &s.cq}, d) ||
+            !operand(a[2], dev, {&s.n, &s.t, &s.ck}, k) || !operand(a[3], dev, {&s.n, &s.t, &s.ck}, v) || !operand(a[4], dev, {&s.n, &s.t, &s.cq}, o) ||
+            !vector(a[5], dev, s.n * s.heads * s.t, at::kFloat, lse) || !operand(a[6], dev, {&s.n, &s.t, &s.cq}, dq) || !operand(a[7], dev, {&s.n, &s.t, &s.ck}, dk) ||
+            !operand(a[8], dev, {&s.n, &s.t, &s.ck}, dv) || !starts_of(a[11], dev, s.n, st, sequences) || !small(a[12], window) || !small(a[13], sinks) ||
+            !scale_of(a[14], s.head, scale) || !stream_of(a[15], dev, stream))
+            return NOT_MINE;
+        const size_t need = blocks.attention_grad_workspace(static_cast<int>(s.heads), static_cast<int>(s.kv), static_cast<int>(s.head), window, sinks,
+                                                            static_cast<int>(sequences), static_cast<int>(s.n), s.t);
+        if (!workspace(dev, need, stream, room)) return NOT_MINE;
+        Unlocked run;
+        return blocks.attention_grad(d.get(), q.get(), k.get(), v.get(), o.get(), lse, st.get(), dq.get(), dk.get(), dv.get(), static_cast<int>(s.heads),
+                                     static_cast<int>(s.kv), static_cast<int>(s.head), window, sinks, scale, static_cast<int>(sequences), static_cast<int>(s.n), s.t,
+                                     room.get(), need, stream);
+    });
+}
+
+bool cache_of(PyObject* o, int dev, const Heads& s, int64_t& slots, psgd_cache& c) {
+    const at::Tensor* t = plain(o, dev);
+    if (!t || t->dim() != 4 || t->size(0) != s.n || t->size(1) != s.t || t->size(2) < 1 || t->size(3) != s.ck || (s.ck > 1 && t->stride(3) != 1)) return false;
+    if (t->scalar_type() != at::kFloat && t->scalar_type() != at::kBFloat16) return false;
+    if (slots < 0) slots = t->size(2);
+    c = psgd_cache{t->data_ptr(), s.n > 1 ? t->stride(0) : 0, s.t > 1 ? t->stride(1) : 0, slots > 1 ? t->stride(2) : 0,
+                   t->scalar_type() == at::kFloat ? PSGD_F32 : PSGD_BF16};
+    return t->size(2) == slots;
+}
+
+// attention_step(q, k, v, cache_k, cache_v, lengths, out, heads, kv, window, sinks, scale, stream)
+PyObject* attention_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        Heads s;
+        Operand q, k, v, o, len;
+        psgd_cache ck, cv;
+        float scale;
+        int window, sinks;
+        int64_t slots = -1;
+        void* stream;
+        c10::DataPtr room;
+        if (count != 13 || dev < 0 || !operand(a[0], dev, {&s.n, &s.t, &s.cq}, q) || !s.of(a[7], a[8]) || !operand(a[1], dev, {&s.n, &s.t, &s.ck}, k) ||
+            !operand(a[2], dev, {&s.n, &s.t, &s.ck}, v) || !cache_of(a[3], dev, s, slots, ck) || !cache_of(a[4], dev, s, slots, cv) ||
+            !numbers(a[5], dev, s.n, s.t, len) || !operand(a[6], dev, {&s.n, &s.t, &s.cq}, o) || !small(a[9], window) || !small(a[10], sinks) ||
+            !scale_of(a[11], s.head, scale) || !stream_of(a[12], dev, stream))
+            return NOT_MINE;
+        const size_t need = blocks.attention_step_workspace(static_cast<int>(s.heads), static_cast<int>(s.kv), static_cast<int>(s.head), window, sinks,
+                                                            static_cast<int>(s.n), s.t, slots);
+        if (!workspace(dev, need, stream, room)) return NOT_MINE;
+        Unlocked run;
+        return blocks.attention_step(q.get(), k.get(), v.get(), &ck, &cv, len.get(), o.get(), static_cast<int>(s.heads), static_cast<int>(s.kv),
+                                     static_cast<int>(s.head), window, sinks, scale, static_cast<int>(s.n), s.t, slots, room.get(), need, stream);
+    });
+}
+
+// dropout(x, y, p, seed, step, residual, step_dev, stream)
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    return guarded([&]() -> long {
+        const int dev = blocks_device();
+        int64_t n = -1, t = -1, c = -1;
+        Operand x, y, r;
+        float p;
+        uint64_t seed, step;
+        uint64_t* counter = nullptr;
+        void* stream;
+        if (count != 8 || dev < 0 || !operand(a[0], dev, {&n, &t, &c}, x) || n > PSGD_MAX_N || !operand(a[1], dev, {&n, &t, &c}, y) || !number(a[2], p) ||
+            !word_of(a[3], seed) || !word_of(a[4], step) || !operand(a[5], dev, {&n, &t, &c}, r, true) || !stream_of(a[7], dev, stream))
+            return NOT_MINE;
+        if (a[6] != Py_None) {
+            const at::Tensor* d = plain(a[6], dev);
+            if (!d || (d->scalar_type() != at::kLong && d->scalar_type() != at::kUInt64) || d->numel() < 1) return NOT_MINE;
+            counter = static_cast<uint64_t*>(d->data_ptr());
+        }
+        Unlocked run;
+        return blocks.dropout(x.get(), r.get(), y.get(), p, seed, step, counter, static_cast<int>(n), t, c, stream);
+    });
+}
+
+// bind_attention(addresses of the functions, in the order of struct Attention)
+PyObject* bind_attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    void* p[9];
+    if (count != 9) return answer(NOT_MINE);
+    for (int i = 0; i < 9; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (PyErr_Occurred()) return nullptr;
+    }
+    blocks.qk_norm_rope = reinterpret_cast<decltype(blocks.qk_norm_rope)>(p[0]);
+    blocks.qk_norm_rope_grad = reinterpret_cast<decltype(blocks.qk_norm_rope_grad)>(p[1]);
+    blocks.qk_norm_rope_grad_workspace = reinterpret_cast<decltype(blocks.qk_norm_rope_grad_workspace)>(p[2]);
+    blocks.attention = reinterpret_cast<decltype(blocks.attention)>(p[3]);
+    blocks.attention_grad = reinterpret_cast<decltype(blocks.attention_grad)>(p[4]);
+    blocks.attention_grad_workspace = reinterpret_cast<decltype(blocks.attention_grad_workspace)>(p[5]);
+    blocks.attention_step = reinterpret_cast<decltype(blocks.attention_step)>(p[6]);
+    blocks.attention_step_workspace = reinterpret_cast<decltype(blocks.attention_step_workspace)>(p[7]);
+    blocks.dropout = reinterpret_cast<decltype(blocks.dropout)>(p[8]);
+    return answer(0);
+}
+
 #define PSGD_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PSGD_METHOD(mix_step),  PSGD_METHOD(mix_full), PSGD_METHOD(mix_step_d1d), PSGD_METHOD(build_mixing_device),
                          PSGD_METHOD(consensus_dist_async), PSGD_METHOD(consensus_dist), PSGD_METHOD(synth_grad), PSGD_METHOD(bind),
                          PSGD_METHOD(layer_norm), PSGD_METHOD(layer_norm_grad), PSGD_METHOD(linear), PSGD_METHOD(linear_grad),
-                         PSGD_METHOD(token_logprobs), PSGD_METHOD(distill), PSGD_METHOD(bind_layers), {nullptr, nullptr, 0, nullptr}};
+                         PSGD_METHOD(token_logprobs), PSGD_METHOD(distill), PSGD_METHOD(bind_layers),
+                         PSGD_METHOD(qk_norm_rope), PSGD_METHOD(qk_norm_rope_grad), PSGD_METHOD(attention), PSGD_METHOD(attention_grad), PSGD_METHOD(attention_step),
+                         PSGD_METHOD(dropout), PSGD_METHOD(bind_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -5,8 +5,10 @@
 //
 // About ten vector operations an element against 4 bytes (forward, bf16) to 12 (backward, float): bound by HBM, so every array is touched once.  A
 // wavefront takes a token: its lanes make the token's cosines and sines, one pair of columns each, exchange them through LDS, and every head of the
-// token uses them.  A head takes as many lanes as its columns make of pairs of 16-byte groups, so a lane holds both columns of each of its pairs (a
-// group of the first half and one of the second, or two neighbouring ones) and a wavefront works on 64 / lanes heads at once.
+// token uses them.  A lane holds four pairs of columns, both columns of each (four of the first half and four of the second, or two neighbouring fours), so a
+// head of 128 takes 16 lanes and a wavefront works on four heads at once.  What hides memory's latency are the wavefronts beside it, so registers are
+// spared: eight pairs a lane leave half the wavefronts, and loading the next heads ahead a quarter fewer (backward, 4 x 4096 tokens of 40 heads of 128 in
+// bf16: 158 and 138 us, as it is 116).
 //
 // An angle is position times rate in turns, in 64 bits: whole quarters are taken off there and the rest, an eighth of a turn at most, is rounded to 32
 // bits, so it is off by 2^-27 turns, 5e-8 of a radian, wherever the token is.
@@ -40,28 +42,41 @@ struct QkArgs {
     double turn[kMostPairs];     // turns a position, of each pair
 };
 
-// E values next to each other, as floats: 16 bytes, or four bf16.
+// A lane's four columns next to each other: 16 bytes of float, 8 of bf16.
+constexpr int E = 4;
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
-template <typename T, int E> __device__ __forceinline__ void load_group(const T* p, float (&v)[E]) {
-    if constexpr (E * sizeof(T) == 16) {
-        widen<T>(load_raw(p), v);
-    } else {
-        const u32x2 r = *reinterpret_cast<const u32x2_any*>(p);
+template <typename T> struct Four;
+template <> struct Four<float> {
+    u32x4 r;
+    __device__ __forceinline__ void load(const float* p) { r = load_raw(p); }
+    __device__ __forceinline__ void widen_to(float (&v)[E]) const { widen<float>(r, v); }
+};
+template <> struct Four<uint16_t> {
+    u32x2 r;
+    __device__ __forceinline__ void load(const uint16_t* p) { r = *reinterpret_cast<const u32x2_any*>(p); }
+    __device__ __forceinline__ void widen_to(float (&v)[E]) const {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             v[2 * i] = low_bf16(r[i]);
             v[2 * i + 1] = high_bf16(r[i]);
         }
     }
+};
+// PAST: past the caches, which such an output would only push other data out of.
+template <bool PAST> __device__ __forceinline__ void store_group(float* p, const float (&v)[E]) {
+    const u32x4 r = narrow(v, 0.0f);
+    if constexpr (PAST) __builtin_nontemporal_store(r, reinterpret_cast<u32x4_any*>(p));
+    else *reinterpret_cast<u32x4_any*>(p) = r;
 }
-template <typename T, int E> __device__ __forceinline__ void store_group(T* p, const float (&v)[E]) {
-    if constexpr (E * sizeof(T) == 16) *reinterpret_cast<u32x4_any*>(p) = narrow(v, T{});
-    else *reinterpret_cast<u32x2_any*>(p) = (u32x2){two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+template <bool PAST> __device__ __forceinline__ void store_group(uint16_t* p, const float (&v)[E]) {
+    const u32x2 r = {two_bf16(v[0], v[1]), two_bf16(v[2], v[3])};
+    if constexpr (PAST) __builtin_nontemporal_store(r, reinterpret_cast<u32x2_any*>(p));
+    else *reinterpret_cast<u32x2_any*>(p) = r;
 }
 
-// What a lane holds of a head: E pairs of columns.  VEC: as two groups of E columns next to each other, which takes rotary and the columns behind it
-// to be multiples of 2 E; else column by column, any head.
-template <typename T, int E, bool VEC> struct Columns {
+// What a lane holds of a head: four pairs of columns.  VEC: as two groups of four columns next to each other, which takes rotary and the columns behind it
+// to be multiples of eight; else column by column, any head.
+template <typename T, bool VEC> struct Columns {
     int a, b;            // VEC: of the two groups
     int first, head, half;
     bool here, turned, neighbours;
@@ -84,13 +99,15 @@ template <typename T, int E, bool VEC> struct Columns {
     }
     __device__ __forceinline__ void load(const T* p, bool live, float (&va)[E], float (&vb)[E]) const {
         if constexpr (VEC) {
+            Four<T> ra, rb;
+            ra.r = {};
+            rb.r = {};
             if (live) {
-                load_group<T, E>(p + a, va);
-                load_group<T, E>(p + b, vb);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) va[e] = vb[e] = 0.0f;
+                ra.load(p + a);
+                rb.load(p + b);
             }
+            ra.widen_to(va);
+            rb.widen_to(vb);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -101,11 +118,11 @@ template <typename T, int E, bool VEC> struct Columns {
             }
         }
     }
-    __device__ __forceinline__ void store(T* p, bool live, const float (&va)[E], const float (&vb)[E]) const {
+    template <bool PAST> __device__ __forceinline__ void store(T* p, bool live, const float (&va)[E], const float (&vb)[E]) const {
         if (!live) return;
         if constexpr (VEC) {
-            store_group<T, E>(p + a, va);
-            store_group<T, E>(p + b, vb);
+            store_group<PAST>(p + a, va);
+            store_group<PAST>(p + b, vb);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -205,7 +222,7 @@ __device__ __forceinline__ void angles(const QkArgs& q, const double (&turn)[2],
         if (lane + 64 * k < q.rotary / 2) cos_sin(at * turn[k], cs[lane + 64 * k], cs[kMostPairs + lane + 64 * k]);
     wave_meets();
 }
-template <int E> __device__ __forceinline__ void pair_angles(const float* cs, int first, int half, float (&c)[E], float (&s)[E]) {
+__device__ __forceinline__ void pair_angles(const float* cs, int first, int half, float (&c)[E], float (&s)[E]) {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const bool yes = first + e < half;
@@ -214,29 +231,37 @@ template <int E> __device__ __forceinline__ void pair_angles(const float* cs, in
     }
 }
 
-template <typename T, int E, bool VEC> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_kernel(QkArgs a) {
+template <typename T, bool VEC, bool PAST> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_kernel(QkArgs a) {
+    using Cols = Columns<T, VEC>;
     __shared__ float trig[kHeadWaves][2 * kMostPairs];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane / a.lanes, at_once = kWave / a.lanes;
     const int64_t i = blockIdx.y;
-    const Columns<T, E, VEC> cols(a, lane % a.lanes);
+    const Cols cols(a, lane % a.lanes);
     const double turn[2] = {a.turn[lane], a.turn[lane + 64]};
     const bool norm = a.gain[0].p != nullptr || a.gain[1].p != nullptr;
+    float ga[2][E], gb[2][E];
+    if (norm) {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) cols.gains(a.gain[which], a.gain_bf16, i, ga[which], gb[which]);
+    }
     for (int64_t r = (int64_t)blockIdx.x * kHeadWaves + wave; r < a.t; r += (int64_t)gridDim.x * kHeadWaves) {
-        angles(a, turn, i, r, lane, trig[wave]);
-        float c[E], s[E];
-        pair_angles<E>(trig[wave], cols.first, cols.half, c, s);
+        const T* in[2];
+        T* out[2];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            if (a.heads[which] == 0) continue;
-            float ga[E], gb[E];
-            if (norm) cols.gains(a.gain[which], a.gain_bf16, i, ga, gb);
-            const T* in = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row;
-            T* out = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row;
-            for (int h0 = 0; h0 < a.heads[which]; h0 += at_once) {
-                const int h = h0 + sub;
-                const bool live = cols.here && h < a.heads[which];
+            in[which] = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row + sub * a.head;
+            out[which] = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row + sub * a.head;
+        }
+        angles(a, turn, i, r, lane, trig[wave]);
+        float c[E], s[E];
+        pair_angles(trig[wave], cols.first, cols.half, c, s);
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const int heads = a.heads[which], steps = (heads + at_once - 1) / at_once;
+            for (int step = 0; step < steps; ++step) {
+                const int h = step * at_once;
                 float va[E], vb[E];
-                cols.load(in + (int64_t)h * a.head, live, va, vb);
+                cols.load(in[which] + (int64_t)h * a.head, cols.here && h + sub < heads, va, vb);
                 if (norm) {
                     float sq = 0.0f;
 #pragma unroll
@@ -244,75 +269,77 @@ template <typename T, int E, bool VEC> __global__ __launch_bounds__(kHeadWaves* 
                     const float rs = 1.0f / sqrtf(head_sum(sq, a.lanes) * a.inv_head + a.eps);
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        va[e] = va[e] * rs * ga[e];
-                        vb[e] = vb[e] * rs * gb[e];
+                        va[e] = va[e] * rs * ga[which][e];
+                        vb[e] = vb[e] * rs * gb[which][e];
                     }
                 }
                 cols.turn(c, s, va, vb);
-                cols.store(out + (int64_t)h * a.head, live, va, vb);
+                cols.template store<PAST>(out[which] + (int64_t)h * a.head, cols.here && h + sub < heads, va, vb);
             }
         }
     }
 }
 
-template <typename T, int E, bool VEC> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_grad_kernel(QkArgs a) {
+template <typename T, bool VEC, bool PAST> __global__ __launch_bounds__(kHeadWaves* kWave) void qk_grad_kernel(QkArgs a) {
+    using Cols = Columns<T, VEC>;
     __shared__ float trig[kHeadWaves][2 * kMostPairs];
     __shared__ float sums[kHeadWaves][2][PSGD_MAX_HEAD];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, sub = lane / a.lanes, at_once = kWave / a.lanes;
     const int64_t i = blockIdx.y;
-    const Columns<T, E, VEC> cols(a, lane % a.lanes);
+    const Cols cols(a, lane % a.lanes);
     const double turn[2] = {a.turn[lane], a.turn[lane + 64]};
     const bool norm = a.gain[0].p != nullptr || a.gain[1].p != nullptr;
-    float da[2][E], db[2][E];
+    float ga[2][E], gb[2][E], da[2][E], db[2][E];
 #pragma unroll
-    for (int which = 0; which < 2; ++which)
+    for (int which = 0; which < 2; ++which) {
+        if (norm) cols.gains(a.gain[which], a.gain_bf16, i, ga[which], gb[which]);
 #pragma unroll
         for (int e = 0; e < E; ++e) da[which][e] = db[which][e] = 0.0f;
+    }
     for (int64_t r = (int64_t)blockIdx.x * kHeadWaves + wave; r < a.t; r += (int64_t)gridDim.x * kHeadWaves) {
+        const T *in[2], *px[2];
+        T* out[2];
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            in[which] = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row + sub * a.head;
+            px[which] = reinterpret_cast<const T*>(a.x[which].p) + i * a.x[which].learner + r * a.x[which].row + sub * a.head;
+            out[which] = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row + sub * a.head;
+        }
         angles(a, turn, i, r, lane, trig[wave]);
         float c[E], s[E];
-        pair_angles<E>(trig[wave], cols.first, cols.half, c, s);
+        pair_angles(trig[wave], cols.first, cols.half, c, s);
 #pragma unroll
         for (int e = 0; e < E; ++e) s[e] = -s[e];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
-            if (a.heads[which] == 0) continue;
-            float ga[E], gb[E];
-            if (norm) cols.gains(a.gain[which], a.gain_bf16, i, ga, gb);
-            const T* in = reinterpret_cast<const T*>(a.in[which].p) + i * a.in[which].learner + r * a.in[which].row;
-            const T* px = norm ? reinterpret_cast<const T*>(a.x[which].p) + i * a.x[which].learner + r * a.x[which].row : nullptr;
-            T* out = reinterpret_cast<T*>(a.out[which].p) + i * a.out[which].learner + r * a.out[which].row;
-            for (int h0 = 0; h0 < a.heads[which]; h0 += at_once) {
-                const int h = h0 + sub;
-                const bool live = cols.here && h < a.heads[which];
-                float va[E], vb[E];
-                cols.load(in + (int64_t)h * a.head, live, va, vb);
-                if (!norm) {
-                    cols.turn(c, s, va, vb);
-                    cols.store(out + (int64_t)h * a.head, live, va, vb);
-                    continue;
-                }
-                float xa[E], xb[E];
-                cols.load(px + (int64_t)h * a.head, live, xa, xb);
+            const int heads = a.heads[which], steps = (heads + at_once - 1) / at_once;
+            for (int step = 0; step < steps; ++step) {
+                const int h = step * at_once;
+                float va[E], vb[E], xa[E], xb[E];
+                const bool live = cols.here && h + sub < heads;
+                cols.load(in[which] + (int64_t)h * a.head, live, va, vb);
+                cols.load(px[which] + (int64_t)h * a.head, live && norm, xa, xb);
                 cols.turn(c, s, va, vb);
-                float sq = 0.0f, wx = 0.0f;
+                if (norm) {
+                    float sq = 0.0f, wx = 0.0f;
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    sq = __builtin_fmaf(xa[e], xa[e], __builtin_fmaf(xb[e], xb[e], sq));
-                    wx = __builtin_fmaf(va[e] * ga[e], xa[e], __builtin_fmaf(vb[e] * gb[e], xb[e], wx));
-                }
-                sq = head_sum(sq, a.lanes);
-                wx = head_sum(wx, a.lanes);
-                const float rs = 1.0f / sqrtf(sq * a.inv_head + a.eps), along = wx * rs * a.inv_head;      // mean(w h)
+                    for (int e = 0; e < E; ++e) {
+                        sq = __builtin_fmaf(xa[e], xa[e], __builtin_fmaf(xb[e], xb[e], sq));
+                        wx = __builtin_fmaf(va[e] * ga[which][e], xa[e], __builtin_fmaf(vb[e] * gb[which][e], xb[e], wx));
+                    }
+                    sq = head_sum(sq, a.lanes);
+                    wx = head_sum(wx, a.lanes);
+                    const float rs = 1.0f / sqrtf(sq * a.inv_head + a.eps), along = wx * rs * a.inv_head;      // mean(w h)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float ha = xa[e] * rs, hb = xb[e] * rs;
-                    da[which][e] = __builtin_fmaf(va[e], ha, da[which][e]);
-                    db[which][e] = __builtin_fmaf(vb[e], hb, db[which][e]);
-                    va[e] = rs * __builtin_fmaf(-ha, along, va[e] * ga[e]);
-                    vb[e] = rs * __builtin_fmaf(-hb, along, vb[e] * gb[e]);
+                    for (int e = 0; e < E; ++e) {
+                        const float ha = xa[e] * rs, hb = xb[e] * rs;
+                        da[which][e] = __builtin_fmaf(va[e], ha, da[which][e]);
+                        db[which][e] = __builtin_fmaf(vb[e], hb, db[which][e]);
+                        va[e] = rs * __builtin_fmaf(-ha, along, va[e] * ga[which][e]);
+                        vb[e] = rs * __builtin_fmaf(-hb, along, vb[e] * gb[which][e]);
+                    }
                 }
-                cols.store(out + (int64_t)h * a.head, live, va, vb);
+                cols.template store<PAST>(out[which] + (int64_t)h * a.head, cols.here && h + sub < heads, va, vb);
             }
         }
     }
@@ -378,20 +405,20 @@ inline int64_t forward_groups(int n, int64_t t, int cus) {
     const int64_t most = parts_of(t, kHeadWaves), fair = parts_of((int64_t)cus * 8, n);
     return most < fair ? most : fair;
 }
-// Backward they leave a partial row each behind.  The same for any device, since the workspace's size is asked for without one.
+// Backward they leave a partial row each behind, and there are as many as are resident.  The same for any device, since the workspace's size is asked for without one.
 inline int64_t grad_slabs(int n, int64_t t) {
-    const int64_t most = parts_of(t, kHeadWaves), fair = parts_of(2048, n);
+    const int64_t most = parts_of(t, kHeadWaves), fair = parts_of(1024, n);
     const int64_t g = most < fair ? most : fair;
     return g < 1 ? 1 : g;
 }
 
-// How a lane holds a head: two groups of 16 bytes, two of four bf16, or column by column.
-enum { kGroups16, kGroups8, kColumns };
-inline int head_way(int head, int rotary, int bytes) {
-    if (rotary % (32 / bytes) == 0 && (head - rotary) % (32 / bytes) == 0) return kGroups16;
-    return bytes == 2 && rotary % 8 == 0 && (head - rotary) % 8 == 0 ? kGroups8 : kColumns;
+// Calls that move more than the last-level cache holds write past it: 4 x 4096 tokens of 40 heads of 128 in bf16 forward 83 us, so 64, backward 116 and 106; of 64,
+// which fit, 34 and 37.
+inline bool past_caches(int n, int64_t t, int heads, int head, int bytes, int arrays) {
+    return (double)n * t * heads * head * bytes * arrays > (double)(256 << 20);
 }
-inline int pairs_of_lane(int way, int bytes) { return way == kGroups16 ? 16 / bytes : 4; }
+// Whether a lane's columns are two groups of four next to each other.
+inline bool in_groups(int head, int rotary) { return rotary % 8 == 0 && (head - rotary) % 8 == 0; }
 
 inline int fill_args(const char* name, QkArgs& a, int heads, int kv, int head, int rotary, int pairs, double base, float eps, int n, int64_t t) {
     if (int rc = check_counts(name, n, t, head)) return rc;
@@ -476,11 +503,15 @@ int psgd_qk_norm_rope(const psgd_view* q, const psgd_view* k, const psgd_view* p
         a.pos_learner = positions->learner;
         a.pos_row = positions->row;
     }
-    const int bytes = elem_bytes(one->type), way = head_way(head, rotary, bytes);
     a.lanes = 1;
-    while (2 * a.lanes * pairs_of_lane(way, bytes) < head) a.lanes *= 2;
-    void (*fn)(QkArgs) = one->type == PSGD_F32 ? (way == kGroups16 ? qk_kernel<float, 4, true> : qk_kernel<float, 4, false>)
-                                               : (way == kGroups16 ? qk_kernel<uint16_t, 8, true> : way == kGroups8 ? qk_kernel<uint16_t, 4, true> : qk_kernel<uint16_t, 4, false>);
+    while (2 * a.lanes * E < head) a.lanes *= 2;
+    const bool groups = in_groups(head, rotary);
+    const bool past = past_caches(n, t, heads + kv, head, elem_bytes(one->type), 2);
+    auto pick = [&](auto type) -> void (*)(QkArgs) {
+        using T = decltype(type);
+        return !groups ? qk_kernel<T, false, false> : past ? qk_kernel<T, true, true> : qk_kernel<T, true, false>;
+    };
+    void (*const fn)(QkArgs) = one->type == PSGD_F32 ? pick(0.0f) : pick((uint16_t)0);
     hipLaunchKernelGGL(fn, dim3((unsigned)forward_groups(n, t, cus), n), dim3(kHeadWaves * kWave), 0, static_cast<hipStream_t>(stream), a);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);
@@ -563,14 +594,17 @@ int psgd_qk_norm_rope_grad(const psgd_view* dq_out, const psgd_view* dk_out, con
         a.pos_row = positions->row;
     }
     a.partial = params ? static_cast<float*>(workspace) : nullptr;
-    const int bytes = elem_bytes(type), way = head_way(head, rotary, bytes);
     a.lanes = 1;
-    while (2 * a.lanes * pairs_of_lane(way, bytes) < head) a.lanes *= 2;
+    while (2 * a.lanes * E < head) a.lanes *= 2;
+    const bool groups = in_groups(head, rotary);
     const int64_t slabs = grad_slabs(n, t);
     if (one && t > 0) {
-        void (*fn)(QkArgs) = type == PSGD_F32
-                                 ? (way == kGroups16 ? qk_grad_kernel<float, 4, true> : qk_grad_kernel<float, 4, false>)
-                                 : (way == kGroups16 ? qk_grad_kernel<uint16_t, 8, true> : way == kGroups8 ? qk_grad_kernel<uint16_t, 4, true> : qk_grad_kernel<uint16_t, 4, false>);
+        const bool past = past_caches(n, t, heads + kv, head, elem_bytes(type), norm ? 3 : 2);
+        auto pick = [&](auto zero) -> void (*)(QkArgs) {
+            using T = decltype(zero);
+            return !groups ? qk_grad_kernel<T, false, false> : past ? qk_grad_kernel<T, true, true> : qk_grad_kernel<T, true, false>;
+        };
+        void (*const fn)(QkArgs) = type == PSGD_F32 ? pick(0.0f) : pick((uint16_t)0);
         hipLaunchKernelGGL(fn, dim3((unsigned)slabs, n), dim3(kHeadWaves * kWave), 0, s, a);
     }
     if (params) {
