@@ -15,7 +15,7 @@ namespace {
 
 __device__ int g_attention_status = 0;
 
-template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (Shape<T, H>::kTwice)) void attention_kernel(AttentionArgs a) {
+template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (DIRECT && H * sizeof(T) == 256 ? 3 : Shape<T, H>::kTwice)) void attention_kernel(AttentionArgs a) {
     using S = Shape<T, H>;
     using Lds = typename S::Lds;
     extern __shared__ __attribute__((aligned(16))) char lds[];       // two of keys, two of values
@@ -69,16 +69,17 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
         if (mine < len && any_sees(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks)) {
             f32x4 s[S::kOwnBlocks][S::kBlocks];
 #pragma unroll
-            for (int kb = 0; kb < S::kBlocks; ++kb) {
+            for (int kb = 0; kb < S::kBlocks; ++kb)
 #pragma unroll
                 for (int b = 0; b < S::kOwnBlocks; ++b) s[b][kb] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                for (int kc = 0; kc < S::kSteps; ++kc) {
+            for (int kc = 0; kc < S::kSteps; ++kc)
+#pragma unroll
+                for (int kb = 0; kb < S::kBlocks; ++kb) {
                     const Eight<T> k = Lds::along(along_at + buffer, kb, kc);
 #pragma unroll
                     for (int b = 0; b < S::kOwnBlocks; ++b) s[b][kb] = mma(k, q[b][kc], s[b][kb]);
                 }
-            }
             const bool full = all_see(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks);
             if (!full) {
 #pragma unroll
@@ -88,23 +89,31 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[b][kb][e] = sees(mine + 16 * b + col, key0 + 16 * kb + 4 * g + e, a.window, a.sinks) ? s[b][kb][e] : -INFINITY;
             }
+            // the maximum that p is taken against lags behind while no score is 2^kLag times it: sums and outputs are seldom scaled
+            float most[S::kOwnBlocks];
+            bool more = false;
 #pragma unroll
             for (int b = 0; b < S::kOwnBlocks; ++b) {
-                float m = -INFINITY;
+                most[b] = -INFINITY;
 #pragma unroll
                 for (int kb = 0; kb < S::kBlocks; ++kb)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) m = fmaxf(m, s[b][kb][e]);
-                // the maximum that p is taken against lags behind while no score is 2^kLag times it: sums and outputs are seldom scaled
-                m *= to_log2;
-                if (__any(m > top[b] + kLag)) {
-                    m = fmaxf(top[b], column_all<Larger>(m));
-                    const float less = m == -INFINITY ? 1.0f : exp_2(top[b] - m);
+                    for (int e = 0; e < 4; ++e) most[b] = fmaxf(most[b], s[b][kb][e]);
+                most[b] *= to_log2;
+                more |= most[b] > top[b] + kLag;
+            }
+            if (__any(more)) {
+#pragma unroll
+                for (int b = 0; b < S::kOwnBlocks; ++b) {
+                    const float m = fmaxf(top[b], column_all<Larger>(most[b])), less = m == -INFINITY ? 1.0f : exp_2(top[b] - m);
                     top[b] = m;
                     sum[b] *= less;
 #pragma unroll
                     for (int d = 0; d < S::kCols; ++d) o[b][d] *= less;
                 }
+            }
+#pragma unroll
+            for (int b = 0; b < S::kOwnBlocks; ++b) {
                 const float safe = top[b] == -INFINITY ? 0.0f : top[b];
                 float part = 0.0f;
 #pragma unroll
@@ -162,6 +171,7 @@ template <typename T, int H> int launch_forward(const char* name, AttentionArgs 
 }
 template <typename T> int forward_of(const char* name, const AttentionArgs& a, hipStream_t s) {
     switch (held_head(a.head)) {
+        case 32: return launch_forward<T, 32>(name, a, s);
         case 64: return launch_forward<T, 64>(name, a, s);
         case 128: return launch_forward<T, 128>(name, a, s);
         default: return launch_forward<T, 256>(name, a, s);

@@ -73,6 +73,15 @@ template <typename T> __device__ __forceinline__ Eight<T> as_operand(f32x4 low, 
     }
     return r;
 }
+// What that rounding left of the two blocks.
+__device__ __forceinline__ Eight<uint16_t> rest_of(const Eight<uint16_t>& r, f32x4 low, f32x4 high) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        low[e] -= e % 2 ? high_bf16(r.v[e / 2]) : low_bf16(r.v[e / 2]);
+        high[e] -= e % 2 ? high_bf16(r.v[2 + e / 2]) : low_bf16(r.v[2 + e / 2]);
+    }
+    return as_operand<uint16_t>(low, high);
+}
 __device__ __forceinline__ float dot(const Eight<uint16_t>& a, const Eight<uint16_t>& b) {
     float s = 0.0f;
 #pragma unroll
@@ -122,8 +131,8 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_
 template <typename T, int H, int ROWS> struct Tile {
     static constexpr int kGroups = H * (int)sizeof(T) / 16;          // of a row
     static constexpr int kBytes = ROWS * kGroups * 16;
-    static __device__ __forceinline__ int turn(int row) {
-        return kGroups == 8 ? (row >> 1 & 3) << 1 | (row >> 3 & 1) : (row & 7) << 1 | (row >> 3 & 1);
+    static __host__ __device__ __forceinline__ constexpr int turn(int row) {
+        return kGroups == 4 ? (row >> 2 & 1) << 1 | (row >> 3 & 1) : kGroups == 8 ? (row >> 1 & 3) << 1 | (row >> 3 & 1) : (row & 7) << 1 | (row >> 3 & 1);
     }
     static __device__ __forceinline__ int place(int row, int group) { return (row * kGroups + (group ^ turn(row))) * 16; }
 
@@ -162,7 +171,7 @@ template <typename T, int H, int ROWS> struct Tile {
             r.v = (u32x4){x[0], x[1], y[0], y[1]};
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) r.v[e] = *lds_at<float>((from ^ (block * 64 ^ e % 4 * 32)) + rows + (e / 4 * 16 + e % 4) * kGroups * 16);
+            for (int e = 0; e < 8; ++e) r.v[e] = *lds_at<float>((from ^ (block * 64 ^ turn(e % 4) * 16)) + rows + (e / 4 * 16 + e % 4) * kGroups * 16);
         }
         return r;
     }

@@ -23,6 +23,9 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     const bool whole = a.head % kPer<T> == 0;
     const int mine = row0 + wave * 16 * S::kOwnBlocks;
     constexpr bool kStart = sizeof(T) == 2;                           // as in the other kernel
+    // A narrow head's keys are few directions, in which the terms of dq cancel while their roundings do not (heads of 16 in bf16: 0.0025 of itself from 64 bits,
+    // where wider heads are 0.0024): there ds is the sum of two bf16.
+    constexpr bool kFine = sizeof(T) == 2 && H == 32;
     const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f), lse_by = kStart ? kLog2E / to_log2 : kLog2E;
     const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo;
 
@@ -102,7 +105,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                             for (int e = 0; e < 4; ++e)
                                 s[b][kb][e] = sees(mine + 16 * b + col, key0 + 16 * (2 * half + kb) + 4 * g + e, a.window, a.sinks) ? s[b][kb][e] : -INFINITY;
                 }
-                Eight<T> ds[S::kOwnBlocks];
+                Eight<T> ds[S::kOwnBlocks], rest[S::kOwnBlocks];
 #pragma unroll
                 for (int b = 0; b < S::kOwnBlocks; ++b) {
 #pragma unroll
@@ -113,12 +116,16 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                             s[b][kb][e] = p * (kStart ? dp[b][kb][e] : dp[b][kb][e] + along[b]);
                         }
                     ds[b] = as_operand<T>(s[b][0], s[b][1]);
+                    if constexpr (kFine) rest[b] = rest_of(ds[b], s[b][0], s[b][1]);
                 }
 #pragma unroll
                 for (int c = 0; c < S::kCols; ++c) {
                     const Eight<T> k = Lds::across(across_at + buffer, c, half);
 #pragma unroll
-                    for (int b = 0; b < S::kOwnBlocks; ++b) dq[b][c] = mma(k, ds[b], dq[b][c]);
+                    for (int b = 0; b < S::kOwnBlocks; ++b) {
+                        dq[b][c] = mma(k, ds[b], dq[b][c]);
+                        if constexpr (kFine) dq[b][c] = mma(k, rest[b], dq[b][c]);
+                    }
                 }
             }
         }
@@ -411,6 +418,7 @@ template <typename T, int H> int launch_backward(const char* name, AttentionArgs
 }
 template <typename T> int backward_of(const char* name, const AttentionArgs& a, hipStream_t s) {
     switch (held_head(a.head)) {
+        case 32: return launch_backward<T, 32>(name, a, s);
         case 64: return launch_backward<T, 64>(name, a, s);
         case 128: return launch_backward<T, 128>(name, a, s);
         default: return launch_backward<T, 256>(name, a, s);

@@ -15,13 +15,14 @@ namespace psgd {
 constexpr int kChipUnits = 256;
 
 // A head's columns as the kernels hold them: the rest is zero.
-inline int held_head(int head) { return head <= 64 ? 64 : head <= 128 ? 128 : 256; }
+inline int held_head(int head) { return head <= 32 ? 32 : head <= 64 ? 64 : head <= 128 ? 128 : 256; }
 
-// Rows of a workgroup's own, a matrix instruction's 16 columns or two times that for each of its wavefronts, and rows of the tiles that it walks.
+// Rows of a workgroup's own, a matrix instruction's 16 columns or two times that for each of its wavefronts, and rows of the tiles that it walks.  (32 of those at a
+// head of 128 in bf16: three workgroups fit a compute unit then, forward 4 x 8192 tokens of 8 heads 538 us, with 64 and two workgroups 564.)
 constexpr int kAttentionWaves = 4;
 constexpr int own_blocks(int held, int bytes) { return bytes == 2 && held <= 128 ? 2 : 1; }
 constexpr int own_rows(int held, int bytes) { return kAttentionWaves * 16 * own_blocks(held, bytes); }
-constexpr int walked_rows(int held, int bytes) { return held * bytes <= 256 ? 64 : 32; }
+constexpr int walked_rows(int held, int bytes) { return held * bytes < 256 ? 64 : 32; }
 
 // Places for the own tiles of a learner's sequences: sequence s has its from starts[s] / rows + s on, which leaves every sequence room for all of its
 // tiles whatever their lengths, so that a workgroup finds its sequence by itself and no launch depends on device memory.
@@ -85,7 +86,7 @@ constexpr int step_waves(int held, int bytes) { return held * bytes <= 256 ? 4 :
 // Parts that a sequence's keys are cut into: as many workgroups as are there at once, and no fewer keys than two tiles a wavefront.  (One sequence of 131 072
 // positions with twice the workgroups 134 us, with four times 168.)
 inline int step_parts(int64_t units, int64_t most_keys, int head, int bytes) {
-    const int64_t most = parts_of(most_keys, step_waves(held_head(head), bytes) * kStepKeys * 2), fair = parts_of(held_head(head) * bytes == 128 ? 2 * kChipUnits : kChipUnits, units);
+    const int64_t most = parts_of(most_keys, step_waves(held_head(head), bytes) * kStepKeys * 2), fair = parts_of(held_head(head) * bytes <= 128 ? 2 * kChipUnits : kChipUnits, units);
     const int64_t p = most < fair ? most : fair;
     return (int)(p < 1 ? 1 : p > 1024 ? 1024 : p);
 }

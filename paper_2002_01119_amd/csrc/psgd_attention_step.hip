@@ -277,6 +277,7 @@ template <typename T, int H> int launch_step(const char* name, StepArgs a, int64
 }
 template <typename T> int step_of(const char* name, const StepArgs& a, int64_t units, int64_t rows, hipStream_t s) {
     switch (held_head(a.head)) {
+        case 32: return launch_step<T, 32>(name, a, units, rows, s);
         case 64: return launch_step<T, 64>(name, a, units, rows, s);
         case 128: return launch_step<T, 128>(name, a, units, rows, s);
         default: return launch_step<T, 256>(name, a, units, rows, s);

@@ -92,6 +92,12 @@ template <int ROWS, bool PARTS = false> __device__ __forceinline__ Work find_wor
     return w;
 }
 
+// An address that is the same in every lane, in scalar registers.  (The builtin's results are signed: as they are, an address's lower half would spread its sign.)
+__device__ __forceinline__ uint64_t same_in_all_lanes(uint64_t p) {
+    const uint32_t low = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)p), high = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(p >> 32));
+    return (uint64_t)high << 32 | (uint64_t)low;
+}
+
 // Brings a tile, rows row0 ... of a sequence (its first row `seq`, `len` rows), from memory to LDS.  DIRECT: straight there, 16 bytes a lane, which takes rows
 // and heads that start and end on 16 bytes; rows behind the sequence's last are that one again, which p = 0 leaves out.  Else through registers, any element
 // alignment, rows behind the last as zero.  `fetch` starts what a tile needs, `land` ends it: after the workgroup's next meeting the tile is there.
@@ -102,7 +108,7 @@ template <typename T, int H, int ROWS, int THREADS, bool DIRECT> struct Mover {
     u32x4 held[DIRECT ? 1 : kEach];
     __device__ __forceinline__ void fetch(char* tile, const T* seq, int64_t row_stride, int row0, int len, int head, bool whole) {
         if constexpr (DIRECT) {
-            const char* const from = reinterpret_cast<const char*>(seq + row0 * row_stride);
+            const uint64_t from = same_in_all_lanes(reinterpret_cast<uint64_t>(seq + row0 * row_stride));
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), stride = (int)row_stride * (int)sizeof(T), last = len - 1 - row0;
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(tile)) + wave * kWave * 16;
 #pragma unroll
