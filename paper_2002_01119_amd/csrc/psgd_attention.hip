@@ -49,7 +49,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     }
     const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
     const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
-    Mover<T, H, S::kWalked, S::kThreads, DIRECT> mk, mv;
+    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
     if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
     mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
@@ -173,6 +173,7 @@ template <typename T> int forward_of(const char* name, const AttentionArgs& a, h
     switch (held_head(a.head)) {
         case 32: return launch_forward<T, 32>(name, a, s);
         case 64: return launch_forward<T, 64>(name, a, s);
+        case 96: return launch_forward<T, 96>(name, a, s);
         case 128: return launch_forward<T, 128>(name, a, s);
         default: return launch_forward<T, 256>(name, a, s);
     }

@@ -57,7 +57,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     }
     const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
     const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
-    Mover<T, H, S::kWalked, S::kThreads, DIRECT> mk, mv;
+    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
     if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
     mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
@@ -88,7 +88,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                     }
 #pragma unroll
                     for (int kc = 0; kc < S::kSteps; ++kc) {
-                        const Eight<T> k = Lds::along(along_at + buffer, 2 * half + kb, kc), v = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + kb, kc);
+                            const Eight<T> k = Lds::along(along_at + buffer, 2 * half + kb, kc), v = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + kb, kc);
 #pragma unroll
                         for (int b = 0; b < S::kOwnBlocks; ++b) {
                             s[b][kb] = mma(k, q[b][kc], s[b][kb]);
@@ -192,8 +192,8 @@ template <typename T, int H> struct KeyShape : Shape<T, H> {
     static constexpr bool kValuesInLds = values_in_lds(H, sizeof(T));
     static constexpr int kRows = query_rows(H, sizeof(T));
     static constexpr int kTwice = sizeof(T) == 2 && H <= 128 ? 2 : 1;
-    using Lds = Tile<T, H, kRows>;
-    using Own = Tile<T, H, Shape<T, H>::kOwn>;
+    using Lds = Tile<T, in_lds(H), kRows>;
+    using Own = Tile<T, in_lds(H), Shape<T, H>::kOwn>;
     static constexpr size_t kTiles = 4 * (size_t)Lds::kBytes, kStats = kTiles + (kValuesInLds ? Own::kBytes : 0), kBytes = kStats + 4 * kRows * sizeof(float);
 };
 
@@ -220,10 +220,10 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
 
     Eight<T> k[S::kOwnBlocks][S::kSteps], v[S::kValuesInLds ? 1 : S::kOwnBlocks][S::kSteps];
     f32x4 dk[S::kOwnBlocks][S::kCols], dv[S::kOwnBlocks][S::kCols];
-    Mover<T, H, S::kRows, S::kThreads, DIRECT> mq, md;
+    Mover<T, in_lds(H), S::kRows, S::kThreads, DIRECT> mq, md;
     if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, S::kStats);
     if constexpr (S::kValuesInLds) {
-        Mover<T, H, S::kOwn, S::kThreads, DIRECT> mv;
+        Mover<T, in_lds(H), S::kOwn, S::kThreads, DIRECT> mv;
         mv.fetch(lds + S::kTiles, at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head), a.v.row, key0, len, a.head, whole);
         mv.land(lds + S::kTiles);
     }
@@ -420,6 +420,7 @@ template <typename T> int backward_of(const char* name, const AttentionArgs& a, 
     switch (held_head(a.head)) {
         case 32: return launch_backward<T, 32>(name, a, s);
         case 64: return launch_backward<T, 64>(name, a, s);
+        case 96: return launch_backward<T, 96>(name, a, s);
         case 128: return launch_backward<T, 128>(name, a, s);
         default: return launch_backward<T, 256>(name, a, s);
     }

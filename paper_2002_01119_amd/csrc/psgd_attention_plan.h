@@ -14,15 +14,16 @@ namespace psgd {
 // Compute units that parts are made for: the whole accelerator's, whatever the device has, so that a workspace's size and the order of sums are the same on any.
 constexpr int kChipUnits = 256;
 
-// A head's columns as the kernels hold them: the rest is zero.
-inline int held_head(int head) { return head <= 32 ? 32 : head <= 64 ? 64 : head <= 128 ? 128 : 256; }
+// A head's columns as the kernels hold them, the rest zero, and as their tiles in LDS do, whose rows are a power of two.
+inline int held_head(int head) { return head <= 32 ? 32 : head <= 64 ? 64 : head <= 96 ? 96 : head <= 128 ? 128 : 256; }
+constexpr int in_lds(int held) { return held == 96 ? 128 : held; }
 
 // Rows of a workgroup's own, a matrix instruction's 16 columns or two times that for each of its wavefronts, and rows of the tiles that it walks.  (32 of those at a
 // head of 128 in bf16: three workgroups fit a compute unit then, forward 4 x 8192 tokens of 8 heads 538 us, with 64 and two workgroups 564.)
 constexpr int kAttentionWaves = 4;
 constexpr int own_blocks(int held, int bytes) { return bytes == 2 && held <= 128 ? 2 : 1; }
 constexpr int own_rows(int held, int bytes) { return kAttentionWaves * 16 * own_blocks(held, bytes); }
-constexpr int walked_rows(int held, int bytes) { return held * bytes < 256 ? 64 : 32; }
+constexpr int walked_rows(int held, int bytes) { return in_lds(held) * bytes < 256 ? 64 : 32; }
 
 // Places for the own tiles of a learner's sequences: sequence s has its from starts[s] / rows + s on, which leaves every sequence room for all of its
 // tiles whatever their lengths, so that a workgroup finds its sequence by itself and no launch depends on device memory.
@@ -32,7 +33,7 @@ inline int64_t tile_places(int64_t t, int sequences, int rows) { return t / rows
 // A tile of keys is walked by one workgroup, query head after query head; how many steps (tiles of queries) that are is seen on the device.  Where that leaves
 // compute units idle a tile's steps are cut into parts, whose sums a second kernel joins in order: all tiles' where there are few of them, and the first
 // tokens' that stay visible, which every query sees while the window spares the others most.
-constexpr bool values_in_lds(int held, int bytes) { return bytes == 2 && held == 128; }
+constexpr bool values_in_lds(int held, int bytes) { return bytes == 2 && in_lds(held) == 128; }
 constexpr int query_rows(int held, int bytes) { return values_in_lds(held, bytes) ? 32 : walked_rows(held, bytes); }
 
 struct KeyParts {
@@ -51,9 +52,10 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
     const int64_t most_steps = (parts_of(narrow && window + own < t ? window + own : t, rows) + 1) * members;      // of a tile that is not a first one
     const int64_t all = tiles * (narrow ? most_steps : (most_steps + 1) / 2);
     KeyParts p{1, 1, 0, 1, 1, 0, 0, 2 * (size_t)own * held * sizeof(float)};
-    // Two rounds of what is resident, and no less than 16 steps: writing a part and reading it again takes as long as five.
+    // Two rounds of what is resident, and no less than 16 steps, 4 in float: writing a part and reading it again takes as long as five, or one.
+    const int64_t least = bytes == 4 ? 4 : 16;
     if (tiles < (narrow ? 2 : 4) * (int64_t)cus) {
-        const int64_t fair = parts_of(all, 4 * (int64_t)cus), steps = fair > 16 ? fair : 16;
+        const int64_t fair = parts_of(all, 4 * (int64_t)cus), steps = fair > least ? fair : least;
         int64_t most = parts_of(most_steps, steps);
         while (most > 1 && places * units * most > 16 * (int64_t)cus) --most;
         p.most = (int)most;
@@ -62,7 +64,7 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
     }
     if (narrow && sinks > 0) {
         // an eighth of what the others take, since they are few and the last to end; no more than 256 MB
-        const int64_t first_steps = (parts_of(t, rows) + 1) * members, steps = most_steps / 8 > 16 ? most_steps / 8 : 16;
+        const int64_t first_steps = (parts_of(t, rows) + 1) * members, steps = most_steps / 8 > least ? most_steps / 8 : least;
         const int64_t first_tiles = parts_of(sinks < t ? sinks : t, own), slots = (sequences > 0 ? sequences : 1) * first_tiles;
         const int64_t room = ((int64_t)256 << 20) / ((int64_t)p.slot_bytes * units * slots), most = parts_of(first_steps, steps);
         p.first_most = (int)(most < room ? most : room > 1 ? room : 1);
@@ -82,7 +84,7 @@ constexpr int kStepKeys = 32;               // of a wavefront at a time
 // 122 / 141, 96 of up to 4100 265 / 330, 64 of 2048 111 / 112 (all 8 key heads of 128 in bf16); four tiles for the narrowest, 256 sequences of 512 with 8 heads of 64
 // in bf16 72, two 48.
 constexpr int kStepStages = 2;
-constexpr int step_waves(int held, int bytes) { return held * bytes <= 256 ? 4 : held * bytes == 512 ? 2 : 1; }
+constexpr int step_waves(int held, int bytes) { return in_lds(held) * bytes <= 256 ? 4 : in_lds(held) * bytes == 512 ? 2 : 1; }
 // Parts that a sequence's keys are cut into: as many workgroups as are there at once, and no fewer keys than two tiles a wavefront.  (One sequence of 131 072
 // positions with twice the workgroups 134 us, with four times 168.)
 inline int step_parts(int64_t units, int64_t most_keys, int head, int bytes) {

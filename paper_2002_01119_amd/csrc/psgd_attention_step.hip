@@ -58,7 +58,7 @@ struct Seen {
 
 template <typename T, int H> struct StepShape {
     static constexpr int kSteps = H / 32, kCols = H / 16, kWaves = step_waves(H, sizeof(T)), kStages = kStepStages;
-    using Lds = Tile<T, H, kStepKeys>;
+    using Lds = Tile<T, in_lds(H), kStepKeys>;
     static constexpr int kMoves = kStepKeys * Lds::kGroups / kWave;      // 16-byte groups of a tile that a lane moves
     static constexpr size_t kTiles = (size_t)kWaves * kStages * 2 * Lds::kBytes, kJoin = (size_t)kWaves * 16 * (H + 2) * sizeof(float);
     static constexpr size_t kLds = kTiles > kJoin ? kTiles : kJoin;
@@ -279,6 +279,7 @@ template <typename T> int step_of(const char* name, const StepArgs& a, int64_t u
     switch (held_head(a.head)) {
         case 32: return launch_step<T, 32>(name, a, units, rows, s);
         case 64: return launch_step<T, 64>(name, a, units, rows, s);
+        case 96: return launch_step<T, 96>(name, a, units, rows, s);
         case 128: return launch_step<T, 128>(name, a, units, rows, s);
         default: return launch_step<T, 256>(name, a, units, rows, s);
     }

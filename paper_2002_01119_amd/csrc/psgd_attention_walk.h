@@ -166,10 +166,10 @@ template <typename T, int H> struct Shape {
     static constexpr int kOwnBlocks = own_blocks(H, sizeof(T)), kOwn = own_rows(H, sizeof(T)), kWalked = walked_rows(H, sizeof(T));
     static constexpr int kThreads = kAttentionWaves * kWave, kBlocks = kWalked / 16, kSteps = H / 32, kCols = H / 16;
     static constexpr int kTwice = H * sizeof(T) < 1024 ? 2 : 1;      // workgroups of a compute unit, which its registers are shared out to
-    using Lds = Tile<T, H, kWalked>;
+    using Lds = Tile<T, in_lds(H), kWalked>;
 };
 
-template <typename T, int H> constexpr size_t kTileLds = 4 * (size_t)Tile<T, H, walked_rows(H, sizeof(T))>::kBytes;
+template <typename T, int H> constexpr size_t kTileLds = 4 * (size_t)Tile<T, in_lds(H), walked_rows(H, sizeof(T))>::kBytes;
 using AttentionKernel = void (*)(AttentionArgs);
 
 // Whether tiles of these operands can go straight to LDS: heads and rows on 16 bytes, a tile within 31 bits.
