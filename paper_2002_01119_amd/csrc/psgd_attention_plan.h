@@ -52,8 +52,9 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
     const int64_t most_steps = (parts_of(narrow && window + own < t ? window + own : t, rows) + 1) * members;      // of a tile that is not a first one
     const int64_t all = tiles * (narrow ? most_steps : (most_steps + 1) / 2);
     KeyParts p{1, 1, 0, 1, 1, 0, 0, 2 * (size_t)own * held * sizeof(float)};
-    // Two rounds of what is resident, and no less than 16 steps, 4 in float: writing a part and reading it again takes as long as five, or one.
-    const int64_t least = bytes == 4 ? 4 : 16;
+    // Two rounds of what is resident, and no less than 16 steps: writing a part and reading it again takes as long as five.  No less than 4 in float, where a
+    // step takes as long as that, and where the chip would not be full of longer ones.  (512 tokens of 8 heads of 128, two key heads, bf16, backward 68 us, so 52.)
+    const int64_t least = bytes == 4 || all < 16 * (int64_t)cus ? 4 : 16;
     if (tiles < (narrow ? 2 : 4) * (int64_t)cus) {
         const int64_t fair = parts_of(all, 4 * (int64_t)cus), steps = fair > least ? fair : least;
         int64_t most = parts_of(most_steps, steps);
