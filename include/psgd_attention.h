@@ -42,7 +42,7 @@ enum { PSGD_PAIRS_HALVES = 0, PSGD_PAIRS_NEIGHBOURS = 1 };
  *   q, q_out [n, t, heads * head], k, k_out [n, t, kv * head], one type, float or bf16; q_out may be q and k_out k (same pointer and strides)
  *   positions  int32 [n, t] (`row` is the stride between tokens) or NULL: the row's number
  *   q_gain, k_gain  [n, head], float or bf16 alike, or both NULL: no norm, the rotation alone
- * rotary even, in 0..head; base > 0 and finite; eps >= 0.  heads or kv may be 0 (its operands are then ignored).
+ * rotary even, in 0..head; base finite, 1 or more; eps >= 0.  heads or kv may be 0 (its operands are then ignored).
  */
 int psgd_qk_norm_rope(const psgd_view* q, const psgd_view* k, const psgd_view* positions, const psgd_view* q_gain, const psgd_view* k_gain,
                       const psgd_view* q_out, const psgd_view* k_out, int heads, int kv, int head, int rotary, int pairs, double base, float eps,

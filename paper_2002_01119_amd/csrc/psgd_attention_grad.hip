@@ -433,7 +433,8 @@ extern "C" {
 
 size_t psgd_attention_grad_workspace(int heads, int kv, int head, int window, int sinks, int sequences, int n, int64_t t) {
     using namespace psgd;
-    if (n < 1 || n > PSGD_MAX_N || t < 1 || t > INT32_MAX || heads < 1 || kv < 1 || heads % kv || head < 1 || head > PSGD_MAX_HEAD || sequences < 0) return 0;
+    clear_error();
+    if (t == 0 || check_sizes("psgd_attention_grad_workspace", heads, kv, head, window, sinks, sequences, n, t)) return 0;
     size_t most = 0;             // of either type
     for (int bytes : {2, 4}) most = std::max(most, key_parts(heads, kv, head, bytes, window, sinks, sequences, n, t).bytes(n * kv));
     return up256((size_t)n * heads * t * sizeof(float)) + most;

@@ -67,7 +67,7 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
         // an eighth of what the others take, since they are few and the last to end; no more than 256 MB
         const int64_t first_steps = (parts_of(t, rows) + 1) * members, steps = most_steps / 8 > least ? most_steps / 8 : least;
         const int64_t first_tiles = parts_of(sinks < t ? sinks : t, own), slots = (sequences > 0 ? sequences : 1) * first_tiles;
-        const int64_t room = ((int64_t)256 << 20) / ((int64_t)p.slot_bytes * units * slots), most = parts_of(first_steps, steps);
+        const int64_t room = (int64_t)((double)(256 << 20) / ((double)p.slot_bytes * (double)units * (double)slots)), most = parts_of(first_steps, steps);
         p.first_most = (int)(most < room ? most : room > 1 ? room : 1);
         if (p.first_most > 1) {
             p.first_tiles = (int)first_tiles;

@@ -287,36 +287,50 @@ template <typename T> int step_of(const char* name, const StepArgs& a, int64_t u
 
 inline int64_t most_seen(int window, int sinks, int64_t slots) { return window && (int64_t)window + sinks < slots ? (int64_t)window + sinks : slots; }
 
+// A cache's strides that are stepped along, the smallest first: each has to step over what those before it cover.
+struct Counts {
+    struct {
+        int64_t stride, count;
+    } at[3];
+    int many = 0;
+    Counts(const psgd_cache& c, int64_t n, int64_t b, int64_t slots) {
+        const int64_t strides[3] = {c.learner, c.sequence, c.row}, counts[3] = {n, b, slots};
+        for (int i = 0; i < 3; ++i)
+            if (counts[i] > 1) at[many++] = {strides[i], counts[i]};
+        std::sort(at, at + many, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    }
+};
+
 // A cache as an output: no two of its rows share an address.
 inline int check_cache(const char* name, const char* what, const psgd_cache& c, int n, int64_t b, int64_t slots, int64_t width) {
     if (!c.data) return fail(PSGD_EINVAL, "%s: %s is a null pointer", name, what);
     if (reinterpret_cast<uintptr_t>(c.data) % elem_bytes(c.type)) return fail(PSGD_EALIGN, "%s: %s is not aligned to its element size", name, what);
     if (c.learner < 0 || c.sequence < 0 || c.row < 0) return fail(PSGD_EINVAL, "%s: a stride of %s is negative", name, what);
     if (c.learner > kMostElements / n || c.sequence > kMostElements / b || c.row > kMostElements / slots) return fail(PSGD_EINVAL, "%s: %s is too large", name, what);
-    // the three counts by stride: each has to step over what those of smaller strides cover
-    struct {
-        int64_t stride, count;
-    } d[3] = {{c.learner, n}, {c.sequence, b}, {c.row, slots}};
-    std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    const Counts d(c, n, b, slots);
     int64_t covered = width;
-    for (const auto& x : d) {
-        if (x.count == 1) continue;
-        if (x.stride < covered) return fail(PSGD_EALIAS, "%s: rows of %s overlap", name, what);
-        covered += (x.count - 1) * x.stride;
+    for (int i = 0; i < d.many; ++i) {
+        if (d.at[i].stride < covered) return fail(PSGD_EALIAS, "%s: rows of %s overlap", name, what);
+        covered += (d.at[i].count - 1) * d.at[i].stride;
     }
     return PSGD_OK;
 }
-// Whether the caches share a byte: unless their rows, sequences or learners are as far apart and interleave.
+// Whether two caches, each in order, share a byte: unless, at one of their strides, what lies within one step of it interleaves.
 inline bool caches_meet(const psgd_cache& a, const psgd_cache& b, int n, int64_t s, int64_t slots, int64_t width) {
     const int64_t unit = elem_bytes(a.type), span = ((n - 1) * a.learner + (s - 1) * a.sequence + (slots - 1) * a.row + width) * unit;
     const int64_t span_b = ((n - 1) * b.learner + (s - 1) * b.sequence + (slots - 1) * b.row + width) * unit;
     const uintptr_t x = reinterpret_cast<uintptr_t>(a.data), y = reinterpret_cast<uintptr_t>(b.data);
     if (x + span <= y || y + span_b <= x) return false;
-    if (a.learner != b.learner || a.sequence != b.sequence || a.row != b.row) return true;
-    const int64_t in_sequence = ((slots - 1) * a.row + width) * unit, in_learner = in_sequence + (s - 1) * a.sequence * unit;
-    if (n > 1 && !combs_meet(x, in_learner, y, in_learner, a.learner * unit)) return false;
-    if (s > 1 && (n == 1 || a.learner % a.sequence == 0) && !combs_meet(x, in_sequence, y, in_sequence, a.sequence * unit)) return false;
-    return slots == 1 || (s > 1 && a.sequence % a.row) || (n > 1 && a.learner % a.row) || combs_meet(x, width * unit, y, width * unit, a.row * unit);
+    if ((n > 1 && a.learner != b.learner) || (s > 1 && a.sequence != b.sequence) || (slots > 1 && a.row != b.row)) return true;
+    const Counts d(a, n, s, slots);
+    int64_t inner = width;
+    for (int i = 0; i < d.many; ++i) {
+        bool steps = true;          // whether the larger strides are whole steps of this one
+        for (int k = i + 1; k < d.many; ++k) steps &= d.at[k].stride % d.at[i].stride == 0;
+        if (steps && !combs_meet(x, inner * unit, y, inner * unit, d.at[i].stride * unit)) return false;
+        inner += (d.at[i].count - 1) * d.at[i].stride;
+    }
+    return true;
 }
 // Its bytes from the first to behind the last, as one operand.
 inline Extent cache_extent(const char* what, const psgd_cache& c, int n, int64_t b, int64_t slots, int64_t width, psgd_view* room) {

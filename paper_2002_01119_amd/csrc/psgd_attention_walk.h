@@ -180,17 +180,22 @@ template <typename T, int H> bool straight(int head, std::initializer_list<Heads
     return true;
 }
 
-inline int check_shape(const char* name, int heads, int kv, int head, int window, int sinks, float scale, int sequences, const psgd_view* starts, int n, int64_t t) {
+inline int check_sizes(const char* name, int heads, int kv, int head, int window, int sinks, int sequences, int n, int64_t t) {
     if (heads < 1 || kv < 1 || heads % kv) return fail(PSGD_EINVAL, "%s: kv=%d does not divide heads=%d", name, kv, heads);
     if (head < 1 || head > PSGD_MAX_HEAD) return fail(PSGD_EINVAL, "%s: head=%d outside 1..%d", name, head, (int)PSGD_MAX_HEAD);
     if (int rc = check_counts(name, n, t, (int64_t)heads * head)) return rc;
     if (window < 0 || sinks < 0 || (sinks && !window)) return fail(PSGD_EINVAL, "%s: window=%d with sinks=%d", name, window, sinks);
-    if (!std::isfinite(scale)) return fail(PSGD_EINVAL, "%s: scale=%g", name, (double)scale);
-    if (sequences < 0 || (sequences > 0) != (starts != nullptr)) return fail(PSGD_EINVAL, "%s: sequences=%d %s starts", name, sequences, starts ? "with" : "without");
-    if (starts && starts->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: starts must be int32", name);
+    if (sequences < 0) return fail(PSGD_EINVAL, "%s: sequences=%d", name, sequences);
     // a row's number and a tile's end are counted in 32 bits, and so are all learners' heads
     if (t > INT32_MAX - 1024 || (int64_t)n * heads > INT32_MAX || sequences > INT32_MAX - 1024 || (double)n * heads * ((double)t + sequences) > 1e15)
         return fail(PSGD_EINVAL, "%s: a size beyond 2^31 - 1", name);
+    return PSGD_OK;
+}
+inline int check_shape(const char* name, int heads, int kv, int head, int window, int sinks, float scale, int sequences, const psgd_view* starts, int n, int64_t t) {
+    if (int rc = check_sizes(name, heads, kv, head, window, sinks, sequences, n, t)) return rc;
+    if (!std::isfinite(scale)) return fail(PSGD_EINVAL, "%s: scale=%g", name, (double)scale);
+    if ((sequences > 0) != (starts != nullptr)) return fail(PSGD_EINVAL, "%s: sequences=%d %s starts", name, sequences, starts ? "with" : "without");
+    if (starts && starts->type != PSGD_I32) return fail(PSGD_EINVAL, "%s: starts must be int32", name);
     return PSGD_OK;
 }
 

@@ -427,7 +427,8 @@ inline int fill_args(const char* name, QkArgs& a, int heads, int kv, int head, i
     if ((int64_t)heads * head > INT32_MAX || (int64_t)kv * head > INT32_MAX) return fail(PSGD_EINVAL, "%s: a size beyond 2^31 - 1", name);
     if (rotary < 0 || rotary > head || rotary % 2) return fail(PSGD_EINVAL, "%s: rotary=%d is not an even number in 0..%d", name, rotary, head);
     if (pairs != PSGD_PAIRS_HALVES && pairs != PSGD_PAIRS_NEIGHBOURS) return fail(PSGD_EINVAL, "%s: pairs=%d", name, pairs);
-    if (!(base > 0.0) || !std::isfinite(base)) return fail(PSGD_EINVAL, "%s: base=%g", name, base);
+    // (below 1 a rate would be above a turn for each radian and an angle beyond what 64 bits resolve)
+    if (!(base >= 1.0) || !std::isfinite(base)) return fail(PSGD_EINVAL, "%s: base=%g", name, base);
     if (!(eps >= 0.0f) || !std::isfinite(eps)) return fail(PSGD_EINVAL, "%s: eps=%g", name, (double)eps);
     a.t = t;
     a.heads[0] = heads;
@@ -438,8 +439,6 @@ inline int fill_args(const char* name, QkArgs& a, int heads, int kv, int head, i
     a.eps = eps;
     a.inv_head = 1.0f / (float)head;
     for (int p = 0; p < kMostPairs; ++p) a.turn[p] = p < rotary / 2 ? std::pow(base, -2.0 * p / rotary) / (2.0 * M_PI) : 0.0;
-    for (int p = 0; p < rotary / 2; ++p)
-        if (!std::isfinite(a.turn[p])) return fail(PSGD_EINVAL, "%s: base=%g", name, base);
     return PSGD_OK;
 }
 

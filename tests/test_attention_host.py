@@ -59,7 +59,7 @@ def qk(lib, heads=HEADS, kv=KV, head=HEAD, rotary=HEAD, pairs=0, base=10000.0, e
     (dict(n=0), psgd.EINVAL, "n=0"), (dict(n=513), psgd.EINVAL, "n=513"), (dict(t=-1), psgd.EINVAL, "negative"), (dict(t=1 << 31), psgd.EINVAL, "2^31"),
     (dict(head=0), psgd.EINVAL, "head=0"), (dict(head=257), psgd.EINVAL, "head=257"), (dict(heads=-1), psgd.EINVAL, "heads=-1"), (dict(heads=1 << 30), psgd.EINVAL, "2^31"),
     (dict(rotary=3), psgd.EINVAL, "rotary=3"), (dict(rotary=10), psgd.EINVAL, "rotary=10"), (dict(rotary=-2), psgd.EINVAL, "rotary=-2"), (dict(pairs=2), psgd.EINVAL, "pairs=2"),
-    (dict(base=0.0), psgd.EINVAL, "base"), (dict(base=float("nan")), psgd.EINVAL, "base"), (dict(base=float("inf")), psgd.EINVAL, "base"), (dict(base=5e-324), psgd.EINVAL, None),
+    (dict(base=0.0), psgd.EINVAL, "base"), (dict(base=0.99), psgd.EINVAL, "base"), (dict(base=float("nan")), psgd.EINVAL, "base"), (dict(base=float("inf")), psgd.EINVAL, "base"), (dict(base=5e-324), psgd.EINVAL, "base"),
     (dict(eps=-1.0), psgd.EINVAL, "eps"), (dict(eps=float("inf")), psgd.EINVAL, "eps"), (dict(q=None), psgd.EINVAL, "null operand"), (dict(k_out=None), psgd.EINVAL, "null operand"),
     (dict(k_gain=None), psgd.EINVAL, "go together"), (dict(q=wide(1, BF16)), psgd.EINVAL, "alike"), (dict(k=narrow(2, I32)), psgd.EINVAL, "alike"),
     (dict(q_gain=flat(3, BF16)), psgd.EINVAL, "alike"), (dict(q_gain=flat(3, I32), k_gain=flat(4, I32)), psgd.EINVAL, "alike"),
@@ -70,9 +70,6 @@ def qk(lib, heads=HEADS, kv=KV, head=HEAD, rotary=HEAD, pairs=0, base=10000.0, e
     (dict(k_out=View(place(5) + 64, T * CK, CK, F32)), psgd.EALIAS, "q_out overlaps k_out"), (dict(q_out=wide(3)), psgd.EALIAS, "q_out overlaps q_gain"),
 ])
 def test_qk_norm_rope_refusals(change, code, text):
-    if text is None:                                       # a base so small that a rate is beyond the 64 bits
-        change, text = dict(base=5e-324, head=256, rotary=256, q=View(place(1), 1 << 16, 1 << 10, F32), k=View(place(2), 1 << 16, 1 << 9, F32),
-                            q_out=View(place(5), 1 << 16, 1 << 10, F32), k_out=View(place(6), 1 << 16, 1 << 9, F32)), "base"
     refused(qk(attention.load(), **change), code, text)
 
 
@@ -172,6 +169,17 @@ def test_attention_step_refusals(change, code, text):
     refused(step(attention.load(), **change), code, text)
 
 
+@pytest.mark.parametrize("strides,apart,meet", [
+    ((960, 320, 32), 16, False), ((960, 320, 32), 15, True), ((960, 320, 32), 17, True),             # rows side by side
+    ((960, 32, 96), 16, False), ((32, 64, 320), 16, False), ((32, 64, 320), 8, True),                # sequences or learners innermost
+    ((960, 320, 16), 160, False), ((960, 320, 16), 144, True),                                      # a sequence's keys, then its values
+])
+def test_caches_between_each_others_rows(strides, apart, meet):
+    lib = attention.load()
+    rc = step(lib, ck=Cache(place(4), *strides, F32), cv=Cache(place(4) + 4 * apart, *strides, F32), out=View(place(4), B * CQ, CQ, F32))
+    refused(rc, psgd.EALIAS, "cache_k overlaps cache_v") if meet else refused(rc, psgd.EALIAS, "cache_k overlaps out")
+
+
 def dropout(lib, p=0.5, n=N, t=T, c=8, step_dev=None, **over):
     v = dict(x=View(place(1), T * 8, 8, F32), residual=None, y=View(place(2), T * 8, 8, F32))
     v.update(over)
@@ -195,6 +203,12 @@ def test_workspaces_of_nothing():
     assert lib.psgd_qk_norm_rope_grad_workspace(4, 10, 100) % 256 == 0 and lib.psgd_qk_norm_rope_grad_workspace(4, 10, 100) >= 4 * 2 * 100 * 4
     assert lib.psgd_attention_grad_workspace(4, 2, 64, 0, 0, 0, 0, 5) == 0 and lib.psgd_attention_grad_workspace(4, 2, 64, 0, 0, 0, 2, 0) == 0
     assert lib.psgd_attention_grad_workspace(4, 2, 64, 0, 0, 0, 2, 100) >= 2 * 4 * 100 * 4
+    big = 2 ** 31 - 1                                      # sizes that would overflow, each refused before they are multiplied
+    for sizes in ((big, big, 64, 0, 0, 0, 256, 5), (4, 2, 64, -1, 0, 0, 2, 100), (4, 2, 64, 0, 3, 0, 2, 100), (4, 2, 64, 8, 1, big, 2, 100), (4, 2, 64, 8, 1, 1, 2, big),
+                  (1 << 22, 1 << 22, 1, 1 << 15, 1 << 15, 1 << 20, 512, 1 << 16)):
+        assert lib.psgd_attention_grad_workspace(*sizes) == 0
+    assert 0 < lib.psgd_attention_grad_workspace(1 << 10, 1 << 10, 256, 1 << 15, 1 << 15, 1 << 20, 1, 1 << 16) < 1 << 40
+    assert lib.psgd_attention_step_workspace(4, 2, 64, 0, 0, 1, 0, 9) == 0 and lib.psgd_attention_step_workspace(4, 2, 64, 0, 0, 1, 1, 1 << 31) == 0
 
 
 def test_binding_refuses_host_tensors_and_shapes():
