@@ -29,6 +29,12 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     // a negative scale's sign goes to the queries; one of 0 is next to nothing, which leaves what is masked at -inf
     const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f);
 
+    const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
+    const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
+    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
+    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
+    mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
+    mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     Eight<T> q[S::kOwnBlocks][S::kSteps];
     f32x4 o[S::kOwnBlocks][S::kCols];
     float top[S::kOwnBlocks], sum[S::kOwnBlocks];
@@ -47,12 +53,6 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
         top[b] = -INFINITY;
         sum[b] = 0.0f;
     }
-    const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
-    const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
-    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
-    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
-    mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
-    mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     mk.land(lds);
     mv.land(lds + Lds::kBytes);
     __syncthreads();

@@ -82,19 +82,6 @@ __device__ __forceinline__ Eight<uint16_t> rest_of(const Eight<uint16_t>& r, f32
     }
     return as_operand<uint16_t>(low, high);
 }
-__device__ __forceinline__ float dot(const Eight<uint16_t>& a, const Eight<uint16_t>& b) {
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s = __builtin_fmaf(low_bf16(a.v[i]), low_bf16(b.v[i]), __builtin_fmaf(high_bf16(a.v[i]), high_bf16(b.v[i]), s));
-    return s;
-}
-__device__ __forceinline__ float dot(const Eight<float>& a, const Eight<float>& b) {
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s = __builtin_fmaf(a.v[i], b.v[i], s);
-    return s;
-}
-
 // 16 bytes of a row of `left` elements more; `whole`: rows are a whole number of them.  Nothing is read where left <= 0.
 template <typename T> __device__ __forceinline__ u32x4 load_group(const T* p, int left, bool whole) {
     if (whole) {

@@ -2,21 +2,50 @@
 //
 //     D_i = do_i . o_i,   ds_ij = p_ij (do_i . v_j - D_i),   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,   dv_j = sum_i p_ij do_i
 //
-// In two kernels, so that every sum has one owner and a fixed order: the first owns queries and makes dq (and D, which the second reads), the second owns keys,
-// walks the queries that see them, of all heads that share the key head, and makes dk and dv.  Both compute s and p again from lse: seven products, of which
-// five are what the gradients cannot do without.
+// Every sum has one owner and a fixed order: one kind of workgroup owns queries and makes dq, the other owns keys, walks the queries that see them, of all heads that
+// share the key head, and makes dk and dv.  Both compute s and p again from lse: seven products, of which five are what the gradients cannot do without.  D, which both
+// read, comes first, in a pass of its own (4 x 4096 tokens of 32 heads of 128 in bf16 54 us, 5.0 TB/s).  The two kinds are one launch, keys first: those are
+// fewer and longer, and the queries' fill what they leave idle (a launch each: 4 x 4096 tokens in sequences of 1024 810 us, so 717; 1024 tokens of 8 heads 114, so 87).
+//
+// Bound by the matrix units' pace together with what feeds them: 4 x 4096 tokens of 32 heads of 128, eight key heads, in bf16 2065 us, 665 Tflop/s counted by five
+// products, 930 by the seven that are computed.
 #include "psgd_attention_walk.h"
 
 namespace psgd {
 namespace {
 
-// dq and D.  Queries and their gradients stay in registers, keys and values are walked as above, 32 rows of a tile at a time.
-template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (Shape<T, H>::kTwice)) void attention_dq_kernel(AttentionArgs a) {
+// D, of every row of a sequence.  One pass over two arrays: `lanes` of a wavefront take a row, 16 bytes each, a workgroup kAlongRows of a head.
+constexpr int kAlongRows = 64;
+template <typename T> __global__ __launch_bounds__(kAttentionWaves* kWave) void attention_along_kernel(AttentionArgs a, int lanes) {
+    const int64_t id = a.first + blockIdx.x, pair = id / a.heads, blocks = (a.t + kAlongRows - 1) / kAlongRows;
+    const int h = (int)(id % a.heads), i = (int)(pair / blocks), at_once = kWave / lanes * kAttentionWaves;
+    const int row0 = (int)(pair % blocks) * kAlongRows, col = threadIdx.x % lanes * kPer<T>;
+    int lo = 0, hi = (int)a.t;                  // the sequences follow each other
+    if (a.starts) {
+        const int32_t* const starts = a.starts + i * a.starts_learner;
+        lo = std::max(starts[0], 0);
+        hi = std::min(starts[a.sequences], hi);
+    }
+    const bool whole = a.head % kPer<T> == 0;
+    for (int r = threadIdx.x / lanes; r < kAlongRows; r += at_once) {
+        const int row = row0 + r, left = row >= lo && row < hi ? a.head - col : 0;
+        const u32x4 x = load_group(at<T>(a.dout, i, row, (int64_t)h * a.head + col), left, whole), y = load_group(at<T>(a.o, i, row, (int64_t)h * a.head + col), left, whole);
+        float u[kPer<T>], v[kPer<T>], d = 0.0f;
+        widen<T>(x, u);
+        widen<T>(y, v);
+#pragma unroll
+        for (int e = 0; e < kPer<T>; ++e) d = __builtin_fmaf(u[e], v[e], d);
+        for (int m = 1; m < lanes; m *= 2) d += __shfl_xor(d, m);
+        if (col == 0 && left > 0) a.along[((int64_t)i * a.heads + h) * a.t + row] = d;
+    }
+}
+
+// dq.  Queries and their gradients stay in registers, keys and values are walked as in the forward pass, 32 rows of a tile at a time.
+template <typename T, int H, bool DIRECT> __device__ __forceinline__ void queries_gradients(AttentionArgs a, int64_t id, char* lds) {
     using S = Shape<T, H>;
     using Lds = typename S::Lds;
-    extern __shared__ __attribute__((aligned(16))) char lds[];
     const int members = a.heads / a.kv;
-    const Work w = find_work<S::kOwn>(a, a.first + blockIdx.x, members, true);
+    const Work w = find_work<S::kOwn>(a, id, members, true);
     if (!w.there) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo;
     const int h = w.kv_head * members + w.member, row0 = w.tile * S::kOwn, row1 = std::min(row0 + S::kOwn, len);
@@ -29,25 +58,26 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f), lse_by = kStart ? kLog2E / to_log2 : kLog2E;
     const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo;
 
+    const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
+    const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
+    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
+    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
+    mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
+    mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     Eight<T> q[S::kOwnBlocks][S::kSteps], dy[S::kOwnBlocks][S::kSteps];
     f32x4 dq[S::kOwnBlocks][S::kCols];
     float lse[S::kOwnBlocks], along[S::kOwnBlocks];
 #pragma unroll
     for (int b = 0; b < S::kOwnBlocks; ++b) {
         const int row = mine + 16 * b + col, left = row < len ? a.head : 0;
-        const T *pq = at<T>(a.q, w.learner, w.lo + row, (int64_t)h * a.head), *pd = at<T>(a.dout, w.learner, w.lo + row, (int64_t)h * a.head),
-                *po = at<T>(a.o, w.learner, w.lo + row, (int64_t)h * a.head);
-        float d = 0.0f;
+        const T *pq = at<T>(a.q, w.learner, w.lo + row, (int64_t)h * a.head), *pd = at<T>(a.dout, w.learner, w.lo + row, (int64_t)h * a.head);
 #pragma unroll
         for (int kc = 0; kc < S::kSteps; ++kc) {
             q[b][kc] = load_eight(pq, kc, g, left, whole);
             dy[b][kc] = load_eight(pd, kc, g, left, whole);
-            d += dot(dy[b][kc], load_eight(po, kc, g, left, whole));
         }
-        d = column_all<Sum>(d);
-        along[b] = -d;
+        along[b] = row < len ? -a.along[stat + row] : 0.0f;
         lse[b] = row < len ? -a.lse[stat + row] * lse_by : -INFINITY;     // rows that are not there: p = 0
-        if (row < len && g == 0) a.along[stat + row] = d;
         if (a.scale < 0.0f) {
 #pragma unroll
             for (int kc = 0; kc < S::kSteps; ++kc) q[b][kc] = negative(q[b][kc]);
@@ -55,12 +85,6 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
 #pragma unroll
         for (int c = 0; c < S::kCols; ++c) dq[b][c] = (f32x4){0, 0, 0, 0};
     }
-    const T *keys = at<T>(a.k, w.learner, w.lo, (int64_t)w.kv_head * a.head), *values = at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head);
-    const KeyWalk walk(row0, row1, a.window, a.sinks, S::kWalked);
-    Mover<T, in_lds(H), S::kWalked, S::kThreads, DIRECT> mk, mv;
-    if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
-    mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
-    mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     mk.land(lds);
     mv.land(lds + Lds::kBytes);
     __syncthreads();
@@ -83,12 +107,12 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                 for (int kb = 0; kb < 2; ++kb) {
 #pragma unroll
                     for (int b = 0; b < S::kOwnBlocks; ++b) {
-                        s[b][kb] = kStart ? (f32x4){lse[b], lse[b], lse[b], lse[b]} : (f32x4){0, 0, 0, 0};
-                        dp[b][kb] = kStart ? (f32x4){along[b], along[b], along[b], along[b]} : (f32x4){0, 0, 0, 0};
+                        s[b][kb] = dp[b][kb] = (f32x4){0, 0, 0, 0};
+                        if constexpr (kStart) s[b][kb] += lse[b], dp[b][kb] += along[b];
                     }
 #pragma unroll
                     for (int kc = 0; kc < S::kSteps; ++kc) {
-                            const Eight<T> k = Lds::along(along_at + buffer, 2 * half + kb, kc), v = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + kb, kc);
+                        const Eight<T> k = Lds::along(along_at + buffer, 2 * half + kb, kc), v = Lds::along(along_at + buffer + Lds::kBytes, 2 * half + kb, kc);
 #pragma unroll
                         for (int b = 0; b < S::kOwnBlocks; ++b) {
                             s[b][kb] = mma(k, q[b][kc], s[b][kb]);
@@ -191,17 +215,16 @@ template <typename T, int H> struct KeyShape : Shape<T, H> {
     // 128 columns in bf16: keys and both gradients are 160 registers, and with the values' 32 two workgroups would not fit a compute unit
     static constexpr bool kValuesInLds = values_in_lds(H, sizeof(T));
     static constexpr int kRows = query_rows(H, sizeof(T));
-    static constexpr int kTwice = sizeof(T) == 2 && H <= 128 ? 2 : 1;
+    static constexpr int kTwice = H <= 128 ? 2 : 1;
     using Lds = Tile<T, in_lds(H), kRows>;
     using Own = Tile<T, in_lds(H), Shape<T, H>::kOwn>;
     static constexpr size_t kTiles = 4 * (size_t)Lds::kBytes, kStats = kTiles + (kValuesInLds ? Own::kBytes : 0), kBytes = kStats + 4 * kRows * sizeof(float);
 };
 
-template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (KeyShape<T, H>::kTwice)) void attention_dkv_kernel(AttentionArgs a) {
+// In LDS: two tiles of queries and gradients, values, two of [2][rows] statistics.
+template <typename T, int H, bool DIRECT> __device__ __forceinline__ void keys_gradients(AttentionArgs a, int64_t id, char* lds) {
     using S = KeyShape<T, H>;
     using Lds = typename S::Lds;
-    extern __shared__ __attribute__((aligned(16))) char lds[];       // two of queries and gradients, values, two of [2][rows] statistics
-    const int64_t id = a.first + blockIdx.x;
     const Work w = id < a.firsts ? first_work<S::kOwn>(a, id, a.first_parts) : find_work<S::kOwn, true>(a, id - a.firsts, a.most_parts, false);
     if (!w.there || (id >= a.firsts && w.tile < a.first_tiles)) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo, members = a.heads / a.kv;
@@ -225,7 +248,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     if constexpr (S::kValuesInLds) {
         Mover<T, in_lds(H), S::kOwn, S::kThreads, DIRECT> mv;
         mv.fetch(lds + S::kTiles, at<T>(a.v, w.learner, w.lo, (int64_t)w.kv_head * a.head), a.v.row, key0, len, a.head, whole);
-        mv.land(lds + S::kTiles);
+        if (!DIRECT) mv.land(lds + S::kTiles);       // else with the first tiles
     }
 #pragma unroll
     for (int b = 0; b < S::kOwnBlocks; ++b) {
@@ -244,16 +267,21 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     auto fetch = [&](int step) {
         char* const tile = lds + (step & 1) * 2 * Lds::kBytes;
         const int h = w.kv_head * members + step / walk.tiles, row0 = (walk.first + step % walk.tiles) * S::kRows, row = row0 + threadIdx.x;
-        mq.fetch(tile, at<T>(a.q, w.learner, w.lo, (int64_t)h * a.head), a.q.row, row0, len, a.head, whole);
-        md.fetch(tile + Lds::kBytes, at<T>(a.dout, w.learner, w.lo, (int64_t)h * a.head), a.dout.row, row0, len, a.head, whole);
+        const T *const pq = at<T>(a.q, w.learner, w.lo, (int64_t)h * a.head), *const pd = at<T>(a.dout, w.learner, w.lo, (int64_t)h * a.head);
+        if constexpr (DIRECT) {
+            mq.fetch(tile, pq, a.q.row, row0, len, a.head, whole);
+            md.fetch(tile + Lds::kBytes, pd, a.dout.row, row0, len, a.head, whole);
+        } else {
+            mq.carry(tile, pq, a.q.row, row0, len, a.head, whole);
+            md.carry(tile + Lds::kBytes, pd, a.dout.row, row0, len, a.head, whole);
+        }
         const int64_t stat = ((int64_t)w.learner * a.heads + h) * a.t + w.lo + row;
         const bool there = threadIdx.x < S::kRows && row < len;
         held[0] = there ? -a.lse[stat] * lse_by : -INFINITY;
         held[1] = there ? -a.along[stat] : 0.0f;
     };
     auto land = [&](int buffer) {
-        mq.land(lds + buffer * 2 * Lds::kBytes);
-        md.land(lds + buffer * 2 * Lds::kBytes + Lds::kBytes);
+        if constexpr (DIRECT) mq.land(lds + buffer * 2 * Lds::kBytes);
         if (threadIdx.x < S::kRows) {
             stats[buffer * 2 * S::kRows + threadIdx.x] = held[0];
             stats[(buffer * 2 + 1) * S::kRows + threadIdx.x] = held[1];
@@ -282,8 +310,8 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                     along[qb] = *reinterpret_cast<const f32x4*>(st + S::kRows + row);
 #pragma unroll
                     for (int b = 0; b < S::kOwnBlocks; ++b) {
-                        s[b][qb] = kStart ? lse[qb] : (f32x4){0, 0, 0, 0};
-                        dp[b][qb] = kStart ? along[qb] : (f32x4){0, 0, 0, 0};
+                        s[b][qb] = dp[b][qb] = (f32x4){0, 0, 0, 0};
+                        if constexpr (kStart) s[b][qb] = lse[qb], dp[b][qb] = along[qb];
                     }
                 }
 #pragma unroll
@@ -369,6 +397,13 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     }
 }
 
+template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (KeyShape<T, H>::kTwice)) void attention_grad_kernel(AttentionArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int64_t id = a.first + blockIdx.x;
+    if (id < a.of_keys) keys_gradients<T, H, DIRECT>(a, id, lds);
+    else queries_gradients<T, H, DIRECT>(a, id - a.of_keys, lds);
+}
+
 // Joins the parts of a tile, in order: a workgroup for 1024 of a tile's numbers, which is one load of each lane's from each part.
 template <typename T, int H> __global__ __launch_bounds__(256) void attention_join_kernel(AttentionArgs a) {
     constexpr int OWN = own_rows(H, sizeof(T));
@@ -389,23 +424,24 @@ template <typename T, int H> __global__ __launch_bounds__(256) void attention_jo
 }
 
 template <typename T, int H> int launch_backward(const char* name, AttentionArgs a, hipStream_t s) {
-    static LdsRecord record_q[2] = {}, record_kv[2] = {};
-    const bool dq = straight<T, H>(a.head, {a.k, a.v}), dkv = straight<T, H>(a.head, {a.q, a.dout, a.v});
-    const AttentionKernel fq = dq ? attention_dq_kernel<T, H, true> : attention_dq_kernel<T, H, false>;
-    const AttentionKernel fkv = dkv ? attention_dkv_kernel<T, H, true> : attention_dkv_kernel<T, H, false>;
-    const size_t lds = kTileLds<T, H>, more = KeyShape<T, H>::kBytes;
-    if (int rc = allow_lds(reinterpret_cast<const void*>(fq), lds, record_q[dq])) return rc;
-    if (int rc = allow_lds(reinterpret_cast<const void*>(fkv), more, record_kv[dkv])) return rc;
-    a.places = tile_places(a.t, a.sequences, own_rows(H, sizeof(T)));
-    in_slices(a.places * a.n * a.heads, [&](int64_t first, unsigned groups) {
+    static LdsRecord record[2] = {};
+    const bool direct = straight<T, H>(a.head, {a.q, a.k, a.v, a.dout});
+    const AttentionKernel fn = direct ? attention_grad_kernel<T, H, true> : attention_grad_kernel<T, H, false>;
+    const size_t lds = std::max(kTileLds<T, H>, KeyShape<T, H>::kBytes);
+    if (int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, record[direct])) return rc;
+    int lanes = 1;
+    while (lanes * kPer<T> < a.head) lanes *= 2;
+    in_slices(parts_of(a.t, kAlongRows) * a.n * a.heads, [&](int64_t first, unsigned groups) {
         a.first = first;
-        hipLaunchKernelGGL(fq, dim3(groups), dim3(kAttentionWaves * kWave), lds, s, a);
+        hipLaunchKernelGGL(attention_along_kernel<T>, dim3(groups), dim3(kAttentionWaves * kWave), 0, s, a, lanes);
     });
+    a.places = tile_places(a.t, a.sequences, own_rows(H, sizeof(T)));
     const int64_t tiles = a.places * a.n * a.kv, first_tiles = (int64_t)std::max(1, a.sequences) * a.first_tiles * a.n * a.kv;
     a.firsts = first_tiles * a.first_parts;
-    in_slices(a.firsts + tiles * a.most_parts, [&](int64_t first, unsigned groups) {
+    a.of_keys = a.firsts + tiles * a.most_parts;
+    in_slices(a.of_keys + a.places * a.n * a.heads, [&](int64_t first, unsigned groups) {
         a.first = first;
-        hipLaunchKernelGGL(fkv, dim3(groups), dim3(kAttentionWaves * kWave), more, s, a);
+        hipLaunchKernelGGL(fn, dim3(groups), dim3(kAttentionWaves * kWave), lds, s, a);
     });
     a.split = 2 * own_rows(H, sizeof(T)) * H / 1024;
     a.firsts = first_tiles * a.split;

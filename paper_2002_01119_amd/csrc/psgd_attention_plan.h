@@ -52,11 +52,13 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
     const int64_t most_steps = (parts_of(narrow && window + own < t ? window + own : t, rows) + 1) * members;      // of a tile that is not a first one
     const int64_t all = tiles * (narrow ? most_steps : (most_steps + 1) / 2);
     KeyParts p{1, 1, 0, 1, 1, 0, 0, 2 * (size_t)own * held * sizeof(float)};
-    // Two rounds of what is resident, and no less than 16 steps: writing a part and reading it again takes as long as five.  No less than 4 in float, where a
-    // step takes as long as that, and where the chip would not be full of longer ones.  (512 tokens of 8 heads of 128, two key heads, bf16, backward 68 us, so 52.)
+    // A part as long as a compute unit's share, since the queries' workgroups fill what is left idle, and no less than 16 steps: writing a part and reading it
+    // again takes as long as five.  No less than 4 in float, where a step takes as long as that, and where the chip would not be full of longer ones.  (Backward, us,
+    // parts of a share / half of it / a quarter: 2 x 2048 tokens of 16 heads of 80, four key heads, bf16 154 / 176 / 192; 2 x 2048, 8 heads of 256 334 / 381 / 416; 4096, 8
+    // heads of 128, two key heads 304 / 268 / 337; 2 x 1024, 8 heads of 64, float 137 / 159 / 157.  512 tokens of 8 heads of 128 at least 16 steps each 68, 4 steps 52.)
     const int64_t least = bytes == 4 || all < 16 * (int64_t)cus ? 4 : 16;
     if (tiles < (narrow ? 2 : 4) * (int64_t)cus) {
-        const int64_t fair = parts_of(all, 4 * (int64_t)cus), steps = fair > least ? fair : least;
+        const int64_t fair = parts_of(all, cus), steps = fair > least ? fair : least;
         int64_t most = parts_of(most_steps, steps);
         while (most > 1 && places * units * most > 16 * (int64_t)cus) --most;
         p.most = (int)most;

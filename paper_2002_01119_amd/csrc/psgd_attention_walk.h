@@ -21,7 +21,7 @@ struct AttentionArgs {
     HeadsView q, k, v, o, dout, dq, dk, dv;
     float *lse, *along;          // [n, heads, t]; along: D
     const int32_t* starts;
-    int64_t starts_learner, t, first, total, places;      // first, total: workgroups of this launch and of all
+    int64_t starts_learner, t, first, of_keys, places;      // first: of this launch's workgroups; of_keys: those that have dk and dv
     int* status;
     int sequences, heads, kv, head, window, sinks, n;      // no window: the largest number
     float scale;
@@ -30,6 +30,9 @@ struct AttentionArgs {
     int most_parts, part_steps, first_tiles, first_parts, first_steps, split;
     int64_t part_slots, first_slots, firsts;
 };
+
+// a / b of numbers that are not negative: those of 32 bits, as all but the largest calls have, take a fifth of the instructions.
+__device__ __forceinline__ int64_t over(int64_t a, int64_t b) { return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b); }
 
 // Which learner, head and tile a workgroup has.  Workgroups that read the same keys are on one die: dies take workgroups in turn, so where the pairs of
 // learner and key head are a multiple of eight each die keeps its own, and else each takes eight workgroups that follow each other.
@@ -45,20 +48,22 @@ template <int ROWS, bool PARTS = false> __device__ __forceinline__ Work find_wor
     const int units = a.n * a.kv;
     int64_t unit, in;
     if (PARTS && units % 8 == 0) {
-        unit = id / 8 % (units / 8) * 8 + id % 8;
-        in = id / units;
+        in = over(id, units);
+        unit = ((id - in * units) / 8 + in) % (units / 8) * 8 + id % 8;      // turned with each place, else all of a long learner's would be one shader engine's
     } else if (units % 8 == 0) {
-        unit = id / (8 * members) % (units / 8) * 8 + id % 8;
-        in = id / (units * members) * members + id / 8 % members;
+        const int64_t turn = id / 8, row = over(turn, members), column = over(row, units / 8);
+        unit = (row + column) % (units / 8) * 8 + id % 8;
+        in = column * members + (turn - row * members);
     } else {
         const int64_t even = inner * units / 64 * 64, at = id < even ? id / 64 * 64 + id % 8 * 8 + id / 8 % 8 : id;
-        unit = at / inner;
-        in = at % inner;
+        unit = over(at, inner);
+        in = at - unit * inner;
     }
-    const int member = (int)(PARTS ? in / a.places : in % members);
-    int64_t place = PARTS ? in % a.places : in / members;
+    const int64_t outer = over(in, PARTS ? a.places : members), inside = in - outer * (PARTS ? a.places : members);
+    const int member = (int)(PARTS ? outer : inside), learner = (int)over(unit, a.kv);
+    int64_t place = PARTS ? inside : outer;
     if (last_first) place = a.places - 1 - place;
-    Work w{(int)(unit / a.kv), (int)(unit % a.kv), member, 0, (int)a.t, 0, true, 0, place};
+    Work w{learner, (int)unit - learner * a.kv, member, 0, (int)a.t, 0, true, 0, place};
     if (!a.starts) {
         w.tile = (int)place;
     } else {
@@ -77,15 +82,15 @@ template <int ROWS, bool PARTS = false> __device__ __forceinline__ Work find_wor
             if (at / ROWS + mid <= place) lo = mid;
             else hi = mid;
         }
-        const int s = lo + lane, at = s < hi ? std::min(std::max(starts[s], 0), t) : 0;
+        const int s = lo + lane, at = s < hi ? std::min(std::max(starts[s], 0), t) : 0, end = s < hi ? std::min(std::max(starts[s + 1], 0), t) : 0;
         const int found = __popcll(__ballot(s < hi && at / ROWS + s <= place)) - 1;
         if (found < 0) {
             w.there = false;
             return w;
         }
         const int seq = w.sequence = lo + found;
-        w.lo = std::min(std::max(starts[seq], 0), t);
-        w.hi = std::min(std::max(starts[seq + 1], 0), t);
+        w.lo = __builtin_amdgcn_readlane(at, found);
+        w.hi = __builtin_amdgcn_readlane(end, found);
         w.tile = (int)(place - (w.lo / ROWS + seq));
     }
     w.there = w.tile >= 0 && (int64_t)w.tile * ROWS < w.hi - w.lo;
@@ -124,6 +129,14 @@ template <typename T, int H, int ROWS, int THREADS, bool DIRECT> struct Mover {
                 const int at = threadIdx.x + j * THREADS, row = row0 + at / Lds::kGroups, col = at % Lds::kGroups * kPer<T>;
                 held[j] = load_group(seq + row * row_stride + col, row < len ? head - col : 0, whole);
             }
+        }
+    }
+    // Both, through the registers of one group.
+    static __device__ __forceinline__ void carry(char* tile, const T* seq, int64_t row_stride, int row0, int len, int head, bool whole) {
+#pragma unroll 1
+        for (int j = 0; j < kEach; ++j) {
+            const int at = threadIdx.x + j * THREADS, row = row0 + at / Lds::kGroups, col = at % Lds::kGroups * kPer<T>;
+            Lds::put(tile, at / Lds::kGroups, at % Lds::kGroups, load_group(seq + row * row_stride + col, row < len ? head - col : 0, whole));
         }
     }
     __device__ __forceinline__ void land(char* tile) const {
