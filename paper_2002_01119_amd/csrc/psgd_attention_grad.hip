@@ -14,12 +14,11 @@
 namespace psgd {
 namespace {
 
-// D, of every row of a sequence.  One pass over two arrays: `lanes` of a wavefront take a row, 16 bytes each, a workgroup kAlongRows of a head.
-constexpr int kAlongRows = 64;
-template <typename T> __global__ __launch_bounds__(kAttentionWaves* kWave) void attention_along_kernel(AttentionArgs a, int lanes) {
-    const int64_t id = a.first + blockIdx.x, pair = id / a.heads, blocks = (a.t + kAlongRows - 1) / kAlongRows;
+// D, of every row of a sequence.  One pass over two arrays: `lanes` of a wavefront take a row, 16 bytes each, a workgroup `rows` of a head.
+template <typename T> __global__ __launch_bounds__(kAttentionWaves* kWave) void attention_along_kernel(AttentionArgs a, int lanes, int rows) {
+    const int64_t id = a.first + blockIdx.x, pair = id / a.heads, blocks = (a.t + rows - 1) / rows;
     const int h = (int)(id % a.heads), i = (int)(pair / blocks), at_once = kWave / lanes * kAttentionWaves;
-    const int row0 = (int)(pair % blocks) * kAlongRows, col = threadIdx.x % lanes * kPer<T>;
+    const int row0 = (int)(pair % blocks) * rows, col = threadIdx.x % lanes * kPer<T>;
     int lo = 0, hi = (int)a.t;                  // the sequences follow each other
     if (a.starts) {
         const int32_t* const starts = a.starts + i * a.starts_learner;
@@ -27,7 +26,8 @@ template <typename T> __global__ __launch_bounds__(kAttentionWaves* kWave) void 
         hi = std::min(starts[a.sequences], hi);
     }
     const bool whole = a.head % kPer<T> == 0;
-    for (int r = threadIdx.x / lanes; r < kAlongRows; r += at_once) {
+#pragma unroll 4
+    for (int r = threadIdx.x / lanes; r < rows; r += at_once) {
         const int row = row0 + r, left = row >= lo && row < hi ? a.head - col : 0;
         const u32x4 x = load_group(at<T>(a.dout, i, row, (int64_t)h * a.head + col), left, whole), y = load_group(at<T>(a.o, i, row, (int64_t)h * a.head + col), left, whole);
         float u[kPer<T>], v[kPer<T>], d = 0.0f;
@@ -431,9 +431,11 @@ template <typename T, int H> int launch_backward(const char* name, AttentionArgs
     if (int rc = allow_lds(reinterpret_cast<const void*>(fn), lds, record[direct])) return rc;
     int lanes = 1;
     while (lanes * kPer<T> < a.head) lanes *= 2;
-    in_slices(parts_of(a.t, kAlongRows) * a.n * a.heads, [&](int64_t first, unsigned groups) {
+    // a trip to memory for each workgroup, or four where that still makes ten rounds of them (517 tokens of six heads of 72, float, 64 rows each 11 us)
+    const int at_once = kWave / lanes * kAttentionWaves, rows = parts_of(a.t, 4 * at_once) * a.n * a.heads < 20 * kChipUnits ? at_once : 4 * at_once;
+    in_slices(parts_of(a.t, rows) * a.n * a.heads, [&](int64_t first, unsigned groups) {
         a.first = first;
-        hipLaunchKernelGGL(attention_along_kernel<T>, dim3(groups), dim3(kAttentionWaves * kWave), 0, s, a, lanes);
+        hipLaunchKernelGGL(attention_along_kernel<T>, dim3(groups), dim3(kAttentionWaves * kWave), 0, s, a, lanes, rows);
     });
     a.places = tile_places(a.t, a.sequences, own_rows(H, sizeof(T)));
     const int64_t tiles = a.places * a.n * a.kv, first_tiles = (int64_t)std::max(1, a.sequences) * a.first_tiles * a.n * a.kv;

@@ -84,12 +84,12 @@ inline KeyParts key_parts(int heads, int kv, int head, int bytes, int64_t window
 constexpr int kStepKeys = 32;               // of a wavefront at a time
 // A wavefront has two tiles of 32 keys and values in LDS, which makes 128 KB of a workgroup and one of those a compute unit (two of the narrowest heads): 64 KB are
 // on their way at any time, three times what the memory's latency takes.  us, four wavefronts / two and twice the workgroups: one sequence of 131 072 positions
-// 122 / 141, 96 of up to 4100 265 / 330, 64 of 2048 111 / 112 (all 8 key heads of 128 in bf16); four tiles for the narrowest, 256 sequences of 512 with 8 heads of 64
+// 122 / 141, 9 of them the join's then, 96 of up to 4100 265 / 330, 64 of 2048 111 / 112 (all 8 key heads of 128 in bf16); four tiles for the narrowest, 256 sequences of 512 with 8 heads of 64
 // in bf16 72, two 48.
 constexpr int kStepStages = 2;
 constexpr int step_waves(int held, int bytes) { return in_lds(held) * bytes <= 256 ? 4 : in_lds(held) * bytes == 512 ? 2 : 1; }
 // Parts that a sequence's keys are cut into: as many workgroups as are there at once, and no fewer keys than two tiles a wavefront.  (One sequence of 131 072
-// positions with twice the workgroups 134 us, with four times 168.)
+// positions with twice the workgroups 134 us, with four times 168, when it took 122.)
 inline int step_parts(int64_t units, int64_t most_keys, int head, int bytes) {
     const int64_t most = parts_of(most_keys, step_waves(held_head(head), bytes) * kStepKeys * 2), fair = parts_of(held_head(head) * bytes <= 128 ? 2 * kChipUnits : kChipUnits, units);
     const int64_t p = most < fair ? most : fair;
