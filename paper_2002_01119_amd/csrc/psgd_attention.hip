@@ -3,7 +3,7 @@
 //     s_ij = scale q_i . k_j,   p_ij = exp(s_ij - lse_i),   o_i = sum_j p_ij v_j
 //
 // A workgroup owns a tile of one head's queries and walks the keys that they see, a tile at a time, with the running maximum and sum of the
-// softmax; the wavefronts share the tile in LDS and own 16 or 32 queries each.  Scores are computed as keys times queries, so a lane has four
+// softmax; the wavefronts share the tile in LDS and own 16 or, where there are tiles enough, 32 queries each.  Scores are computed as keys times queries, so a lane has four
 // keys of one query: maximum, sum and scale of a query are a lane's own, and the exponentials are the next product's operand as they stand.  Two products,
 // 4 pairs head operations.
 //
@@ -19,17 +19,19 @@ namespace {
 
 __device__ int g_attention_status = 0;
 
-template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentionWaves* kWave, (DIRECT && H * sizeof(T) == 256 ? 3 : Shape<T, H>::kTwice)) void attention_kernel(AttentionArgs a) {
+// BLOCKS: of 16 queries, of each wavefront.
+template <typename T, int H, bool DIRECT, int BLOCKS> __global__ __launch_bounds__(kAttentionWaves* kWave, (DIRECT && H * sizeof(T) == 256 ? 3 : Shape<T, H>::kTwice)) void attention_kernel(AttentionArgs a) {
     using S = Shape<T, H>;
     using Lds = typename S::Lds;
+    constexpr int kOwn = kAttentionWaves * 16 * BLOCKS;
     extern __shared__ __attribute__((aligned(16))) char lds[];       // two of keys, two of values
     const int members = a.heads / a.kv;
-    const Work w = find_work<S::kOwn>(a, a.first + blockIdx.x, members, true);
+    const Work w = find_work<kOwn>(a, a.first + blockIdx.x, members, true);
     if (!w.there) return;
     const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), col = lane % 16, g = lane / 16, len = w.hi - w.lo;
-    const int h = w.kv_head * members + w.member, row0 = w.tile * S::kOwn, row1 = std::min(row0 + S::kOwn, len);
+    const int h = w.kv_head * members + w.member, row0 = w.tile * kOwn, row1 = std::min(row0 + kOwn, len);
     const bool whole = a.head % kPer<T> == 0;
-    const int mine = row0 + wave * 16 * S::kOwnBlocks;               // the wavefront's first query
+    const int mine = row0 + wave * 16 * BLOCKS;               // the wavefront's first query
     // a negative scale's sign goes to the queries; one of 0 is next to nothing, which leaves what is masked at -inf
     const float to_log2 = fmaxf(fabsf(a.scale) * kLog2E, 1e-30f);
 
@@ -39,11 +41,11 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     if (DIRECT && a.head < H) clear_lds<S::kThreads>(lds, 4 * Lds::kBytes);
     mk.fetch(lds, keys, a.k.row, walk.tile(0) * S::kWalked, len, a.head, whole);
     mv.fetch(lds + Lds::kBytes, values, a.v.row, walk.tile(0) * S::kWalked, len, a.head, whole);
-    Eight<T> q[S::kOwnBlocks][S::kSteps];
-    f32x4 o[S::kOwnBlocks][S::kCols];
-    float top[S::kOwnBlocks], sum[S::kOwnBlocks];
+    Eight<T> q[BLOCKS][S::kSteps];
+    f32x4 o[BLOCKS][S::kCols];
+    float top[BLOCKS], sum[BLOCKS];
 #pragma unroll
-    for (int b = 0; b < S::kOwnBlocks; ++b) {
+    for (int b = 0; b < BLOCKS; ++b) {
         const int row = mine + 16 * b + col;
         const T* p = at<T>(a.q, w.learner, w.lo + row, (int64_t)h * a.head);
 #pragma unroll
@@ -70,34 +72,34 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
             mk.fetch(next, keys, a.k.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
             mv.fetch(next + Lds::kBytes, values, a.v.row, walk.tile(step + 1) * S::kWalked, len, a.head, whole);
         }
-        if (mine < len && any_sees(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks)) {
-            f32x4 s[S::kOwnBlocks][S::kBlocks];
+        if (mine < len && any_sees(mine, mine + 16 * BLOCKS - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks)) {
+            f32x4 s[BLOCKS][S::kBlocks];
 #pragma unroll
             for (int kb = 0; kb < S::kBlocks; ++kb)
 #pragma unroll
-                for (int b = 0; b < S::kOwnBlocks; ++b) s[b][kb] = (f32x4){0, 0, 0, 0};
+                for (int b = 0; b < BLOCKS; ++b) s[b][kb] = (f32x4){0, 0, 0, 0};
 #pragma unroll
             for (int kc = 0; kc < S::kSteps; ++kc)
 #pragma unroll
                 for (int kb = 0; kb < S::kBlocks; ++kb) {
                     const Eight<T> k = Lds::along(along_at + buffer, kb, kc);
 #pragma unroll
-                    for (int b = 0; b < S::kOwnBlocks; ++b) s[b][kb] = mma(k, q[b][kc], s[b][kb]);
+                    for (int b = 0; b < BLOCKS; ++b) s[b][kb] = mma(k, q[b][kc], s[b][kb]);
                 }
-            const bool full = all_see(mine, mine + 16 * S::kOwnBlocks - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks);
+            const bool full = all_see(mine, mine + 16 * BLOCKS - 1, key0, key0 + S::kWalked - 1, a.window, a.sinks);
             if (!full) {
 #pragma unroll
-                for (int b = 0; b < S::kOwnBlocks; ++b)
+                for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                     for (int kb = 0; kb < S::kBlocks; ++kb)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[b][kb][e] = sees(mine + 16 * b + col, key0 + 16 * kb + 4 * g + e, a.window, a.sinks) ? s[b][kb][e] : -INFINITY;
             }
             // the maximum that p is taken against lags behind while no score is 2^kLag times it: sums and outputs are seldom scaled
-            float most[S::kOwnBlocks];
+            float most[BLOCKS];
             bool more = false;
 #pragma unroll
-            for (int b = 0; b < S::kOwnBlocks; ++b) {
+            for (int b = 0; b < BLOCKS; ++b) {
                 most[b] = -INFINITY;
 #pragma unroll
                 for (int kb = 0; kb < S::kBlocks; ++kb)
@@ -108,7 +110,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
             }
             if (__any(more)) {
 #pragma unroll
-                for (int b = 0; b < S::kOwnBlocks; ++b) {
+                for (int b = 0; b < BLOCKS; ++b) {
                     const float m = fmaxf(top[b], column_all<Larger>(most[b])), less = m == -INFINITY ? 1.0f : exp_2(top[b] - m);
                     top[b] = m;
                     sum[b] *= less;
@@ -117,7 +119,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
                 }
             }
 #pragma unroll
-            for (int b = 0; b < S::kOwnBlocks; ++b) {
+            for (int b = 0; b < BLOCKS; ++b) {
                 const float safe = top[b] == -INFINITY ? 0.0f : top[b];
                 float part = 0.0f;
 #pragma unroll
@@ -131,14 +133,14 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
             }
 #pragma unroll
             for (int kc = 0; kc < S::kBlocks / 2; ++kc) {
-                Eight<T> p[S::kOwnBlocks];
+                Eight<T> p[BLOCKS];
 #pragma unroll
-                for (int b = 0; b < S::kOwnBlocks; ++b) p[b] = as_operand<T>(s[b][2 * kc], s[b][2 * kc + 1]);
+                for (int b = 0; b < BLOCKS; ++b) p[b] = as_operand<T>(s[b][2 * kc], s[b][2 * kc + 1]);
 #pragma unroll
                 for (int d = 0; d < S::kCols; ++d) {
                     const Eight<T> v = Lds::across(across_at + buffer + Lds::kBytes, d, kc);
 #pragma unroll
-                    for (int b = 0; b < S::kOwnBlocks; ++b) o[b][d] = mma(v, p[b], o[b][d]);
+                    for (int b = 0; b < BLOCKS; ++b) o[b][d] = mma(v, p[b], o[b][d]);
                 }
             }
         }
@@ -149,7 +151,7 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
         __syncthreads();
     }
 #pragma unroll
-    for (int b = 0; b < S::kOwnBlocks; ++b) {
+    for (int b = 0; b < BLOCKS; ++b) {
         const int row = mine + 16 * b + col;
         const float all = column_all<Sum>(sum[b]), by = 1.0f / all;
         if (row >= len) continue;
@@ -160,18 +162,23 @@ template <typename T, int H, bool DIRECT> __global__ __launch_bounds__(kAttentio
     }
 }
 
-template <typename T, int H> int launch_forward(const char* name, AttentionArgs a, hipStream_t s) {
+template <typename T, int H, int BLOCKS> int launch_forward_of(const char* name, AttentionArgs a, hipStream_t s) {
     static LdsRecord record[2] = {};
     const bool direct = straight<T, H>(a.head, {a.k, a.v});
-    const AttentionKernel fn = direct ? attention_kernel<T, H, true> : attention_kernel<T, H, false>;
+    const AttentionKernel fn = direct ? attention_kernel<T, H, true, BLOCKS> : attention_kernel<T, H, false, BLOCKS>;
     if (int rc = allow_lds(reinterpret_cast<const void*>(fn), kTileLds<T, H>, record[direct])) return rc;
-    a.places = tile_places(a.t, a.sequences, own_rows(H, sizeof(T)));
+    a.places = tile_places(a.t, a.sequences, kAttentionWaves * 16 * BLOCKS);
     in_slices(a.places * a.n * a.heads, [&](int64_t first, unsigned groups) {
         a.first = first;
         hipLaunchKernelGGL(fn, dim3(groups), dim3(kAttentionWaves * kWave), (kTileLds<T, H>), s, a);
     });
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? PSGD_OK : hip_error(e, name);
+}
+template <typename T, int H> int launch_forward(const char* name, const AttentionArgs& a, hipStream_t s) {
+    constexpr int most = own_blocks(H, sizeof(T));
+    if (most > 1 && forward_blocks(H, sizeof(T), a.t, (int64_t)a.n * a.heads) == 1) return launch_forward_of<T, H, 1>(name, a, s);
+    return launch_forward_of<T, H, most>(name, a, s);
 }
 template <typename T> int forward_of(const char* name, const AttentionArgs& a, hipStream_t s) {
     switch (held_head(a.head)) {

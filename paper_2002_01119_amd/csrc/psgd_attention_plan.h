@@ -25,6 +25,13 @@ constexpr int own_blocks(int held, int bytes) { return bytes == 2 && held <= 128
 constexpr int own_rows(int held, int bytes) { return kAttentionWaves * 16 * own_blocks(held, bytes); }
 constexpr int walked_rows(int held, int bytes) { return in_lds(held) * bytes < 256 ? 64 : 32; }
 
+// Forward calls of fewer own tiles have tiles of half the rows, so that more compute units have work.  (us, half / whole, bf16, heads of 128: 512 tokens of 8 heads, 32
+// tiles, 14.8 / 20.6; 2048 tokens of 32 heads, 512 tiles, 70 / 82; 2 x 4096 tokens of 16 heads, 1024 tiles, 191 / 172; of 64: 512 tiles 38.5 / 44.6, 1024 tiles 64 / 55.)
+inline int forward_blocks(int held, int bytes, int64_t t, int64_t heads) {      // heads: of all learners
+    const int blocks = own_blocks(held, bytes);
+    return blocks > 1 && parts_of(t, own_rows(held, bytes)) * heads < 3 * kChipUnits ? 1 : blocks;
+}
+
 // Places for the own tiles of a learner's sequences: sequence s has its from starts[s] / rows + s on, which leaves every sequence room for all of its
 // tiles whatever their lengths, so that a workgroup finds its sequence by itself and no launch depends on device memory.
 inline int64_t tile_places(int64_t t, int sequences, int rows) { return t / rows + (sequences > 0 ? sequences : 1); }

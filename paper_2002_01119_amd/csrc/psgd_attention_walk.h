@@ -47,13 +47,19 @@ template <int ROWS, bool PARTS = false> __device__ __forceinline__ Work find_wor
     const int64_t inner = members * a.places;
     const int units = a.n * a.kv;
     int64_t unit, in;
-    if (PARTS && units % 8 == 0) {
-        in = over(id, units);
-        unit = ((id - in * units) / 8 + in) % (units / 8) * 8 + id % 8;      // turned with each place, else all of a long learner's would be one shader engine's
-    } else if (units % 8 == 0) {
-        const int64_t turn = id / 8, row = over(turn, members), column = over(row, units / 8);
-        unit = (row + column) % (units / 8) * 8 + id % 8;
-        in = column * members + (turn - row * members);
+    if (units % 8 == 0) {
+        // learners are turned with each place, else all of a long one's would be one shader engine's
+        const int each = units / 8;
+        int64_t turned;
+        if (PARTS) {
+            in = over(id, units);
+            turned = (id - in * units) / 8 + in;
+        } else {
+            const int64_t turn = id / 8, row = over(turn, members), column = over(row, each);
+            in = column * members + (turn - row * members);
+            turned = row + column;
+        }
+        unit = (turned - over(turned, each) * each) * 8 + id % 8;
     } else {
         const int64_t even = inner * units / 64 * 64, at = id < even ? id / 64 * 64 + id % 8 * 8 + id / 8 % 8 : id;
         unit = over(at, inner);

@@ -18,6 +18,10 @@ int main() {
             for (int i = 0; i < 4; ++i)
                 if (std::scanf("%lld", &a[i]) != 1) return 1;
             std::printf("%d\n", psgd::step_parts(a[1], a[2], (int)a[3], (int)a[0]));
+        } else if (!std::strcmp(kind, "forward")) {   // bytes head t heads
+            for (int i = 0; i < 4; ++i)
+                if (std::scanf("%lld", &a[i]) != 1) return 1;
+            std::printf("%d\n", psgd::forward_blocks(psgd::held_head((int)a[1]), (int)a[0], a[2], a[3]));
         } else if (!std::strcmp(kind, "shape")) {  // bytes head
             for (int i = 0; i < 2; ++i)
                 if (std::scanf("%lld", &a[i]) != 1) return 1;

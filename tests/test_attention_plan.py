@@ -108,3 +108,9 @@ def test_a_steps_parts(ask):
     parts = lambda *a: ask(["step " + " ".join(map(str, a))])[0][0]  # noqa: E731
     assert parts(2, 8, 131072, 128) == 32 and parts(2, 768, 4100, 128) == 1 and parts(2, 1, 1, 64) == 1 and parts(2, 1, 256, 64) == 1 and parts(2, 1, 257, 64) == 2
     assert parts(2, 10 ** 6, 1 << 30, 128) == 1 and parts(4, 1, 1 << 30, 256) == 256 and parts(2, 1, 1 << 30, 16) == 512
+
+
+def test_heights_of_forward_tiles(ask):
+    blocks = lambda *a: ask(["forward %d %d %d %d" % a])[0][0]  # noqa: E731
+    assert [blocks(2, h, 260, 15 * 16) for h in (24, 64, 80, 128, 144)] == [1, 1, 1, 1, 1] and [blocks(2, h, 260, 256) for h in (24, 64, 80, 128, 144)] == [2, 2, 2, 2, 1]
+    assert blocks(4, 64, 4096, 128) == 1

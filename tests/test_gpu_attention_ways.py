@@ -72,6 +72,15 @@ def test_either_way_to_the_steps_tiles(attention, head, dtype):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("n", [15, 16])
+@pytest.mark.parametrize("lead", [0, 1])
+@pytest.mark.parametrize("head", [24, 64, 80, 128, 144])
+def test_tiles_of_either_height(attention, head, lead, n):
+    """16 heads of 260 tokens are 720 tiles of 128 rows for 15 learners, which go in tiles of half of them, and 768 for 16, which go whole."""
+    starts = cuts([[0, 64 + i, 120, 120, 259] for i in range(n)])
+    check(attention, n, 260, 16, 2, head, BF16, window=100, sinks=3, starts=starts, lead=lead, backward=False)
+
+
 def test_short_way_and_long_way(attention, monkeypatch):
     """Every call makes the same bits either way, and the short way is the one that is taken."""
     n, t, heads, kv, head, slots = 2, 90, 4, 2, 32, 40
